@@ -20,7 +20,7 @@
  *   - the return value is a moe_status; nothing throws or aborts.
  *       MOE_ERR_NULL        a required pointer is NULL
  *       MOE_ERR_SHAPE       non-positive dimension, k > E, T % n != 0, cf <= 0,
- *                           partition index out of range
+ *                           partition index out of range, a row stride below the row
  *       MOE_ERR_UNSUPPORTED E > 64, k > 8, n > 64, M % 8 != 0, H % 8 != 0, unknown dtype or
  *                           reuse mode, a reuse mode the entry point does not serve
  *       MOE_ERR_WORKSPACE   workspace smaller than moe_workspace_bytes(), or not
@@ -52,7 +52,8 @@ typedef enum {
     MOE_ERR_WORKSPACE = 4, MOE_ERR_HIP = 5
 } moe_status;
 
-typedef enum { MOE_F32 = 0, MOE_BF16 = 1 } moe_dtype;
+typedef enum { MOE_F32 = 0, MOE_BF16 = 1,
+               MOE_E4M3 = 2 /* 8-bit float, 4 exponent and 3 mantissa bits, largest 448, no infinities; only where stated */ } moe_dtype;
 
 /* Memory-reuse modes (Section III-D, Table II).
  *   NONE      every partition's T_DI, T_M, T_DO is kept for backward (row "none").
@@ -317,7 +318,8 @@ moe_status moe_layer_backward(const moe_config* cfg, const void* x, const void* 
 /* Counters of this process's work on the device since the last reset, by class:
  * out[0] GEMMs, out[1] permutations (dispatch, combine, dispatch-backward),
  * out[2] everything else (a gate 1, a slot assignment 2, a partition's gate
- * backward 3).  Units of work and not kernels launched: a launch that does the
+ * backward 3; of the operators around the layer a product on 4-bit weights counts in out[0],
+ * any other call 1 here).  Units of work and not kernels launched: a launch that does the
  * work of several counts as all of them, and a unit counts the same whether it
  * took a launch of its own, a part of one, or (slot assignment) one or two.
  * Host only. */
@@ -335,7 +337,8 @@ moe_status moe_launch_counts(int64_t out[3], int32_t reset);
  * (GeLU epilogue), 1 second FFN GEMM and recomputation, 2 GEMM with the
  * GeLU-backward epilogue, 3 input-gradient GEMM, 4 weight-gradient GEMMs,
  * 5 dispatch, 6 combine, 7 dispatch backward, 8 gate, 9 slot assignment,
- * 10 gate backward.  Arrays of `kinds` entries (at most 11).  Host only; not
+ * 10 gate backward, 11 norm, 12 norm backward, 13 router, 14 router backward, 15 products on
+ * 4-bit weights (each one whole call).  Arrays of `kinds` entries (at most 16).  Host only; not
  * for use under stream capture. */
 moe_status moe_profile_enable(int32_t on);
 moe_status moe_profile_read(int32_t kinds, int64_t* launches, double* total_ms);
@@ -345,6 +348,114 @@ const char* moe_status_string(moe_status s);
 /* Text of the most recent HIP failure behind a MOE_ERR_HIP (HIP's message and the
  * source line of the failing call); empty if there was none.  Host only. */
 const char* moe_last_error(void);
+
+/* ---- the operators around the layer ------------------------------------------------
+ * A norm in front of the gate, a router on logits that are there already, and the experts'
+ * products on 4-bit weights.  The conventions at the top hold, with these differences:
+ *   - rows may lie apart (the ld* fields, in elements, 0 = dense) and need the alignment of
+ *     their elements only; sizes need not be multiples of anything unless stated;
+ *   - T = 0 is a batch without tokens: MOE_OK, no tensor is read, no pointer required
+ *     (moe_norm_bwd still writes a gain gradient that it overwrites, then zero);
+ *   - E and k have limits of their own, given with each call;
+ *   - outputs may not overlap inputs or each other unless stated. */
+
+/* Root-mean-square norm of the sum of two rows. */
+typedef struct {
+    int32_t T, M;           /* M <= 32768 */
+    float eps;              /* >= 0 */
+    int32_t dtype;          /* MOE_F32 or MOE_BF16: x, residual, h, dy, dh, dx, and y unless out is MOE_E4M3 */
+    int32_t out;            /* of y: dtype or MOE_E4M3 */
+    int32_t group;          /* MOE_E4M3: 128 columns share a scale (the last of a row may be fewer), or 0: the row */
+    int32_t grad_overwrite; /* dgain: 0 accumulated into, 1 stored */
+    int64_t ldx, ldr, ldh, ldy;  /* row strides of x and dx; residual; h and dh; y and dy */
+} moe_norm_config;
+
+/* h = x + residual;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h * rstd * gain.  The float sum h goes into the
+ * norm before it is rounded to its storage type, and y is rounded once.
+ * MOE_E4M3: scale = max(largest |y| of the group / 448, 2^-126), y / scale rounded to the nearest, ties to even; a NaN
+ * among a group's y makes its scale and all of its values NaN.
+ *   x [T,M]; residual [T,M], may be NULL; gain [M] float, may be NULL (ones);
+ *   h [T,M] out, may be NULL, may be x or residual themselves (with their stride);
+ *   y [T,M] out; scales [T, ceil(M/128) or 1] float out (MOE_E4M3 only, else unused);
+ *   rstd [T] float out, may be NULL. */
+moe_status moe_norm_fwd(const moe_norm_config* cfg, const void* x, const void* residual, const float* gain,
+                        void* h, void* y, float* scales, float* rstd, void* stream);
+
+/* Its gradients, from the stored h and rstd of forward.  With n = h * rstd:
+ *   dx = dh + rstd * (dy * gain - n * mean(dy * gain * n));  dgain (+)= sum over tokens of dy * n,
+ * in an order that depends on the sizes alone.  dx is the gradient of x and of residual alike.
+ *   dy [T,M]; h [T,M]; gain as in forward; rstd [T]; dh [T,M]: what reaches h past the norm, may be NULL;
+ *   dx [T,M] out, may be dy or dh themselves (with their stride); dgain [M] float, may be NULL;
+ *   scratch: moe_norm_scratch_bytes(cfg) bytes, 4-byte aligned (needed with dgain only). */
+moe_status moe_norm_bwd(const moe_norm_config* cfg, const void* dy, const void* h, const float* gain, const float* rstd,
+                        const void* dh, void* dx, float* dgain, void* scratch, void* stream);
+moe_status moe_norm_scratch_bytes(const moe_norm_config* cfg, size_t* bytes);
+
+/* Router: which k of E experts, and with what weights, from logits. */
+typedef enum { MOE_SOFTMAX = 0, MOE_SIGMOID = 1 } moe_scores;
+typedef struct {
+    int32_t T, E, k;        /* E <= 512, k <= 16, k <= group_k * E / groups */
+    int32_t scores;         /* moe_scores: s = softmax over all E, or the sigmoid of each */
+    int32_t groups;         /* 1: none; up to 16, dividing E: E / groups consecutive experts are a group */
+    int32_t group_k;        /* groups that stay in the choice, 1..groups */
+    int32_t group_top;      /* 1 or 2: a group's score is the sum of so many of its largest s + bias */
+    int32_t renormalize;    /* 1: weights are divided by their sum over the token's choices */
+    float scale;            /* finite; weights are multiplied by it */
+    int32_t dtype;          /* MOE_F32 or MOE_BF16: logits and dlogits */
+    int64_t ld;             /* row stride of logits and dlogits */
+} moe_router_config;
+
+/* topk_idx[t] = the k experts with the largest s + bias (no bias: the largest logits) among the groups that stay,
+ * largest first, equal ones and equal groups by the lower index;  topk_w = scale * s of the chosen, without the bias.
+ * Which comes first is decided as by 64-bit scores (closer than those can tell apart: either).  An expert whose logit is NaN or -inf, or whose bias makes its sum -inf
+ * or NaN, is never chosen and has no share of a softmax if its logit is the reason; where fewer than k are left the
+ * remaining choices are -1 with weight 0.  Infinite logits share a softmax evenly.
+ *   logits [T,E]; bias [E] float, may be NULL; topk_idx [T,k] int32, topk_w [T,k] float out;
+ *   load [E] int32, may be NULL: the number of tokens that chose each expert is ADDED to it. */
+moe_status moe_router_fwd(const moe_router_config* cfg, const void* logits, const float* bias,
+                          int32_t* topk_idx, float* topk_w, int32_t* load, void* stream);
+
+/* dlogits from dw = d loss / d topk_w, the choice held fixed (the bias has no gradient).  Experts that were not
+ * chosen have gradients in a softmax that is not renormalised, else zero.
+ *   topk_idx [T,k] as forward left it (no expert twice in a row; entries outside 0..E-1 are no choice);
+ *   dw [T,k] float; dlogits [T,E] out. */
+moe_status moe_router_bwd(const moe_router_config* cfg, const void* logits, const int32_t* topk_idx, const float* dw,
+                          void* dlogits, void* stream);
+
+/* Products of routed rows with 4-bit weights, for serving (the weights are frozen: no backward).
+ * An expert's matrix is packed as Wq [E, N, K/2] bytes, two values of e2m1 (sign, 2 exponent bits, 1 mantissa bit:
+ * 0, .5, 1, 1.5, 2, 3, 4, 6) in a byte, the lower column in the low half, and Ws [E, N, K/32] bytes: the exponents,
+ * plus 127, of the powers of two that 32 columns share (byte 255: NaN). */
+typedef struct {
+    int32_t T, k, E;        /* k <= 64, E <= 4096, T * k <= 2^24; with combine T <= 65535; E * N * K may pass 2^31 */
+    int32_t K, N;           /* K a multiple of 32 */
+    int32_t dtype;          /* of x: MOE_F32, MOE_BF16 or MOE_E4M3 */
+    int32_t out;            /* of y: MOE_F32 or MOE_BF16 */
+    int32_t group;          /* MOE_E4M3: 128 columns of x share a scale, or 0: the row */
+    int32_t per_choice;     /* 0: x has a row per token, 1: per token and choice */
+    int32_t combine;        /* 0: y has a row per token and choice, 1: per token, the sum over its choices */
+    int32_t gelu;           /* 1: GeLU (erf form) of the product, before a weight */
+    int64_t ldx, ldy;       /* row strides; ldx with MOE_F32 a multiple of 4, else of 8 (MOE_BF16) or 16 (MOE_E4M3) elements */
+} moe_w4_config;
+
+/* y[t,j] = f(x_row W[e]^T) * w[t,j] with e = topk_idx[t,j], or y[t] = their sum over j in ascending order; f is
+ * GeLU or nothing.  Products are exact or those of float, sums float; nothing is rounded but y.
+ * An expert outside 0..E-1 contributes zeros.
+ *   x [T or T*k, K], 16-byte aligned; x_scales [its rows, ceil(K/128) or 1] float (MOE_E4M3 only);
+ *   topk_idx [T,k] int32, NULL: expert 0 for all; topk_w [T,k] float, NULL: ones;
+ *   Wq, Ws as above, Wq 16-byte aligned; y [T*k or T, N] out;
+ *   scratch: moe_w4_scratch_bytes(cfg) bytes, 16-byte aligned (may be 0 bytes, then NULL will do).
+ * x, Wq or scratch not 16-byte aligned: MOE_ERR_UNSUPPORTED. */
+moe_status moe_w4_product(const moe_w4_config* cfg, const void* x, const float* x_scales, const int32_t* topk_idx,
+                          const float* topk_w, const uint8_t* Wq, const uint8_t* Ws, void* y, void* scratch, void* stream);
+moe_status moe_w4_scratch_bytes(const moe_w4_config* cfg, size_t* bytes);
+
+/* Packs the layer's weights: W [E,K,N] of dtype (MOE_F32 or MOE_BF16; W1 or W2 of the calls above) into Wq and Ws.  The
+ * shared power of two is the least that leaves the largest magnitude of its 32 at most 6 (2^-126 at least); values are
+ * rounded to the nearest, ties to even.  Infinities and NaN make their 32 values NaN.  K a multiple of 32, E <= 4096; Wq
+ * 16-byte aligned. */
+moe_status moe_w4_quantize(int32_t E, int32_t K, int32_t N, int32_t dtype, const void* W, uint8_t* Wq, uint8_t* Ws,
+                           void* stream);
 
 /* ---- adaptive pipeline granularity (Algorithm 1, Section III-C) ------------------
  * Which n a batch of B tokens should be cut into, with as few timed searches as

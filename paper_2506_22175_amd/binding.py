@@ -15,7 +15,8 @@ from typing import Optional, Sequence
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoe_hip.so")
 
-MOE_F32, MOE_BF16 = 0, 1
+MOE_F32, MOE_BF16, MOE_E4M3 = 0, 1, 2
+MOE_SOFTMAX, MOE_SIGMOID = 0, 1
 MOE_REUSE_NONE, MOE_REUSE_BUFFERS, MOE_REUSE_RECOMPUTE = 0, 1, 2
 MOE_REUSE_S1, MOE_REUSE_S2, MOE_REUSE_S3 = 3, 4, 5
 
@@ -30,6 +31,8 @@ EXPORTS = [
     "moe_search_best_gran", "moe_gran_get", "moe_strategy_cost", "moe_select_strategy",
     "moe_offload_bytes", "moe_layer_step_offload", "moe_layer_streams",
     "moe_gemm_tile",
+    "moe_norm_fwd", "moe_norm_bwd", "moe_norm_scratch_bytes", "moe_router_fwd", "moe_router_bwd",
+    "moe_w4_product", "moe_w4_scratch_bytes", "moe_w4_quantize",
 ]
 
 
@@ -159,7 +162,7 @@ def moe_launch_counts(reset: bool = False):
 
 
 PROFILE_KINDS = ["gemm_fwd1_gelu", "gemm_nn_store", "gemm_dgelu", "gemm_dgrad", "gemm_wgrad", "dispatch",
-                 "combine", "dispatch_bwd", "route", "slots", "gate_bwd"]
+                 "combine", "dispatch_bwd", "route", "slots", "gate_bwd", "norm", "norm_bwd", "router", "router_bwd", "w4"]
 
 
 def moe_profile_enable(on: bool):
@@ -390,3 +393,84 @@ def moe_layer_step_offload(cfg, x, dy, Wg, gate_bias, W1, W2, y, dx, dWg, dW1, d
                                         ctypes.c_size_t(workspace.numel() * workspace.element_size()),
                                         _p(host_buffer), ctypes.c_size_t(host_buffer.numel() * host_buffer.element_size()),
                                         arr, n), "moe_layer_step_offload")
+
+
+# ---- the operators around the layer --------------------------------------------------------
+
+class MoENormConfig(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("M", ctypes.c_int32), ("eps", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("out", ctypes.c_int32), ("group", ctypes.c_int32), ("grad_overwrite", ctypes.c_int32),
+                ("ldx", ctypes.c_int64), ("ldr", ctypes.c_int64), ("ldh", ctypes.c_int64), ("ldy", ctypes.c_int64)]
+
+
+def make_norm_config(T, M, eps=1e-6, dtype=MOE_BF16, out=None, group=0, grad_overwrite=0, ldx=0, ldr=0, ldh=0,
+                     ldy=0) -> MoENormConfig:
+    return MoENormConfig(int(T), int(M), float(eps), int(dtype), int(dtype if out is None else out), int(group),
+                         int(grad_overwrite), int(ldx), int(ldr), int(ldh), int(ldy))
+
+
+def moe_norm_scratch_bytes(cfg: MoENormConfig) -> int:
+    v = ctypes.c_size_t(0)
+    _check(lib().moe_norm_scratch_bytes(_cfg(cfg), ctypes.byref(v)), "moe_norm_scratch_bytes")
+    return v.value
+
+
+def moe_norm_fwd(cfg, x, residual, gain, h, y, scales=None, rstd=None, stream=None):
+    _check(lib().moe_norm_fwd(_cfg(cfg), _p(x), _p(residual), _p(gain), _p(h), _p(y), _p(scales), _p(rstd),
+                              _s(stream)), "moe_norm_fwd")
+
+
+def moe_norm_bwd(cfg, dy, h, gain, rstd, dh, dx, dgain, scratch, stream=None):
+    _check(lib().moe_norm_bwd(_cfg(cfg), _p(dy), _p(h), _p(gain), _p(rstd), _p(dh), _p(dx), _p(dgain), _p(scratch),
+                              _s(stream)), "moe_norm_bwd")
+
+
+class MoERouterConfig(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("scores", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("group_k", ctypes.c_int32), ("group_top", ctypes.c_int32),
+                ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("ld", ctypes.c_int64)]
+
+
+def make_router_config(T, E, k, scores=MOE_SOFTMAX, groups=1, group_k=1, group_top=2, renormalize=0, scale=1.0,
+                       dtype=MOE_F32, ld=0) -> MoERouterConfig:
+    return MoERouterConfig(int(T), int(E), int(k), int(scores), int(groups), int(group_k), int(group_top),
+                           int(renormalize), float(scale), int(dtype), int(ld))
+
+
+def moe_router_fwd(cfg, logits, bias, topk_idx, topk_w, load=None, stream=None):
+    _check(lib().moe_router_fwd(_cfg(cfg), _p(logits), _p(bias), _p(topk_idx), _p(topk_w), _p(load), _s(stream)),
+           "moe_router_fwd")
+
+
+def moe_router_bwd(cfg, logits, topk_idx, dw, dlogits, stream=None):
+    _check(lib().moe_router_bwd(_cfg(cfg), _p(logits), _p(topk_idx), _p(dw), _p(dlogits), _s(stream)), "moe_router_bwd")
+
+
+class MoEW4Config(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("k", ctypes.c_int32), ("E", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("N", ctypes.c_int32), ("dtype", ctypes.c_int32), ("out", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("per_choice", ctypes.c_int32), ("combine", ctypes.c_int32), ("gelu", ctypes.c_int32),
+                ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64)]
+
+
+def make_w4_config(T, k, E, K, N, dtype=MOE_BF16, out=MOE_BF16, group=0, per_choice=0, combine=0, gelu=0, ldx=0,
+                   ldy=0) -> MoEW4Config:
+    return MoEW4Config(int(T), int(k), int(E), int(K), int(N), int(dtype), int(out), int(group), int(per_choice),
+                       int(combine), int(gelu), int(ldx), int(ldy))
+
+
+def moe_w4_scratch_bytes(cfg: MoEW4Config) -> int:
+    v = ctypes.c_size_t(0)
+    _check(lib().moe_w4_scratch_bytes(_cfg(cfg), ctypes.byref(v)), "moe_w4_scratch_bytes")
+    return v.value
+
+
+def moe_w4_product(cfg, x, x_scales, topk_idx, topk_w, Wq, Ws, y, scratch=None, stream=None):
+    _check(lib().moe_w4_product(_cfg(cfg), _p(x), _p(x_scales), _p(topk_idx), _p(topk_w), _p(Wq), _p(Ws), _p(y),
+                                _p(scratch), _s(stream)), "moe_w4_product")
+
+
+def moe_w4_quantize(E, K, N, dtype, W, Wq, Ws, stream=None):
+    _check(lib().moe_w4_quantize(ctypes.c_int32(E), ctypes.c_int32(K), ctypes.c_int32(N), ctypes.c_int32(dtype), _p(W),
+                                 _p(Wq), _p(Ws), _s(stream)), "moe_w4_quantize")

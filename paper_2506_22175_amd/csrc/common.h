@@ -156,7 +156,8 @@ enum ProfKind {
     PK_GEMM_DGRAD = 3,   // dZ W1^T -> dDI                (NT, plain store)
     PK_GEMM_WGRAD = 4,   // both weight gradients         (TN, float accumulate)
     PK_DISPATCH = 5, PK_COMBINE = 6, PK_DISPATCH_BWD = 7, PK_ROUTE = 8, PK_SLOTS = 9, PK_GATE_BWD = 10,
-    PK_COUNT = 11
+    PK_NORM = 11, PK_NORM_BWD = 12, PK_ROUTER = 13, PK_ROUTER_BWD = 14, PK_W4 = 15,
+    PK_COUNT = 16
 };
 struct ProfScope {
     int idx; hipStream_t s;

@@ -1,0 +1,518 @@
+// Root-mean-square norm behind the residual's addition, and its backward pass.
+//
+//   forward   h = x + r,  rstd = 1 / sqrt(mean(h^2) + eps),  y = h rstd g
+//   backward  n = h rstd,  dx = dh + rstd (g dy - n mean(g dy n)),  dg = sum over rows of dy n
+//
+// Both move each row once and are bound by memory: a row stays in the registers of the threads that loaded it, from the
+// loads through the row's sum to the stores, so nothing is read twice.  A row is dealt out in units of eight columns (16
+// bytes of bfloat16), one or several to a thread; a wavefront has a row to itself as long as that is enough threads, which
+// leaves no barrier in the row's sum.  Rows need the alignment of their elements only: the hardware does wide accesses
+// at any address, and a row's last unit, if it is not full, goes element by element.
+#include "common.h"
+#include "wide.h"
+#include <cmath>
+
+namespace moe {
+
+namespace {
+
+template <int ALIGN> using Any16 = Anywhere<16, ALIGN>;
+using Any8 = Anywhere<8, 1>;
+
+// eight columns as stored
+template <typename T> struct Unit8;
+template <> struct Unit8<bf16_t> {
+    Any16<2> u;
+    __device__ __forceinline__ void load(const bf16_t* p, int left) {
+        if (left >= 8) {
+            u = *reinterpret_cast<const Any16<2>*>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned lo = 2 * i < left ? p[2 * i] : 0, hi = 2 * i + 1 < left ? p[2 * i + 1] : 0;
+                u.w[i] = lo | hi << 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void zero() { u.w[0] = u.w[1] = u.w[2] = u.w[3] = 0; }
+    __device__ __forceinline__ float at(int i) const { return __uint_as_float((i & 1) ? u.w[i / 2] & 0xffff0000u : u.w[i / 2] << 16); }
+    static __device__ __forceinline__ void store(bf16_t* p, const float* v, int left) {
+        if (left >= 8) {
+            Any16<2> o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o.w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            *reinterpret_cast<Any16<2>*>(p) = o;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) p[i] = f32_to_bf16(v[i]);
+        }
+    }
+};
+template <> struct Unit8<float> {
+    Any16<4> u[2];
+    __device__ __forceinline__ void load(const float* p, int left) {
+        if (left >= 8) {
+            u[0] = reinterpret_cast<const Any16<4>*>(p)[0];
+            u[1] = reinterpret_cast<const Any16<4>*>(p)[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i / 4].w[i % 4] = i < left ? __float_as_uint(p[i]) : 0u;
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i / 4].w[i % 4] = 0;
+    }
+    __device__ __forceinline__ float at(int i) const { return __uint_as_float(u[i / 4].w[i % 4]); }
+    static __device__ __forceinline__ void store(float* p, const float* v, int left) {
+        if (left >= 8) {
+            Any16<4> o[2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i / 4].w[i % 4] = __float_as_uint(v[i]);
+            reinterpret_cast<Any16<4>*>(p)[0] = o[0];
+            reinterpret_cast<Any16<4>*>(p)[1] = o[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) p[i] = v[i];
+        }
+    }
+};
+
+__device__ __forceinline__ void load_gain(const float* gain, int col, int left, float* g) {
+    if (!gain) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = 1.0f;
+        return;
+    }
+    Unit8<float> u;
+    u.load(gain + col, left);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = u.at(i);
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+__device__ __forceinline__ unsigned wave_max(unsigned v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        const unsigned o = (unsigned)__shfl_xor((int)v, off, 64);
+        v = v > o ? v : o;
+    }
+    return v;
+}
+// over the 16 lanes whose units make 128 columns: rotations inside a row of lanes
+template <int ROTATE> __device__ __forceinline__ unsigned max_rotated(unsigned v) {
+    const unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + ROTATE, 0xf, 0xf, false);
+    return v > o ? v : o;
+}
+__device__ __forceinline__ unsigned max_of_16(unsigned v) {
+    return max_rotated<1>(max_rotated<2>(max_rotated<4>(max_rotated<8>(v))));
+}
+
+// sum / largest over the threads of a row (one wavefront, or the workgroup's waves through `s`)
+template <int WAVES> __device__ __forceinline__ float row_sum(float v, float* s) {
+    v = wave_sum(v);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) v += s[i];
+        __syncthreads();
+    }
+    return v;
+}
+template <int WAVES> __device__ __forceinline__ unsigned row_max(unsigned v, float* s) {
+    v = wave_max(v);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __uint_as_float(v);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const unsigned o = __float_as_uint(s[i]);
+            v = v > o ? v : o;
+        }
+        __syncthreads();
+    }
+    return v;
+}
+
+struct NormArgs {
+    const void* x; const void* r; const float* gain; void* h; void* y; float* scales; float* rstd;
+    long long ldx, ldr, ldh, ldy;
+    int T, M, group, n_scales;
+    float eps;
+};
+
+constexpr float E4M3_MOST = 448.0f;
+
+// The magnitudes' bits order like the magnitudes, infinities above all numbers and NaN above those, so that a NaN is the
+// largest of its group and makes the scale NaN.
+__device__ __forceinline__ float scale_of(unsigned bits) {
+    const float s = __uint_as_float(bits) / E4M3_MOST;
+    return s < 1.17549435e-38f ? 1.17549435e-38f : s;
+}
+
+// WAVES wavefronts a row, UNITS units of eight columns a thread; four rows to a workgroup of 256 where WAVES = 1
+template <typename T, bool E4M3, int WAVES, int UNITS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(NormArgs a) {
+    constexpr int ROWS = WAVES == 1 ? 4 : 1, THREADS = WAVES * 64;
+    __shared__ float s_part[WAVES > 1 ? WAVES : 1];
+    const long long row = (long long)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
+    if (row >= a.T) return;                                // whole wavefronts, and only where a row is one
+    const int tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
+    const T* r = a.r ? reinterpret_cast<const T*>(a.r) + row * a.ldr : nullptr;
+    Unit8<T> ux[UNITS], ur[UNITS];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const int col = (u * THREADS + tid) * 8, left = a.M - col;
+        ux[u].zero();
+        if (left > 0) ux[u].load(x + col, left);
+    }
+    if (r) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            ur[u].zero();
+            if (left > 0) ur[u].load(r + col, left);
+        }
+    }
+    float h[UNITS][8], sum = 0.0f;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[u][i] = r ? ux[u].at(i) + ur[u].at(i) : ux[u].at(i);
+            sum = fmaf(h[u][i], h[u][i], sum);
+        }
+    if (a.h) {
+        T* ho = reinterpret_cast<T*>(a.h) + row * a.ldh;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            if (left > 0) Unit8<T>::store(ho + col, h[u], left);
+        }
+    }
+    sum = row_sum<WAVES>(sum, s_part);
+    const float rstd = 1.0f / sqrtf(sum / (float)a.M + a.eps);
+    if (a.rstd && tid == 0) a.rstd[row] = rstd;
+    unsigned most[UNITS], row_most = 0;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const int col = (u * THREADS + tid) * 8, left = a.M - col;
+        most[u] = 0;
+        if (left <= 0) {
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[u][i] = 0.0f;   // columns past the row's end: not the NaN of 0 * a row's NaN
+            }
+            continue;
+        }
+        float g[8];
+        load_gain(a.gain, col, left, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[u][i] = h[u][i] * rstd * g[i];
+            if constexpr (E4M3) {
+                const unsigned m = __float_as_uint(h[u][i]) & 0x7fffffffu;
+                if (i < left && m > most[u]) most[u] = m;
+            }
+        }
+        if constexpr (!E4M3) Unit8<T>::store(reinterpret_cast<T*>(a.y) + row * a.ldy + col, h[u], left);
+    }
+    if constexpr (E4M3) {
+        if (a.group) {
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) most[u] = max_of_16(most[u]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) row_most = row_most > most[u] ? row_most : most[u];
+            row_most = row_max<WAVES>(row_most, s_part);
+        }
+        unsigned char* y = reinterpret_cast<unsigned char*>(a.y) + row * a.ldy;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            if (left <= 0) continue;
+            const float scale = scale_of(a.group ? most[u] : row_most);
+            if (a.group ? (tid & 15) == 0 : u == 0 && tid == 0) a.scales[row * a.n_scales + (a.group ? col >> 7 : 0)] = scale;
+            // y / scale as a product with the reciprocal: the quotient may be a unit in its 24th bit off, which moves a value
+            // only where it lies that close to the middle of two of the type's
+            const float inv = 1.0f / scale;
+            Any8 o;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                int w = __builtin_amdgcn_cvt_pk_fp8_f32(h[u][4 * q] * inv, h[u][4 * q + 1] * inv, 0, false);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(h[u][4 * q + 2] * inv, h[u][4 * q + 3] * inv, w, true);
+                o.w[q] = (unsigned)w;
+            }
+            if (left >= 8) {
+                *reinterpret_cast<Any8*>(y + col) = o;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < left) y[col + i] = (unsigned char)(o.w[i / 4] >> (8 * (i % 4)));
+            }
+        }
+    }
+}
+
+struct NormBwdArgs {
+    const void* dy; const void* h; const float* gain; const float* rstd; const void* dh; void* dx;
+    float* part;          // [gridDim.x, M] sums of the gain's gradient; one workgroup: the gradient itself
+    long long ldx, ldh, ldy;
+    int T, M, add;        // add: part is added to (one workgroup)
+};
+
+// Each wavefront (WAVES = 1) or workgroup takes every gridDim-th row and keeps its sums of the gain's gradient in registers.
+template <typename T, int WAVES, int UNITS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_bwd_kernel(NormBwdArgs a) {
+    constexpr int ROWS = WAVES == 1 ? 4 : 1, THREADS = WAVES * 64;
+    __shared__ float s_part[WAVES > 1 ? WAVES : 1];
+    __shared__ float s_dg[WAVES == 1 ? 3 * UNITS * THREADS * 8 : 1];
+    const int tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int sub = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    float dg[UNITS][8];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dg[u][i] = 0.0f;
+    for (long long row = (long long)blockIdx.x * ROWS + sub; row < a.T; row += (long long)gridDim.x * ROWS) {
+        const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.ldy;
+        const T* hp = reinterpret_cast<const T*>(a.h) + row * a.ldh;
+        const T* dh = a.dh ? reinterpret_cast<const T*>(a.dh) + row * a.ldh : nullptr;
+        Unit8<T> ud[UNITS], uh[UNITS], ub[UNITS];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            ud[u].zero();
+            uh[u].zero();
+            if (left > 0) {
+                ud[u].load(dy + col, left);
+                uh[u].load(hp + col, left);
+            }
+        }
+        if (dh) {
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const int col = (u * THREADS + tid) * 8, left = a.M - col;
+                ub[u].zero();
+                if (left > 0) ub[u].load(dh + col, left);
+            }
+        }
+        const float rstd = a.rstd[row];
+        float sum = 0.0f;
+        // two passes over the registers: the gain comes from the L1 cache both times, which is cheaper than 8 UNITS registers
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            if (left <= 0) continue;
+            float g[8];
+            load_gain(a.gain, col, left, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = ud[u].at(i), n = uh[u].at(i) * rstd;
+                dg[u][i] = fmaf(d, n, dg[u][i]);
+                if (i < left) sum = fmaf(d * g[i], n, sum);
+            }
+        }
+        const float mean = row_sum<WAVES>(sum, s_part) / (float)a.M;
+        T* dx = reinterpret_cast<T*>(a.dx) + row * a.ldx;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            if (left <= 0) continue;
+            float g[8], o[8];
+            load_gain(a.gain, col, left, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = ud[u].at(i), n = uh[u].at(i) * rstd;
+                o[i] = rstd * fmaf(-n, mean, d * g[i]);
+                if (dh) o[i] += ub[u].at(i);
+            }
+            Unit8<T>::store(dx + col, o, left);
+        }
+    }
+    if (!a.part) return;
+    if constexpr (WAVES == 1) {
+        // the four wavefronts' sums, in their order
+        if (sub > 0) {
+            float* s = s_dg + (sub - 1) * UNITS * THREADS * 8;
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[(u * 8 + i) * THREADS + tid] = dg[u][i];
+        }
+        __syncthreads();
+        if (sub > 0) return;
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dg[u][i] += s_dg[q * UNITS * THREADS * 8 + (u * 8 + i) * THREADS + tid];
+    }
+    float* part = a.part + (long long)blockIdx.x * a.M;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const int col = (u * THREADS + tid) * 8, left = a.M - col;
+        if (left <= 0) continue;
+        if (a.add) {
+            Unit8<float> old;
+            old.load(part + col, left);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dg[u][i] += old.at(i);
+        }
+        Unit8<float>::store(part + col, dg[u], left);
+    }
+}
+
+// dgain (+)= the sums of `parts` workgroups, 32 columns to a workgroup: 32 threads a column, each takes every 32nd part
+constexpr int DG_COLS = 32, DG_SPLIT = 32;
+__global__ __launch_bounds__(DG_COLS * DG_SPLIT) void norm_dgain_kernel(const float* __restrict__ part, int parts, int M, int add,
+                                                                        float* __restrict__ dgain) {
+    __shared__ float s[DG_SPLIT][DG_COLS + 1];
+    const int c = threadIdx.x % DG_COLS, q = threadIdx.x / DG_COLS;
+    const int col = blockIdx.x * DG_COLS + c;
+    float v = 0.0f;
+    if (col < M) {
+#pragma unroll 8
+        for (int p = q; p < parts; p += DG_SPLIT) v += part[(long long)p * M + col];
+    }
+    s[q][c] = v;
+    __syncthreads();
+    if (q == 0 && col < M) {
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DG_SPLIT; ++i) v += s[i][c];
+        dgain[col] = add ? dgain[col] + v : v;
+    }
+}
+
+struct NormDims { int T, M, es; long long ldx, ldr, ldh, ldy; int n_scales; };
+
+moe_status norm_dims(const moe_norm_config* c, NormDims* d) {
+    if (!c) return MOE_ERR_NULL;
+    if (c->T < 0 || c->M <= 0 || !(c->eps >= 0.0f) || !std::isfinite(c->eps)) return MOE_ERR_SHAPE;
+    if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_UNSUPPORTED;
+    if (c->out != c->dtype && c->out != MOE_E4M3) return MOE_ERR_UNSUPPORTED;
+    if (c->group != 0 && (c->group != 128 || c->out != MOE_E4M3)) return MOE_ERR_UNSUPPORTED;
+    if (c->grad_overwrite != 0 && c->grad_overwrite != 1) return MOE_ERR_UNSUPPORTED;
+    if (c->M > 32768) return MOE_ERR_UNSUPPORTED;
+    d->T = c->T; d->M = c->M; d->es = c->dtype == MOE_F32 ? 4 : 2;
+    const int64_t given[4] = {c->ldx, c->ldr, c->ldh, c->ldy};
+    long long* ld[4] = {&d->ldx, &d->ldr, &d->ldh, &d->ldy};
+    for (int i = 0; i < 4; ++i) {
+        if (given[i] != 0 && given[i] < c->M) return MOE_ERR_SHAPE;
+        *ld[i] = given[i] ? given[i] : c->M;
+    }
+    d->n_scales = c->group ? (c->M + 127) / 128 : 1;
+    return MOE_OK;
+}
+
+// How a row is dealt out: wavefronts per row and units per thread.
+struct RowPlan { int waves, units; };
+RowPlan norm_plan(int T, int M) {
+    const int units = (M + 7) / 8;
+    (void)T;
+    if (units <= 64) return {1, 1};
+    if (units <= 128) return {1, 2};
+    if (units <= 256) return {1, 4};
+    if (units <= 512) return {4, 2};
+    if (units <= 1024) return {4, 4};
+    if (units <= 2048) return {16, 2};
+    return {16, 4};
+}
+
+template <typename T, bool E4M3> void norm_launch(const NormArgs& a, RowPlan p, hipStream_t s) {
+#define NORM_CASE(W, U) if (p.waves == W && p.units == U) { \
+        norm_kernel<T, E4M3, W, U><<<W == 1 ? (a.T + 3) / 4 : a.T, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
+    NORM_CASE(1, 1) NORM_CASE(1, 2) NORM_CASE(1, 4) NORM_CASE(4, 2) NORM_CASE(4, 4) NORM_CASE(16, 2) NORM_CASE(16, 4)
+#undef NORM_CASE
+}
+
+template <typename T> void norm_bwd_launch(const NormBwdArgs& a, RowPlan p, int blocks, hipStream_t s) {
+#define NORM_CASE(W, U) if (p.waves == W && p.units == U) { \
+        norm_bwd_kernel<T, W, U><<<blocks, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
+    NORM_CASE(1, 1) NORM_CASE(1, 2) NORM_CASE(1, 4) NORM_CASE(4, 2) NORM_CASE(4, 4) NORM_CASE(16, 2) NORM_CASE(16, 4)
+#undef NORM_CASE
+}
+
+// Workgroups of the backward kernel.  Each leaves M floats of partial sums, so there are only as many as fill the chip.
+int norm_bwd_blocks(int T, RowPlan p) {
+    const int rows = p.waves == 1 ? 4 : 1;
+    const int want = (T + rows - 1) / rows, most = p.waves == 16 ? 512 : 1024;
+    return want < most ? want : most;
+}
+
+}  // namespace
+
+}  // namespace moe
+
+extern "C" moe_status moe_norm_fwd(const moe_norm_config* cfg, const void* x, const void* residual, const float* gain,
+                                   void* h, void* y, float* scales, float* rstd, void* stream) {
+    moe::NormDims d;
+    MOE_TRY(moe::norm_dims(cfg, &d));
+    if (d.T == 0) return MOE_OK;
+    if (!x || !y || (cfg->out == MOE_E4M3 && !scales)) return MOE_ERR_NULL;
+    moe::NormArgs a = {x, residual, gain, h, y, scales, rstd, d.ldx, d.ldr, d.ldh, d.ldy, d.T, d.M, cfg->group, d.n_scales, cfg->eps};
+    const moe::RowPlan p = moe::norm_plan(d.T, d.M);
+    hipStream_t s = (hipStream_t)stream;
+    {
+        moe::ProfScope prof(moe::PK_NORM, s);
+        if (cfg->dtype == MOE_F32) {
+            if (cfg->out == MOE_E4M3) moe::norm_launch<float, true>(a, p, s); else moe::norm_launch<float, false>(a, p, s);
+        } else {
+            if (cfg->out == MOE_E4M3) moe::norm_launch<moe::bf16_t, true>(a, p, s); else moe::norm_launch<moe::bf16_t, false>(a, p, s);
+        }
+    }
+    MOE_CHECK_LAUNCH();
+    moe::count_launch(moe::LC_OTHER);
+    return MOE_OK;
+}
+
+extern "C" moe_status moe_norm_scratch_bytes(const moe_norm_config* cfg, size_t* bytes) {
+    moe::NormDims d;
+    MOE_TRY(moe::norm_dims(cfg, &d));
+    if (!bytes) return MOE_ERR_NULL;
+    const int blocks = moe::norm_bwd_blocks(d.T, moe::norm_plan(d.T, d.M));
+    *bytes = blocks > 1 ? (size_t)blocks * d.M * sizeof(float) : 0;
+    return MOE_OK;
+}
+
+extern "C" moe_status moe_norm_bwd(const moe_norm_config* cfg, const void* dy, const void* h, const float* gain, const float* rstd,
+                                   const void* dh, void* dx, float* dgain, void* scratch, void* stream) {
+    moe::NormDims d;
+    MOE_TRY(moe::norm_dims(cfg, &d));
+    if (cfg->out == MOE_E4M3) return MOE_ERR_UNSUPPORTED;      // gradients of rounded rows are not defined here
+    const moe::RowPlan p = moe::norm_plan(d.T, d.M);
+    const int blocks = moe::norm_bwd_blocks(d.T, p);
+    if (d.T > 0 && (!dy || !h || !rstd || !dx)) return MOE_ERR_NULL;
+    if (dgain && blocks > 1 && !scratch) return MOE_ERR_NULL;
+    hipStream_t s = (hipStream_t)stream;
+    const int add = !cfg->grad_overwrite;
+    if (d.T == 0 && (!dgain || add)) return MOE_OK;
+    {
+        moe::ProfScope prof(moe::PK_NORM_BWD, s);
+        if (d.T > 0) {
+            const bool direct = blocks == 1;
+            moe::NormBwdArgs a = {dy, h, gain, rstd, dh, dx, dgain ? (direct ? dgain : (float*)scratch) : nullptr, d.ldx, d.ldh, d.ldy,
+                                  d.T, d.M, direct && add};
+            if (cfg->dtype == MOE_F32) moe::norm_bwd_launch<float>(a, p, blocks, s); else moe::norm_bwd_launch<moe::bf16_t>(a, p, blocks, s);
+            MOE_CHECK_LAUNCH();
+        }
+        if (dgain && blocks != 1) {
+            moe::norm_dgain_kernel<<<(d.M + moe::DG_COLS - 1) / moe::DG_COLS, moe::DG_COLS * moe::DG_SPLIT, 0, s>>>(
+                (const float*)scratch, blocks, d.M, add, dgain);
+            MOE_CHECK_LAUNCH();
+        }
+    }
+    moe::count_launch(moe::LC_OTHER);
+    return MOE_OK;
+}

@@ -1,0 +1,301 @@
+"""The router and its backward pass against the definition in 64 bits, token by token in numpy.
+
+Choices are whole numbers and have to be equal.  A weight's roundings: the exponential's argument x, whose product with log2(e) is
+rounded (1.45 |x| half steps) and whose exponential and the quotient's parts are a few units off, and a sum over E in lanes and levels
+(E / 16 + 5); 16 more cover the rest: (1.5 |x| + E / 16 + 24) * 2^-24 relative to the weight.
+
+Scores are 64-bit numbers here as in the definition, with errors of their own: where two different inputs lead to scores closer
+than 2^-49 of their size, neither order is wrong, and the token's choices are not compared."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_22175_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = B.MOE_F32, B.MOE_BF16
+DT = {F32: torch.float32, BF16: torch.bfloat16}
+NEG = -np.inf
+
+
+def reference(l, bias, k, sigmoid=0, groups=1, group_k=1, group_top=2, renorm=0, scale=1.0):
+    T, E = l.shape
+    l = np.where(np.isnan(l), NEG, l.astype(np.float64))
+    idx, w, decided = np.full((T, k), -1, np.int32), np.zeros((T, k)), np.ones(T, bool)
+    close = lambda a, b: abs(a) + abs(b) < np.inf and abs(a - b) <= 2.0 ** -49 * max(abs(a), abs(b))  # noqa: E731
+    given = lambda t, e: (l[t, e], bias[e] if bias is not None else 0.0)  # noqa: E731
+    with np.errstate(over="ignore", invalid="ignore"):
+        for t in range(T):
+            if sigmoid:
+                s = 1.0 / (1.0 + np.exp(-l[t]))
+            else:
+                m = l[t].max()
+                s = np.where(l[t] == m, 1.0, np.exp(l[t] - m)) if m > NEG else np.zeros(E)
+                s = np.where(l[t] == NEG, 0.0, s)
+                s = s / s.sum() if m > NEG else s
+            v = s + (bias.astype(np.float64) if bias is not None else 0.0)
+            open_ = (l[t] > NEG) & (v > NEG)
+            by = v if bias is not None else l[t]
+            if groups > 1:
+                size = E // groups
+                score, made_of = [], []
+                for g in range(groups):
+                    top = sorted((e for e in range(g * size, (g + 1) * size) if open_[e]), key=lambda e: -v[e])[:group_top]
+                    score.append(sum(v[e] for e in top) if top else NEG)
+                    made_of.append(sorted(given(t, e) for e in top))
+                ranked = sorted(range(groups), key=lambda g: (-score[g], g))
+                stay = ranked[:group_k]
+                decided[t] &= not any(close(score[g], score[o]) and made_of[g] != made_of[o] for g in stay for o in ranked[group_k:])
+                open_ &= np.isin(np.arange(E) // size, stay)
+            order = sorted((e for e in range(E) if open_[e]), key=lambda e: (-by[e], e))
+            decided[t] &= bias is None or not any(close(by[a], by[b]) and given(t, a) != given(t, b) for a, b in zip(order[:k], order[1:]))
+            order = order[:k]
+            idx[t, :len(order)] = order
+            if order:
+                if renorm:
+                    z = l[t][order]
+                    a = np.minimum(z, 0) - np.log1p(np.exp(-np.abs(z))) if sigmoid else np.where(z == z.max(), 0.0, z - z.max())
+                    q = np.exp(a - a.max())
+                    w[t, :len(order)] = q / q.sum() * scale
+                else:
+                    w[t, :len(order)] = s[order] * scale
+    return idx, w, decided
+
+
+def run(l, bias, k, dtype=F32, ld=0, load=False, **kw):
+    T, E = l.shape
+    cfg = B.make_router_config(T, E, k, kw.get("sigmoid", 0), kw.get("groups", 1), kw.get("group_k", 1), kw.get("group_top", 2),
+                               kw.get("renorm", 0), kw.get("scale", 1.0), dtype, ld)
+    idx, w = torch.full((T, k), -9, dtype=torch.int32, device=DEV), torch.full((T, k), -9.0, device=DEV)
+    counts = torch.full((E,), 3, dtype=torch.int32, device=DEV) if load else None
+    b = torch.from_numpy(bias).to(DEV) if bias is not None else None
+    B.moe_router_fwd(cfg, l, b, idx, w, counts)
+    torch.cuda.synchronize()
+    return (idx.cpu().numpy(), w.cpu().numpy()) + ((counts.cpu().numpy(),) if load else ())
+
+
+def check(l, bias, k, dtype=F32, **kw):
+    """l: a float32 array; compared as the storage type holds it."""
+    d = torch.from_numpy(l).to(DT[dtype]).to(DEV)
+    l = d.float().cpu().numpy()
+    idx, w, counts = run(d, bias, k, dtype, load=True, **kw)
+    ridx, rw, decided = reference(l, bias, k, **kw)
+    assert decided.mean() > 0.85 and np.array_equal(idx[decided], ridx[decided])
+    finite = l[np.isfinite(l)]
+    most = min(110.0, float(np.abs(finite).max()) * 2) if finite.size else 0.0     # below exp(-110) there is no float
+    off = np.abs(w - rw) <= rw * (1.5 * most + l.shape[1] / 16 + 24) * 2.0 ** -24 + 1e-37
+    assert off[decided].all()
+    assert np.array_equal(counts, 3 + np.bincount(idx[idx >= 0], minlength=l.shape[1]))
+
+
+def logits(T, E, seed, std=2.0):
+    return (np.random.default_rng(seed).standard_normal((T, E)) * std).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 2, 2), (3, 5, 3), (17, 16, 16), (33, 17, 2), (64, 33, 4), (100, 64, 8), (5, 65, 1),
+                                   (40, 128, 6), (31, 200, 8), (50, 256, 16), (3, 257, 8), (9, 512, 16)])
+def test_choices_and_weights(T, E, k, dtype):
+    bias = (0.2 * np.random.default_rng(E).standard_normal(E)).astype(np.float32)
+    for sigmoid in (0, 1):
+        for b in (None, bias):
+            for renorm in (0, 1):
+                check(logits(T, E, T + E + k), b, k, dtype, sigmoid=sigmoid, renorm=renorm, scale=2.5 if renorm else 1.0)
+
+
+@pytest.mark.parametrize("E,groups,group_k,k", [(64, 8, 4, 8), (256, 8, 4, 8), (24, 4, 1, 6), (33, 11, 3, 4), (100, 4, 2, 8),
+                                                (512, 16, 5, 16), (16, 16, 16, 16), (16, 16, 2, 2), (48, 2, 1, 3)])
+def test_groups(E, groups, group_k, k):
+    bias = (0.2 * np.random.default_rng(E + 1).standard_normal(E)).astype(np.float32)
+    for sigmoid in (0, 1):
+        for b in (None, bias):
+            for top in (1, 2):
+                check(logits(70, E, E + groups), b, k, sigmoid=sigmoid, groups=groups, group_k=group_k, group_top=top, renorm=1)
+
+
+def test_scores_that_float_cannot_tell_apart():
+    """Neighbouring floats as logits, and biases that undo a difference: only more bits than a float's say which is larger."""
+    rng = np.random.default_rng(0)
+    T, E, k = 400, 64, 8
+    base = rng.standard_normal((T, 1)).astype(np.float32)
+    l = np.repeat(base, E, 1)
+    steps = rng.integers(0, 4, (T, E))
+    for s in range(1, 4):
+        l = np.where(steps >= s, np.nextafter(l, np.float32(100)), l)
+    small = (rng.integers(-2, 3, E) * 1e-9).astype(np.float32)
+    for sigmoid in (0, 1):
+        check(l, None, k, sigmoid=sigmoid)
+        check(l, small, k, sigmoid=sigmoid)
+        check(l, small, k, sigmoid=sigmoid, groups=8, group_k=4)
+        check(l, None, k, sigmoid=sigmoid, groups=8, group_k=4)
+
+
+def test_ties_go_to_the_lower_index():
+    l = np.zeros((5, 96), np.float32)
+    l[1, 40:] = 1.0
+    l[2, ::3] = -1.0
+    for kw in (dict(), dict(sigmoid=1), dict(groups=8, group_k=2), dict(sigmoid=1, groups=4, group_k=1)):
+        check(l, None, 8, **kw)
+        check(l, np.zeros(96, np.float32), 8, **kw)
+    check(l.repeat(20, 0), np.full(96, 0.5, np.float32), 3, BF16, sigmoid=1)
+
+
+def test_masked_experts_infinities_and_nan():
+    l = logits(40, 64, 7)
+    l[0] = NEG                                            # nothing is left
+    l[1] = np.nan
+    l[2, 1:] = NEG                                        # one expert is left
+    l[3, :60] = NEG
+    l[4, 5] = np.inf
+    l[5, [3, 9]] = np.inf
+    l[6, ::2] = np.nan
+    l[7] = np.finfo(np.float32).min                       # masks of the type's lowest value
+    l[8, 4:] = np.finfo(np.float32).min
+    l[9] = np.inf
+    bias = (0.1 * np.random.default_rng(1).standard_normal(64)).astype(np.float32)
+    out = bias.copy()
+    out[[0, 5, 6]] = NEG
+    out[9] = np.nan
+    out[11] = np.inf
+    for sigmoid in (0, 1):
+        for renorm in (0, 1):
+            for b in (None, bias, out):
+                for kw in (dict(), dict(groups=8, group_k=3), dict(groups=16, group_k=2, group_top=1)):
+                    check(l, b, 6, sigmoid=sigmoid, renorm=renorm, **kw)
+    check(l, None, 6, BF16)
+
+
+def test_large_magnitudes_do_not_lose_the_weights():
+    l = (logits(30, 64, 8, 1.0) - 95.0).astype(np.float32)      # sigmoids near the least float
+    check(l, None, 4, sigmoid=1, renorm=1)
+    l = (logits(30, 64, 9, 30.0)).astype(np.float32)
+    check(l, None, 4, sigmoid=0)
+    check(l, None, 4, sigmoid=1, renorm=1)
+
+
+def test_strided_rows_at_any_alignment():
+    T, E, k = 21, 50, 4
+    flat = torch.randn(T * 53 + 60, generator=torch.Generator().manual_seed(1))
+    for dtype in (F32, BF16):
+        d = torch.as_strided(flat.to(DT[dtype]).to(DEV), (T, E), (53, 1), 3)
+        idx, w = run(d, None, k, dtype, 53)
+        ridx, rw, _ = reference(d.float().cpu().numpy(), None, k)
+        assert np.array_equal(idx, ridx) and np.allclose(w, rw, rtol=1e-5, atol=0)
+        dl_flat = torch.full((T * 53 + 60,), 7.0, device=DEV).to(DT[dtype])
+        dl = torch.as_strided(dl_flat, (T, E), (53, 1), 5)
+        B.moe_router_bwd(B.make_router_config(T, E, k, dtype=dtype, ld=53), d, torch.from_numpy(idx).to(DEV), torch.ones((T, k), device=DEV), dl)
+        dl.fill_(7.0)
+        assert (dl_flat == 7.0).all()
+
+
+def ref_backward(l, idx, dw, sigmoid, renorm, scale):
+    """In 64 bits, from the Jacobians."""
+    l = np.where(np.isnan(l), NEG, l.astype(np.float64))
+    out = np.zeros(l.shape)
+    size = np.zeros(l.shape)                              # sum of the magnitudes of the terms
+    for t in range(l.shape[0]):
+        pick = [(int(e), float(d) * scale) for e, d in zip(idx[t], dw[t]) if 0 <= e < l.shape[1]]
+        pick = [(e, d) for e, d in pick if l[t, e] > NEG]
+        if not pick:
+            continue
+        e, d = np.array([p[0] for p in pick]), np.array([p[1] for p in pick])
+        z = l[t, e]
+        if renorm:
+            a = np.minimum(z, 0) - np.log1p(np.exp(-np.abs(z))) if sigmoid else z
+            q = np.exp(a - a.max())
+            w = q / q.sum()
+            g, s = w * (d - (w * d).sum()), w * (np.abs(d) + (w * np.abs(d)).sum())
+            if sigmoid:
+                g, s = g / (1.0 + np.exp(z)), s / (1.0 + np.exp(z))
+            out[t, e], size[t, e] = g, s
+        elif sigmoid:
+            s = 1.0 / (1.0 + np.exp(-z))
+            out[t, e] = d * s / (1.0 + np.exp(z))
+            size[t, e] = np.abs(out[t, e])
+        else:
+            p = np.exp(l[t] - l[t].max())
+            p /= p.sum()
+            ds, ads = np.zeros(l.shape[1]), np.zeros(l.shape[1])
+            ds[e], ads[e] = d, np.abs(d)
+            out[t], size[t] = p * (ds - (ds * p).sum()), p * (ads + (ads * p).sum())
+    return out, size
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (3, 5, 3), (17, 16, 16), (33, 33, 2), (100, 64, 8), (40, 128, 6), (50, 256, 16), (9, 512, 16)])
+def test_backward(T, E, k, dtype):
+    rng = np.random.default_rng(T + E)
+    l = torch.from_numpy(logits(T, E, 3 * T + E)).to(DT[dtype])
+    if T > 5:
+        l[2, E // 2:] = NEG
+        l[3] = NEG
+        l[4, 0] = float("nan")
+    host = l.float().numpy()
+    dw = rng.standard_normal((T, k)).astype(np.float32)
+    for sigmoid in (0, 1):
+        for renorm in (0, 1):
+            idx = reference(host, None, k, sigmoid=sigmoid)[0]
+            if T > 8:
+                idx[7, 0], idx[8, 0] = -1, E              # no choice
+            dl = torch.full((T, E), float("nan"), device=DEV).to(DT[dtype])
+            B.moe_router_bwd(B.make_router_config(T, E, k, sigmoid, renormalize=renorm, scale=1.5, dtype=dtype), l.to(DEV),
+                             torch.from_numpy(idx).to(DEV), torch.from_numpy(dw).to(DEV), dl)
+            want, size = ref_backward(host, idx, dw, sigmoid, renorm, 1.5)
+            tol = (1.5 * 20 + E / 16 + 32) * 2.0 ** -24 * size + np.abs(want) * (0 if dtype == F32 else 2.0 ** -8) + 1e-37
+            assert (np.abs(dl.float().cpu().numpy() - want) <= tol).all(), (sigmoid, renorm)
+
+
+def test_gradients_against_differences():
+    l, k = logits(4, 12, 5, 1.0), 3
+    dw = np.random.default_rng(2).standard_normal((4, k)).astype(np.float32)
+    for sigmoid in (0, 1):
+        for renorm in (0, 1):
+            idx = reference(l, None, k, sigmoid=sigmoid)[0]
+
+            def loss(z):
+                s = 1.0 / (1.0 + np.exp(-z)) if sigmoid else np.exp(z) / np.exp(z).sum(1, keepdims=True)
+                w = np.take_along_axis(s, idx, 1)
+                return ((w / w.sum(1, keepdims=True) if renorm else w) * dw).sum()
+
+            dl = torch.empty((4, 12), device=DEV)
+            B.moe_router_bwd(B.make_router_config(4, 12, k, sigmoid, renormalize=renorm), torch.from_numpy(l).to(DEV),
+                             torch.from_numpy(idx).to(DEV), torch.from_numpy(dw).to(DEV), dl)
+            for t in range(4):
+                for e in range(12):
+                    d = np.zeros((4, 12))
+                    d[t, e] = 1e-5
+                    num = (loss(l.astype(np.float64) + d) - loss(l.astype(np.float64) - d)) / 2e-5
+                    assert abs(num - float(dl[t, e])) <= 1e-5
+
+
+def test_another_stream_and_a_graph_give_the_same():
+    T, E, k = 2000, 64, 4
+    l = torch.from_numpy(logits(T, E, 1)).to(DEV)
+    cfg = B.make_router_config(T, E, k)
+    idx, w, load = torch.empty((T, k), dtype=torch.int32, device=DEV), torch.empty((T, k), device=DEV), torch.zeros(E, dtype=torch.int32, device=DEV)
+    dl = torch.empty((T, E), device=DEV)
+
+    def both(stream=None):
+        B.moe_router_fwd(cfg, l, None, idx, w, load, stream)
+        B.moe_router_bwd(cfg, l, idx, w, dl, stream)
+
+    both()
+    torch.cuda.synchronize()
+    first = [v.clone() for v in (idx, w, dl, load)]
+    side = torch.cuda.Stream()
+    load.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    both(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((idx, w, dl, load), first))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for n in range(4):
+        idx.zero_(), w.zero_(), dl.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((idx, w, dl), first[:3])) and torch.equal(load, first[3] * (2 * n + 2))
+        both()                                            # the load goes on counting
+        torch.cuda.synchronize()
