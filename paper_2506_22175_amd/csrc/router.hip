@@ -3,15 +3,15 @@
 //   s = softmax(l) or sigmoid(l);  v = s + bias;  groups of experts rank by the sum of their largest v;  the k largest v (no
 //   bias: the largest l) among the groups that stay are chosen;  w = scale s [/ sum of the chosen s]
 //
-// A token is dealt out to LANES neighbouring lanes of a wavefront, VALUES logits to each, so that a choice is LANES-wide
-// maximum after maximum in registers, without LDS or barriers.  What bounds it is that selection: for each choice a lane
-// goes through its VALUES twice and the maximum travels through log2(LANES) lanes.  Few lanes with many values each need fewest
-// instructions per token; many lanes the shortest chain for a single token.
+// A token is dealt out to 16 neighbouring lanes of a wavefront, VALUES neighbouring logits to each, and its choice is one
+// maximum after another in registers: what a lane hands to the others goes through the vector unit's lane permutations,
+// without LDS or barriers.  What bounds it is that selection: for every choice a lane goes through its VALUES twice.
 //
 // Which of two experts comes first is defined by their exact scores, and float scores are some 2^-22 off.  So the scores
 // are compared in float, and where two that follow one another lie within that error (one token in a few hundred) the
 // wavefront's tokens are done again with 64-bit scores.
 #include "common.h"
+#include "wide.h"
 #include <cmath>
 
 namespace moe {
@@ -22,232 +22,437 @@ struct RouterArgs {
     const void* logits; const float* bias; int* idx; float* w; int* load;
     long long ld;
     int T, E, k, sigmoid, groups, group_k, group_top, renorm;
-    unsigned per_group;              // experts of a group
-    unsigned group_mul;              // e / per_group = e * group_mul >> 20 for e < 512
+    int group_lanes;                 // lanes that hold a group, if that is a whole number and a power of two, else 0
+    int exact_lanes;                 // the same with a token dealt out to 64 lanes, up to 16
+    unsigned group_mul;              // e / (experts of a group) = e * group_mul >> 20 for e < 512
     float scale;
 };
-
-template <typename F> struct Minus;
-template <> struct Minus<float> { static __device__ __forceinline__ float inf() { return -__builtin_inff(); } };
-template <> struct Minus<double> { static __device__ __forceinline__ double inf() { return -__builtin_inf(); } };
 
 __device__ __forceinline__ float exp_of(float x) { return __expf(x); }
 __device__ __forceinline__ double exp_of(double x) { return exp(x); }
 
-template <int LANES, typename V> __device__ __forceinline__ V lanes_max(V v) {
-#pragma unroll
-    for (int off = LANES / 2; off >= 1; off >>= 1) {
-        const V o = __shfl_xor(v, off, LANES);
-        v = o > v ? o : v;
-    }
-    return v;
+constexpr int LANES = 16;            // of a token: as many as there may be choices and groups
+constexpr int BLOCK = 512;
+
+// A lane's value of another lane of its 16: 1 and 2 away, mirrored in 8, mirrored in 16 (what is 4 and 8 away once the nearer
+// ones agree), or rotated.  All lanes add and compare the same pairs, so that all end with the same bits.
+template <int CTRL> __device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+template <int CTRL> __device__ __forceinline__ float from_lane(float v) { return __int_as_float(from_lane<CTRL>(__float_as_int(v))); }
+template <int CTRL> __device__ __forceinline__ double from_lane(double v) {
+    const long long b = __double_as_longlong(v);
+    return __longlong_as_double((long long)from_lane<CTRL>((int)(b >> 32)) << 32 | (unsigned)from_lane<CTRL>((int)b));
 }
-template <int LANES, typename V> __device__ __forceinline__ V lanes_sum(V v) {
-#pragma unroll
-    for (int off = LANES / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, LANES);
-    return v;
+constexpr int AWAY_1 = 0xB1, AWAY_2 = 0x4E, MIRROR_8 = 0x141, MIRROR_16 = 0x140, ROTATE = 0x120;
+
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
+__device__ __forceinline__ double smaller(double a, double b) { return fmin(a, b); }
+__device__ __forceinline__ int smaller(int a, int b) { return a < b ? a : b; }
+
+template <typename V> __device__ __forceinline__ V lanes_max(V v) {
+    v = larger(v, from_lane<AWAY_1>(v));
+    v = larger(v, from_lane<AWAY_2>(v));
+    v = larger(v, from_lane<MIRROR_8>(v));
+    return larger(v, from_lane<MIRROR_16>(v));
 }
-template <int LANES> __device__ __forceinline__ int lanes_min(int v) {
-#pragma unroll
-    for (int off = LANES / 2; off >= 1; off >>= 1) {
-        const int o = __shfl_xor(v, off, LANES);
-        v = o < v ? o : v;
-    }
-    return v;
+template <typename V> __device__ __forceinline__ V lanes_sum(V v) {
+    v += from_lane<AWAY_1>(v);
+    v += from_lane<AWAY_2>(v);
+    v += from_lane<MIRROR_8>(v);
+    return v + from_lane<MIRROR_16>(v);
+}
+__device__ __forceinline__ int lanes_min(int v) {
+    v = smaller(v, from_lane<AWAY_1>(v));
+    v = smaller(v, from_lane<AWAY_2>(v));
+    v = smaller(v, from_lane<MIRROR_8>(v));
+    return smaller(v, from_lane<MIRROR_16>(v));
 }
 
 constexpr int K_MOST = 16;
 
+// NaN counts as -inf.
 template <typename T> __device__ __forceinline__ float load_logit(const T* p) {
     const float v = Elem<T>::ld(p);
     return v != v ? -__builtin_inff() : v;
 }
-
-// The scores of a lane's logits.  -inf has none; infinite logits share a softmax evenly.
-template <typename F, int LANES, int VALUES>
-__device__ __forceinline__ void scores_of(const float* l, int sigmoid, F* s, F* largest) {
-    if (sigmoid) {
+// A lane's VALUES elements of a row of E; `past` where there are none.
+template <typename T, int VALUES> __device__ __forceinline__ void load_values(const T* row, int E, int lane, bool there, float past, float* l) {
+    constexpr int WIDE = VALUES < 16 / (int)sizeof(T) ? VALUES : 16 / (int)sizeof(T);       // elements of an access
+    if (there && (lane + 1) * VALUES <= E && WIDE * sizeof(T) >= 4) {
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v) s[v] = F(1) / (F(1) + exp_of(-F(l[v])));
-        *largest = F(1);
-        return;
+        for (int v = 0; v < VALUES; v += WIDE) {
+            constexpr int BYTES = WIDE * (int)sizeof(T) < 4 ? 4 : WIDE * (int)sizeof(T);
+            const auto u = *reinterpret_cast<const Anywhere<BYTES, (int)sizeof(T)>*>(row + lane * VALUES + v);
+#pragma unroll
+            for (int i = 0; i < WIDE; ++i) {
+                if constexpr (sizeof(T) == 4) l[v + i] = __uint_as_float(u.w[i]);
+                else l[v + i] = __uint_as_float((i & 1) ? u.w[i / 2] & 0xffff0000u : u.w[i / 2] << 16);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) {
+            const int e = lane * VALUES + v;
+            l[v] = there && e < E ? Elem<T>::ld(row + e) : past;
+        }
     }
+}
+template <typename T, int VALUES> __device__ __forceinline__ void load_logits(const T* row, int E, int lane, bool there, float* l) {
+    load_values<T, VALUES>(row, E, lane, there, -__builtin_inff(), l);
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) l[v] = l[v] != l[v] ? -__builtin_inff() : l[v];
+}
+
+// Of a softmax: the largest logit and 1 / the sum of exp(l - it).  Infinite logits share it evenly.
+template <typename F> struct Softmax { float m; F inv; };
+template <typename F> __device__ __forceinline__ F softmax_term(float l, float m) {
+    return l == -__builtin_inff() ? F(0) : l == m ? F(1) : exp_of(F(l) - F(m));
+}
+template <typename F, int VALUES> __device__ __forceinline__ Softmax<F> softmax_of(const float* l, F* s) {
     float m = l[0];
 #pragma unroll
     for (int v = 1; v < VALUES; ++v) m = fmaxf(m, l[v]);
-    m = lanes_max<LANES>(m);
+    m = lanes_max(m);
     F sum = F(0);
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) {
-        s[v] = l[v] == -__builtin_inff() ? F(0) : l[v] == m ? F(1) : exp_of(F(l[v]) - F(m));
+        s[v] = softmax_term<F>(l[v], m);
         sum += s[v];
     }
-    sum = lanes_sum<LANES>(sum);
+    sum = lanes_sum(sum);
     const F inv = sum > F(0) ? F(1) / sum : F(0);
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) s[v] *= inv;
-    *largest = inv;
+    return {m, inv};
 }
 
-// The choices of a wavefront's tokens in F.  Lane j of a token returns its j-th choice in *chosen (-1: none).  False in
-// any lane: float scores do not decide, nothing has been chosen.
-template <typename F, int LANES, int VALUES>
-__device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, F* s_chosen, int* chosen) {
-    constexpr bool FLOAT = sizeof(F) == 4;
-    const int lane = threadIdx.x & (LANES - 1);
-    F s[VALUES], rank[VALUES], largest;
-    scores_of<F, LANES, VALUES>(l, a.sigmoid, s, &largest);
-    const bool by_score = a.bias != nullptr;
+// first, second: the two largest of what was in them and of f >= q
+template <typename F> __device__ __forceinline__ void join_two(F& first, F& second, F f, F q) {
+    const F lo = smaller(first, f);
+    first = larger(first, f);
+    second = larger(larger(second, lo), q);
+}
+
+// The choices of a wavefront's four tokens by float scores: lane j of a token returns its j-th choice in *chosen (-1:
+// none).  False in a token's lanes: float scores do not decide.
+template <int VALUES>
+__device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, const float* bias, Softmax<float>* soft, int* chosen) {
+    constexpr float NONE = -__builtin_inff();
+    const int lane = threadIdx.x & (LANES - 1), e0 = lane * VALUES;
+    const bool by_score = a.bias != nullptr, scored = by_score || a.groups > 1;
+    // How far apart two scores have to be.  A sigmoid is less than 2.5 units of 2^-24 off (the exponential's rounded argument,
+    // itself, the sum, the reciprocal), a softmax's part 11 of them times the largest part (its exponential, and the sum's
+    // error, which all parts share but the bias does not), the sum with the bias half a unit of its size.
+    float rank[VALUES], error = 0x1p-21f;
+    if (scored || !a.sigmoid) {                       // a softmax's parts are wanted for the weights in any case
+        if (a.sigmoid) {
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) rank[v] = __builtin_amdgcn_rcpf(1.0f + __expf(-l[v]));
+        } else {
+            *soft = softmax_of<float, VALUES>(l, rank);
+            error = 0x1p-19f * soft->inv;
+        }
+    }
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) {
-        const int e = v * LANES + lane;
-        F r = s[v];
-        if (by_score && e < a.E) {
-            r += F(a.bias[e]);
-            if (!(r > Minus<F>::inf())) r = Minus<F>::inf();
+        if (by_score) {
+            rank[v] += bias[v];
+            if (!(rank[v] > NONE)) rank[v] = NONE;
         }
-        if (l[v] == -__builtin_inff() || e >= a.E) r = Minus<F>::inf();
-        rank[v] = r;
+        if (!scored) rank[v] = l[v];
+        if (l[v] == NONE) rank[v] = NONE;
     }
     bool sure = true;
-    unsigned long long stays = ~0ull;
     if (a.groups > 1) {
-        // Each lane keeps the two largest of its own v of every group; the lanes' pairs join by shuffles.
-        F mine = Minus<F>::inf();
-        for (int g = 0; g < a.groups; ++g) {
-            F first = Minus<F>::inf(), second = Minus<F>::inf();
+        float mine = NONE;                            // this lane's group's score; the slow way: that of group number `lane`
+        if (a.group_lanes) {
+            // a group is group_lanes (a power of two) whole lanes
+            float first = NONE, second = NONE;
 #pragma unroll
             for (int v = 0; v < VALUES; ++v) {
-                const unsigned e = v * LANES + lane;
-                const F r = (e * a.group_mul >> 20) == (unsigned)g ? rank[v] : Minus<F>::inf();
-                const F lo = r < first ? r : first;
-                first = r > first ? r : first;
-                second = lo > second ? lo : second;
+                second = larger(second, smaller(first, rank[v]));
+                first = larger(first, rank[v]);
             }
+            if (a.group_lanes > 1) join_two(first, second, from_lane<AWAY_1>(first), from_lane<AWAY_1>(second));
+            if (a.group_lanes > 2) join_two(first, second, from_lane<AWAY_2>(first), from_lane<AWAY_2>(second));
+            if (a.group_lanes > 4) join_two(first, second, from_lane<MIRROR_8>(first), from_lane<MIRROR_8>(second));
+            mine = a.group_top == 2 && second > NONE ? first + second : first;
+        } else {
+            for (int g = 0; g < a.groups; ++g) {
+                float first = NONE, second = NONE;
 #pragma unroll
-            for (int off = LANES / 2; off >= 1; off >>= 1) {
-                const F f = __shfl_xor(first, off, LANES), q = __shfl_xor(second, off, LANES);
-                const F lo = f < first ? f : first;
-                first = f > first ? f : first;
-                second = lo > second ? lo : second;
-                second = q > second ? q : second;
+                for (int v = 0; v < VALUES; ++v) {
+                    const float r = ((unsigned)(e0 + v) * a.group_mul >> 20) == (unsigned)g ? rank[v] : NONE;
+                    second = larger(second, smaller(first, r));
+                    first = larger(first, r);
+                }
+                join_two(first, second, from_lane<AWAY_1>(first), from_lane<AWAY_1>(second));
+                join_two(first, second, from_lane<AWAY_2>(first), from_lane<AWAY_2>(second));
+                join_two(first, second, from_lane<MIRROR_8>(first), from_lane<MIRROR_8>(second));
+                join_two(first, second, from_lane<MIRROR_16>(first), from_lane<MIRROR_16>(second));
+                const float score = a.group_top == 2 && second > NONE ? first + second : first;
+                if (lane == g) mine = score;
             }
-            const F score = a.group_top == 2 && second > Minus<F>::inf() ? first + second : first;
-            if (lane == g) mine = score;
         }
-        // a group stays if fewer than group_k others are ahead of it
+        // a group stays if fewer than group_k others are ahead of it; each lane meets all others by rotations
+        const int lanes = a.group_lanes ? a.group_lanes : 1;
+        const int group = a.group_lanes ? lane / a.group_lanes : lane;
         int ahead = 0;
-        const F most = lanes_max<LANES>(mine == mine && mine > Minus<F>::inf() && mine < -Minus<F>::inf() ? (mine < 0 ? -mine : mine) : F(0));
-        const F near = F(0x1p-19) * (F(2) * largest + most);
-        for (int g = 0; g < a.groups; ++g) {
-            const F o = __shfl(mine, g, LANES);
-            ahead += o > mine || (o == mine && g < lane);
-            if (FLOAT && lane < a.groups && g != lane && mine > Minus<F>::inf() && o > Minus<F>::inf()) {
-                const F d = o - mine;
-                sure = sure && (d > near || d < -near);
-            }
-        }
-        const unsigned long long b = __ballot(lane < a.groups && ahead < a.group_k);
-        stays = b >> ((threadIdx.x & 63) & ~(LANES - 1));
-    }
-    if (!by_score || a.groups > 1) {
+#define ROUTER_MEET(R) do { \
+            const float o = from_lane<ROTATE + R>(mine); \
+            const int og = from_lane<ROTATE + R>(group); \
+            ahead += o > mine || (o == mine && og < group); } while (0)
+        ROUTER_MEET(1); ROUTER_MEET(2); ROUTER_MEET(3); ROUTER_MEET(4); ROUTER_MEET(5);
+        ROUTER_MEET(6); ROUTER_MEET(7); ROUTER_MEET(8); ROUTER_MEET(9); ROUTER_MEET(10);
+        ROUTER_MEET(11); ROUTER_MEET(12); ROUTER_MEET(13); ROUTER_MEET(14); ROUTER_MEET(15);
+#undef ROUTER_MEET
+        const bool in = ahead < a.group_k * lanes;
+        // the last that stays and the first that does not; their scores are sums of two
+        const float last = -lanes_max(in && mine > NONE ? -mine : NONE), next = lanes_max(in ? NONE : mine);
+        sure = next == NONE || last - next > 2.0f * error + 0x1p-20f * fabsf(last);
+        const unsigned stays = (unsigned)(__ballot(in && group < a.groups) >> ((threadIdx.x & 63) & ~(LANES - 1))) & 0xffffu;
 #pragma unroll
         for (int v = 0; v < VALUES; ++v) {
-            const unsigned e = v * LANES + lane;
-            if (!by_score && rank[v] > Minus<F>::inf()) rank[v] = F(l[v]);
-            if (a.groups > 1 && !(stays >> (e * a.group_mul >> 20) & 1)) rank[v] = Minus<F>::inf();
+            const bool mine_in = a.group_lanes ? in : (stays >> ((unsigned)(e0 + v) * a.group_mul >> 20) & 1) != 0;
+            if (!by_score && rank[v] > NONE) rank[v] = l[v];
+            if (!mine_in) rank[v] = NONE;
         }
     }
-    // k + 1 maxima, so that the last choice too is compared with the next
-    const int rounds = FLOAT && by_score ? a.k + 1 : a.k;
-    F before = Minus<F>::inf();
     *chosen = -1;
-    *s_chosen = F(0);
-    for (int j = 0; j < rounds; ++j) {
-        F m = rank[0];
-#pragma unroll
-        for (int v = 1; v < VALUES; ++v) m = rank[v] > m ? rank[v] : m;
-        m = lanes_max<LANES>(m);
-        if (FLOAT && by_score) {
-            if (j > 0 && m > Minus<F>::inf()) {
-                const F size = before < 0 ? -before : before;
-                sure = sure && before - m > F(0x1p-20) * (F(2) * largest + size);   // infinite scores: not sure either
-            }
-            before = m;
-            if (j == a.k) break;
-        }
-        int at = 1 << 30;
-        if (m > Minus<F>::inf()) {
-#pragma unroll
-            for (int v = VALUES - 1; v >= 0; --v) at = rank[v] == m ? v * LANES + lane : at;
-        }
-        at = lanes_min<LANES>(at);
-        F won = F(0);
+    const int shift = (threadIdx.x & 63) & ~(LANES - 1);
+    if (by_score) {
+        // The lowest bits of a score give way to its place in the lane, so that the largest says by itself which it is and
+        // taking it out is one comparison; the error grows by as much.  k + 1 maxima: the last choice too is compared with the next.
+        constexpr int PLACE = VALUES - 1;
+        float before = NONE;
 #pragma unroll
         for (int v = 0; v < VALUES; ++v)
-            if (at == v * LANES + lane) {
-                rank[v] = Minus<F>::inf();
-                won = s[v];
+            rank[v] = rank[v] > NONE ? __uint_as_float((__float_as_uint(fminf(rank[v], 0x1.fffffep127f)) & ~(unsigned)PLACE) | v) : NONE;
+        for (int j = 0; j <= a.k; ++j) {
+            float mine = rank[0];
+#pragma unroll
+            for (int v = 1; v < VALUES; ++v) mine = larger(mine, rank[v]);
+            const float m = lanes_max(mine);
+            if (j > 0 && m > NONE) sure = sure && before - m > error + (0x1p-21f + 0x1p-23f * VALUES) * fabsf(before);
+            before = m;
+            if (j == a.k) break;
+            const unsigned owners = (unsigned)(__ballot(mine == m && m > NONE) >> shift) & 0xffffu;
+            const int owner = __builtin_ctz(owners | 0x10000u);
+            if (lane == owner) {
+#pragma unroll
+                for (int v = 0; v < VALUES; ++v) rank[v] = rank[v] == m ? NONE : rank[v];
             }
-        won = __shfl(won, at & (LANES - 1), LANES);
-        if (lane == j && at < a.E) {
-            *chosen = at;
-            *s_chosen = won;
+            if (lane == j && owner < LANES) *chosen = owner * VALUES + (int)(__float_as_uint(m) & PLACE);
+        }
+    } else {
+        for (int j = 0; j < a.k; ++j) {
+            float mine = rank[0];
+#pragma unroll
+            for (int v = 1; v < VALUES; ++v) mine = larger(mine, rank[v]);
+            const float m = lanes_max(mine);
+            int at = 1 << 30;
+#pragma unroll
+            for (int v = VALUES - 1; v >= 0; --v) at = rank[v] == m ? e0 + v : at;
+            at = m > NONE ? lanes_min(at) : 1 << 30;
+            const int won = at - e0;
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) rank[v] = won == v ? NONE : rank[v];
+            if (lane == j && at < a.E) *chosen = at;
         }
     }
-    return __all(sure);
+    return sure;
 }
 
-template <typename T, int LANES, int VALUES>
-__global__ __launch_bounds__(256) void router_kernel(RouterArgs a) {
-    constexpr int TOKENS = 256 / LANES;
+// a lane's value, the same for all (its number has to be)
+__device__ __forceinline__ int of_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float of_lane(float v, int lane) { return __int_as_float(of_lane(__float_as_int(v), lane)); }
+__device__ __forceinline__ double of_lane(double v, int lane) {
+    const long long b = __double_as_longlong(v);
+    return __longlong_as_double((long long)of_lane((int)(b >> 32), lane) << 32 | (unsigned)of_lane((int)b, lane));
+}
+template <typename V> __device__ __forceinline__ V wave_max(V v) {
+    v = lanes_max(v);
+    return larger(larger(of_lane(v, 0), of_lane(v, 16)), larger(of_lane(v, 32), of_lane(v, 48)));
+}
+
+// The choices of one token by 64-bit scores, by a whole wavefront: lane j returns the j-th.  Few tokens come here, but the
+// launch waits for the last one, so what counts is the length of the chain.
+template <typename T, int VALUES>
+__device__ __forceinline__ int choose_exactly(const RouterArgs& a, const T* row) {
+    constexpr double NONE = -__builtin_inf();
+    const int lane = threadIdx.x & 63, e0 = lane * VALUES;
+    const bool by_score = a.bias != nullptr;
+    double s[VALUES];
+    float l[VALUES], bias[VALUES], m = -__builtin_inff();
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        l[v] = e0 + v < a.E ? load_logit(row + e0 + v) : -__builtin_inff();
+        bias[v] = by_score && e0 + v < a.E ? a.bias[e0 + v] : 0.0f;
+    }
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) m = fmaxf(m, l[v]);
+    if (a.sigmoid) {
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) s[v] = 1.0 / (1.0 + exp(-(double)l[v]));
+    } else {
+        m = wave_max(m);
+        double sum = 0.0;
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) {
+            s[v] = softmax_term<double>(l[v], m);
+            sum += s[v];
+        }
+        sum = lanes_sum(sum);
+        sum = (of_lane(sum, 0) + of_lane(sum, 16)) + (of_lane(sum, 32) + of_lane(sum, 48));
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) s[v] = sum > 0.0 ? s[v] / sum : 0.0;
+    }
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        s[v] += (double)bias[v];
+        if (!(s[v] > NONE) || l[v] == -__builtin_inff()) s[v] = NONE;
+    }
+    if (a.groups > 1) {
+        double mine = NONE;                               // lane g: the score of group g
+        if (a.exact_lanes) {
+            // a group is exact_lanes (a power of two up to 16) whole lanes of the 64
+            double first = NONE, second = NONE;
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) {
+                second = larger(second, smaller(first, s[v]));
+                first = larger(first, s[v]);
+            }
+            if (a.exact_lanes > 1) join_two(first, second, from_lane<AWAY_1>(first), from_lane<AWAY_1>(second));
+            if (a.exact_lanes > 2) join_two(first, second, from_lane<AWAY_2>(first), from_lane<AWAY_2>(second));
+            if (a.exact_lanes > 4) join_two(first, second, from_lane<MIRROR_8>(first), from_lane<MIRROR_8>(second));
+            if (a.exact_lanes > 8) join_two(first, second, from_lane<MIRROR_16>(first), from_lane<MIRROR_16>(second));
+            const double score = a.group_top == 2 && second > NONE ? first + second : first;
+            mine = __shfl(score, lane * a.exact_lanes & 63, 64);
+            if (lane >= a.groups) mine = NONE;
+        } else for (int g = 0; g < a.groups; ++g) {
+            double first = NONE, second = NONE;
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) {
+                const double r = ((unsigned)(e0 + v) * a.group_mul >> 20) == (unsigned)g ? s[v] : NONE;
+                second = larger(second, smaller(first, r));
+                first = larger(first, r);
+            }
+            join_two(first, second, from_lane<AWAY_1>(first), from_lane<AWAY_1>(second));
+            join_two(first, second, from_lane<AWAY_2>(first), from_lane<AWAY_2>(second));
+            join_two(first, second, from_lane<MIRROR_8>(first), from_lane<MIRROR_8>(second));
+            join_two(first, second, from_lane<MIRROR_16>(first), from_lane<MIRROR_16>(second));
+            double f = of_lane(first, 0), q = of_lane(second, 0);
+            join_two(f, q, of_lane(first, 16), of_lane(second, 16));
+            join_two(f, q, of_lane(first, 32), of_lane(second, 32));
+            join_two(f, q, of_lane(first, 48), of_lane(second, 48));
+            const double score = a.group_top == 2 && q > NONE ? f + q : f;
+            if (lane == g) mine = score;
+        }
+        int ahead = 0;
+        for (int g = 0; g < a.groups; ++g) {
+            const double o = of_lane(mine, g);
+            ahead += o > mine || (o == mine && g < lane);
+        }
+        const unsigned stays = (unsigned)__ballot(lane < a.groups && ahead < a.group_k);
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v)
+            if (!(stays >> ((unsigned)(e0 + v) * a.group_mul >> 20) & 1)) s[v] = NONE;
+    }
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v)
+        if (!by_score && s[v] > NONE) s[v] = (double)l[v];
+    int chosen = -1;
+    for (int j = 0; j < a.k; ++j) {
+        double mine = s[0];
+#pragma unroll
+        for (int v = 1; v < VALUES; ++v) mine = larger(mine, s[v]);
+        const double most = wave_max(mine);
+        if (!(most > NONE)) break;
+        int at = 0;
+#pragma unroll
+        for (int v = VALUES - 1; v >= 0; --v) at = s[v] == most ? e0 + v : at;
+        at = of_lane(at, __builtin_ctzll(__ballot(mine == most)));       // the lowest lane has the lowest experts
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) s[v] = at == e0 + v ? NONE : s[v];
+        if (lane == j) chosen = at;
+    }
+    return chosen;
+}
+
+template <typename T, int VALUES>
+__global__ __launch_bounds__(BLOCK, VALUES <= 16 ? 4 : 2) void router_kernel(RouterArgs a) {
+    constexpr int TOKENS = BLOCK / LANES;
     __shared__ int hist[512];
     const int lane = threadIdx.x & (LANES - 1);
     if (a.load) {
-        for (int e = threadIdx.x; e < a.E; e += 256) hist[e] = 0;
+        for (int e = threadIdx.x; e < a.E; e += BLOCK) hist[e] = 0;
         __syncthreads();
     }
-    const long long t = (long long)blockIdx.x * TOKENS + threadIdx.x / LANES;
+    const long long base = (long long)blockIdx.x * TOKENS, t = base + threadIdx.x / LANES;
     const bool there = t < a.T;
     const T* row = reinterpret_cast<const T*>(a.logits) + (there ? t : 0) * a.ld;
-    float l[VALUES];
+    float l[VALUES], bias[VALUES];
 #pragma unroll
-    for (int v = 0; v < VALUES; ++v) {
-        const int e = v * LANES + lane;
-        l[v] = there && e < a.E ? load_logit(row + e) : -__builtin_inff();
-    }
+    for (int v = 0; v < VALUES; ++v) bias[v] = 0.0f;
+    if (a.bias) load_values<float, VALUES>(a.bias, a.E, lane, true, 0.0f, bias);
+    load_logits<T, VALUES>(row, a.E, lane, there, l);
     int chosen;
-    float s;
-    if (!choose<float, LANES, VALUES>(a, l, &s, &chosen)) {
-        double s64;
-        choose<double, LANES, VALUES>(a, l, &s64, &chosen);
-        s = (float)s64;
+    Softmax<float> soft = {0.0f, 0.0f};
+    const bool sure = choose<VALUES>(a, l, bias, &soft, &chosen);
+    unsigned long long unsure = __ballot(!sure && there);
+    while (unsure) {
+        const int token = __builtin_ctzll(unsure) / LANES;           // of the wavefront
+        unsure &= ~(0xffffull << (token * LANES));
+        const long long ut = base + (threadIdx.x >> 6) * (64 / LANES) + token;
+        const int c = choose_exactly<T, (VALUES + 3) / 4>(a, reinterpret_cast<const T*>(a.logits) + ut * a.ld);
+        const int mine = __shfl(c, lane, 64);
+        if (((threadIdx.x & 63) / LANES) == token) chosen = mine;
     }
-    float w = s;
+    const float z = chosen >= 0 ? load_logit(row + chosen) : -__builtin_inff();
+    float w;
     if (a.renorm) {
         // Scores that are all tiny are scaled up together before they are divided by their sum.
-        const float mine = chosen >= 0 ? Elem<T>::ld(row + chosen) : -__builtin_inff();
-        float m = lanes_max<LANES>(mine);
+        const float m = lanes_max(z);
         if (a.sigmoid) {
             const float shift = fminf(m, 0.0f);
-            w = mine >= 0.0f ? 1.0f / (1.0f + __expf(-mine)) : __expf(mine - shift) / (1.0f + __expf(mine));
+            w = z >= 0.0f ? 1.0f / (1.0f + __expf(-z)) : __expf(z - shift) / (1.0f + __expf(z));
         } else {
-            w = mine == m ? 1.0f : __expf(mine - m);
+            w = z == m ? 1.0f : __expf(z - m);
         }
         if (chosen < 0) w = 0.0f;
-        const float sum = lanes_sum<LANES>(w);
+        const float sum = lanes_sum(w);
         w = sum > 0.0f ? w / sum : 0.0f;
+    } else {
+        w = a.sigmoid ? 1.0f / (1.0f + __expf(-z)) : softmax_term<float>(z, soft.m) * soft.inv;
     }
     if (there && lane < a.k) {
         a.idx[t * a.k + lane] = chosen;
         a.w[t * a.k + lane] = w * a.scale;
-        if (a.load && chosen >= 0) atomicAdd(&hist[chosen], 1);           // whole numbers: the order does not matter
+        if (a.load && chosen >= 0) atomicAdd(&hist[chosen], 1);       // whole numbers: the order does not matter
     }
     if (a.load) {
         __syncthreads();
-        for (int e = threadIdx.x; e < a.E; e += 256)
+        for (int e = threadIdx.x; e < a.E; e += BLOCK)
             if (hist[e]) atomicAdd(&a.load[e], hist[e]);
     }
+}
+
+// load[e] += how often e is in idx.  For the router's own workgroups to add their counts up would take as long as they
+// have taken to choose: what they add meets in a few cache lines, which take a request about every 5 ns.
+__global__ __launch_bounds__(1024) void router_load_kernel(const int* __restrict__ idx, long long n, int E, int* __restrict__ load) {
+    __shared__ int hist[512];
+    for (int e = threadIdx.x; e < E; e += 1024) hist[e] = 0;
+    __syncthreads();
+    const long long step = (long long)gridDim.x * 1024;
+#pragma unroll 4
+    for (long long i = (long long)blockIdx.x * 1024 + threadIdx.x; i < n; i += step) {
+        const int e = idx[i];
+        if (e >= 0) atomicAdd(&hist[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += 1024)
+        if (hist[e]) atomicAdd(&load[e], hist[e]);
 }
 
 struct RouterBwdArgs {
@@ -259,28 +464,26 @@ struct RouterBwdArgs {
 
 // Lane j of a token holds its j-th choice: expert, logit and weight gradient.  Only a softmax over all experts needs the
 // other logits.
-template <typename T, int LANES, int VALUES>
+template <typename T, int VALUES>
 __global__ __launch_bounds__(256) void router_bwd_kernel(RouterBwdArgs a) {
     constexpr int TOKENS = 256 / LANES;
-    const int lane = threadIdx.x & (LANES - 1);
+    const int lane = threadIdx.x & (LANES - 1), e0 = lane * VALUES;
     const long long t = (long long)blockIdx.x * TOKENS + threadIdx.x / LANES;
     const bool there = t < a.T;
     const T* row = reinterpret_cast<const T*>(a.logits) + (there ? t : 0) * a.ld;
     const bool full = !a.sigmoid && !a.renorm;
-    float l[VALUES];
-    if (full) {
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) {
-            const int e = v * LANES + lane;
-            l[v] = there && e < a.E ? load_logit(row + e) : -__builtin_inff();
-        }
-    }
+    float s[VALUES];
+    if (full) load_logits<T, VALUES>(row, a.E, lane, there, s);
     int mine = there && lane < a.k ? a.idx[t * a.k + lane] : -1;
     if ((unsigned)mine >= (unsigned)a.E) mine = -1;
-    float d = mine >= 0 ? a.dw[t * a.k + lane] * a.scale : 0.0f;
-    float g = 0.0f;                                    // what the lane's choice contributes to its logit's gradient
-    float sub = 0.0f;                                  // softmax over all: sum of ds * s
-    if (!full) {
+    const float d = mine >= 0 ? a.dw[t * a.k + lane] * a.scale : 0.0f;
+    float g = d;                                       // what the lane's choice contributes to its logit's gradient
+    if (full) {
+        float l[VALUES];
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) l[v] = s[v];
+        softmax_of<float, VALUES>(l, s);
+    } else {
         const float z = mine >= 0 ? load_logit(row + mine) : -__builtin_inff();
         const bool open = z > -__builtin_inff();
         if (!a.renorm) {
@@ -288,7 +491,7 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(RouterBwdArgs a) {
             const float e = __expf(-fabsf(z)), q = 1.0f + e;
             g = open ? d * (e / (q * q)) : 0.0f;
         } else {
-            const float m = lanes_max<LANES>(z);
+            const float m = lanes_max(z);
             float w;
             if (a.sigmoid) {
                 const float shift = fminf(m, 0.0f);
@@ -297,44 +500,43 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(RouterBwdArgs a) {
                 w = z == m ? 1.0f : __expf(z - m);
             }
             if (!open) w = 0.0f;
-            const float sum = lanes_sum<LANES>(w);
+            const float sum = lanes_sum(w);
             w = sum > 0.0f ? w / sum : 0.0f;
-            const float inner = lanes_sum<LANES>(open ? w * d : 0.0f);
+            const float inner = lanes_sum(open ? w * d : 0.0f);
             g = open ? w * (d - inner) : 0.0f;
             if (a.sigmoid) g *= 1.0f / (1.0f + __expf(z));             // ds/dl = s (1 - s)
             if (!open) g = 0.0f;
         }
-    } else {
-        float largest;
-        float s[VALUES];
-        scores_of<float, LANES, VALUES>(l, 0, s, &largest);
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) l[v] = s[v];
-        g = d;
     }
     float ds[VALUES];
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) ds[v] = 0.0f;
     for (int j = 0; j < a.k; ++j) {
-        const int e = __shfl(mine, j, LANES);
+        const int at = __shfl(mine, j, LANES) - e0;
         const float q = __shfl(g, j, LANES);
 #pragma unroll
         for (int v = 0; v < VALUES; ++v)
-            if (e == v * LANES + lane) ds[v] = q;
+            if (at == v) ds[v] = q;
     }
     if (full) {
+        float sub = 0.0f;
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v) sub = fmaf(ds[v], l[v], sub);
-        sub = lanes_sum<LANES>(sub);
+        for (int v = 0; v < VALUES; ++v) sub = fmaf(ds[v], s[v], sub);
+        sub = lanes_sum(sub);
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v) ds[v] = l[v] * (ds[v] - sub);
+        for (int v = 0; v < VALUES; ++v) ds[v] = s[v] * (ds[v] - sub);
     }
     if (!there) return;
-    T* out = reinterpret_cast<T*>(a.dl) + t * a.ld;
+    T* out = reinterpret_cast<T*>(a.dl) + t * a.ld + e0;
 #pragma unroll
-    for (int v = 0; v < VALUES; ++v) {
-        const int e = v * LANES + lane;
-        if (e < a.E) Elem<T>::st(out + e, ds[v]);
+    for (int v = 0; v < VALUES; v += 4) {
+        if constexpr (VALUES >= 4) {
+            store_columns(out + v, ds + v, a.E - e0 - v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VALUES; ++i)
+                if (e0 + i < a.E) Elem<T>::st(out + i, ds[i]);
+        }
     }
 }
 
@@ -352,19 +554,30 @@ moe_status router_check(const moe_router_config* c) {
     return MOE_OK;
 }
 
-// Sixteen lanes to a token (as many as there may be choices and groups), as many values as the experts need.
-#define ROUTER_BY_EXPERTS(E, LAUNCH) do { \
-        if ((E) <= 16) { LAUNCH(16, 1); } else if ((E) <= 32) { LAUNCH(16, 2); } else if ((E) <= 64) { LAUNCH(16, 4); } \
-        else if ((E) <= 128) { LAUNCH(16, 8); } else if ((E) <= 256) { LAUNCH(16, 16); } else { LAUNCH(16, 32); } } while (0)
+// As many values to a lane as the experts need.
+int router_values(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <= 128 ? 8 : E <= 256 ? 16 : 32; }
+#define ROUTER_BY_VALUES(E, LAUNCH) do { switch (router_values(E)) { \
+        case 1: LAUNCH(1); break; case 2: LAUNCH(2); break; case 4: LAUNCH(4); break; \
+        case 8: LAUNCH(8); break; case 16: LAUNCH(16); break; default: LAUNCH(32); } } while (0)
 
-template <typename T> void router_launch(const RouterArgs& a, hipStream_t s) {
-#define ROUTER_LAUNCH(L, V) router_kernel<T, L, V><<<(a.T + 256 / L - 1) / (256 / L), 256, 0, s>>>(a)
-    ROUTER_BY_EXPERTS(a.E, ROUTER_LAUNCH);
+// Workgroups of the router that still count by themselves.
+constexpr int COUNT_BLOCKS = 32;
+
+template <typename T> void router_launch(RouterArgs a, hipStream_t s) {
+    const int tokens = BLOCK / LANES, blocks = (a.T + tokens - 1) / tokens;
+    int* const load = a.load;
+    if (blocks > COUNT_BLOCKS) a.load = nullptr;
+#define ROUTER_LAUNCH(V) router_kernel<T, V><<<blocks, BLOCK, 0, s>>>(a)
+    ROUTER_BY_VALUES(a.E, ROUTER_LAUNCH);
 #undef ROUTER_LAUNCH
+    if (load && !a.load) {
+        const long long n = (long long)a.T * a.k, most = (n + 4095) / 4096;
+        router_load_kernel<<<most < COUNT_BLOCKS ? (int)most : COUNT_BLOCKS, 1024, 0, s>>>(a.idx, n, a.E, load);
+    }
 }
 template <typename T> void router_bwd_launch(const RouterBwdArgs& a, hipStream_t s) {
-#define ROUTER_LAUNCH(L, V) router_bwd_kernel<T, L, V><<<(a.T + 256 / L - 1) / (256 / L), 256, 0, s>>>(a)
-    ROUTER_BY_EXPERTS(a.E, ROUTER_LAUNCH);
+#define ROUTER_LAUNCH(V) router_bwd_kernel<T, V><<<(a.T + 256 / LANES - 1) / (256 / LANES), 256, 0, s>>>(a)
+    ROUTER_BY_VALUES(a.E, ROUTER_LAUNCH);
 #undef ROUTER_LAUNCH
 }
 
@@ -377,9 +590,13 @@ extern "C" moe_status moe_router_fwd(const moe_router_config* cfg, const void* l
     MOE_TRY(moe::router_check(cfg));
     if (cfg->T == 0) return MOE_OK;
     if (!logits || !topk_idx || !topk_w) return MOE_ERR_NULL;
-    const unsigned per = (unsigned)(cfg->E / cfg->groups);
+    const int per = cfg->E / cfg->groups, values = moe::router_values(cfg->E);
+    // lanes that hold a group, where that is a power of two
+    auto whole = [per](int v) { return per % v == 0 && ((per / v) & (per / v - 1)) == 0 ? per / v : 0; };
+    const int exact = whole((values + 3) / 4);
     moe::RouterArgs a = {logits, bias, topk_idx, topk_w, load, cfg->ld ? (long long)cfg->ld : (long long)cfg->E, cfg->T, cfg->E, cfg->k,
-                         cfg->scores == MOE_SIGMOID, cfg->groups, cfg->group_k, cfg->group_top, cfg->renormalize, per,
+                         cfg->scores == MOE_SIGMOID, cfg->groups, cfg->group_k, cfg->group_top, cfg->renormalize, whole(values),
+                         exact <= 16 ? exact : 0,
                          ((1u << 20) + per - 1) / per, cfg->scale};
     hipStream_t s = (hipStream_t)stream;
     {

@@ -166,6 +166,16 @@ def test_masked_experts_infinities_and_nan():
     check(l, None, 6, BF16)
 
 
+def test_a_score_of_nothing_is_a_choice_still():
+    """Scores that are zero, or below the normal floats, alone among what is left."""
+    l = np.full((6, 64), NEG, np.float32)
+    l[0, 37], l[1, 5], l[2, 63], l[3, [9, 50]], l[4, [12, 13]], l[5, 1] = -200, -95, -104, (-200, -3), (-94, -96), -1e30
+    for bias in (None, np.zeros(64, np.float32)):
+        check(l, bias, 2, sigmoid=1)
+        check(l, bias, 2)
+        check(l, bias, 2, sigmoid=1, groups=8, group_k=2, renorm=1)
+
+
 def test_large_magnitudes_do_not_lose_the_weights():
     l = (logits(30, 64, 8, 1.0) - 95.0).astype(np.float32)      # sigmoids near the least float
     check(l, None, 4, sigmoid=1, renorm=1)
