@@ -427,8 +427,8 @@ moe_status moe_router_bwd(const moe_router_config* cfg, const void* logits, cons
  * 0, .5, 1, 1.5, 2, 3, 4, 6) in a byte, the lower column in the low half, and Ws [E, N, K/32] bytes: the exponents,
  * plus 127, of the powers of two that 32 columns share (byte 255: NaN). */
 typedef struct {
-    int32_t T, k, E;        /* k <= 64, E <= 4096, T * k <= 2^24; with combine T <= 65535; E * N * K may pass 2^31 */
-    int32_t K, N;           /* K a multiple of 32 */
+    int32_t T, k, E;        /* k <= 64, E <= 4096, T * k <= 2^24; with combine T <= 65535 */
+    int32_t K, N;           /* K a multiple of 32, N * K < 2^31 (E * N * K may be any) */
     int32_t dtype;          /* of x: MOE_F32, MOE_BF16 or MOE_E4M3 */
     int32_t out;            /* of y: MOE_F32 or MOE_BF16 */
     int32_t group;          /* MOE_E4M3: 128 columns of x share a scale, or 0: the row */
@@ -438,8 +438,8 @@ typedef struct {
     int64_t ldx, ldy;       /* row strides; ldx with MOE_F32 a multiple of 4, else of 8 (MOE_BF16) or 16 (MOE_E4M3) elements */
 } moe_w4_config;
 
-/* y[t,j] = f(x_row W[e]^T) * w[t,j] with e = topk_idx[t,j], or y[t] = their sum over j in ascending order; f is
- * GeLU or nothing.  Products are exact or those of float, sums float; nothing is rounded but y.
+/* y[t,j] = f(x_row W[e]^T) * w[t,j] with e = topk_idx[t,j], or y[t] = their sum over j, in an order that depends
+ * on the sizes alone; f is GeLU or nothing.  Products are exact or those of float, sums float; nothing is rounded but y.
  * An expert outside 0..E-1 contributes zeros.
  *   x [T or T*k, K], 16-byte aligned; x_scales [its rows, ceil(K/128) or 1] float (MOE_E4M3 only);
  *   topk_idx [T,k] int32, NULL: expert 0 for all; topk_w [T,k] float, NULL: ones;

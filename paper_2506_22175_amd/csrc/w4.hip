@@ -26,50 +26,48 @@ namespace {
 typedef __bf16 bf16x8_hw __attribute__((ext_vector_type(8)));
 typedef float f32x4_hw __attribute__((ext_vector_type(4)));
 
-constexpr int W4_WAVES = 4;
-
 struct W4Args {
     const void* x; const float* x_scales; const int* idx; const float* w; const uint8_t* Wq; const uint8_t* Ws;
     void* y;
     long long ldx, ldy;
     int n_rows;                      // T * k assignments
-    int k, E, K, N, n_scales, per_choice, gelu;
-    int by_choice;                   // blockIdx.y is an assignment (whose expert it serves if it is its first), else an expert
+    int k, E, K, N, n_scales, per_choice, gelu, out_f32;
 };
 
-// 32 columns of a routed row: the right operand's share of a lane
-template <int XT> struct Rows32;
-template <> struct Rows32<MOE_BF16> {
-    uint4 u[4];
-    __device__ __forceinline__ void load(const void* row, int col) {
-        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(row) + col);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = p[i];
-    }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = make_uint4(0, 0, 0, 0);
-    }
-    static constexpr int PARTS = 1;
-    __device__ __forceinline__ void parts(int i, bf16x8_hw* o) const { o[0] = __builtin_bit_cast(bf16x8_hw, u[i]); }
+__host__ __device__ constexpr int row_bytes(int xt, int cols) { return xt == MOE_F32 ? 4 * cols : xt == MOE_BF16 ? 2 * cols : cols; }
+__host__ __device__ constexpr int row_parts(int xt) { return xt == MOE_F32 ? 3 : 1; }
+
+// Eight columns of a routed row as the matrix instructions take them: PARTS times eight bfloat16.
+template <int XT> struct Rows8;
+template <> struct Rows8<MOE_BF16> {
+    uint4 u;
+    __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const char* p) { u = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void parts(uint4* o) const { o[0] = u; }
 };
-template <> struct Rows32<MOE_F32> {
-    float4 u[8];
-    __device__ __forceinline__ void load(const void* row, int col) {
-        const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(row) + col);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = p[i];
+template <> struct Rows8<MOE_E4M3> {
+    uint2 u;
+    __device__ __forceinline__ void zero() { u = make_uint2(0, 0); }
+    __device__ __forceinline__ void load(const char* p) { u = *reinterpret_cast<const uint2*>(p); }
+    __device__ __forceinline__ void parts(uint4* o) const {
+        o[0].x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u.x, 1.0f, false));
+        o[0].y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u.x, 1.0f, true));
+        o[0].z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u.y, 1.0f, false));
+        o[0].w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u.y, 1.0f, true));
     }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = make_float4(0, 0, 0, 0);
+};
+template <> struct Rows8<MOE_F32> {
+    float4 u[2];
+    __device__ __forceinline__ void zero() { u[0] = u[1] = make_float4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const char* p) {
+        u[0] = reinterpret_cast<const float4*>(p)[0];
+        u[1] = reinterpret_cast<const float4*>(p)[1];
     }
-    static constexpr int PARTS = 3;
     // Cut, not rounded: 8 + 8 + 8 bits of mantissa, exact, and no part is larger than the whole.  Infinities and NaN have
     // one part.
-    __device__ __forceinline__ void parts(int i, bf16x8_hw* o) const {
+    __device__ __forceinline__ void parts(uint4* o) const {
         unsigned hi[4], mid[4], lo[4];
-        const float v[8] = {u[2 * i].x, u[2 * i].y, u[2 * i].z, u[2 * i].w, u[2 * i + 1].x, u[2 * i + 1].y, u[2 * i + 1].z, u[2 * i + 1].w};
+        const float v[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             unsigned h[2], m[2], l[2];
@@ -87,38 +85,206 @@ template <> struct Rows32<MOE_F32> {
             mid[j] = m[0] >> 16 | m[1];
             lo[j] = l[0] >> 16 | l[1];
         }
-        o[0] = __builtin_bit_cast(bf16x8_hw, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-        o[1] = __builtin_bit_cast(bf16x8_hw, make_uint4(mid[0], mid[1], mid[2], mid[3]));
-        o[2] = __builtin_bit_cast(bf16x8_hw, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-    }
-};
-template <> struct Rows32<MOE_E4M3> {
-    uint4 u[2];
-    __device__ __forceinline__ void load(const void* row, int col) {
-        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row) + col);
-        u[0] = p[0];
-        u[1] = p[1];
-    }
-    __device__ __forceinline__ void zero() { u[0] = u[1] = make_uint4(0, 0, 0, 0); }
-    static constexpr int PARTS = 1;
-    __device__ __forceinline__ void parts(int i, bf16x8_hw* o) const {
-        const uint4& v = u[i / 2];
-        const unsigned a = i % 2 ? v.z : v.x, b = i % 2 ? v.w : v.y;
-        uint4 d;
-        d.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false));
-        d.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true));
-        d.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false));
-        d.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true));
-        o[0] = __builtin_bit_cast(bf16x8_hw, d);
+        o[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        o[1] = make_uint4(mid[0], mid[1], mid[2], mid[3]);
+        o[2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
 };
 
+// Eight columns of the 4-bit weights in `w` as bfloat16: exact, the scale is a power of two.
+__device__ __forceinline__ bf16x8_hw decode_weights(unsigned w, unsigned scale_byte) {
+    const float scale = __uint_as_float(scale_byte << 23);
+    uint4 d;
+    d.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+    d.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+    d.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+    d.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+    return __builtin_bit_cast(bf16x8_hw, d);
+}
+// Four lanes r, 16 + r, 32 + r, 48 + r with four dwords each: lane q's dword i becomes lane i's dword q.
+__device__ __forceinline__ void transpose_words(uint4& u) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 a = __builtin_amdgcn_permlane32_swap(u.x, u.z, false, false), b = __builtin_amdgcn_permlane32_swap(u.y, u.w, false, false);
+    const u32x2 c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    u = make_uint4(c[0], c[1], d[0], d[1]);
+}
+__device__ __forceinline__ unsigned word_of(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+
+// 32 columns of a weight row, or nothing: zeros.
+__device__ __forceinline__ uint4 load_weights(const uint8_t* Wq, int col, int K) {
+    return Wq && col < K ? *reinterpret_cast<const uint4*>(Wq + col / 2) : make_uint4(0, 0, 0, 0);
+}
+// The scales of TILES tiles of a weight row, a byte for each 32 columns; 1 where there are none.
+template <int TILES> __device__ __forceinline__ void load_scales(const uint8_t* Ws, int tile, int K, unsigned* s) {
+    if (Ws && (tile + TILES) * 128 <= K) {
+        const auto u = *reinterpret_cast<const Anywhere<4 * TILES, 1>*>(Ws + tile * 4);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) s[t] = u.w[t];
+    } else {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            s[t] = 0x7f7f7f7f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                if (Ws && (tile + t) * 128 + b * 32 < K) s[t] = (s[t] & ~(0xffu << (8 * b))) | (unsigned)Ws[(tile + t) * 4 + b] << (8 * b);
+        }
+    }
+}
+
+// A lane's weights of TILES consecutive tiles of 128 columns: lane (r, q) has columns 32 q .. 32 q + 31 of a tile in weight row r,
+// and the four scales of the row in each tile.
+template <int TILES> struct Weights {
+    uint4 u[TILES];
+    unsigned s[TILES];
+    // Wq, Ws: the weight row, NULL if there is none
+    __device__ __forceinline__ void load(const uint8_t* Wq, const uint8_t* Ws, int tile, int q, int K) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) u[t] = load_weights(Wq, (tile + t) * 128 + q * 32, K);
+        load_scales<TILES>(Ws, tile, K, s);
+    }
+    __device__ __forceinline__ bf16x8_hw decode(int t, int i, int q) const {
+        return decode_weights(word_of(u[t], i), s[t] >> (8 * q) & 0xffu);
+    }
+};
+
+__device__ __forceinline__ float w4_finish(float v, int gelu, float weight) {
+    if (gelu) v = v * (0.5f + 0.5f * erff(v * 0.70710678118654752440f));
+    return v * weight;
+}
+__device__ __forceinline__ void w4_store(const W4Args& a, long long row, int n, const float* v) {
+    if (a.out_f32) store_columns(reinterpret_cast<float*>(a.y) + row * a.ldy + n, v, a.N - n);
+    else store_columns(reinterpret_cast<bf16_t*>(a.y) + row * a.ldy + n, v, a.N - n);
+}
+
+// ---- one token ---------------------------------------------------------------------------------
+// A workgroup has 16 weight rows of one choice's expert (SUM: of all choices' experts, and adds them up), its wavefronts share out
+// the choices and K in pieces of 512 columns.  A piece of the routed row is one request of the wavefront and goes through LDS
+// that no other wavefront uses, from where all 16 columns of the right operand get the same.
+constexpr int TOKEN_TILES = 4;       // of a piece
+constexpr int TOKEN_WAVES = 16;      // at most
+
+template <int XT> struct TokenPiece {
+    Weights<TOKEN_TILES> w;
+    Rows8<XT> x;
+    float xs[TOKEN_TILES];
+    // row: of the assignment; xs_row: its scales
+    __device__ __forceinline__ void load(const uint8_t* Wq, const uint8_t* Ws, const char* row, const float* xs_row, int n_scales, int tile, int K) {
+        const int lane = threadIdx.x & 63, q = lane >> 4, col = tile * 128 + lane * 8;
+        w.load(Wq, Ws, tile, q, K);
+        x.zero();
+        if (col < K) x.load(row + row_bytes(XT, col));
+        if constexpr (XT == MOE_E4M3) {
+#pragma unroll
+            for (int t = 0; t < TOKEN_TILES; ++t) xs[t] = (tile + t) * 128 < K ? xs_row[n_scales > 1 ? tile + t : 0] : 0.0f;
+        }
+    }
+};
+
+template <int XT, bool SUM>
+__global__ __launch_bounds__(TOKEN_WAVES * 64) void w4_token_kernel(W4Args a, int slices) {
+    constexpr int PARTS = row_parts(XT);
+    __shared__ uint4 s_x[TOKEN_WAVES][PARTS][64];
+    __shared__ float4 s_sum[TOKEN_WAVES][4];
+    const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63, r = lane & 15, q = lane >> 4;
+    const int n0 = blockIdx.x * 16, n = n0 + r;
+    const int pieces = (a.K + 128 * TOKEN_TILES - 1) / (128 * TOKEN_TILES), waves = blockDim.x >> 6;
+    // the wavefront's choices: one, or (SUM, more choices than wavefronts) every `waves`-th
+    const int first = SUM ? wid / slices : (int)blockIdx.y, slice = SUM ? wid % slices : wid, step = waves / slices;
+    float4 sum = make_float4(0, 0, 0, 0);                 // SUM and slices = 1: of the wavefront's choices, weighted
+    for (int j = first; j < a.k; j += step) {
+        const int e = a.idx ? a.idx[j] : 0;
+        f32x4_hw acc = {0, 0, 0, 0};
+        if ((unsigned)e < (unsigned)a.E) {
+            const long long wrow = (long long)e * a.N + n, xr = a.per_choice ? j : 0;
+            const uint8_t* Wq = n < a.N ? a.Wq + wrow * (a.K / 2) : nullptr;
+            const uint8_t* Ws = n < a.N ? a.Ws + wrow * (a.K / 32) : nullptr;
+            const char* row = reinterpret_cast<const char*>(a.x) + xr * row_bytes(XT, 1) * a.ldx;
+            const float* xs_row = a.x_scales + xr * a.n_scales;
+            TokenPiece<XT> now, next;
+            if (slice < pieces) now.load(Wq, Ws, row, xs_row, a.n_scales, slice * TOKEN_TILES, a.K);
+            for (int piece = slice; piece < pieces; piece += slices) {
+                if (piece + slices < pieces) next.load(Wq, Ws, row, xs_row, a.n_scales, (piece + slices) * TOKEN_TILES, a.K);
+                uint4 p[PARTS];
+                now.x.parts(p);
+#pragma unroll
+                for (int c = 0; c < PARTS; ++c) s_x[wid][c][lane] = p[c];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int t = 0; t < TOKEN_TILES; ++t) {
+                    f32x4_hw part = XT == MOE_E4M3 ? f32x4_hw{0, 0, 0, 0} : acc;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bf16x8_hw d = now.w.decode(t, i, q);
+#pragma unroll
+                        for (int c = PARTS - 1; c >= 0; --c)
+                            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                d, __builtin_bit_cast(bf16x8_hw, s_x[wid][c][t * 16 + q * 4 + i]), part, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i] = XT == MOE_E4M3 ? fmaf(now.xs[t], part[i], acc[i]) : part[i];
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                now = next;
+            }
+        }
+        if (SUM && slices == 1) {
+            const float weight = a.w ? a.w[j] : 1.0f;
+            if ((unsigned)e < (unsigned)a.E) {
+                sum.x += w4_finish(acc[0], a.gelu, weight); sum.y += w4_finish(acc[1], a.gelu, weight);
+                sum.z += w4_finish(acc[2], a.gelu, weight); sum.w += w4_finish(acc[3], a.gelu, weight);
+            }
+        } else {
+            sum = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            break;
+        }
+    }
+    // every column has the row's sums
+    if (r == 0) s_sum[wid][q] = sum;
+    const int tq = tid & 3;                                // thread q < 4 will have columns n0 + 4 q .. + 3
+    const float weight = !SUM && a.w ? a.w[first] : 1.0f;
+    __syncthreads();
+    if (tid >= 4) return;
+    float v[4] = {0, 0, 0, 0};
+    if (!SUM || slices == 1) {
+        for (int w = 0; w < waves; ++w) {
+            const float4 p = s_sum[w][tq];
+            v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+        }
+        if (!SUM) {
+            // (an expert out of range has sums of zero, and GeLU keeps them)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = w4_finish(v[i], a.gelu, weight);
+            const int e = a.idx ? a.idx[first] : 0;
+            if ((unsigned)e >= (unsigned)a.E) v[0] = v[1] = v[2] = v[3] = 0.0f;      // whatever its weight
+        }
+    } else {
+        for (int j = 0; j < a.k; ++j) {
+            const int e = a.idx ? a.idx[j] : 0;
+            if ((unsigned)e >= (unsigned)a.E) continue;
+            const float wj = a.w ? a.w[j] : 1.0f;
+            float c[4] = {0, 0, 0, 0};
+            for (int w = 0; w < slices; ++w) {
+                const float4 p = s_sum[j * slices + w][tq];
+                c[0] += p.x; c[1] += p.y; c[2] += p.z; c[3] += p.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += w4_finish(c[i], a.gelu, wj);
+        }
+    }
+    if (n0 + 4 * tq < a.N) w4_store(a, SUM ? 0 : first, n0 + 4 * tq, v);
+}
+
+// ---- several tokens ----------------------------------------------------------------------------
+constexpr int W4_WAVES = 8;
+
 // Rows of assignments with expert e (e < 0: with none of the experts), number `from` to from + cap - 1 of them, into `list`;
 // returns how many there are in all.  Every thread of the workgroup calls it.
-__device__ int collect_rows(const int* idx, int n, int e, int E, int from, int cap, int* list, int* s_count) {
+template <int WAVES> __device__ int collect_rows(const int* idx, int n, int e, int E, int from, int cap, int* list, int* s_count) {
     const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
     int total = 0;
-    for (int base = 0; base < n; base += W4_WAVES * 64) {
+    for (int base = 0; base < n; base += WAVES * 64) {
         const int i = base + threadIdx.x;
         bool mine = false;
         if (i < n) {
@@ -130,7 +296,7 @@ __device__ int collect_rows(const int* idx, int n, int e, int E, int from, int c
         __syncthreads();
         int rank = total + __popcll(b & ((1ull << lane) - 1));
 #pragma unroll
-        for (int w = 0; w < W4_WAVES; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             if (w < wid) rank += s_count[w];
             total += s_count[w];
         }
@@ -140,158 +306,417 @@ __device__ int collect_rows(const int* idx, int n, int e, int E, int from, int c
     return total;
 }
 
-__device__ __forceinline__ void decode_weights(const uint4& q, float scale, int i, bf16x8_hw* o) {
-    const unsigned w = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
-    uint4 d;
-    d.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
-    d.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
-    d.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
-    d.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
-    *o = __builtin_bit_cast(bf16x8_hw, d);
+// Up to 32 rows to an expert, mostly: a wavefront has 64 weight rows and a share of K, which it streams by itself; `shares` of the
+// workgroup's wavefronts have the same weight rows and add up their sums at the end.  The routed rows come straight from the L2
+// cache, once for 64 weight rows.  With no barrier on the way and the next tile's requests out while one is multiplied, the
+// wavefronts of a compute unit keep some 64 KiB under way.  shares is such that the wavefronts fill the chip about once: each of
+// them pays the way to its first weights (its rows' numbers, their addresses, the first request) of some 5 us once.
+//
+// The unit that takes the requests apart was the limit here: it takes a cycle for every 64 bytes that neighbouring lanes have in
+// common, or every lane that stands alone.  So the four lanes of a weight row change words among themselves, after which an
+// instruction's columns are 32 neighbouring ones of the routed rows as well, and scales come for four tiles at a time.
+constexpr int FEW_WAVES = 4;
+
+// What a wavefront reads of a tile of 128 columns: TILES times 16 weight rows, RT times 16 routed rows.
+template <int XT, int TILES, int RT> struct FewTile {
+    uint4 w[TILES];
+    Rows8<XT> x[RT][4];              // of instruction i: columns 32 i + 8 q .. + 7
+    float xs[RT];
+    // A tile that is full: nothing is asked, so that all requests go out in one go.  offset[t]: of the lane's columns of tile 0 in
+    // its weight row of the 16 with number t; weight and routed rows past the last are the last again, and their sums of no use.
+    __device__ __forceinline__ void load(const uint8_t* Wq, const unsigned* offset, const char* const* row, const float* const* xs_row,
+                                         int n_scales, int tile, int q) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) w[t] = *reinterpret_cast<const uint4*>(Wq + (offset[t] + tile * 64));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[rt][i].load(row[rt] + row_bytes(XT, tile * 128 + 32 * i + 8 * q));
+            if (XT == MOE_E4M3) xs[rt] = xs_row[rt][n_scales > 1 ? tile : 0];
+        }
+    }
+    // The row's last columns, zeros behind them.
+    __device__ __forceinline__ void load_rest(const uint8_t* Wq, const unsigned* offset, const char* const* row, const float* const* xs_row,
+                                              int n_scales, int tile, int q, int K) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+            w[t] = tile * 128 + q * 32 < K ? *reinterpret_cast<const uint4*>(Wq + (offset[t] + tile * 64)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[rt][i].zero();
+                if (tile * 128 + 32 * i < K) x[rt][i].load(row[rt] + row_bytes(XT, tile * 128 + 32 * i + 8 * q));
+            }
+            if (XT == MOE_E4M3) xs[rt] = xs_row[rt][n_scales > 1 ? tile : 0];
+        }
+    }
+};
+
+// A wavefront's share: full tiles begin .. end - 1 of `tiles`, and what is behind those if it is its.
+struct FewShare { const uint8_t* Wq; const uint8_t* Ws; int n0, begin, end, tiles; bool rest; };
+
+// The sums of TILES x 16 weight rows with the first `here` rows of the list.
+template <int XT, int TILES, int RT>
+__device__ __forceinline__ void few_stream(const W4Args& a, const FewShare& f, const int* s_list, int here, f32x4_hw (*acc)[RT]) {
+    constexpr int PARTS = row_parts(XT);
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    unsigned offset[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+        const int n = f.n0 + t * 16 + r;
+        offset[t] = (unsigned)(n < a.N ? n : a.N - 1) * (unsigned)(a.K / 2) + q * 16;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[t][rt] = f32x4_hw{0, 0, 0, 0};
+    }
+    const char* row[RT];
+    const float* xs_row[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int at = s_list[rt * 16 + r < here ? rt * 16 + r : 0];
+        const long long xr = a.per_choice ? at : at / a.k;
+        row[rt] = reinterpret_cast<const char*>(a.x) + xr * row_bytes(XT, 1) * a.ldx;
+        xs_row[rt] = a.x_scales + xr * a.n_scales;
+    }
+    typedef FewTile<XT, TILES, RT> Tile;
+    constexpr int AHEAD = 1;                           // tiles under way behind the one that is multiplied
+    // scales: of weight row `lane` of the 64 in the tile
+    auto multiply = [&](Tile& v, unsigned scales) {
+        f32x4_hw part[TILES][RT];
+        unsigned s[TILES];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) part[t][rt] = XT == MOE_E4M3 ? f32x4_hw{0, 0, 0, 0} : acc[t][rt];
+            s[t] = (unsigned)__builtin_amdgcn_ds_bpermute((t * 16 + r) * 4, (int)scales);
+            transpose_words(v.w[t]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint4 p[RT][PARTS];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) v.x[rt][i].parts(p[rt]);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const bf16x8_hw d = decode_weights(word_of(v.w[t], i), s[t] >> (8 * i) & 0xffu);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int c = PARTS - 1; c >= 0; --c)
+                        part[t][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, __builtin_bit_cast(bf16x8_hw, p[rt][c]), part[t][rt], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[t][rt][j] = XT == MOE_E4M3 ? fmaf(v.xs[rt], part[t][rt][j], acc[t][rt][j]) : part[t][rt][j];
+    };
+    // Four tiles a round: their scales are one request, the next round's scales and the tile AHEAD are requested before a tile
+    // is multiplied (the barriers keep the compiler from moving the requests behind it).
+    const int rounds = (f.end - f.begin) / 4, last = f.begin + 4 * rounds - 1;
+    if (rounds > 0) {
+        Tile v[AHEAD + 1];
+        Anywhere<16, 1> now = *reinterpret_cast<const Anywhere<16, 1>*>(f.Ws + f.begin * 4), next;
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t) v[t].load(f.Wq, offset, row, xs_row, a.n_scales, f.begin + t, q);
+        for (int tile = f.begin; tile <= last; tile += 4) {
+            next = *reinterpret_cast<const Anywhere<16, 1>*>(f.Ws + (tile + 4 <= last ? tile + 4 : tile) * 4);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                // (behind the last tile that one again, whose sums are not formed)
+                v[(t + AHEAD) % (AHEAD + 1)].load(f.Wq, offset, row, xs_row, a.n_scales, tile + t + AHEAD < last ? tile + t + AHEAD : last, q);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(v[t % (AHEAD + 1)], now.w[t]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            now = next;
+        }
+    }
+    for (int tile = f.begin + 4 * rounds; tile < f.end; ++tile) {
+        Tile v;
+        v.load(f.Wq, offset, row, xs_row, a.n_scales, tile, q);
+        multiply(v, reinterpret_cast<const Anywhere<4, 1>*>(f.Ws + tile * 4)->w[0]);
+    }
+    if (f.rest) {
+        Tile v;
+        unsigned s;
+        v.load_rest(f.Wq, offset, row, xs_row, a.n_scales, f.tiles, q, a.K);
+        load_scales<1>(f.Ws, f.tiles, a.K, &s);
+        multiply(v, s);
+    }
 }
 
-// NT tiles of 16 weight rows and RT tiles of 16 routed rows to a workgroup
-template <int XT, typename OUT, int NT, int RT>
-__global__ __launch_bounds__(W4_WAVES * 64) void w4_kernel(W4Args a) {
-    constexpr int CAP = 16 * RT;
-    __shared__ int s_list[CAP], s_count[W4_WAVES];
-    __shared__ float4 s_sum[W4_WAVES][NT * RT][64];
+template <int XT>
+__global__ __launch_bounds__(FEW_WAVES * 64, 2) void w4_few_kernel(W4Args a, int shares) {
+    constexpr int CAP = 32;
+    __shared__ float4 s_sum[FEW_WAVES][8][64];
+    __shared__ int s_list[CAP], s_count[FEW_WAVES];
     const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63, r = lane & 15, q = lane >> 4;
-    const int n0 = blockIdx.x * 16 * NT;
-    int e = 0;
-    if (a.idx) {
-        e = a.by_choice ? a.idx[blockIdx.y] : (int)blockIdx.y;
-        if ((unsigned)e >= (unsigned)a.E) e = -1;
-    }
-    const uint8_t* Wq = a.Wq + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 2);
-    const uint8_t* Ws = a.Ws + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 32);
-    const int tiles = (a.K + 127) / 128;
+    const int group = wid / shares, part_k = wid % shares, groups = FEW_WAVES / shares;
+    const int n0 = (blockIdx.x * groups + group) * 64;
+    int e = a.idx ? (int)blockIdx.y : 0;
+    if (e >= a.E) e = -1;                                  // the rows of no expert, which are zeroed
+    FewShare f;
+    f.n0 = n0;
+    f.tiles = a.K / 128;
+    const int share = (f.tiles + shares - 1) / shares;
+    f.begin = part_k * share < f.tiles ? part_k * share : f.tiles;
+    f.end = f.begin + share < f.tiles ? f.begin + share : f.tiles;
+    f.rest = part_k == shares - 1 && a.K % 128 != 0;
+    f.Wq = a.Wq + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 2);
+    f.Ws = a.Ws + ((long long)(e < 0 ? 0 : e) * a.N + (n0 + lane < a.N ? n0 + lane : a.N - 1)) * (a.K / 32);
     for (int from = 0;; from += CAP) {
         int total;
         if (a.idx) {
-            total = collect_rows(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
+            total = collect_rows<FEW_WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
             if (total <= from) return;
-            if (from == 0 && a.by_choice && s_list[0] != (int)blockIdx.y) return;     // an earlier assignment has this expert too
         } else {
             total = a.n_rows;
             if (total <= from) return;
-            __syncthreads();
             if (tid < CAP) s_list[tid] = from + tid;
             __syncthreads();
         }
         const int here = total - from < CAP ? total - from : CAP;
-        f32x4_hw acc[NT][RT];
+        // sums of 16 weight rows and 16 routed rows each, of four times one or four times two
+        const int rts = here <= 16 ? 1 : 2;
+        float weight[2] = {1.0f, 1.0f};
+        if (a.w) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+            for (int rt = 0; rt < 2; ++rt) weight[rt] = a.w[s_list[rt * 16 + r < here ? rt * 16 + r : 0]];
+        }
+        f32x4_hw acc[8];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) acc[nt][rt] = f32x4_hw{0, 0, 0, 0};
-        if (e >= 0) {
-            const void* row[RT];
-            const float* row_scale[RT];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const int at = rt * 16 + r;
-                row[rt] = nullptr;
-                row_scale[rt] = nullptr;
-                if (at < here) {
-                    const long long xr = a.per_choice ? s_list[at] : s_list[at] / a.k;
-                    row[rt] = reinterpret_cast<const char*>(a.x) + xr * a.ldx * (XT == MOE_F32 ? 4 : XT == MOE_BF16 ? 2 : 1);
-                    if (XT == MOE_E4M3) row_scale[rt] = a.x_scales + xr * a.n_scales;
-                }
-            }
-            for (int tile = wid; tile < tiles; tile += W4_WAVES) {
-                const int col = tile * 128 + q * 32;
-                const bool inside = col < a.K;
-                uint4 wq[NT];
-                int ws[NT];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int n = n0 + nt * 16 + r;
-                    wq[nt] = make_uint4(0, 0, 0, 0);
-                    ws[nt] = 127;
-                    if (inside && n < a.N) {
-                        wq[nt] = *reinterpret_cast<const uint4*>(Wq + (long long)n * (a.K / 2) + col / 2);
-                        ws[nt] = Ws[(long long)n * (a.K / 32) + col / 32];
-                    }
-                }
-                Rows32<XT> x[RT];
-                f32x4_hw part[NT][RT];                          // e4m3: the tile's sums, before their 128 columns' scale
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    x[rt].zero();
-                    if (row[rt] && inside) x[rt].load(row[rt], col);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) part[nt][rt] = XT == MOE_E4M3 ? f32x4_hw{0, 0, 0, 0} : acc[nt][rt];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    bf16x8_hw w[NT];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) decode_weights(wq[nt], __uint_as_float((unsigned)ws[nt] << 23), i, &w[nt]);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        bf16x8_hw p[Rows32<XT>::PARTS];
-                        x[rt].parts(i, p);
-#pragma unroll
-                        for (int c = Rows32<XT>::PARTS - 1; c >= 0; --c)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-                                part[nt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[nt], p[c], part[nt][rt], 0, 0, 0);
-                    }
-                }
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const float xs = XT == MOE_E4M3 && row[rt] ? row_scale[rt][a.n_scales > 1 ? tile : 0] : 0.0f;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            acc[nt][rt][j] = XT == MOE_E4M3 ? fmaf(xs, part[nt][rt][j], acc[nt][rt][j]) : part[nt][rt][j];
-                }
-            }
+        for (int c = 0; c < 8; ++c) acc[c] = f32x4_hw{0, 0, 0, 0};
+        if (e >= 0 && n0 < a.N) {
+            if (rts == 1) few_stream<XT, 4, 1>(a, f, s_list, here, reinterpret_cast<f32x4_hw(*)[1]>(acc));
+            else few_stream<XT, 4, 2>(a, f, s_list, here, reinterpret_cast<f32x4_hw(*)[2]>(acc));
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-                s_sum[wid][nt * RT + rt][lane] = make_float4(acc[nt][rt][0], acc[nt][rt][1], acc[nt][rt][2], acc[nt][rt][3]);
-        __syncthreads();
-        for (int i = tid; i < NT * RT * 64; i += W4_WAVES * 64) {
-            const int tile = i >> 6, l = i & 63, at = (tile % RT) * 16 + (l & 15);
-            if (at >= here) continue;
+        for (int c = 0; c < 8; ++c)
+            if (c < 4 * rts) s_sum[wid][c][lane] = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+        if (shares > 1) __syncthreads();
+        // each wavefront finishes its share of its group's sums
+        for (int c = part_k; c < 4 * rts; c += shares) {
+            const int n = n0 + c / rts * 16 + q * 4, at = c % rts * 16 + r;
+            if (at >= here || n >= a.N) continue;
             float v[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int w = 0; w < W4_WAVES; ++w) {
-                const float4 p = s_sum[w][tile][l];
+            for (int w = group * shares; w < (group + 1) * shares; ++w) {
+                const float4 p = s_sum[w][c][lane];
                 v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
             }
-            const int n = n0 + (tile / RT) * 16 + (l >> 4) * 4;
-            const float weight = a.w ? a.w[s_list[at]] : 1.0f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (a.gelu) v[j] = v[j] * (0.5f + 0.5f * erff(v[j] * 0.70710678118654752440f));
-                v[j] = e < 0 ? 0.0f : v[j] * weight;
-            }
-            store_columns(reinterpret_cast<OUT*>(a.y) + s_list[at] * a.ldy + n, v, a.N - n);
+            for (int j = 0; j < 4; ++j) v[j] = e < 0 ? 0.0f : w4_finish(v[j], a.gelu, weight[c % rts]);
+            w4_store(a, s_list[at], n, v);
         }
         __syncthreads();
     }
 }
 
-// y[t] = sum over j, ascending, of the rows of assignments with an expert
+// How many tiles of 128 columns are staged at a time for each share of K: as many as 16 RT rows leave room for.
+template <int XT, int RT, int WK> constexpr int staged_tiles() {
+    constexpr int unit = row_parts(XT) * RT * WK;
+    return unit <= 2 ? 4 : unit <= 4 ? 2 : 1;
+}
+// Shares of K where there are too few workgroups: as many as leave room for two stages.
+template <int XT, int RT> constexpr int most_shares() {
+    return row_parts(XT) * RT <= 3 ? 4 : row_parts(XT) * RT <= 6 ? 2 : 1;
+}
+
+// A workgroup's eight wavefronts have 8 / WK tiles of 16 weight rows and WK shares of K.  The routed rows, RT tiles of 16, pass
+// through LDS in the order in which the matrix instructions take them, converted on the way once for all wavefronts, while
+// the weights of the next columns are on their way into registers.
+template <int XT, int RT, int WK>
+__global__ __launch_bounds__(W4_WAVES * 64) void w4_rows_kernel(W4Args a) {
+    constexpr int CAP = 16 * RT, PARTS = row_parts(XT), TILES = staged_tiles<XT, RT, WK>(), WN = W4_WAVES / WK;
+    // 16 bytes of lane (r, q) for instruction i of a tile: slots padded so that neighbouring columns are not all in one bank
+    constexpr int Q_SLOTS = 17, I_SLOTS = 4 * Q_SLOTS + 1, TILE_SLOTS = 4 * I_SLOTS;
+    constexpr int STAGE = TILES * RT * PARTS * TILE_SLOTS;                    // of one share of K
+    constexpr int UNITS = WK * CAP * TILES * 16, PER_THREAD = (UNITS + W4_WAVES * 64 - 1) / (W4_WAVES * 64);
+    __shared__ uint4 s_x[2][WK * STAGE];
+    __shared__ float s_scale[2][XT == MOE_E4M3 ? WK * TILES * CAP : 1];
+    __shared__ int s_list[CAP], s_count[W4_WAVES];
+    static_assert(sizeof(s_x) >= (size_t)(WK > 1 ? W4_WAVES * RT * 64 * 16 : 0), "the joined sums need room");
+    const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63, r = lane & 15, q = lane >> 4;
+    const int part_k = wid / WN, n0 = (blockIdx.x * WN + wid % WN) * 16, n = n0 + r;
+    int e = a.idx ? (int)blockIdx.y : 0;
+    if (e >= a.E) e = -1;                                  // the rows of no expert, which are zeroed
+    const long long wrow = (long long)(e < 0 ? 0 : e) * a.N + n;
+    const uint8_t* Wq = n < a.N ? a.Wq + wrow * (a.K / 2) : nullptr;
+    const uint8_t* Ws = n < a.N ? a.Ws + wrow * (a.K / 32) : nullptr;
+    const int tiles = (a.K + 127) / 128, per_share = ((tiles + WK - 1) / WK + TILES - 1) / TILES * TILES;
+    for (int from = 0;; from += CAP) {
+        int total;
+        if (a.idx) {
+            total = collect_rows<W4_WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
+            if (total <= from) return;
+        } else {
+            total = a.n_rows;
+            if (total <= from) return;
+            if (tid < CAP) s_list[tid] = from + tid;
+            __syncthreads();
+        }
+        const int here = total - from < CAP ? total - from : CAP;
+        if (e < 0) {
+            const float zero[4] = {0, 0, 0, 0};
+            for (int i = tid; i < here * WN * 4; i += W4_WAVES * 64) {
+                const int col = (blockIdx.x * WN * 4 + i % (WN * 4)) * 4;
+                if (col < a.N) w4_store(a, s_list[i / (WN * 4)], col, zero);
+            }
+            __syncthreads();
+            continue;
+        }
+        f32x4_hw acc[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt] = f32x4_hw{0, 0, 0, 0};
+        // what this thread stages: unit u is eight columns of a row of a share of K
+        const char* src[PER_THREAD];
+        int dst[PER_THREAD], col0[PER_THREAD];
+#pragma unroll
+        for (int u = 0; u < PER_THREAD; ++u) {
+            const int unit = u * W4_WAVES * 64 + tid, c8 = unit % (TILES * 16), row = unit / (TILES * 16) % CAP, share = unit / (TILES * 16 * CAP);
+            src[u] = nullptr;
+            col0[u] = share * per_share * 128 + c8 * 8;
+            dst[u] = -1;
+            if (UNITS % (W4_WAVES * 64) == 0 || unit < UNITS) {
+                const int t = c8 / 16, sq = c8 % 16 / 4, i = c8 % 4;
+                dst[u] = share * STAGE + ((t * RT + row / 16) * PARTS) * TILE_SLOTS + i * I_SLOTS + sq * Q_SLOTS + row % 16;
+                if (row < here) {
+                    const long long xr = a.per_choice ? s_list[row] : s_list[row] / a.k;
+                    src[u] = reinterpret_cast<const char*>(a.x) + xr * row_bytes(XT, 1) * a.ldx;
+                }
+            }
+        }
+        Rows8<XT> staged[PER_THREAD];
+        float scale = 0.0f;
+        auto request = [&](int tile) {                     // tile: of a share, the first of those to be staged
+#pragma unroll
+            for (int u = 0; u < PER_THREAD; ++u) {
+                staged[u].zero();
+                const int col = col0[u] + tile * 128;
+                if (src[u] && col < a.K) staged[u].load(src[u] + row_bytes(XT, col));
+            }
+            if (XT == MOE_E4M3 && tid < WK * TILES * CAP) {
+                const int row = tid % CAP, t = tid / CAP % TILES, share = tid / (CAP * TILES), at = share * per_share + tile + t;
+                scale = 0.0f;
+                if (row < here && at < tiles) {
+                    const long long xr = a.per_choice ? s_list[row] : s_list[row] / a.k;
+                    scale = a.x_scales[xr * a.n_scales + (a.n_scales > 1 ? at : 0)];
+                }
+            }
+        };
+        auto put = [&](int buf) {
+#pragma unroll
+            for (int u = 0; u < PER_THREAD; ++u) {
+                uint4 p[PARTS];
+                staged[u].parts(p);
+                if (dst[u] >= 0) {
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c) s_x[buf][dst[u] + c * TILE_SLOTS] = p[c];
+                }
+            }
+            if (XT == MOE_E4M3 && tid < WK * TILES * CAP) s_scale[buf][tid] = scale;
+        };
+        Weights<TILES> now, next;
+        const int w_tile0 = part_k * per_share;
+        now.load(Wq, Ws, w_tile0, q, a.K);
+        request(0);
+        put(0);
+        __syncthreads();
+        for (int tile = 0, buf = 0; tile < per_share; tile += TILES, buf ^= 1) {
+            const bool more = tile + TILES < per_share;
+            if (more) {
+                next.load(Wq, Ws, w_tile0 + tile + TILES, q, a.K);
+                request(tile + TILES);
+            }
+            const uint4* x = s_x[buf] + part_k * STAGE;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                f32x4_hw part[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) part[rt] = XT == MOE_E4M3 ? f32x4_hw{0, 0, 0, 0} : acc[rt];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bf16x8_hw d = now.decode(t, i, q);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int c = PARTS - 1; c >= 0; --c)
+                            part[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                d, __builtin_bit_cast(bf16x8_hw, x[((t * RT + rt) * PARTS + c) * TILE_SLOTS + i * I_SLOTS + q * Q_SLOTS + r]),
+                                part[rt], 0, 0, 0);
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float xs = XT == MOE_E4M3 ? s_scale[buf][(part_k * TILES + t) * CAP + rt * 16 + r] : 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[rt][j] = XT == MOE_E4M3 ? fmaf(xs, part[rt][j], acc[rt][j]) : part[rt][j];
+                }
+            }
+            if (more) {
+                put(buf ^ 1);
+                now = next;
+            }
+            __syncthreads();
+        }
+        if constexpr (WK > 1) {
+            // the shares' sums, in their order
+            float4* s_sum = reinterpret_cast<float4*>(&s_x[0][0]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s_sum[(wid * RT + rt) * 64 + lane] = make_float4(acc[rt][0], acc[rt][1], acc[rt][2], acc[rt][3]);
+            __syncthreads();
+            if (part_k == 0) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int s = 1; s < WK; ++s) {
+                        const float4 p = s_sum[((s * WN + wid) * RT + rt) * 64 + lane];
+                        acc[rt][0] += p.x; acc[rt][1] += p.y; acc[rt][2] += p.z; acc[rt][3] += p.w;
+                    }
+            }
+        }
+        if (part_k == 0 && n0 + q * 4 < a.N) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int at = rt * 16 + r;
+                if (at >= here) continue;
+                const float weight = a.w ? a.w[s_list[at]] : 1.0f;
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = w4_finish(acc[rt][j], a.gelu, weight);
+                w4_store(a, s_list[at], n0 + q * 4, v);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// y[t] = sum over j, ascending, of the rows of assignments with an expert.  All rows of up to eight choices are requested at
+// once, before it is known which count.
+constexpr int JOIN_THREADS = 64;
 template <typename OUT>
-__global__ __launch_bounds__(256) void w4_join_kernel(const float* __restrict__ rows, const int* __restrict__ idx, OUT* __restrict__ y,
-                                                      long long ldy, int k, int E, int N) {
-    const int n = (blockIdx.x * 256 + threadIdx.x) * 4;
+__global__ __launch_bounds__(JOIN_THREADS) void w4_join_kernel(const float* __restrict__ rows, const int* __restrict__ idx, OUT* __restrict__ y,
+                                                               long long ldy, int k, int E, int N) {
+    const int n = (blockIdx.x * JOIN_THREADS + threadIdx.x) * 4;
     const long long t = blockIdx.y;
     if (n >= N) return;
     float v[4] = {0, 0, 0, 0};
-    for (int j = 0; j < k; ++j) {
-        if (idx && (unsigned)idx[t * k + j] >= (unsigned)E) continue;
-        float p[4];
-        load_columns(rows + (t * k + j) * N + n, p, N - n);
+    for (int j0 = 0; j0 < k; j0 += 8) {
+        float p[8][4];
+        int e[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += p[i];
+        for (int j = 0; j < 8; ++j) {
+            e[j] = -1;
+            if (j0 + j >= k) continue;
+            e[j] = idx ? idx[t * k + j0 + j] : 0;
+            load_columns(rows + (t * k + j0 + j) * N + n, p[j], N - n);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += (unsigned)e[j] < (unsigned)E ? p[j][i] : 0.0f;
     }
     store_columns(y + t * ldy + n, v, N - n);
 }
@@ -331,7 +756,7 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
     Ws[(e * N + n) * (K / 32) + b] = (uint8_t)scale;
 }
 
-struct W4Plan { long long ldx, ldy; int n_scales, NT, RT; size_t scratch; };
+struct W4Plan { long long ldx, ldy; int n_scales; size_t scratch; };
 
 moe_status w4_plan(const moe_w4_config* c, W4Plan* p) {
     if (!c) return MOE_ERR_NULL;
@@ -345,21 +770,59 @@ moe_status w4_plan(const moe_w4_config* c, W4Plan* p) {
     p->ldx = c->ldx ? (long long)c->ldx : (long long)c->K;
     p->ldy = c->ldy ? (long long)c->ldy : (long long)c->N;
     if (p->ldx % (c->dtype == MOE_F32 ? 4 : c->dtype == MOE_BF16 ? 8 : 16) != 0) return MOE_ERR_UNSUPPORTED;
+    if ((long long)c->N * c->K > INT_MAX) return MOE_ERR_UNSUPPORTED;          // offsets within an expert are 32-bit
     if ((long long)c->T * c->k > (1 << 24) || (c->combine && c->T > 65535)) return MOE_ERR_UNSUPPORTED;
     p->n_scales = c->group ? (c->K + 127) / 128 : 1;
-    p->scratch = c->combine && c->k > 1 ? (size_t)c->T * c->k * c->N * sizeof(float) : 0;
-    p->NT = 1;
-    p->RT = 1;
+    // rows of several tokens' choices that are still to be added up; a single token's workgroups do that themselves
+    p->scratch = c->combine && c->k > 1 && c->T > 1 ? (size_t)c->T * c->k * c->N * sizeof(float) : 0;
     return MOE_OK;
 }
 
-template <int XT, typename OUT> void w4_launch(const W4Args& a, dim3 grid, hipStream_t s) {
-    w4_kernel<XT, OUT, 1, 1><<<grid, W4_WAVES * 64, 0, s>>>(a);
+template <int XT> void w4_token_launch(const W4Args& a, bool sum, hipStream_t s) {
+    const int blocks = (a.N + 15) / 16, want = (a.K + 128 * TOKEN_TILES - 1) / (128 * TOKEN_TILES);
+    if (sum && a.k > 1) {
+        // the choices first, then K, among sixteen wavefronts; beyond sixteen choices a wavefront has several
+        int slices = a.k <= TOKEN_WAVES ? TOKEN_WAVES / a.k : 1;
+        slices = slices < want ? slices : want;
+        const int waves = a.k <= TOKEN_WAVES ? slices * a.k : TOKEN_WAVES;
+        w4_token_kernel<XT, true><<<blocks, waves * 64, 0, s>>>(a, slices);
+    } else {
+        const int waves = want < TOKEN_WAVES ? want : TOKEN_WAVES;
+        w4_token_kernel<XT, false><<<dim3(blocks, a.k), waves * 64, 0, s>>>(a, waves);
+    }
 }
-template <typename OUT> void w4_launch_x(int dtype, const W4Args& a, dim3 grid, hipStream_t s) {
-    if (dtype == MOE_F32) w4_launch<MOE_F32, OUT>(a, grid, s);
-    else if (dtype == MOE_BF16) w4_launch<MOE_BF16, OUT>(a, grid, s);
-    else w4_launch<MOE_E4M3, OUT>(a, grid, s);
+
+template <int XT, int RT> void w4_rows_launch(const W4Args& a, int experts, int slots, hipStream_t s) {
+    // All eight wavefronts side by side where that leaves a workgroup for every compute unit, else K in shares.
+    constexpr int WK = most_shares<XT, RT>();
+    const int wide = (a.N + 127) / 128, narrow = (a.N + 128 / WK - 1) / (128 / WK);
+    if (WK == 1 || (long long)wide * experts >= compute_units())
+        w4_rows_kernel<XT, RT, 1><<<dim3(wide, slots), W4_WAVES * 64, 0, s>>>(a);
+    else
+        w4_rows_kernel<XT, RT, WK><<<dim3(narrow, slots), W4_WAVES * 64, 0, s>>>(a);
+}
+template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hipStream_t s) {
+    if (T == 1) {
+        w4_token_launch<XT>(a, sum, s);
+        return;
+    }
+    // experts that may be expected to be chosen, and the rows of each; and one more slot for rows of no expert
+    const int experts = !a.idx ? 1 : a.n_rows < a.E ? a.n_rows : a.E, slots = !a.idx ? 1 : join ? a.E : a.E + 1;
+    const int rows = (a.n_rows + experts - 1) / experts;
+    if constexpr (XT != MOE_F32) {
+        // (three parts of a float row do not fit into the registers beside two tiles)
+        if (rows <= 10) {
+            const int columns = (a.N + 63) / 64, tiles = (a.K + 127) / 128;
+            int shares = 1;
+            while (shares < FEW_WAVES && (long long)experts * columns * shares < 16 * compute_units() && 2 * shares <= tiles) shares *= 2;
+            const int groups = FEW_WAVES / shares;
+            w4_few_kernel<XT><<<dim3((columns + groups - 1) / groups, slots), FEW_WAVES * 64, 0, s>>>(a, shares);
+            return;
+        }
+    }
+    if (rows <= 10) w4_rows_launch<XT, 1>(a, experts, slots, s);
+    else if (rows <= 24) w4_rows_launch<XT, 2>(a, experts, slots, s);
+    else w4_rows_launch<XT, 4>(a, experts, slots, s);
 }
 
 }  // namespace
@@ -385,21 +848,19 @@ extern "C" moe_status moe_w4_product(const moe_w4_config* cfg, const void* x, co
     const int rows = cfg->T * cfg->k;
     const bool join = p.scratch != 0;
     moe::W4Args a = {x, x_scales, topk_idx, topk_w, Wq, Ws, join ? scratch : y, p.ldx, join ? cfg->N : p.ldy, rows,
-                     cfg->k, cfg->E, cfg->K, cfg->N, p.n_scales, cfg->per_choice, cfg->gelu, rows <= cfg->E};
-    // without an assignment each: the expert's number, and one more for the assignments without an expert, whose rows are zeroed
-    const int slots = !topk_idx ? 1 : a.by_choice ? rows : join ? cfg->E : cfg->E + 1;
-    const dim3 grid((cfg->N + 16 * p.NT - 1) / (16 * p.NT), slots);
+                     cfg->k, cfg->E, cfg->K, cfg->N, p.n_scales, cfg->per_choice, cfg->gelu, join || cfg->out == MOE_F32};
     {
         moe::ProfScope prof(moe::PK_W4, s);
-        if (join || cfg->out == MOE_F32) moe::w4_launch_x<float>(cfg->dtype, a, grid, s);
-        else moe::w4_launch_x<moe::bf16_t>(cfg->dtype, a, grid, s);
+        if (cfg->dtype == MOE_F32) moe::w4_launch<MOE_F32>(a, cfg->T, join, cfg->combine, s);
+        else if (cfg->dtype == MOE_BF16) moe::w4_launch<MOE_BF16>(a, cfg->T, join, cfg->combine, s);
+        else moe::w4_launch<MOE_E4M3>(a, cfg->T, join, cfg->combine, s);
         MOE_CHECK_LAUNCH();
         if (join) {
-            const dim3 jgrid((cfg->N + 1023) / 1024, cfg->T);
+            const dim3 jgrid((cfg->N + 4 * moe::JOIN_THREADS - 1) / (4 * moe::JOIN_THREADS), cfg->T);
             if (cfg->out == MOE_F32)
-                moe::w4_join_kernel<float><<<jgrid, 256, 0, s>>>((const float*)scratch, topk_idx, (float*)y, p.ldy, cfg->k, cfg->E, cfg->N);
+                moe::w4_join_kernel<float><<<jgrid, moe::JOIN_THREADS, 0, s>>>((const float*)scratch, topk_idx, (float*)y, p.ldy, cfg->k, cfg->E, cfg->N);
             else
-                moe::w4_join_kernel<moe::bf16_t><<<jgrid, 256, 0, s>>>((const float*)scratch, topk_idx, (moe::bf16_t*)y, p.ldy, cfg->k, cfg->E, cfg->N);
+                moe::w4_join_kernel<moe::bf16_t><<<jgrid, moe::JOIN_THREADS, 0, s>>>((const float*)scratch, topk_idx, (moe::bf16_t*)y, p.ldy, cfg->k, cfg->E, cfg->N);
             MOE_CHECK_LAUNCH();
         }
     }
