@@ -18,6 +18,7 @@
 #include "common.h"
 #include "wide.h"
 #include <climits>
+#include <cmath>
 
 namespace moe {
 
@@ -101,51 +102,114 @@ __device__ __forceinline__ bf16x8_hw decode_weights(unsigned w, unsigned scale_b
     d.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
     return __builtin_bit_cast(bf16x8_hw, d);
 }
-// Four lanes r, 16 + r, 32 + r, 48 + r with four dwords each: lane q's dword i becomes lane i's dword q.
-__device__ __forceinline__ void transpose_words(uint4& u) {
-    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 a = __builtin_amdgcn_permlane32_swap(u.x, u.z, false, false), b = __builtin_amdgcn_permlane32_swap(u.y, u.w, false, false);
-    const u32x2 c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    u = make_uint4(c[0], c[1], d[0], d[1]);
-}
 __device__ __forceinline__ unsigned word_of(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
 
-// 32 columns of a weight row, or nothing: zeros.
-__device__ __forceinline__ uint4 load_weights(const uint8_t* Wq, int col, int K) {
-    return Wq && col < K ? *reinterpret_cast<const uint4*>(Wq + col / 2) : make_uint4(0, 0, 0, 0);
-}
-// The scales of TILES tiles of a weight row, a byte for each 32 columns; 1 where there are none.
-template <int TILES> __device__ __forceinline__ void load_scales(const uint8_t* Ws, int tile, int K, unsigned* s) {
-    if (Ws && (tile + TILES) * 128 <= K) {
-        const auto u = *reinterpret_cast<const Anywhere<4 * TILES, 1>*>(Ws + tile * 4);
+// 16 weight rows of TILES tiles of 128 columns on their way to a wavefront's registers.
+//
+// The matrix instructions want the four lanes of a row 16 lanes apart, but the unit that takes requests apart needs a cycle for
+// each 64 bytes of neighbouring lanes: loaded as they are wanted, every lane's 16 bytes were a cycle of their own, and that
+// unit the limit (16 experts of 2048 x 8192, a row each: 39 us).  So neighbouring lanes load neighbouring pieces of a row
+// and the rows change lanes through LDS that the wavefront has for itself; piece p of row r goes to place p ^ (r TILES / 4) of its
+// row, so that the 16 rows' pieces, which are read at a time, are in different banks.
+template <int TILES> struct Block16 {
+    static constexpr int PIECES = 4 * TILES, ROWS = 64 / PIECES;           // of a row; rows of a request
+    static constexpr int SLOTS = 64 * TILES;                               // of 16 bytes in LDS
+    uint4 u[TILES];
+    unsigned mask;                   // of the columns that are there; what is loaded is not looked at before put()
+    static __device__ __forceinline__ int slot(int row, int piece) { return row * PIECES + (piece ^ (row * PIECES / 16)); }
+    // Offsets in an expert's weights of the rows that the lane loads from; rows past the last are the last again, their products
+    // of no use.
+    static __device__ __forceinline__ void offsets(int n0, int N, int K, int lane, unsigned* o) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) s[t] = u.w[t];
-    } else {
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            s[t] = 0x7f7f7f7f;
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-                if (Ws && (tile + t) * 128 + b * 32 < K) s[t] = (s[t] & ~(0xffu << (8 * b))) | (unsigned)Ws[(tile + t) * 4 + b] << (8 * b);
+        for (int j = 0; j < TILES; ++j) {
+            const int n = n0 + j * ROWS + lane / PIECES;
+            o[j] = (unsigned)(n < N ? n : N - 1) * (unsigned)(K / 2);
         }
     }
+    // From the first column of `tile` on.  Columns past the last are zeros: loaded from the row's beginning, so that nothing branches.
+    __device__ __forceinline__ void load(const uint8_t* Wq, const unsigned* o, int tile, int lane, int K) {
+        const bool there = tile * 128 + lane % PIECES * 32 < K;
+        const unsigned at = there ? tile * 64 + lane % PIECES * 16 : 0;
+        mask = there ? ~0u : 0u;
+#pragma unroll
+        for (int j = 0; j < TILES; ++j) u[j] = *reinterpret_cast<const uint4*>(Wq + (o[j] + at));
+    }
+    __device__ __forceinline__ void put(uint4* lds, int lane) const {
+#pragma unroll
+        for (int j = 0; j < TILES; ++j)
+            lds[slot(j * ROWS + lane / PIECES, lane % PIECES)] = make_uint4(u[j].x & mask, u[j].y & mask, u[j].z & mask, u[j].w & mask);
+    }
+    // columns 32 q .. + 31 of row r in tile t
+    static __device__ __forceinline__ uint4 get(const uint4* lds, int t, int r, int q) { return lds[slot(r, t * 4 + q)]; }
+};
+
+// What a wavefront writes to LDS and reads from there stays in this order; nothing is waited for.
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
-// A lane's weights of TILES consecutive tiles of 128 columns: lane (r, q) has columns 32 q .. 32 q + 31 of a tile in weight row r,
-// and the four scales of the row in each tile.
-template <int TILES> struct Weights {
-    uint4 u[TILES];
-    unsigned s[TILES];
-    // Wq, Ws: the weight row, NULL if there is none
-    __device__ __forceinline__ void load(const uint8_t* Wq, const uint8_t* Ws, int tile, int q, int K) {
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) u[t] = load_weights(Wq, (tile + t) * 128 + q * 32, K);
-        load_scales<TILES>(Ws, tile, K, s);
+// The scales of a tile of a weight row, a byte for each 32 columns; 1 where there are no columns.  Four bytes of the row that has
+// them are loaded, those before the row's end where the tile is not full (K < 128: byte by byte).
+struct Scales {
+    unsigned u;
+    int past;                        // bytes of u that belong to the tile before; 4 and more: none is this tile's
+    __device__ __forceinline__ void load(const uint8_t* Ws, int tile, int K) {
+        const int blocks = K / 32, first = tile * 4, at = first + 4 <= blocks ? first : blocks - 4;
+        past = first - at;
+        if (blocks >= 4) {
+            u = reinterpret_cast<const Anywhere<4, 1>*>(Ws + at)->w[0];
+        } else {
+            u = 0x7f7f7f7f;
+            past = 0;
+            if (first < blocks) u = (u & ~0xffu) | Ws[first];
+            if (first + 1 < blocks) u = (u & ~0xff00u) | (unsigned)Ws[first + 1] << 8;
+            if (first + 2 < blocks) u = (u & ~0xff0000u) | (unsigned)Ws[first + 2] << 16;
+        }
     }
-    __device__ __forceinline__ bf16x8_hw decode(int t, int i, int q) const {
-        return decode_weights(word_of(u[t], i), s[t] >> (8 * q) & 0xffu);
+    __device__ __forceinline__ unsigned get() const {
+        return past == 0 ? u : past >= 4 ? 0x7f7f7f7fu : u >> (8 * past) | 0x7f7f7f7fu << (32 - 8 * past);
     }
 };
+// The scales of 64 weight rows in 16 tiles, 64 bytes of each, through the wavefront's LDS as well: four bytes of 64 rows at a time
+// would cost as many cycles as the 4 KiB of weights that they belong to (16 experts of 2048 x 8192, a row each: 42 us, and 32
+// without any scales).
+constexpr int SCALE_TILES = 16, SCALE_SLOTS = 256;
+__device__ __forceinline__ int scale_slot(int row, int piece) { return row * 4 + (piece ^ (row / 4 & 3)); }
+__device__ __forceinline__ void fetch_scales(const uint8_t* Ws, int n0, int N, int K, int tile, int lane, uint4* lds) {
+    const int bytes = K / 32, at = tile * 4 + lane % 4 * 16;
+    uint4 u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + j * 16 + lane / 4;
+        const uint8_t* row = Ws + (long long)(n < N ? n : N - 1) * bytes;
+        if (at + 16 <= bytes) {
+            const auto v = *reinterpret_cast<const Anywhere<16, 1>*>(row + at);
+            u[j] = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+        } else if (at >= bytes) {
+            u[j] = make_uint4(0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f);
+        } else {
+            // the row's last bytes one by one, 1 behind them
+            unsigned w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = 0;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) w[i] |= (at + 4 * i + b < bytes ? (unsigned)row[at + 4 * i + b] : 0x7fu) << (8 * b);
+            }
+            u[j] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lds[scale_slot(j * 16 + lane / 4, lane % 4)] = u[j];
+}
+// of columns 32 q .. + 31 of a row's tile
+__device__ __forceinline__ unsigned scale_at(const uint4* lds, int row, int tile, int q) {
+    tile %= SCALE_TILES;
+    return reinterpret_cast<const uint8_t*>(lds + scale_slot(row, tile / 4))[tile % 4 * 4 + q];
+}
+
+__device__ __forceinline__ unsigned from_any_lane(unsigned v, int lane) { return (unsigned)__builtin_amdgcn_ds_bpermute(lane * 4, (int)v); }
 
 __device__ __forceinline__ float w4_finish(float v, int gelu, float weight) {
     if (gelu) v = v * (0.5f + 0.5f * erff(v * 0.70710678118654752440f));
@@ -161,18 +225,22 @@ __device__ __forceinline__ void w4_store(const W4Args& a, long long row, int n, 
 // the choices and K in pieces of 512 columns.  A piece of the routed row is one request of the wavefront and goes through LDS
 // that no other wavefront uses, from where all 16 columns of the right operand get the same.
 constexpr int TOKEN_TILES = 4;       // of a piece
-constexpr int TOKEN_WAVES = 16;      // at most
+constexpr int TOKEN_WAVES = 16;      // at most; four where that is enough, so that LDS has room for more workgroups
 
 template <int XT> struct TokenPiece {
-    Weights<TOKEN_TILES> w;
+    Block16<TOKEN_TILES> w;
+    Scales s;                        // lane l: the scales of weight row l / 4 in tile l % 4
     Rows8<XT> x;
+    bool there;                      // x is not past the row's end
     float xs[TOKEN_TILES];
     // row: of the assignment; xs_row: its scales
-    __device__ __forceinline__ void load(const uint8_t* Wq, const uint8_t* Ws, const char* row, const float* xs_row, int n_scales, int tile, int K) {
-        const int lane = threadIdx.x & 63, q = lane >> 4, col = tile * 128 + lane * 8;
-        w.load(Wq, Ws, tile, q, K);
-        x.zero();
-        if (col < K) x.load(row + row_bytes(XT, col));
+    __device__ __forceinline__ void load(const uint8_t* Wq, const unsigned* offset, const uint8_t* Ws, const char* row, const float* xs_row,
+                                         int n_scales, int tile, int K) {
+        const int lane = threadIdx.x & 63, col = tile * 128 + lane * 8;
+        w.load(Wq, offset, tile, lane, K);
+        s.load(Ws, tile + lane % 4, K);
+        x.load(row + row_bytes(XT, col < K ? col : 0));
+        there = col < K;
         if constexpr (XT == MOE_E4M3) {
 #pragma unroll
             for (int t = 0; t < TOKEN_TILES; ++t) xs[t] = (tile + t) * 128 < K ? xs_row[n_scales > 1 ? tile + t : 0] : 0.0f;
@@ -180,13 +248,16 @@ template <int XT> struct TokenPiece {
     }
 };
 
-template <int XT, bool SUM>
-__global__ __launch_bounds__(TOKEN_WAVES * 64) void w4_token_kernel(W4Args a, int slices) {
+template <int XT, bool SUM, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slices) {
     constexpr int PARTS = row_parts(XT);
-    __shared__ uint4 s_x[TOKEN_WAVES][PARTS][64];
-    __shared__ float4 s_sum[TOKEN_WAVES][4];
+    __shared__ uint4 s_w[WAVES][Block16<TOKEN_TILES>::SLOTS], s_x[WAVES][PARTS][64];
+    __shared__ float4 s_sum[WAVES][4];
     const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63, r = lane & 15, q = lane >> 4;
-    const int n0 = blockIdx.x * 16, n = n0 + r;
+    const int n0 = blockIdx.x * 16;
+    unsigned offset[TOKEN_TILES];
+    Block16<TOKEN_TILES>::offsets(n0, a.N, a.K, lane, offset);
+    const int scale_row = n0 + lane / 4 < a.N ? n0 + lane / 4 : a.N - 1;
     const int pieces = (a.K + 128 * TOKEN_TILES - 1) / (128 * TOKEN_TILES), waves = blockDim.x >> 6;
     // the wavefront's choices: one, or (SUM, more choices than wavefronts) every `waves`-th
     const int first = SUM ? wid / slices : (int)blockIdx.y, slice = SUM ? wid % slices : wid, step = waves / slices;
@@ -195,38 +266,44 @@ __global__ __launch_bounds__(TOKEN_WAVES * 64) void w4_token_kernel(W4Args a, in
         const int e = a.idx ? a.idx[j] : 0;
         f32x4_hw acc = {0, 0, 0, 0};
         if ((unsigned)e < (unsigned)a.E) {
-            const long long wrow = (long long)e * a.N + n, xr = a.per_choice ? j : 0;
-            const uint8_t* Wq = n < a.N ? a.Wq + wrow * (a.K / 2) : nullptr;
-            const uint8_t* Ws = n < a.N ? a.Ws + wrow * (a.K / 32) : nullptr;
+            const long long xr = a.per_choice ? j : 0;
+            const uint8_t* Wq = a.Wq + (long long)e * a.N * (a.K / 2);
+            const uint8_t* Ws = a.Ws + ((long long)e * a.N + scale_row) * (a.K / 32);
             const char* row = reinterpret_cast<const char*>(a.x) + xr * row_bytes(XT, 1) * a.ldx;
             const float* xs_row = a.x_scales + xr * a.n_scales;
-            TokenPiece<XT> now, next;
-            if (slice < pieces) now.load(Wq, Ws, row, xs_row, a.n_scales, slice * TOKEN_TILES, a.K);
+            TokenPiece<XT> v;
+            if (slice < pieces) v.load(Wq, offset, Ws, row, xs_row, a.n_scales, slice * TOKEN_TILES, a.K);
             for (int piece = slice; piece < pieces; piece += slices) {
-                if (piece + slices < pieces) next.load(Wq, Ws, row, xs_row, a.n_scales, (piece + slices) * TOKEN_TILES, a.K);
                 uint4 p[PARTS];
-                now.x.parts(p);
+                v.x.parts(p);
 #pragma unroll
-                for (int c = 0; c < PARTS; ++c) s_x[wid][c][lane] = p[c];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+                for (int c = 0; c < PARTS; ++c) s_x[wid][c][lane] = v.there ? p[c] : make_uint4(0, 0, 0, 0);
+                v.w.put(s_w[wid], lane);
+                wave_order();
+                const unsigned scales = v.s.get();
+                float xs[TOKEN_TILES];
+                if constexpr (XT == MOE_E4M3) {
+#pragma unroll
+                    for (int t = 0; t < TOKEN_TILES; ++t) xs[t] = v.xs[t];
+                }
+                if (piece + slices < pieces) v.load(Wq, offset, Ws, row, xs_row, a.n_scales, (piece + slices) * TOKEN_TILES, a.K);
 #pragma unroll
                 for (int t = 0; t < TOKEN_TILES; ++t) {
+                    const uint4 w = Block16<TOKEN_TILES>::get(s_w[wid], t, r, q);
+                    const unsigned scale = from_any_lane(scales, r * 4 + t) >> (8 * q) & 0xffu;
                     f32x4_hw part = XT == MOE_E4M3 ? f32x4_hw{0, 0, 0, 0} : acc;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const bf16x8_hw d = now.w.decode(t, i, q);
+                        const bf16x8_hw d = decode_weights(word_of(w, i), scale);
 #pragma unroll
                         for (int c = PARTS - 1; c >= 0; --c)
                             part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                                 d, __builtin_bit_cast(bf16x8_hw, s_x[wid][c][t * 16 + q * 4 + i]), part, 0, 0, 0);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i] = XT == MOE_E4M3 ? fmaf(now.xs[t], part[i], acc[i]) : part[i];
+                    for (int i = 0; i < 4; ++i) acc[i] = XT == MOE_E4M3 ? fmaf(xs[t], part[i], acc[i]) : part[i];
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                now = next;
+                wave_order();
             }
         }
         if (SUM && slices == 1) {
@@ -306,172 +383,172 @@ template <int WAVES> __device__ int collect_rows(const int* idx, int n, int e, i
     return total;
 }
 
-// Up to 32 rows to an expert, mostly: a wavefront has 64 weight rows and a share of K, which it streams by itself; `shares` of the
+// Few rows to an expert (RT times 16, mostly): a wavefront has 64 weight rows and a share of K, which it streams by itself; `shares` of the
 // workgroup's wavefronts have the same weight rows and add up their sums at the end.  The routed rows come straight from the L2
-// cache, once for 64 weight rows.  With no barrier on the way and the next tile's requests out while one is multiplied, the
-// wavefronts of a compute unit keep some 64 KiB under way.  shares is such that the wavefronts fill the chip about once: each of
-// them pays the way to its first weights (its rows' numbers, their addresses, the first request) of some 5 us once.
-//
-// The unit that takes the requests apart was the limit here: it takes a cycle for every 64 bytes that neighbouring lanes have in
-// common, or every lane that stands alone.  So the four lanes of a weight row change words among themselves, after which an
-// instruction's columns are 32 neighbouring ones of the routed rows as well, and scales come for four tiles at a time.
-constexpr int FEW_WAVES = 4;
+// cache, once for 64 weight rows.  There is no barrier on the way, and the next tile's requests are out while one is
+// multiplied.  shares is such that there are some sixteen wavefronts to a compute unit in all: each of them pays the way to its
+// first weights (its rows' numbers, their addresses, the first request), and experts with more rows take longer.
+constexpr int FEW_WAVES = 4, FEW_MORE = 8;       // of a workgroup; more where K has to be cut finer to fill the chip
 
-// What a wavefront reads of a tile of 128 columns: TILES times 16 weight rows, RT times 16 routed rows.
-template <int XT, int TILES, int RT> struct FewTile {
-    uint4 w[TILES];
-    Rows8<XT> x[RT][4];              // of instruction i: columns 32 i + 8 q .. + 7
-    float xs[RT];
-    // A tile that is full: nothing is asked, so that all requests go out in one go.  offset[t]: of the lane's columns of tile 0 in
-    // its weight row of the 16 with number t; weight and routed rows past the last are the last again, and their sums of no use.
-    __device__ __forceinline__ void load(const uint8_t* Wq, const unsigned* offset, const char* const* row, const float* const* xs_row,
-                                         int n_scales, int tile, int q) {
+// A tile of 16 routed rows: as stored, in pieces of 16 bytes, neighbouring lanes with neighbouring pieces.  Through LDS to the lanes
+// that want them as the weights.
+template <int XT> struct RowTile {
+    static constexpr int PIECES = row_bytes(XT, 128) / 16, ROWS = 64 / PIECES, LOADS = 16 / ROWS;
+    static constexpr int SLOTS = 16 * PIECES;
+    uint4 u[LOADS];
+    unsigned mask;                   // as Block16's
+    static __device__ __forceinline__ int slot(int row, int piece) { return row * PIECES + (piece ^ (row % PIECES)); }
+    // row[j]: the offset in x of the lane's row of load j; loads of nothing but rows past `here` are left out
+    __device__ __forceinline__ void load(const char* x, const unsigned* row, int here, int tile, int lane, int K) {
+        const unsigned col = tile * 128 + lane % PIECES * (16 / row_bytes(XT, 1));
+        const bool there = col < (unsigned)K;
+        const unsigned at = there ? row_bytes(XT, 1) * col : 0;
+        mask = there ? ~0u : 0u;
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) w[t] = *reinterpret_cast<const uint4*>(Wq + (offset[t] + tile * 64));
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[rt][i].load(row[rt] + row_bytes(XT, tile * 128 + 32 * i + 8 * q));
-            if (XT == MOE_E4M3) xs[rt] = xs_row[rt][n_scales > 1 ? tile : 0];
-        }
+        for (int j = 0; j < LOADS; ++j)
+            if (j == 0 || j * ROWS < here) u[j] = *reinterpret_cast<const uint4*>(x + (row[j] + at));
     }
-    // The row's last columns, zeros behind them.
-    __device__ __forceinline__ void load_rest(const uint8_t* Wq, const unsigned* offset, const char* const* row, const float* const* xs_row,
-                                              int n_scales, int tile, int q, int K) {
+    __device__ __forceinline__ void put(uint4* lds, int lane) const {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t)
-            w[t] = tile * 128 + q * 32 < K ? *reinterpret_cast<const uint4*>(Wq + (offset[t] + tile * 64)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[rt][i].zero();
-                if (tile * 128 + 32 * i < K) x[rt][i].load(row[rt] + row_bytes(XT, tile * 128 + 32 * i + 8 * q));
-            }
-            if (XT == MOE_E4M3) xs[rt] = xs_row[rt][n_scales > 1 ? tile : 0];
+        for (int j = 0; j < LOADS; ++j)
+            lds[slot(j * ROWS + lane / PIECES, lane % PIECES)] = make_uint4(u[j].x & mask, u[j].y & mask, u[j].z & mask, u[j].w & mask);
+    }
+    // columns 32 q + 8 i .. + 7 of row r
+    static __device__ __forceinline__ Rows8<XT> get(const uint4* lds, int r, int q, int i) {
+        Rows8<XT> x;
+        if constexpr (XT == MOE_BF16) {
+            x.u = lds[slot(r, q * 4 + i)];
+        } else {
+            static_assert(XT == MOE_E4M3, "");
+            x.u = reinterpret_cast<const uint2*>(&lds[slot(r, q * 2 + i / 2)])[i % 2];
         }
+        return x;
     }
 };
 
-// A wavefront's share: full tiles begin .. end - 1 of `tiles`, and what is behind those if it is its.
-struct FewShare { const uint8_t* Wq; const uint8_t* Ws; int n0, begin, end, tiles; bool rest; };
+// A wavefront's share: tiles begin .. end - 1.
+struct FewShare { const uint8_t* Wq; const uint8_t* Ws; int n0, begin, end; };
 
-// The sums of TILES x 16 weight rows with the first `here` rows of the list.
-template <int XT, int TILES, int RT>
-__device__ __forceinline__ void few_stream(const W4Args& a, const FewShare& f, const int* s_list, int here, f32x4_hw (*acc)[RT]) {
-    constexpr int PARTS = row_parts(XT);
+// The sums of 4 x 16 weight rows with the first `here` rows of the list.
+template <int XT, int RT>
+__device__ __forceinline__ void few_stream(const W4Args& a, const FewShare& f, const int* s_list, int here, uint4* s_w, uint4* s_x, uint4* s_s, f32x4_hw (*acc)[RT]) {
+    typedef RowTile<XT> X;
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-    unsigned offset[TILES];
+    unsigned offset[4][1];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-        const int n = f.n0 + t * 16 + r;
-        offset[t] = (unsigned)(n < a.N ? n : a.N - 1) * (unsigned)(a.K / 2) + q * 16;
+    for (int t = 0; t < 4; ++t) {
+        Block16<1>::offsets(f.n0 + t * 16, a.N, a.K, lane, offset[t]);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) acc[t][rt] = f32x4_hw{0, 0, 0, 0};
     }
-    const char* row[RT];
-    const float* xs_row[RT];
+    // of the lane's row in each load; and the scales of row r
+    const char* const x = reinterpret_cast<const char*>(a.x);
+    unsigned row[RT][X::LOADS], xs_row[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int at = s_list[rt * 16 + r < here ? rt * 16 + r : 0];
-        const long long xr = a.per_choice ? at : at / a.k;
-        row[rt] = reinterpret_cast<const char*>(a.x) + xr * row_bytes(XT, 1) * a.ldx;
-        xs_row[rt] = a.x_scales + xr * a.n_scales;
-    }
-    typedef FewTile<XT, TILES, RT> Tile;
-    constexpr int AHEAD = 1;                           // tiles under way behind the one that is multiplied
-    // scales: of weight row `lane` of the 64 in the tile
-    auto multiply = [&](Tile& v, unsigned scales) {
-        f32x4_hw part[TILES][RT];
-        unsigned s[TILES];
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
+        for (int j = 0; j < X::LOADS; ++j) {
+            const int i = rt * 16 + j * X::ROWS + lane / X::PIECES, at = s_list[i < here ? i : 0];
+            row[rt][j] = (unsigned)(a.per_choice ? at : at / a.k) * (unsigned)row_bytes(XT, 1) * (unsigned)a.ldx;
+        }
+        const int at = s_list[rt * 16 + r < here ? rt * 16 + r : 0];
+        xs_row[rt] = (unsigned)(a.per_choice ? at : at / a.k) * (unsigned)a.n_scales;
+    }
+    struct Next {                                                          // a tile on its way
+        Block16<1> w[4];
+        X x[RT];
+        float xs[RT];
+    };
+    float xs[RT];
+    auto request = [&](Next& v, int tile) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v.w[t].load(f.Wq, offset[t], tile, lane, a.K);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            v.x[rt].load(x, row[rt], here - rt * 16, tile, lane, a.K);
+            if (XT == MOE_E4M3) v.xs[rt] = a.x_scales[xs_row[rt] + (a.n_scales > 1 ? tile : 0)];
+        }
+    };
+    auto put = [&](const Next& v) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v.w[t].put(s_w + t * Block16<1>::SLOTS, lane);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            v.x[rt].put(s_x + rt * X::SLOTS, lane);
+            if (XT == MOE_E4M3) xs[rt] = v.xs[rt];
+        }
+        wave_order();
+    };
+    auto multiply = [&](int tile) {                                        // which is in LDS
+        f32x4_hw part[4][RT];
+        uint4 w[4];
+        unsigned s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) part[t][rt] = XT == MOE_E4M3 ? f32x4_hw{0, 0, 0, 0} : acc[t][rt];
-            s[t] = (unsigned)__builtin_amdgcn_ds_bpermute((t * 16 + r) * 4, (int)scales);
-            transpose_words(v.w[t]);
+            w[t] = Block16<1>::get(s_w + t * Block16<1>::SLOTS, 0, r, q);
+            s[t] = scale_at(s_s, t * 16 + r, tile - f.begin, q);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint4 p[RT][PARTS];
+            uint4 p[RT][row_parts(XT)];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) v.x[rt][i].parts(p[rt]);
+            for (int rt = 0; rt < RT; ++rt) X::get(s_x + rt * X::SLOTS, r, q, i).parts(p[rt]);
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                const bf16x8_hw d = decode_weights(word_of(v.w[t], i), s[t] >> (8 * i) & 0xffu);
+            for (int t = 0; t < 4; ++t) {
+                const bf16x8_hw d = decode_weights(word_of(w[t], i), s[t]);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int c = PARTS - 1; c >= 0; --c)
-                        part[t][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, __builtin_bit_cast(bf16x8_hw, p[rt][c]), part[t][rt], 0, 0, 0);
+                    part[t][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, __builtin_bit_cast(bf16x8_hw, p[rt][0]), part[t][rt], 0, 0, 0);
             }
         }
 #pragma unroll
-        for (int t = 0; t < TILES; ++t)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    acc[t][rt][j] = XT == MOE_E4M3 ? fmaf(v.xs[rt], part[t][rt][j], acc[t][rt][j]) : part[t][rt][j];
+                    acc[t][rt][j] = XT == MOE_E4M3 ? fmaf(xs[rt], part[t][rt][j], acc[t][rt][j]) : part[t][rt][j];
+        wave_order();
     };
-    // Four tiles a round: their scales are one request, the next round's scales and the tile AHEAD are requested before a tile
-    // is multiplied (the barriers keep the compiler from moving the requests behind it).
-    const int rounds = (f.end - f.begin) / 4, last = f.begin + 4 * rounds - 1;
-    if (rounds > 0) {
-        Tile v[AHEAD + 1];
-        Anywhere<16, 1> now = *reinterpret_cast<const Anywhere<16, 1>*>(f.Ws + f.begin * 4), next;
-#pragma unroll
-        for (int t = 0; t < AHEAD; ++t) v[t].load(f.Wq, offset, row, xs_row, a.n_scales, f.begin + t, q);
-        for (int tile = f.begin; tile <= last; tile += 4) {
-            next = *reinterpret_cast<const Anywhere<16, 1>*>(f.Ws + (tile + 4 <= last ? tile + 4 : tile) * 4);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                // (behind the last tile that one again, whose sums are not formed)
-                v[(t + AHEAD) % (AHEAD + 1)].load(f.Wq, offset, row, xs_row, a.n_scales, tile + t + AHEAD < last ? tile + t + AHEAD : last, q);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(v[t % (AHEAD + 1)], now.w[t]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            now = next;
-        }
-    }
-    for (int tile = f.begin + 4 * rounds; tile < f.end; ++tile) {
-        Tile v;
-        v.load(f.Wq, offset, row, xs_row, a.n_scales, tile, q);
-        multiply(v, reinterpret_cast<const Anywhere<4, 1>*>(f.Ws + tile * 4)->w[0]);
-    }
-    if (f.rest) {
-        Tile v;
-        unsigned s;
-        v.load_rest(f.Wq, offset, row, xs_row, a.n_scales, f.tiles, q, a.K);
-        load_scales<1>(f.Ws, f.tiles, a.K, &s);
-        multiply(v, s);
+    // A tile goes to LDS, the next one's requests go out, and then it is multiplied (the barriers keep the compiler from moving
+    // the requests behind that).  Behind the last one it is requested again, and not multiplied.
+    if (f.begin >= f.end) return;
+    Next v;
+    request(v, f.begin);
+    for (int tile = f.begin; tile < f.end; ++tile) {
+        if ((tile - f.begin) % SCALE_TILES == 0) fetch_scales(f.Ws, f.n0, a.N, a.K, tile, lane, s_s);
+        put(v);
+        request(v, tile + 1 < f.end ? tile + 1 : tile);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(tile);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-template <int XT>
-__global__ __launch_bounds__(FEW_WAVES * 64, 2) void w4_few_kernel(W4Args a, int shares) {
-    constexpr int CAP = 32;
-    __shared__ float4 s_sum[FEW_WAVES][8][64];
-    __shared__ int s_list[CAP], s_count[FEW_WAVES];
+template <int XT, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void w4_few_kernel(W4Args a, int shares) {
+    constexpr int CAP = 16 * RT, W_SLOTS = 4 * Block16<1>::SLOTS, X_SLOTS = RowTile<XT>::SLOTS;
+    __shared__ uint4 s_own[WAVES][W_SLOTS + RT * X_SLOTS], s_scales[WAVES][SCALE_SLOTS];    // a wavefront's tile, later its sums
+    __shared__ int s_list[CAP], s_count[WAVES];
+    static_assert(W_SLOTS + RT * X_SLOTS >= 4 * RT * 64, "4 RT sums of 64 lanes");
     const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63, r = lane & 15, q = lane >> 4;
-    const int group = wid / shares, part_k = wid % shares, groups = FEW_WAVES / shares;
+    const int group = wid / shares, part_k = wid % shares, groups = WAVES / shares;
     const int n0 = (blockIdx.x * groups + group) * 64;
     int e = a.idx ? (int)blockIdx.y : 0;
     if (e >= a.E) e = -1;                                  // the rows of no expert, which are zeroed
     FewShare f;
     f.n0 = n0;
-    f.tiles = a.K / 128;
-    const int share = (f.tiles + shares - 1) / shares;
-    f.begin = part_k * share < f.tiles ? part_k * share : f.tiles;
-    f.end = f.begin + share < f.tiles ? f.begin + share : f.tiles;
-    f.rest = part_k == shares - 1 && a.K % 128 != 0;
+    const int tiles = (a.K + 127) / 128, share = (tiles + shares - 1) / shares;
+    f.begin = part_k * share;
+    f.end = f.begin + share < tiles ? f.begin + share : tiles;
     f.Wq = a.Wq + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 2);
-    f.Ws = a.Ws + ((long long)(e < 0 ? 0 : e) * a.N + (n0 + lane < a.N ? n0 + lane : a.N - 1)) * (a.K / 32);
+    f.Ws = a.Ws + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 32);
     for (int from = 0;; from += CAP) {
         int total;
         if (a.idx) {
-            total = collect_rows<FEW_WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
+            total = collect_rows<WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
             if (total <= from) return;
         } else {
             total = a.n_rows;
@@ -480,35 +557,33 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void w4_few_kernel(W4Args a, int
             __syncthreads();
         }
         const int here = total - from < CAP ? total - from : CAP;
-        // sums of 16 weight rows and 16 routed rows each, of four times one or four times two
-        const int rts = here <= 16 ? 1 : 2;
-        float weight[2] = {1.0f, 1.0f};
-        if (a.w) {
+        float weight[RT];
 #pragma unroll
-            for (int rt = 0; rt < 2; ++rt) weight[rt] = a.w[s_list[rt * 16 + r < here ? rt * 16 + r : 0]];
-        }
-        f32x4_hw acc[8];
+        for (int rt = 0; rt < RT; ++rt) weight[rt] = a.w ? a.w[s_list[rt * 16 + r < here ? rt * 16 + r : 0]] : 1.0f;
+        f32x4_hw acc[4][RT];                               // of 16 weight rows and 16 routed rows each
 #pragma unroll
-        for (int c = 0; c < 8; ++c) acc[c] = f32x4_hw{0, 0, 0, 0};
-        if (e >= 0 && n0 < a.N) {
-            if (rts == 1) few_stream<XT, 4, 1>(a, f, s_list, here, reinterpret_cast<f32x4_hw(*)[1]>(acc));
-            else few_stream<XT, 4, 2>(a, f, s_list, here, reinterpret_cast<f32x4_hw(*)[2]>(acc));
-        }
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-            if (c < 4 * rts) s_sum[wid][c][lane] = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+            for (int rt = 0; rt < RT; ++rt) acc[t][rt] = f32x4_hw{0, 0, 0, 0};
+        if (e >= 0 && n0 < a.N) few_stream<XT, RT>(a, f, s_list, here, s_own[wid], s_own[wid] + W_SLOTS, s_scales[wid], acc);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                reinterpret_cast<float4*>(s_own[wid])[(t * RT + rt) * 64 + lane] = make_float4(acc[t][rt][0], acc[t][rt][1], acc[t][rt][2], acc[t][rt][3]);
         if (shares > 1) __syncthreads();
+        else wave_order();
         // each wavefront finishes its share of its group's sums
-        for (int c = part_k; c < 4 * rts; c += shares) {
-            const int n = n0 + c / rts * 16 + q * 4, at = c % rts * 16 + r;
+        for (int c = part_k; c < 4 * RT; c += shares) {
+            const int n = n0 + c / RT * 16 + q * 4, at = c % RT * 16 + r;
             if (at >= here || n >= a.N) continue;
             float v[4] = {0, 0, 0, 0};
             for (int w = group * shares; w < (group + 1) * shares; ++w) {
-                const float4 p = s_sum[w][c][lane];
+                const float4 p = reinterpret_cast<const float4*>(s_own[w])[c * 64 + lane];
                 v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = e < 0 ? 0.0f : w4_finish(v[j], a.gelu, weight[c % rts]);
+            for (int j = 0; j < 4; ++j) v[j] = e < 0 ? 0.0f : w4_finish(v[j], a.gelu, c % RT ? weight[RT - 1] : weight[0]);
             w4_store(a, s_list[at], n, v);
         }
         __syncthreads();
@@ -535,17 +610,20 @@ __global__ __launch_bounds__(W4_WAVES * 64) void w4_rows_kernel(W4Args a) {
     constexpr int Q_SLOTS = 17, I_SLOTS = 4 * Q_SLOTS + 1, TILE_SLOTS = 4 * I_SLOTS;
     constexpr int STAGE = TILES * RT * PARTS * TILE_SLOTS;                    // of one share of K
     constexpr int UNITS = WK * CAP * TILES * 16, PER_THREAD = (UNITS + W4_WAVES * 64 - 1) / (W4_WAVES * 64);
-    __shared__ uint4 s_x[2][WK * STAGE];
+    __shared__ uint4 s_x[2][WK * STAGE], s_w[W4_WAVES][Block16<TILES>::SLOTS];
     __shared__ float s_scale[2][XT == MOE_E4M3 ? WK * TILES * CAP : 1];
     __shared__ int s_list[CAP], s_count[W4_WAVES];
     static_assert(sizeof(s_x) >= (size_t)(WK > 1 ? W4_WAVES * RT * 64 * 16 : 0), "the joined sums need room");
     const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63, r = lane & 15, q = lane >> 4;
-    const int part_k = wid / WN, n0 = (blockIdx.x * WN + wid % WN) * 16, n = n0 + r;
+    const int part_k = wid / WN, n0 = (blockIdx.x * WN + wid % WN) * 16;
     int e = a.idx ? (int)blockIdx.y : 0;
     if (e >= a.E) e = -1;                                  // the rows of no expert, which are zeroed
-    const long long wrow = (long long)(e < 0 ? 0 : e) * a.N + n;
-    const uint8_t* Wq = n < a.N ? a.Wq + wrow * (a.K / 2) : nullptr;
-    const uint8_t* Ws = n < a.N ? a.Ws + wrow * (a.K / 32) : nullptr;
+    const uint8_t* Wq = a.Wq + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 2);
+    unsigned offset[TILES];
+    Block16<TILES>::offsets(n0, a.N, a.K, lane, offset);
+    // lane l has the scales of weight row l / TILES in tile l % TILES (of 16 rows: then they begin again)
+    const int scale_row = n0 + lane / TILES % 16 < a.N ? n0 + lane / TILES % 16 : a.N - 1;
+    const uint8_t* Ws = a.Ws + ((long long)(e < 0 ? 0 : e) * a.N + scale_row) * (a.K / 32);
     const int tiles = (a.K + 127) / 128, per_share = ((tiles + WK - 1) / WK + TILES - 1) / TILES * TILES;
     for (int from = 0;; from += CAP) {
         int total;
@@ -619,27 +697,39 @@ __global__ __launch_bounds__(W4_WAVES * 64) void w4_rows_kernel(W4Args a) {
             }
             if (XT == MOE_E4M3 && tid < WK * TILES * CAP) s_scale[buf][tid] = scale;
         };
-        Weights<TILES> now, next;
+        Block16<TILES> w;
+        Scales next;
+        unsigned now;
         const int w_tile0 = part_k * per_share;
-        now.load(Wq, Ws, w_tile0, q, a.K);
+        auto request_weights = [&](int tile) {
+            w.load(Wq, offset, tile, lane, a.K);
+            next.load(Ws, tile + lane % TILES, a.K);
+        };
+        request_weights(w_tile0);
         request(0);
         put(0);
         __syncthreads();
         for (int tile = 0, buf = 0; tile < per_share; tile += TILES, buf ^= 1) {
             const bool more = tile + TILES < per_share;
+            w.put(s_w[wid], lane);
+            now = next.get();
+            wave_order();
             if (more) {
-                next.load(Wq, Ws, w_tile0 + tile + TILES, q, a.K);
+                request_weights(w_tile0 + tile + TILES);
                 request(tile + TILES);
             }
+            __builtin_amdgcn_sched_barrier(0);
             const uint4* x = s_x[buf] + part_k * STAGE;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 f32x4_hw part[RT];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) part[rt] = XT == MOE_E4M3 ? f32x4_hw{0, 0, 0, 0} : acc[rt];
+                const uint4 wt = Block16<TILES>::get(s_w[wid], t, r, q);
+                const unsigned st = from_any_lane(now, r * TILES + t) >> (8 * q) & 0xffu;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bf16x8_hw d = now.decode(t, i, q);
+                    const bf16x8_hw d = decode_weights(word_of(wt, i), st);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -655,10 +745,8 @@ __global__ __launch_bounds__(W4_WAVES * 64) void w4_rows_kernel(W4Args a) {
                     for (int j = 0; j < 4; ++j) acc[rt][j] = XT == MOE_E4M3 ? fmaf(xs, part[rt][j], acc[rt][j]) : part[rt][j];
                 }
             }
-            if (more) {
-                put(buf ^ 1);
-                now = next;
-            }
+            wave_order();
+            if (more) put(buf ^ 1);
             __syncthreads();
         }
         if constexpr (WK > 1) {
@@ -785,10 +873,12 @@ template <int XT> void w4_token_launch(const W4Args& a, bool sum, hipStream_t s)
         int slices = a.k <= TOKEN_WAVES ? TOKEN_WAVES / a.k : 1;
         slices = slices < want ? slices : want;
         const int waves = a.k <= TOKEN_WAVES ? slices * a.k : TOKEN_WAVES;
-        w4_token_kernel<XT, true><<<blocks, waves * 64, 0, s>>>(a, slices);
+        if (waves <= 4) w4_token_kernel<XT, true, 4><<<blocks, waves * 64, 0, s>>>(a, slices);
+        else w4_token_kernel<XT, true, TOKEN_WAVES><<<blocks, waves * 64, 0, s>>>(a, slices);
     } else {
         const int waves = want < TOKEN_WAVES ? want : TOKEN_WAVES;
-        w4_token_kernel<XT, false><<<dim3(blocks, a.k), waves * 64, 0, s>>>(a, waves);
+        if (waves <= 4) w4_token_kernel<XT, false, 4><<<dim3(blocks, a.k), waves * 64, 0, s>>>(a, waves);
+        else w4_token_kernel<XT, false, TOKEN_WAVES><<<dim3(blocks, a.k), waves * 64, 0, s>>>(a, waves);
     }
 }
 
@@ -811,12 +901,25 @@ template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hi
     const int rows = (a.n_rows + experts - 1) / experts;
     if constexpr (XT != MOE_F32) {
         // (three parts of a float row do not fit into the registers beside two tiles)
-        if (rows <= 10) {
+        // (and offsets in x are 32-bit there)
+        const long long x_bytes = (a.per_choice ? (long long)a.n_rows : (long long)T) * a.ldx * row_bytes(XT, 1);
+        if (rows <= 10 && x_bytes < (1ll << 32)) {
+            // As many shares of K as still let all wavefronts be there at once (eight to a compute unit): with a third more of
+            // them than that, a second round for these few takes as long as the first.
             const int columns = (a.N + 63) / 64, tiles = (a.K + 127) / 128;
+            const double chosen = a.idx ? a.E * (1.0 - std::pow(1.0 - (double)a.k / a.E, (double)T)) : 1.0;   // experts, expected
+            const int waves = 2 * FEW_WAVES * chosen * columns <= 8.0 * compute_units() && 2 * FEW_WAVES <= tiles ? FEW_MORE : FEW_WAVES;
             int shares = 1;
-            while (shares < FEW_WAVES && (long long)experts * columns * shares < 16 * compute_units() && 2 * shares <= tiles) shares *= 2;
-            const int groups = FEW_WAVES / shares;
-            w4_few_kernel<XT><<<dim3((columns + groups - 1) / groups, slots), FEW_WAVES * 64, 0, s>>>(a, shares);
+            while (shares < waves && 2 * shares * chosen * columns <= 8.0 * compute_units() && 2 * shares <= tiles) shares *= 2;
+            const int groups = waves / shares;
+            const dim3 grid((columns + groups - 1) / groups, slots);
+            if (rows <= 4) {
+                if (waves == FEW_WAVES) w4_few_kernel<XT, 1, FEW_WAVES><<<grid, FEW_WAVES * 64, 0, s>>>(a, shares);
+                else w4_few_kernel<XT, 1, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
+            } else {
+                if (waves == FEW_WAVES) w4_few_kernel<XT, 2, FEW_WAVES><<<grid, FEW_WAVES * 64, 0, s>>>(a, shares);
+                else w4_few_kernel<XT, 2, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
+            }
             return;
         }
     }
