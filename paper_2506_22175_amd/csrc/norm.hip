@@ -9,6 +9,7 @@
 // leaves no barrier in the row's sum.  Rows need the alignment of their elements only: the hardware does wide accesses
 // at any address, and a row's last unit, if it is not full, goes element by element.
 #include "common.h"
+#include "lanes.h"
 #include "wide.h"
 #include <cmath>
 
@@ -92,28 +93,6 @@ __device__ __forceinline__ void load_gain(const float* gain, int col, int left, 
     for (int i = 0; i < 8; ++i) g[i] = u.at(i);
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
-__device__ __forceinline__ unsigned wave_max(unsigned v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        const unsigned o = (unsigned)__shfl_xor((int)v, off, 64);
-        v = v > o ? v : o;
-    }
-    return v;
-}
-// over the 16 lanes whose units make 128 columns: rotations inside a row of lanes
-template <int ROTATE> __device__ __forceinline__ unsigned max_rotated(unsigned v) {
-    const unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + ROTATE, 0xf, 0xf, false);
-    return v > o ? v : o;
-}
-__device__ __forceinline__ unsigned max_of_16(unsigned v) {
-    return max_rotated<1>(max_rotated<2>(max_rotated<4>(max_rotated<8>(v))));
-}
-
 // sum / largest over the threads of a row (one wavefront, or the workgroup's waves through `s`)
 template <int WAVES> __device__ __forceinline__ float row_sum(float v, float* s) {
     v = wave_sum(v);
@@ -128,7 +107,7 @@ template <int WAVES> __device__ __forceinline__ float row_sum(float v, float* s)
     return v;
 }
 template <int WAVES> __device__ __forceinline__ unsigned row_max(unsigned v, float* s) {
-    v = wave_max(v);
+    v = wave_max_bits(v);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __uint_as_float(v);
         __syncthreads();
@@ -191,6 +170,16 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(Nor
             h[u][i] = r ? ux[u].at(i) + ur[u].at(i) : ux[u].at(i);
             sum = fmaf(h[u][i], h[u][i], sum);
         }
+    // The gain is requested before the stores of h, behind which it cannot go ahead, where it does not cost wavefronts.
+    constexpr bool EARLY = UNITS <= 2;
+    Unit8<float> ug[EARLY ? UNITS : 1];
+    if (EARLY && a.gain) {
+#pragma unroll
+        for (int u = 0; u < (EARLY ? UNITS : 0); ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            if (left > 0) ug[u].load(a.gain + col, left);
+        }
+    }
     if (a.h) {
         T* ho = reinterpret_cast<T*>(a.h) + row * a.ldh;
 #pragma unroll
@@ -214,11 +203,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(Nor
             }
             continue;
         }
-        float g[8];
-        load_gain(a.gain, col, left, g);
+        if (!EARLY && a.gain) ug[0].load(a.gain + col, left);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            h[u][i] = h[u][i] * rstd * g[i];
+            h[u][i] *= rstd;
+            if (a.gain) h[u][i] *= ug[EARLY ? u : 0].at(i);
             if constexpr (E4M3) {
                 const unsigned m = __float_as_uint(h[u][i]) & 0x7fffffffu;
                 if (i < left && m > most[u]) most[u] = m;
@@ -229,7 +218,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(Nor
     if constexpr (E4M3) {
         if (a.group) {
 #pragma unroll
-            for (int u = 0; u < UNITS; ++u) most[u] = max_of_16(most[u]);
+            for (int u = 0; u < UNITS; ++u) most[u] = row_max_bits(most[u]);        // 16 lanes' units make 128 columns
         } else {
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) row_most = row_most > most[u] ? row_most : most[u];
@@ -283,58 +272,60 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_bwd_kernel
     for (int u = 0; u < UNITS; ++u)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dg[u][i] = 0.0f;
-    for (long long row = (long long)blockIdx.x * ROWS + sub; row < a.T; row += (long long)gridDim.x * ROWS) {
+    const long long step = (long long)gridDim.x * ROWS;
+    Unit8<T> ud[UNITS], uh[UNITS], ub[UNITS];
+    float rstd = 0.0f;
+    auto request = [&](long long row) {
         const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.ldy;
         const T* hp = reinterpret_cast<const T*>(a.h) + row * a.ldh;
-        const T* dh = a.dh ? reinterpret_cast<const T*>(a.dh) + row * a.ldh : nullptr;
-        Unit8<T> ud[UNITS], uh[UNITS], ub[UNITS];
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            const int col = (u * THREADS + tid) * 8, left = a.M - col;
-            ud[u].zero();
-            uh[u].zero();
-            if (left > 0) {
-                ud[u].load(dy + col, left);
-                uh[u].load(hp + col, left);
-            }
-        }
-        if (dh) {
-#pragma unroll
-            for (int u = 0; u < UNITS; ++u) {
-                const int col = (u * THREADS + tid) * 8, left = a.M - col;
-                ub[u].zero();
-                if (left > 0) ub[u].load(dh + col, left);
-            }
-        }
-        const float rstd = a.rstd[row];
-        float sum = 0.0f;
-        // two passes over the registers: the gain comes from the L1 cache both times, which is cheaper than 8 UNITS registers
+        const T* dh = reinterpret_cast<const T*>(a.dh) + row * a.ldh;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             const int col = (u * THREADS + tid) * 8, left = a.M - col;
             if (left <= 0) continue;
+            ud[u].load(dy + col, left);
+            uh[u].load(hp + col, left);
+            if (a.dh) ub[u].load(dh + col, left);
+        }
+        rstd = a.rstd[row];
+    };
+    // Where the registers allow it the next row is on its way while one is summed up and stored.
+    constexpr bool AHEAD = UNITS <= 2;
+    long long row = (long long)blockIdx.x * ROWS + sub;
+    if (AHEAD && row < a.T) request(row);
+    for (; row < a.T; row += step) {
+        if (!AHEAD) request(row);
+        float n[UNITS][8], d[UNITS][8], sum = 0.0f;
+        Unit8<T> plus[UNITS];
+        const float r = rstd;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int col = (u * THREADS + tid) * 8, left = a.M - col;
+            if (left <= 0) continue;
+            plus[u] = ub[u];
             float g[8];
             load_gain(a.gain, col, left, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = ud[u].at(i), n = uh[u].at(i) * rstd;
-                dg[u][i] = fmaf(d, n, dg[u][i]);
-                if (i < left) sum = fmaf(d * g[i], n, sum);
+                n[u][i] = uh[u].at(i) * r;
+                d[u][i] = ud[u].at(i);
+                dg[u][i] = fmaf(d[u][i], n[u][i], dg[u][i]);
+                d[u][i] *= g[i];
+                if (i < left) sum = fmaf(d[u][i], n[u][i], sum);
             }
         }
+        if (AHEAD && row + step < a.T) request(row + step);
         const float mean = row_sum<WAVES>(sum, s_part) / (float)a.M;
         T* dx = reinterpret_cast<T*>(a.dx) + row * a.ldx;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             const int col = (u * THREADS + tid) * 8, left = a.M - col;
             if (left <= 0) continue;
-            float g[8], o[8];
-            load_gain(a.gain, col, left, g);
+            float o[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = ud[u].at(i), n = uh[u].at(i) * rstd;
-                o[i] = rstd * fmaf(-n, mean, d * g[i]);
-                if (dh) o[i] += ub[u].at(i);
+                o[i] = r * fmaf(-n[u][i], mean, d[u][i]);
+                if (a.dh) o[i] += plus[u].at(i);
             }
             Unit8<T>::store(dx + col, o, left);
         }
@@ -373,8 +364,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_bwd_kernel
     }
 }
 
-// dgain (+)= the sums of `parts` workgroups, 32 columns to a workgroup: 32 threads a column, each takes every 32nd part
-constexpr int DG_COLS = 32, DG_SPLIT = 32;
+// dgain (+)= the sums of `parts` workgroups, 16 columns to a workgroup: 64 threads a column, each takes every 64th part
+constexpr int DG_COLS = 16, DG_SPLIT = 64;
 __global__ __launch_bounds__(DG_COLS * DG_SPLIT) void norm_dgain_kernel(const float* __restrict__ part, int parts, int M, int add,
                                                                         float* __restrict__ dgain) {
     __shared__ float s[DG_SPLIT][DG_COLS + 1];
@@ -420,12 +411,25 @@ moe_status norm_dims(const moe_norm_config* c, NormDims* d) {
 struct RowPlan { int waves, units; };
 RowPlan norm_plan(int T, int M) {
     const int units = (M + 7) / 8;
-    (void)T;
+    const bool alone = T < 64;
     if (units <= 64) return {1, 1};
+    if (alone && units <= 256) return {4, 1};
     if (units <= 128) return {1, 2};
     if (units <= 256) return {1, 4};
     if (units <= 512) return {4, 2};
+    if (alone && units <= 1024) return {16, 1};
     if (units <= 1024) return {4, 4};
+    if (units <= 2048) return {16, 2};
+    return {16, 4};
+}
+
+// Backward keeps more to a column: few units to a thread, so that the next row can be on its way.
+RowPlan norm_bwd_plan(int M) {
+    const int units = (M + 7) / 8;
+    if (units <= 64) return {1, 1};
+    if (units <= 256) return {4, 1};
+    if (units <= 512) return {4, 2};
+    if (units <= 1024) return {16, 1};
     if (units <= 2048) return {16, 2};
     return {16, 4};
 }
@@ -433,14 +437,14 @@ RowPlan norm_plan(int T, int M) {
 template <typename T, bool E4M3> void norm_launch(const NormArgs& a, RowPlan p, hipStream_t s) {
 #define NORM_CASE(W, U) if (p.waves == W && p.units == U) { \
         norm_kernel<T, E4M3, W, U><<<W == 1 ? (a.T + 3) / 4 : a.T, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
-    NORM_CASE(1, 1) NORM_CASE(1, 2) NORM_CASE(1, 4) NORM_CASE(4, 2) NORM_CASE(4, 4) NORM_CASE(16, 2) NORM_CASE(16, 4)
+    NORM_CASE(1, 1) NORM_CASE(1, 2) NORM_CASE(1, 4) NORM_CASE(4, 1) NORM_CASE(4, 2) NORM_CASE(4, 4) NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(16, 4)
 #undef NORM_CASE
 }
 
 template <typename T> void norm_bwd_launch(const NormBwdArgs& a, RowPlan p, int blocks, hipStream_t s) {
 #define NORM_CASE(W, U) if (p.waves == W && p.units == U) { \
         norm_bwd_kernel<T, W, U><<<blocks, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
-    NORM_CASE(1, 1) NORM_CASE(1, 2) NORM_CASE(1, 4) NORM_CASE(4, 2) NORM_CASE(4, 4) NORM_CASE(16, 2) NORM_CASE(16, 4)
+    NORM_CASE(1, 1) NORM_CASE(4, 1) NORM_CASE(4, 2) NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(16, 4)
 #undef NORM_CASE
 }
 
@@ -481,7 +485,7 @@ extern "C" moe_status moe_norm_scratch_bytes(const moe_norm_config* cfg, size_t*
     moe::NormDims d;
     MOE_TRY(moe::norm_dims(cfg, &d));
     if (!bytes) return MOE_ERR_NULL;
-    const int blocks = moe::norm_bwd_blocks(d.T, moe::norm_plan(d.T, d.M));
+    const int blocks = moe::norm_bwd_blocks(d.T, moe::norm_bwd_plan(d.M));
     *bytes = blocks > 1 ? (size_t)blocks * d.M * sizeof(float) : 0;
     return MOE_OK;
 }
@@ -491,7 +495,7 @@ extern "C" moe_status moe_norm_bwd(const moe_norm_config* cfg, const void* dy, c
     moe::NormDims d;
     MOE_TRY(moe::norm_dims(cfg, &d));
     if (cfg->out == MOE_E4M3) return MOE_ERR_UNSUPPORTED;      // gradients of rounded rows are not defined here
-    const moe::RowPlan p = moe::norm_plan(d.T, d.M);
+    const moe::RowPlan p = moe::norm_bwd_plan(d.M);
     const int blocks = moe::norm_bwd_blocks(d.T, p);
     if (d.T > 0 && (!dy || !h || !rstd || !dx)) return MOE_ERR_NULL;
     if (dgain && blocks > 1 && !scratch) return MOE_ERR_NULL;

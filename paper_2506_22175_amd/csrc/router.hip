@@ -11,6 +11,7 @@
 // are compared in float, and where two that follow one another lie within that error (one token in a few hundred) the
 // wavefront's tokens are done again with 64-bit scores.
 #include "common.h"
+#include "lanes.h"
 #include "wide.h"
 #include <cmath>
 
@@ -33,16 +34,6 @@ __device__ __forceinline__ double exp_of(double x) { return exp(x); }
 
 constexpr int LANES = 16;            // of a token: as many as there may be choices and groups
 constexpr int BLOCK = 512;
-
-// A lane's value of another lane of its 16: 1 and 2 away, mirrored in 8, mirrored in 16 (what is 4 and 8 away once the nearer
-// ones agree), or rotated.  All lanes add and compare the same pairs, so that all end with the same bits.
-template <int CTRL> __device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
-template <int CTRL> __device__ __forceinline__ float from_lane(float v) { return __int_as_float(from_lane<CTRL>(__float_as_int(v))); }
-template <int CTRL> __device__ __forceinline__ double from_lane(double v) {
-    const long long b = __double_as_longlong(v);
-    return __longlong_as_double((long long)from_lane<CTRL>((int)(b >> 32)) << 32 | (unsigned)from_lane<CTRL>((int)b));
-}
-constexpr int AWAY_1 = 0xB1, AWAY_2 = 0x4E, MIRROR_8 = 0x141, MIRROR_16 = 0x140, ROTATE = 0x120;
 
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
@@ -409,7 +400,17 @@ __global__ __launch_bounds__(BLOCK, VALUES <= 16 ? 4 : 2) void router_kernel(Rou
         const int mine = __shfl(c, lane, 64);
         if (((threadIdx.x & 63) / LANES) == token) chosen = mine;
     }
-    const float z = chosen >= 0 ? load_logit(row + chosen) : -__builtin_inff();
+    // the chosen logits: from the lanes that have them, or, where those have many, from memory again
+    float z = -__builtin_inff();
+    if constexpr (VALUES <= 4) {
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) {
+            const float o = __shfl(l[v], chosen / VALUES, LANES);
+            z = chosen >= 0 && chosen % VALUES == v ? o : z;
+        }
+    } else if (chosen >= 0) {
+        z = load_logit(row + chosen);
+    }
     float w;
     if (a.renorm) {
         // Scores that are all tiny are scaled up together before they are divided by their sum.
@@ -438,8 +439,9 @@ __global__ __launch_bounds__(BLOCK, VALUES <= 16 ? 4 : 2) void router_kernel(Rou
     }
 }
 
-// load[e] += how often e is in idx.  For the router's own workgroups to add their counts up would take as long as they
-// have taken to choose: what they add meets in a few cache lines, which take a request about every 5 ns.
+// load[e] += how often e is in idx.  Many of the router's own workgroups adding their counts up would take longer than they
+// have taken to choose: what they add meets in a few cache lines, which take a request about every 5 ns (32768 tokens, 64
+// experts: 14 us with that, 8 us with this launch behind it).
 __global__ __launch_bounds__(1024) void router_load_kernel(const int* __restrict__ idx, long long n, int E, int* __restrict__ load) {
     __shared__ int hist[512];
     for (int e = threadIdx.x; e < E; e += 1024) hist[e] = 0;
@@ -560,13 +562,13 @@ int router_values(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <=
         case 1: LAUNCH(1); break; case 2: LAUNCH(2); break; case 4: LAUNCH(4); break; \
         case 8: LAUNCH(8); break; case 16: LAUNCH(16); break; default: LAUNCH(32); } } while (0)
 
-// Workgroups of the router that still count by themselves.
-constexpr int COUNT_BLOCKS = 32;
+// Cache lines that the router's own workgroups may add to; and the workgroups of the launch that counts instead.
+constexpr int COUNT_LINES = 512, COUNT_BLOCKS = 32;
 
 template <typename T> void router_launch(RouterArgs a, hipStream_t s) {
     const int tokens = BLOCK / LANES, blocks = (a.T + tokens - 1) / tokens;
     int* const load = a.load;
-    if (blocks > COUNT_BLOCKS) a.load = nullptr;
+    if ((long long)blocks * ((a.E + 15) / 16) > COUNT_LINES) a.load = nullptr;
 #define ROUTER_LAUNCH(V) router_kernel<T, V><<<blocks, BLOCK, 0, s>>>(a)
     ROUTER_BY_VALUES(a.E, ROUTER_LAUNCH);
 #undef ROUTER_LAUNCH

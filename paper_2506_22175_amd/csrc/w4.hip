@@ -418,8 +418,10 @@ template <int XT> struct RowTile {
         Rows8<XT> x;
         if constexpr (XT == MOE_BF16) {
             x.u = lds[slot(r, q * 4 + i)];
+        } else if constexpr (XT == MOE_F32) {
+            x.u[0] = __builtin_bit_cast(float4, lds[slot(r, q * 8 + 2 * i)]);
+            x.u[1] = __builtin_bit_cast(float4, lds[slot(r, q * 8 + 2 * i + 1)]);
         } else {
-            static_assert(XT == MOE_E4M3, "");
             x.u = reinterpret_cast<const uint2*>(&lds[slot(r, q * 2 + i / 2)])[i % 2];
         }
         return x;
@@ -500,7 +502,9 @@ __device__ __forceinline__ void few_stream(const W4Args& a, const FewShare& f, c
                 const bf16x8_hw d = decode_weights(word_of(w[t], i), s[t]);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    part[t][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, __builtin_bit_cast(bf16x8_hw, p[rt][0]), part[t][rt], 0, 0, 0);
+#pragma unroll
+                    for (int c = row_parts(XT) - 1; c >= 0; --c)
+                        part[t][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, __builtin_bit_cast(bf16x8_hw, p[rt][c]), part[t][rt], 0, 0, 0);
             }
         }
 #pragma unroll
@@ -899,11 +903,10 @@ template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hi
     // experts that may be expected to be chosen, and the rows of each; and one more slot for rows of no expert
     const int experts = !a.idx ? 1 : a.n_rows < a.E ? a.n_rows : a.E, slots = !a.idx ? 1 : join ? a.E : a.E + 1;
     const int rows = (a.n_rows + experts - 1) / experts;
-    if constexpr (XT != MOE_F32) {
-        // (three parts of a float row do not fit into the registers beside two tiles)
-        // (and offsets in x are 32-bit there)
+    {
+        // (offsets in x are 32-bit there)
         const long long x_bytes = (a.per_choice ? (long long)a.n_rows : (long long)T) * a.ldx * row_bytes(XT, 1);
-        if (rows <= 10 && x_bytes < (1ll << 32)) {
+        if (rows <= (XT == MOE_F32 ? 4 : 32) && x_bytes < (1ll << 32)) {
             // As many shares of K as still let all wavefronts be there at once (eight to a compute unit): with a third more of
             // them than that, a second round for these few takes as long as the first.
             const int columns = (a.N + 63) / 64, tiles = (a.K + 127) / 128;
@@ -913,10 +916,11 @@ template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hi
             while (shares < waves && 2 * shares * chosen * columns <= 8.0 * compute_units() && 2 * shares <= tiles) shares *= 2;
             const int groups = waves / shares;
             const dim3 grid((columns + groups - 1) / groups, slots);
+            // 16 rows at a time, or 32 (of float rows 16: more would not fit into LDS)
             if (rows <= 4) {
                 if (waves == FEW_WAVES) w4_few_kernel<XT, 1, FEW_WAVES><<<grid, FEW_WAVES * 64, 0, s>>>(a, shares);
                 else w4_few_kernel<XT, 1, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
-            } else {
+            } else if constexpr (XT != MOE_F32) {
                 if (waves == FEW_WAVES) w4_few_kernel<XT, 2, FEW_WAVES><<<grid, FEW_WAVES * 64, 0, s>>>(a, shares);
                 else w4_few_kernel<XT, 2, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
             }

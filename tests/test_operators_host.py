@@ -13,11 +13,11 @@ F32, BF16, E4M3 = B.MOE_F32, B.MOE_BF16, B.MOE_E4M3
 
 
 def _norm_fwd(cfg, *args):
-    return B.lib().moe_norm_fwd(ctypes.byref(cfg), *(args or (P,) * 8), None)
+    return B.lib().moe_norm_fwd(ctypes.byref(cfg), *(args or (P,) * 7), None)
 
 
 def _norm_bwd(cfg, *args):
-    return B.lib().moe_norm_bwd(ctypes.byref(cfg), *(args or (P,) * 9), None)
+    return B.lib().moe_norm_bwd(ctypes.byref(cfg), *(args or (P,) * 8), None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -39,15 +39,15 @@ def test_norm_refuses(kw, status):
 def test_norm_needs_its_pointers():
     cfg = B.make_norm_config(4, 64)
     for missing in (0, 4):                                       # x, y
-        assert _norm_fwd(cfg, *[NONE if i == missing else P for i in range(8)]) == NULL
-    assert _norm_fwd(B.make_norm_config(4, 64, out=E4M3), *[NONE if i == 5 else P for i in range(8)]) == NULL
+        assert _norm_fwd(cfg, *[NONE if i == missing else P for i in range(7)]) == NULL
+    assert _norm_fwd(B.make_norm_config(4, 64, out=E4M3), *[NONE if i == 5 else P for i in range(7)]) == NULL
     for missing in (0, 1, 3, 5):                                 # dy, h, rstd, dx
         assert _norm_bwd(cfg, *[NONE if i == missing else P for i in range(8)]) == NULL
     many = B.make_norm_config(100, 64)
     assert B.moe_norm_scratch_bytes(many) > 0
     assert _norm_bwd(many, *[NONE if i == 7 else P for i in range(8)]) == NULL
     assert _norm_bwd(B.make_norm_config(4, 64, out=E4M3)) == UNSUPPORTED     # no gradient of rounded rows
-    assert B.lib().moe_norm_fwd(None, *(P,) * 8, None) == NULL
+    assert B.lib().moe_norm_fwd(None, *(P,) * 7, None) == NULL
 
 
 def test_norm_scratch_is_bounded():
@@ -123,8 +123,8 @@ def test_w4_needs_its_pointers_and_their_alignment():
 
 def test_a_batch_without_tokens_is_no_error_and_launches_nothing():
     before = B.moe_launch_counts()
-    assert _norm_fwd(B.make_norm_config(0, 64), *(NONE,) * 8) == 0
-    assert _norm_bwd(B.make_norm_config(0, 64), *(NONE,) * 8, None) == 0
+    assert _norm_fwd(B.make_norm_config(0, 64), *(NONE,) * 7) == 0
+    assert _norm_bwd(B.make_norm_config(0, 64), *(NONE,) * 8) == 0
     assert _router(B.make_router_config(0, 8, 2), (NONE,) * 5, (NONE,) * 4) == (0, 0)
     assert _w4(B.make_w4_config(0, 1, 4, 64, 64), (NONE,) * 8) == 0
     assert B.moe_launch_counts() == before
