@@ -189,13 +189,19 @@ __device__ __forceinline__ void fetch_scales(const uint8_t* Ws, int n0, int N, i
         } else if (at >= bytes) {
             u[j] = make_uint4(0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f);
         } else {
-            // the row's last bytes one by one, 1 behind them
+            // the row's last words, the last one's bytes one by one, 1 behind them
             unsigned w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                w[i] = 0;
+                const int first = at + 4 * i;
+                w[i] = 0x7f7f7f7f;
+                if (first + 4 <= bytes) {
+                    w[i] = reinterpret_cast<const Anywhere<4, 1>*>(row + first)->w[0];
+                } else if (first < bytes) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) w[i] |= (at + 4 * i + b < bytes ? (unsigned)row[at + 4 * i + b] : 0x7fu) << (8 * b);
+                    for (int b = 0; b < 3; ++b)
+                        if (first + b < bytes) w[i] = (w[i] & ~(0xffu << (8 * b))) | (unsigned)row[first + b] << (8 * b);
+                }
             }
             u[j] = make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -357,29 +363,42 @@ __global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slic
 constexpr int W4_WAVES = 8;
 
 // Rows of assignments with expert e (e < 0: with none of the experts), number `from` to from + cap - 1 of them, into `list`;
-// returns how many there are in all.  Every thread of the workgroup calls it.
+// returns how many there are in all.  Every thread of the workgroup calls it.  Each wavefront counts its share of the
+// assignments, and goes through it again when it knows where its numbers begin.
 template <int WAVES> __device__ int collect_rows(const int* idx, int n, int e, int E, int from, int cap, int* list, int* s_count) {
+    constexpr int AT_ONCE = 4;                             // requests of a wavefront under way
     const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int total = 0;
-    for (int base = 0; base < n; base += WAVES * 64) {
-        const int i = base + threadIdx.x;
-        bool mine = false;
-        if (i < n) {
-            const int v = idx[i];
-            mine = e < 0 ? (unsigned)v >= (unsigned)E : v == e;
-        }
-        const unsigned long long b = __ballot(mine);
-        if (lane == 0) s_count[wid] = __popcll(b);
-        __syncthreads();
-        int rank = total + __popcll(b & ((1ull << lane) - 1));
+    const int share = (n + WAVES * 64 - 1) / (WAVES * 64) * 64, begin = wid * share, end = begin + share < n ? begin + share : n;
+    int rank = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int base = begin; base < end; base += AT_ONCE * 64) {
+            int v[AT_ONCE];
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            if (w < wid) rank += s_count[w];
-            total += s_count[w];
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = base + u * 64 + lane;
+                v[u] = idx[i < end ? i : end - 1];
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = base + u * 64 + lane;
+                const bool mine = i < end && (e < 0 ? (unsigned)v[u] >= (unsigned)E : v[u] == e);
+                const unsigned long long b = __ballot(mine);
+                const int at = rank + __popcll(b & ((1ull << lane) - 1));
+                if (pass == 1 && mine && at >= from && at < from + cap) list[at - from] = i;
+                rank += __popcll(b);
+            }
         }
-        if (mine && rank >= from && rank < from + cap) list[rank - from] = i;
-        __syncthreads();
+        if (pass == 0) {
+            if (lane == 0) s_count[wid] = rank;
+            __syncthreads();
+            rank = 0;
+            for (int w = 0; w < wid; ++w) rank += s_count[w];
+        }
     }
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total += s_count[w];
+    __syncthreads();
     return total;
 }
 
@@ -549,7 +568,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void w4_few_kernel(W4Args a, int sha
     f.end = f.begin + share < tiles ? f.begin + share : tiles;
     f.Wq = a.Wq + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 2);
     f.Ws = a.Ws + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 32);
-    for (int from = 0;; from += CAP) {
+    for (int from = blockIdx.z * CAP;; from += gridDim.z * CAP) {
         int total;
         if (a.idx) {
             total = collect_rows<WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
@@ -590,6 +609,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void w4_few_kernel(W4Args a, int sha
             for (int j = 0; j < 4; ++j) v[j] = e < 0 ? 0.0f : w4_finish(v[j], a.gelu, c % RT ? weight[RT - 1] : weight[0]);
             w4_store(a, s_list[at], n, v);
         }
+        if (from + (int)gridDim.z * CAP >= total) return;
         __syncthreads();
     }
 }
@@ -629,7 +649,7 @@ __global__ __launch_bounds__(W4_WAVES * 64) void w4_rows_kernel(W4Args a) {
     const int scale_row = n0 + lane / TILES % 16 < a.N ? n0 + lane / TILES % 16 : a.N - 1;
     const uint8_t* Ws = a.Ws + ((long long)(e < 0 ? 0 : e) * a.N + scale_row) * (a.K / 32);
     const int tiles = (a.K + 127) / 128, per_share = ((tiles + WK - 1) / WK + TILES - 1) / TILES * TILES;
-    for (int from = 0;; from += CAP) {
+    for (int from = blockIdx.z * CAP;; from += gridDim.z * CAP) {
         int total;
         if (a.idx) {
             total = collect_rows<W4_WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
@@ -781,6 +801,7 @@ __global__ __launch_bounds__(W4_WAVES * 64) void w4_rows_kernel(W4Args a) {
                 w4_store(a, s_list[at], n0 + q * 4, v);
             }
         }
+        if (from + (int)gridDim.z * CAP >= total) return;
         __syncthreads();
     }
 }
@@ -886,15 +907,36 @@ template <int XT> void w4_token_launch(const W4Args& a, bool sum, hipStream_t s)
     }
 }
 
-template <int XT, int RT> void w4_rows_launch(const W4Args& a, int experts, int slots, hipStream_t s) {
+// Workgroups that share out an expert's rows: as many as three times the mean number wants (a gate's loads differ), or all of
+// them want where they all have one expert.  Those that find no rows left end at once.
+int w4_row_groups(const W4Args& a, int rows, int cap) {
+    const int most = !a.idx || a.n_rows < 3 * rows ? a.n_rows : 3 * rows, groups = (most + cap - 1) / cap;
+    return groups < 64 ? groups : 64;
+}
+
+template <int XT, int RT> void w4_rows_launch(const W4Args& a, int experts, int slots, int rows, hipStream_t s) {
     // All eight wavefronts side by side where that leaves a workgroup for every compute unit, else K in shares.
     constexpr int WK = most_shares<XT, RT>();
-    const int wide = (a.N + 127) / 128, narrow = (a.N + 128 / WK - 1) / (128 / WK);
-    if (WK == 1 || (long long)wide * experts >= compute_units())
-        w4_rows_kernel<XT, RT, 1><<<dim3(wide, slots), W4_WAVES * 64, 0, s>>>(a);
+    const int wide = (a.N + 127) / 128, narrow = (a.N + 128 / WK - 1) / (128 / WK), groups = w4_row_groups(a, rows, 16 * RT);
+    if (WK == 1 || (long long)wide * experts * groups >= compute_units())
+        w4_rows_kernel<XT, RT, 1><<<dim3(wide, slots, groups), W4_WAVES * 64, 0, s>>>(a);
     else
-        w4_rows_kernel<XT, RT, WK><<<dim3(narrow, slots), W4_WAVES * 64, 0, s>>>(a);
+        w4_rows_kernel<XT, RT, WK><<<dim3(narrow, slots, groups), W4_WAVES * 64, 0, s>>>(a);
 }
+
+template <int XT, int RT> void w4_few_launch(const W4Args& a, double chosen, int slots, int rows, hipStream_t s) {
+    // As many shares of K as still let all wavefronts be there at once (eight to a compute unit): with a third more of them than
+    // that, a second round for these few takes as long as the first.
+    const int columns = (a.N + 63) / 64, tiles = (a.K + 127) / 128, row_groups = w4_row_groups(a, rows, 16 * RT);
+    const int waves = 2 * FEW_WAVES * chosen * columns <= 8.0 * compute_units() && 2 * FEW_WAVES <= tiles ? FEW_MORE : FEW_WAVES;
+    int shares = 1;
+    while (shares < waves && 2 * shares * chosen * columns <= 8.0 * compute_units() && 2 * shares <= tiles) shares *= 2;
+    const int groups = waves / shares;
+    const dim3 grid((columns + groups - 1) / groups, slots, row_groups);
+    if (waves == FEW_WAVES) w4_few_kernel<XT, RT, FEW_WAVES><<<grid, FEW_WAVES * 64, 0, s>>>(a, shares);
+    else w4_few_kernel<XT, RT, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
+}
+
 template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hipStream_t s) {
     if (T == 1) {
         w4_token_launch<XT>(a, sum, s);
@@ -903,33 +945,21 @@ template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hi
     // experts that may be expected to be chosen, and the rows of each; and one more slot for rows of no expert
     const int experts = !a.idx ? 1 : a.n_rows < a.E ? a.n_rows : a.E, slots = !a.idx ? 1 : join ? a.E : a.E + 1;
     const int rows = (a.n_rows + experts - 1) / experts;
-    {
-        // (offsets in x are 32-bit there)
-        const long long x_bytes = (a.per_choice ? (long long)a.n_rows : (long long)T) * a.ldx * row_bytes(XT, 1);
-        if (rows <= (XT == MOE_F32 ? 4 : 32) && x_bytes < (1ll << 32)) {
-            // As many shares of K as still let all wavefronts be there at once (eight to a compute unit): with a third more of
-            // them than that, a second round for these few takes as long as the first.
-            const int columns = (a.N + 63) / 64, tiles = (a.K + 127) / 128;
-            const double chosen = a.idx ? a.E * (1.0 - std::pow(1.0 - (double)a.k / a.E, (double)T)) : 1.0;   // experts, expected
-            const int waves = 2 * FEW_WAVES * chosen * columns <= 8.0 * compute_units() && 2 * FEW_WAVES <= tiles ? FEW_MORE : FEW_WAVES;
-            int shares = 1;
-            while (shares < waves && 2 * shares * chosen * columns <= 8.0 * compute_units() && 2 * shares <= tiles) shares *= 2;
-            const int groups = waves / shares;
-            const dim3 grid((columns + groups - 1) / groups, slots);
-            // 16 rows at a time, or 32 (of float rows 16: more would not fit into LDS)
-            if (rows <= 4) {
-                if (waves == FEW_WAVES) w4_few_kernel<XT, 1, FEW_WAVES><<<grid, FEW_WAVES * 64, 0, s>>>(a, shares);
-                else w4_few_kernel<XT, 1, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
-            } else if constexpr (XT != MOE_F32) {
-                if (waves == FEW_WAVES) w4_few_kernel<XT, 2, FEW_WAVES><<<grid, FEW_WAVES * 64, 0, s>>>(a, shares);
-                else w4_few_kernel<XT, 2, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
+    const double chosen = a.idx ? a.E * (1.0 - std::pow(1.0 - (double)a.k / a.E, (double)T)) : 1.0;
+    // (offsets in x are 32-bit in the kernel for few rows)
+    const long long x_bytes = (a.per_choice ? (long long)a.n_rows : (long long)T) * a.ldx * row_bytes(XT, 1);
+    if (rows <= 32 && x_bytes < (1ll << 32)) {
+        // 16 rows at a time, or 32 (of float rows 16: more would not fit into LDS)
+        if constexpr (XT != MOE_F32) {
+            if (rows > 4) {
+                w4_few_launch<XT, 2>(a, chosen, slots, rows, s);
+                return;
             }
-            return;
         }
+        w4_few_launch<XT, 1>(a, chosen, slots, rows, s);
+        return;
     }
-    if (rows <= 10) w4_rows_launch<XT, 1>(a, experts, slots, s);
-    else if (rows <= 24) w4_rows_launch<XT, 2>(a, experts, slots, s);
-    else w4_rows_launch<XT, 4>(a, experts, slots, s);
+    w4_rows_launch<XT, 4>(a, experts, slots, rows, s);
 }
 
 }  // namespace

@@ -243,3 +243,25 @@ def test_packing_marks_blocks_that_are_not_finite():
     Wq, Ws = torch.empty((1, 2, 48), dtype=torch.uint8, device=DEV), torch.empty((1, 2, 3), dtype=torch.uint8, device=DEV)
     B.moe_w4_quantize(1, 96, 2, F32, W.to(DEV), Wq, Ws)
     assert (Ws.cpu() == 255).tolist() == [[[True, False, False], [False, True, False]]]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, E4M3])
+def test_loads_that_differ(dtype):
+    """One expert with nearly all rows, in several passes and workgroups, beside experts with a row or none."""
+    g = torch.Generator().manual_seed(8)
+    T, k, E, K, N = 150, 2, 40, 288, 70
+    Wq, Ws = weights(g, E, N, K)
+    idx = torch.full((T, k), 7, dtype=torch.int32)
+    idx[:, 1] = torch.arange(T) % 5 + 20
+    idx[3, 0], idx[140, 1] = -1, 39
+    x = torch.randn((T, K), generator=g).to(DT[dtype]).to(DEV)
+    xs = torch.rand((T, 1), generator=g).to(DEV) if dtype == E4M3 else None
+    y = torch.empty((T, k, N), device=DEV)
+    B.moe_w4_product(B.make_w4_config(T, k, E, K, N, dtype, F32), x, xs, idx.to(DEV), None, Wq, Ws, y, None)
+    X, W = x.cpu().float().double() * (xs.cpu().double() if xs is not None else 1.0), unpack(Wq, Ws)
+    for t in range(T):
+        for j in range(k):
+            e = int(idx[t, j])
+            want = W[e] @ X[t] if e >= 0 else torch.zeros(N, dtype=torch.float64)
+            size = W[e].abs() @ X[t].abs() if e >= 0 else torch.zeros(N, dtype=torch.float64)
+            assert ((y[t, j].cpu().double() - want).abs() <= (K / 16 + 129) * 2.0 ** -24 * size).all(), (t, j)
