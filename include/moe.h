@@ -142,7 +142,8 @@ moe_status moe_route(const moe_config* cfg, const void* x, const void* Wg, const
 
 /* Capacity-bounded slot assignment for all n partitions.  Inside a partition,
  * positions are granted choice-major (all first choices in token order, then
- * second choices, ...); an assignment whose position reaches C_p is dropped.
+ * second choices, ...); an assignment whose position reaches C_p is dropped.  An entry of topk_idx outside
+ * 0..E-1 is no choice (moe_router_fwd leaves -1 where no expert is left): its slot is -1 and it takes no position.
  *   slot [T,k] int32 out: partition-local row e*C_p + pos, or -1 if dropped;
  *   counts [n,E] int32 out: kept rows per expert;
  *   slot_w [n*R_p] float out, may be NULL: combine weight of the assignment that

@@ -27,6 +27,9 @@ __device__ __forceinline__ unsigned long long same_expert(int e, int bits) {
     return m;
 }
 
+// An entry outside 0..E-1 is no choice (the router writes -1 where no expert is left): it takes no position.
+__device__ __forceinline__ int a_choice(int e, int E) { return (unsigned)e < (unsigned)E ? e : -1; }
+
 // hist[((p*k + j)*nb + b)*E + e] = number of tokens of block b (partition p) whose
 // j-th choice is expert e
 __global__ __launch_bounds__(SLOT_BLOCK) void slot_hist_kernel(
@@ -37,8 +40,8 @@ __global__ __launch_bounds__(SLOT_BLOCK) void slot_hist_kernel(
     __syncthreads();
     const int tl = b * SLOT_BLOCK + threadIdx.x;
     if (tl < Tp) {
-        int e = topk_idx[(size_t)(p * Tp + tl) * k + j];
-        atomicAdd(&h[e], 1);             // integer counts: order does not matter
+        const int e = a_choice(topk_idx[(size_t)(p * Tp + tl) * k + j], E);
+        if (e >= 0) atomicAdd(&h[e], 1);             // integer counts: order does not matter
     }
     __syncthreads();
     if (threadIdx.x < E) hist[((size_t)(p * k + j) * nb + b) * E + threadIdx.x] = h[threadIdx.x];
@@ -59,9 +62,10 @@ __global__ __launch_bounds__(SLOT_BLOCK) void slot_assign_kernel(
     const int b = blockIdx.x, j = blockIdx.y, p = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     const int tl = b * SLOT_BLOCK + tid;
-    const bool valid = tl < Tp;
+    const bool inside = tl < Tp;
     const int t = p * Tp + tl;
-    const int my_e = valid ? topk_idx[(size_t)t * k + j] : -1;
+    const int my_e = inside ? a_choice(topk_idx[(size_t)t * k + j], E) : -1;
+    const bool valid = my_e >= 0;
     const unsigned long long below = (1ull << lane) - 1ull;
     wcount[wid][lane] = 0;
     if (tid < 64) { before[tid] = 0; total[tid] = 0; }
@@ -71,14 +75,14 @@ __global__ __launch_bounds__(SLOT_BLOCK) void slot_assign_kernel(
         const int n = Tp * k;
         int q[COUNT_PASSES];                     // all on their way before the first is counted
 #pragma unroll
-        for (int r = 0; r < COUNT_PASSES; ++r) q[r] = r * SLOT_BLOCK + tid < n ? idx[r * SLOT_BLOCK + tid] : -1;
+        for (int r = 0; r < COUNT_PASSES; ++r) q[r] = r * SLOT_BLOCK + tid < n ? a_choice(idx[r * SLOT_BLOCK + tid], E) : -1;
 #pragma unroll
         for (int r = 0; r < COUNT_PASSES; ++r) {
             if (r * SLOT_BLOCK >= n) break;
             const int i = r * SLOT_BLOCK + tid, ti = i / k, ji = i - ti * k;
             const unsigned long long ahead = __ballot(ji < j || (ji == j && ti < b * SLOT_BLOCK));
-            const unsigned long long peers = same_expert(q[r], bits) & __ballot(i < n);
-            if (i < n && (peers & below) == 0) {          // the first of an expert's lanes speaks for all of them
+            const unsigned long long peers = same_expert(q[r], bits) & __ballot(q[r] >= 0);
+            if (q[r] >= 0 && (peers & below) == 0) {          // the first of an expert's lanes speaks for all of them
                 atomicAdd(&total[q[r]], __popcll(peers));
                 atomicAdd(&before[q[r]], __popcll(peers & ahead));
             }
@@ -107,12 +111,12 @@ __global__ __launch_bounds__(SLOT_BLOCK) void slot_assign_kernel(
         int pos = before[my_e] + __popcll(peers & below);
         for (int w = 0; w < wid; ++w) pos += wcount[w][my_e];
         s = pos < Cp ? my_e * Cp + pos : -1;
-        slot[(size_t)t * k + j] = s;
         if (s >= 0 && x.slot_w) x.slot_w[(size_t)p * E * Cp + s] = x.topk_w[(size_t)t * k + j];
         if (s >= 0 && x.rows) x.rows[(size_t)p * E * Cp + s] = t;
     }
+    if (inside) slot[(size_t)t * k + j] = s;
     if (x.y) {
-        unsigned long long dropped = __ballot(valid && s < 0);
+        unsigned long long dropped = __ballot(inside && s < 0);
         while (dropped) {
             const int l = __builtin_ctzll(dropped);
             dropped &= dropped - 1;
