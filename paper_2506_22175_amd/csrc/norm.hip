@@ -5,8 +5,8 @@
 //
 // Both move each row once and are bound by memory: a row stays in the registers of the threads that loaded it, from the
 // loads through the row's sum to the stores, so nothing is read twice.  A row is dealt out in units of eight columns (16
-// bytes of bfloat16), one or several to a thread; a wavefront has a row to itself as long as that is enough threads, which
-// leaves no barrier in the row's sum.  Rows need the alignment of their elements only: the hardware does wide accesses
+// bytes of bfloat16), to a thread one (forward) or a few; a wavefront has a row of up to 512 columns to itself, a workgroup a
+// longer one.  Rows need the alignment of their elements only: the hardware does wide accesses
 // at any address, and a row's last unit, if it is not full, goes element by element.
 #include "common.h"
 #include "lanes.h"
@@ -407,23 +407,24 @@ moe_status norm_dims(const moe_norm_config* c, NormDims* d) {
     return MOE_OK;
 }
 
-// How a row is dealt out: wavefronts per row and units per thread.
+// How a row is dealt out: wavefronts per row and units per thread.  One unit to a thread as far as that goes, which leaves the
+// most requests under way: two or four units to a thread and fewer wavefronts without a barrier take longer for few rows (64
+// of 2048, bfloat16: 4.5 us, so 2.9) and for float ones (8192 of 1024: 39 us, so 33; of 4096: 134 and 110), and as long for many
+// of bfloat16 (32768 of 2048: 95 and 95 us; of 600, where the second wavefront has little to do: 32 and 34).
 struct RowPlan { int waves, units; };
-RowPlan norm_plan(int T, int M) {
+RowPlan norm_plan(int M) {
     const int units = (M + 7) / 8;
-    const bool alone = T < 64;
     if (units <= 64) return {1, 1};
-    if (alone && units <= 256) return {4, 1};
-    if (units <= 128) return {1, 2};
-    if (units <= 256) return {1, 4};
-    if (units <= 512) return {4, 2};
-    if (alone && units <= 1024) return {16, 1};
-    if (units <= 1024) return {4, 4};
+    if (units <= 128) return {2, 1};
+    if (units <= 256) return {4, 1};
+    if (units <= 512) return {8, 1};
+    if (units <= 1024) return {16, 1};
     if (units <= 2048) return {16, 2};
     return {16, 4};
 }
 
-// Backward keeps more to a column: few units to a thread, so that the next row can be on its way.
+// Backward has several rows after one another: few units to a thread, so that the next row can be on its way.  Two and four
+// units to the threads of one wavefront instead of a workgroup's: 4096 rows of 2048 25 us, so 20; 512 of 1024 6.9 and 7.5.
 RowPlan norm_bwd_plan(int M) {
     const int units = (M + 7) / 8;
     if (units <= 64) return {1, 1};
@@ -437,7 +438,7 @@ RowPlan norm_bwd_plan(int M) {
 template <typename T, bool E4M3> void norm_launch(const NormArgs& a, RowPlan p, hipStream_t s) {
 #define NORM_CASE(W, U) if (p.waves == W && p.units == U) { \
         norm_kernel<T, E4M3, W, U><<<W == 1 ? (a.T + 3) / 4 : a.T, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
-    NORM_CASE(1, 1) NORM_CASE(1, 2) NORM_CASE(1, 4) NORM_CASE(4, 1) NORM_CASE(4, 2) NORM_CASE(4, 4) NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(16, 4)
+    NORM_CASE(1, 1) NORM_CASE(2, 1) NORM_CASE(4, 1) NORM_CASE(8, 1) NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(16, 4)
 #undef NORM_CASE
 }
 
@@ -448,10 +449,12 @@ template <typename T> void norm_bwd_launch(const NormBwdArgs& a, RowPlan p, int 
 #undef NORM_CASE
 }
 
-// Workgroups of the backward kernel.  Each leaves M floats of partial sums, so there are only as many as fill the chip.
-int norm_bwd_blocks(int T, RowPlan p) {
+// Workgroups of the backward kernel.  Each leaves M floats of partial sums, which the second launch reads, so there are only as many
+// as fill the chip, and half of that where wide rows are fewer (bfloat16, half / all: 1024 rows of 2048 10.4 / 12.7 us, of 8192
+// 20 / 26; 4096 of 8192 56 / 61; 32768 of 2048 108 / 104; 4096 of 768, three quarters of the threads: 13.7 / 12.7).
+int norm_bwd_blocks(int T, int M, RowPlan p) {
     const int rows = p.waves == 1 ? 4 : 1;
-    const int want = (T + rows - 1) / rows, most = p.waves == 16 ? 512 : 1024;
+    const int want = (T + rows - 1) / rows, fill = p.waves == 16 ? 512 : 1024, most = M > 1024 && T < 8192 ? fill / 2 : fill;
     return want < most ? want : most;
 }
 
@@ -466,7 +469,7 @@ extern "C" moe_status moe_norm_fwd(const moe_norm_config* cfg, const void* x, co
     if (d.T == 0) return MOE_OK;
     if (!x || !y || (cfg->out == MOE_E4M3 && !scales)) return MOE_ERR_NULL;
     moe::NormArgs a = {x, residual, gain, h, y, scales, rstd, d.ldx, d.ldr, d.ldh, d.ldy, d.T, d.M, cfg->group, d.n_scales, cfg->eps};
-    const moe::RowPlan p = moe::norm_plan(d.T, d.M);
+    const moe::RowPlan p = moe::norm_plan(d.M);
     hipStream_t s = (hipStream_t)stream;
     {
         moe::ProfScope prof(moe::PK_NORM, s);
@@ -485,7 +488,7 @@ extern "C" moe_status moe_norm_scratch_bytes(const moe_norm_config* cfg, size_t*
     moe::NormDims d;
     MOE_TRY(moe::norm_dims(cfg, &d));
     if (!bytes) return MOE_ERR_NULL;
-    const int blocks = moe::norm_bwd_blocks(d.T, moe::norm_bwd_plan(d.M));
+    const int blocks = moe::norm_bwd_blocks(d.T, d.M, moe::norm_bwd_plan(d.M));
     *bytes = blocks > 1 ? (size_t)blocks * d.M * sizeof(float) : 0;
     return MOE_OK;
 }
@@ -496,7 +499,7 @@ extern "C" moe_status moe_norm_bwd(const moe_norm_config* cfg, const void* dy, c
     MOE_TRY(moe::norm_dims(cfg, &d));
     if (cfg->out == MOE_E4M3) return MOE_ERR_UNSUPPORTED;      // gradients of rounded rows are not defined here
     const moe::RowPlan p = moe::norm_bwd_plan(d.M);
-    const int blocks = moe::norm_bwd_blocks(d.T, p);
+    const int blocks = moe::norm_bwd_blocks(d.T, d.M, p);
     if (d.T > 0 && (!dy || !h || !rstd || !dx)) return MOE_ERR_NULL;
     if (dgain && blocks > 1 && !scratch) return MOE_ERR_NULL;
     hipStream_t s = (hipStream_t)stream;
