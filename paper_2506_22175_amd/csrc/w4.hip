@@ -588,7 +588,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void w4_few_kernel(W4Args a, int sha
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) acc[t][rt] = f32x4_hw{0, 0, 0, 0};
-        if (e >= 0 && n0 < a.N) few_stream<XT, RT>(a, f, s_list, here, s_own[wid], s_own[wid] + W_SLOTS, s_scales[wid], acc);
+        if (e >= 0 && n0 < a.N) {
+            if (RT > 1 && here <= 16) {                    // half of the rows' requests and products
+                f32x4_hw one[4][1];
+                few_stream<XT, 1>(a, f, s_list, here, s_own[wid], s_own[wid] + W_SLOTS, s_scales[wid], one);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t][0] = one[t][0];
+            } else {
+                few_stream<XT, RT>(a, f, s_list, here, s_own[wid], s_own[wid] + W_SLOTS, s_scales[wid], acc);
+            }
+        }
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -938,6 +947,7 @@ template <int XT, int RT> void w4_few_launch(const W4Args& a, double chosen, int
 }
 
 template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hipStream_t s) {
+    // one token by the kernel for several: 2 experts of 2048 x 8192 23 us, so 6.4; 8 of 1024 x 4096 11.3, so 7
     if (T == 1) {
         w4_token_launch<XT>(a, sum, s);
         return;
@@ -946,10 +956,14 @@ template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hi
     const int experts = !a.idx ? 1 : a.n_rows < a.E ? a.n_rows : a.E, slots = !a.idx ? 1 : join ? a.E : a.E + 1;
     const int rows = (a.n_rows + experts - 1) / experts;
     const double chosen = a.idx ? a.E * (1.0 - std::pow(1.0 - (double)a.k / a.E, (double)T)) : 1.0;
-    // (offsets in x are 32-bit in the kernel for few rows)
+    // Two tiles of rows at a time and a workgroup for each 32 are as fast as four and one matrix read for 64 at some 40 rows each
+    // (16 experts of 1024 x 4096: 16 rows 19 / 23 us, 32 rows 22 / 30, 40 rows 34 / 30).  Offsets in x are 32-bit in the kernel
+    // for few rows.
     const long long x_bytes = (a.per_choice ? (long long)a.n_rows : (long long)T) * a.ldx * row_bytes(XT, 1);
     if (rows <= 32 && x_bytes < (1ll << 32)) {
-        // 16 rows at a time, or 32 (of float rows 16: more would not fit into LDS)
+        // 16 rows at a time, or 32 (of float rows 16: more would not fit into LDS).  The mean says little of the experts that have
+        // most: 16 experts of 2048 x 8192 as a skewed gate loads them, mean 4: 16 rows 34 us, 32 rows 38; mean 5: 44, 37; mean 8:
+        // 45, 41; 8192 x 2048, 64 experts, mean 8: 194, 197.
         if constexpr (XT != MOE_F32) {
             if (rows > 4) {
                 w4_few_launch<XT, 2>(a, chosen, slots, rows, s);
