@@ -95,14 +95,23 @@ def _p(t) -> ctypes.c_void_p:
 
 
 def _s(stream) -> ctypes.c_void_p:
+    return ctypes.c_void_p(_h(stream))
+
+
+_now = None      # once torch uses the GPU: what gives the current stream's handle, and the current device
+
+
+def _h(stream):
+    """Handle of a stream, an int, or the current stream's."""
+    global _now
     if stream is None:
+        if _now is not None:                # the handle alone: a Stream object takes 2.8 us to make, more than many a kernel
+            return _now[0](_now[1]())
         import torch
-        if torch.cuda.is_initialized():     # the handle alone: a Stream object takes 2.8 us to make, more than many a kernel
-            return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
         stream = torch.cuda.current_stream()
-    if isinstance(stream, int):
-        return ctypes.c_void_p(stream)
-    return ctypes.c_void_p(stream.cuda_stream)
+        if torch.cuda.is_initialized():
+            _now = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _a(t):
@@ -431,12 +440,12 @@ def moe_norm_scratch_bytes(cfg: MoENormConfig) -> int:
 
 def moe_norm_fwd(cfg, x, residual, gain, h, y, scales=None, rstd=None, stream=None):
     _check(lib().moe_norm_fwd(_cfg(cfg), _a(x), _a(residual), _a(gain), _a(h), _a(y), _a(scales), _a(rstd),
-                              _s(stream)), "moe_norm_fwd")
+                              _h(stream)), "moe_norm_fwd")
 
 
 def moe_norm_bwd(cfg, dy, h, gain, rstd, dh, dx, dgain, scratch, stream=None):
     _check(lib().moe_norm_bwd(_cfg(cfg), _a(dy), _a(h), _a(gain), _a(rstd), _a(dh), _a(dx), _a(dgain), _a(scratch),
-                              _s(stream)), "moe_norm_bwd")
+                              _h(stream)), "moe_norm_bwd")
 
 
 class MoERouterConfig(ctypes.Structure):
@@ -453,12 +462,12 @@ def make_router_config(T, E, k, scores=MOE_SOFTMAX, groups=1, group_k=1, group_t
 
 
 def moe_router_fwd(cfg, logits, bias, topk_idx, topk_w, load=None, stream=None):
-    _check(lib().moe_router_fwd(_cfg(cfg), _a(logits), _a(bias), _a(topk_idx), _a(topk_w), _a(load), _s(stream)),
+    _check(lib().moe_router_fwd(_cfg(cfg), _a(logits), _a(bias), _a(topk_idx), _a(topk_w), _a(load), _h(stream)),
            "moe_router_fwd")
 
 
 def moe_router_bwd(cfg, logits, topk_idx, dw, dlogits, stream=None):
-    _check(lib().moe_router_bwd(_cfg(cfg), _a(logits), _a(topk_idx), _a(dw), _a(dlogits), _s(stream)), "moe_router_bwd")
+    _check(lib().moe_router_bwd(_cfg(cfg), _a(logits), _a(topk_idx), _a(dw), _a(dlogits), _h(stream)), "moe_router_bwd")
 
 
 class MoEW4Config(ctypes.Structure):
@@ -482,7 +491,7 @@ def moe_w4_scratch_bytes(cfg: MoEW4Config) -> int:
 
 def moe_w4_product(cfg, x, x_scales, topk_idx, topk_w, Wq, Ws, y, scratch=None, stream=None):
     _check(lib().moe_w4_product(_cfg(cfg), _a(x), _a(x_scales), _a(topk_idx), _a(topk_w), _a(Wq), _a(Ws), _a(y),
-                                _a(scratch), _s(stream)), "moe_w4_product")
+                                _a(scratch), _h(stream)), "moe_w4_product")
 
 
 def moe_w4_quantize(E, K, N, dtype, W, Wq, Ws, stream=None):
