@@ -226,8 +226,8 @@ __device__ __forceinline__ void w4_store(const W4Args& a, long long row, int n, 
     else store_columns(reinterpret_cast<bf16_t*>(a.y) + row * a.ldy + n, v, a.N - n);
 }
 
-// ---- one token ---------------------------------------------------------------------------------
-// A workgroup has 16 weight rows of one choice's expert (SUM: of all choices' experts, and adds them up), its wavefronts share out
+// ---- tokens by themselves ---------------------------------------------------------------------------------
+// A workgroup has 16 weight rows of one choice of a token (SUM: of all its choices, and adds them up), its wavefronts share out
 // the choices and K in pieces of 512 columns.  A piece of the routed row is one request of the wavefront and goes through LDS
 // that no other wavefront uses, from where all 16 columns of the right operand get the same.
 constexpr int TOKEN_TILES = 4;       // of a piece
@@ -261,6 +261,9 @@ __global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slic
     __shared__ float4 s_sum[WAVES][4];
     const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63, r = lane & 15, q = lane >> 4;
     const int n0 = blockIdx.x * 16;
+    const long long token = blockIdx.z;
+    const int* idx = a.idx ? a.idx + token * a.k : nullptr;
+    const float* weights = a.w ? a.w + token * a.k : nullptr;
     unsigned offset[TOKEN_TILES];
     Block16<TOKEN_TILES>::offsets(n0, a.N, a.K, lane, offset);
     const int scale_row = n0 + lane / 4 < a.N ? n0 + lane / 4 : a.N - 1;
@@ -269,10 +272,10 @@ __global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slic
     const int first = SUM ? wid / slices : (int)blockIdx.y, slice = SUM ? wid % slices : wid, step = waves / slices;
     float4 sum = make_float4(0, 0, 0, 0);                 // SUM and slices = 1: of the wavefront's choices, weighted
     for (int j = first; j < a.k; j += step) {
-        const int e = a.idx ? a.idx[j] : 0;
+        const int e = idx ? idx[j] : 0;
         f32x4_hw acc = {0, 0, 0, 0};
         if ((unsigned)e < (unsigned)a.E) {
-            const long long xr = a.per_choice ? j : 0;
+            const long long xr = a.per_choice ? token * a.k + j : token;
             const uint8_t* Wq = a.Wq + (long long)e * a.N * (a.K / 2);
             const uint8_t* Ws = a.Ws + ((long long)e * a.N + scale_row) * (a.K / 32);
             const char* row = reinterpret_cast<const char*>(a.x) + xr * row_bytes(XT, 1) * a.ldx;
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slic
             }
         }
         if (SUM && slices == 1) {
-            const float weight = a.w ? a.w[j] : 1.0f;
+            const float weight = weights ? weights[j] : 1.0f;
             if ((unsigned)e < (unsigned)a.E) {
                 sum.x += w4_finish(acc[0], a.gelu, weight); sum.y += w4_finish(acc[1], a.gelu, weight);
                 sum.z += w4_finish(acc[2], a.gelu, weight); sum.w += w4_finish(acc[3], a.gelu, weight);
@@ -326,7 +329,7 @@ __global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slic
     // every column has the row's sums
     if (r == 0) s_sum[wid][q] = sum;
     const int tq = tid & 3;                                // thread q < 4 will have columns n0 + 4 q .. + 3
-    const float weight = !SUM && a.w ? a.w[first] : 1.0f;
+    const float weight = !SUM && weights ? weights[first] : 1.0f;
     __syncthreads();
     if (tid >= 4) return;
     float v[4] = {0, 0, 0, 0};
@@ -339,14 +342,14 @@ __global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slic
             // (an expert out of range has sums of zero, and GeLU keeps them)
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = w4_finish(v[i], a.gelu, weight);
-            const int e = a.idx ? a.idx[first] : 0;
+            const int e = idx ? idx[first] : 0;
             if ((unsigned)e >= (unsigned)a.E) v[0] = v[1] = v[2] = v[3] = 0.0f;      // whatever its weight
         }
     } else {
         for (int j = 0; j < a.k; ++j) {
-            const int e = a.idx ? a.idx[j] : 0;
+            const int e = idx ? idx[j] : 0;
             if ((unsigned)e >= (unsigned)a.E) continue;
-            const float wj = a.w ? a.w[j] : 1.0f;
+            const float wj = weights ? weights[j] : 1.0f;
             float c[4] = {0, 0, 0, 0};
             for (int w = 0; w < slices; ++w) {
                 const float4 p = s_sum[j * slices + w][tq];
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(WAVES * 64) void w4_token_kernel(W4Args a, int slic
             for (int i = 0; i < 4; ++i) v[i] += w4_finish(c[i], a.gelu, wj);
         }
     }
-    if (n0 + 4 * tq < a.N) w4_store(a, SUM ? 0 : first, n0 + 4 * tq, v);
+    if (n0 + 4 * tq < a.N) w4_store(a, SUM ? token : token * a.k + first, n0 + 4 * tq, v);
 }
 
 // ---- several tokens ----------------------------------------------------------------------------
@@ -878,7 +881,17 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
     Ws[(e * N + n) * (K / 32) + b] = (uint8_t)scale;
 }
 
-struct W4Plan { long long ldx, ldy; int n_scales; size_t scratch; };
+// by_token: each token by itself (w4_token_kernel).  chosen: experts that may be expected to be chosen by T tokens.
+struct W4Plan { long long ldx, ldy; int n_scales; size_t scratch; bool by_token; double chosen; };
+
+// Tokens by themselves read an expert's weights once for each of its rows, but have neither rows to collect nor shares of K to
+// add up between launches.  That is worth 20 MB of weights more than are chosen, whatever the sizes (by tokens / by experts: 2 tokens, 2
+// of 16 experts of 2048 x 8192 10 / 16 us, 4 tokens 14 / 21, 8 tokens 23.5 / 24, 12 tokens 33 / 26; 4096 x 1024, joined, 2 of 8
+// experts, 4 tokens 6.1 / 11.7, 8 tokens 11.2 / 12.2, 12 tokens 15.2 / 12.5; 1024 x 4096, 8 of 64, 4 tokens 17 / 22, 6 tokens 23.5
+// / 22.6; one token, 2 of 16 experts of 2048 x 8192 6.4 / 23).  Beyond 16 tokens, small matrices: 512 x 2048, 2 of 8 experts, 12
+// tokens 6.2 / 6.4, 24 tokens 9.6 / 7.3.
+constexpr double TOKEN_MORE = 20e6;
+constexpr int TOKENS_MOST = 16;
 
 moe_status w4_plan(const moe_w4_config* c, W4Plan* p) {
     if (!c) return MOE_ERR_NULL;
@@ -895,24 +908,27 @@ moe_status w4_plan(const moe_w4_config* c, W4Plan* p) {
     if ((long long)c->N * c->K > INT_MAX) return MOE_ERR_UNSUPPORTED;          // offsets within an expert are 32-bit
     if ((long long)c->T * c->k > (1 << 24) || (c->combine && c->T > 65535)) return MOE_ERR_UNSUPPORTED;
     p->n_scales = c->group ? (c->K + 127) / 128 : 1;
-    // rows of several tokens' choices that are still to be added up; a single token's workgroups do that themselves
+    p->chosen = c->E * (1.0 - std::pow(1.0 - (double)c->k / c->E, (double)c->T));
+    p->by_token = c->T == 1 || (c->T <= TOKENS_MOST && ((double)c->T * c->k - p->chosen) * c->K * c->N * (17.0 / 32.0) <= TOKEN_MORE);
+    // Rows of several tokens' choices that are still to be added up.  Workgroups that have a token to themselves do that and need
+    // none, but the size is to grow with T alone: a scratch for many tokens does for fewer.
     p->scratch = c->combine && c->k > 1 && c->T > 1 ? (size_t)c->T * c->k * c->N * sizeof(float) : 0;
     return MOE_OK;
 }
 
-template <int XT> void w4_token_launch(const W4Args& a, bool sum, hipStream_t s) {
+template <int XT> void w4_token_launch(const W4Args& a, int T, bool sum, hipStream_t s) {
     const int blocks = (a.N + 15) / 16, want = (a.K + 128 * TOKEN_TILES - 1) / (128 * TOKEN_TILES);
     if (sum && a.k > 1) {
         // the choices first, then K, among sixteen wavefronts; beyond sixteen choices a wavefront has several
         int slices = a.k <= TOKEN_WAVES ? TOKEN_WAVES / a.k : 1;
         slices = slices < want ? slices : want;
         const int waves = a.k <= TOKEN_WAVES ? slices * a.k : TOKEN_WAVES;
-        if (waves <= 4) w4_token_kernel<XT, true, 4><<<blocks, waves * 64, 0, s>>>(a, slices);
-        else w4_token_kernel<XT, true, TOKEN_WAVES><<<blocks, waves * 64, 0, s>>>(a, slices);
+        if (waves <= 4) w4_token_kernel<XT, true, 4><<<dim3(blocks, 1, T), waves * 64, 0, s>>>(a, slices);
+        else w4_token_kernel<XT, true, TOKEN_WAVES><<<dim3(blocks, 1, T), waves * 64, 0, s>>>(a, slices);
     } else {
         const int waves = want < TOKEN_WAVES ? want : TOKEN_WAVES;
-        if (waves <= 4) w4_token_kernel<XT, false, 4><<<dim3(blocks, a.k), waves * 64, 0, s>>>(a, waves);
-        else w4_token_kernel<XT, false, TOKEN_WAVES><<<dim3(blocks, a.k), waves * 64, 0, s>>>(a, waves);
+        if (waves <= 4) w4_token_kernel<XT, false, 4><<<dim3(blocks, a.k, T), waves * 64, 0, s>>>(a, waves);
+        else w4_token_kernel<XT, false, TOKEN_WAVES><<<dim3(blocks, a.k, T), waves * 64, 0, s>>>(a, waves);
     }
 }
 
@@ -946,16 +962,15 @@ template <int XT, int RT> void w4_few_launch(const W4Args& a, double chosen, int
     else w4_few_kernel<XT, RT, FEW_MORE><<<grid, FEW_MORE * 64, 0, s>>>(a, shares);
 }
 
-template <int XT> void w4_launch(const W4Args& a, int T, bool join, bool sum, hipStream_t s) {
-    // one token by the kernel for several: 2 experts of 2048 x 8192 23 us, so 6.4; 8 of 1024 x 4096 11.3, so 7
-    if (T == 1) {
-        w4_token_launch<XT>(a, sum, s);
+template <int XT> void w4_launch(const W4Args& a, const W4Plan& p, int T, bool join, bool sum, hipStream_t s) {
+    if (p.by_token) {
+        w4_token_launch<XT>(a, T, sum, s);
         return;
     }
-    // experts that may be expected to be chosen, and the rows of each; and one more slot for rows of no expert
+    // experts that may have rows, and how many each; and one more slot for rows of no expert
     const int experts = !a.idx ? 1 : a.n_rows < a.E ? a.n_rows : a.E, slots = !a.idx ? 1 : join ? a.E : a.E + 1;
     const int rows = (a.n_rows + experts - 1) / experts;
-    const double chosen = a.idx ? a.E * (1.0 - std::pow(1.0 - (double)a.k / a.E, (double)T)) : 1.0;
+    const double chosen = a.idx ? p.chosen : 1.0;
     // Two tiles of rows at a time and a workgroup for each 32 are as fast as four and one matrix read for 64 at some 40 rows each
     // (16 experts of 1024 x 4096: 16 rows 19 / 23 us, 32 rows 22 / 30, 40 rows 34 / 30).  Offsets in x are 32-bit in the kernel
     // for few rows.
@@ -997,14 +1012,14 @@ extern "C" moe_status moe_w4_product(const moe_w4_config* cfg, const void* x, co
     if (((uintptr_t)x | (uintptr_t)Wq | (uintptr_t)scratch) & 15) return MOE_ERR_UNSUPPORTED;
     hipStream_t s = (hipStream_t)stream;
     const int rows = cfg->T * cfg->k;
-    const bool join = p.scratch != 0;
+    const bool join = p.scratch != 0 && !p.by_token;
     moe::W4Args a = {x, x_scales, topk_idx, topk_w, Wq, Ws, join ? scratch : y, p.ldx, join ? cfg->N : p.ldy, rows,
                      cfg->k, cfg->E, cfg->K, cfg->N, p.n_scales, cfg->per_choice, cfg->gelu, join || cfg->out == MOE_F32};
     {
         moe::ProfScope prof(moe::PK_W4, s);
-        if (cfg->dtype == MOE_F32) moe::w4_launch<MOE_F32>(a, cfg->T, join, cfg->combine, s);
-        else if (cfg->dtype == MOE_BF16) moe::w4_launch<MOE_BF16>(a, cfg->T, join, cfg->combine, s);
-        else moe::w4_launch<MOE_E4M3>(a, cfg->T, join, cfg->combine, s);
+        if (cfg->dtype == MOE_F32) moe::w4_launch<MOE_F32>(a, p, cfg->T, join, cfg->combine, s);
+        else if (cfg->dtype == MOE_BF16) moe::w4_launch<MOE_BF16>(a, p, cfg->T, join, cfg->combine, s);
+        else moe::w4_launch<MOE_E4M3>(a, p, cfg->T, join, cfg->combine, s);
         MOE_CHECK_LAUNCH();
         if (join) {
             const dim3 jgrid((cfg->N + 4 * moe::JOIN_THREADS - 1) / (4 * moe::JOIN_THREADS), cfg->T);

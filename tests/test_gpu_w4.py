@@ -265,3 +265,18 @@ def test_loads_that_differ(dtype):
             want = W[e] @ X[t] if e >= 0 else torch.zeros(N, dtype=torch.float64)
             size = W[e].abs() @ X[t].abs() if e >= 0 else torch.zeros(N, dtype=torch.float64)
             assert ((y[t, j].cpu().double() - want).abs() <= (K / 16 + 129) * 2.0 ** -24 * size).all(), (t, j)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, E4M3])
+@pytest.mark.parametrize("T,k,E,K,N", [(17, 2, 16, 160, 65), (24, 4, 64, 1056, 70), (20, 1, 8, 512, 33), (18, 2, 64, 96, 24), (40, 2, 64, 2080, 40),
+                                       (100, 8, 64, 544, 48), (16, 16, 16, 32, 7)])
+def test_few_rows_to_an_expert(T, k, E, K, N, dtype):
+    check(T, k, E, K, N, dtype, F32, group=128 if dtype == E4M3 else 0, drop=0.2)
+    check(T, k, E, K, N, dtype, BF16, per_choice=1, combine=1)
+    check(T, k, E, K, N, dtype, BF16, gelu=1, weighted=False)
+
+
+def test_a_batch_that_reads_its_experts_weights_once():
+    """Ten tokens whose choices share experts of a size where that counts."""
+    check(10, 2, 4, 4096, 2048, BF16, F32, drop=0.2)
+    check(10, 2, 4, 4096, 2048, BF16, BF16, per_choice=1, combine=1)
