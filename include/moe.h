@@ -408,9 +408,10 @@ typedef struct {
 
 /* topk_idx[t] = the k experts with the largest s + bias (no bias: the largest logits) among the groups that stay,
  * largest first, equal ones and equal groups by the lower index;  topk_w = scale * s of the chosen, without the bias.
- * Which comes first is decided as by 64-bit scores (closer than those can tell apart: either).  An expert whose logit is NaN or -inf, or whose bias makes its sum -inf
- * or NaN, is never chosen and has no share of a softmax if its logit is the reason; where fewer than k are left the
- * remaining choices are -1 with weight 0.  Infinite logits share a softmax evenly.
+ * Which comes first is decided as by 64-bit scores (closer than those can tell apart: either).  An expert whose logit
+ * is NaN or -inf, or whose bias makes its sum -inf or NaN, is never chosen and has no share of a softmax if its logit is
+ * the reason; where fewer than k are left the remaining choices are -1 with weight 0.  Infinite logits share a softmax
+ * evenly.
  *   logits [T,E]; bias [E] float, may be NULL; topk_idx [T,k] int32, topk_w [T,k] float out;
  *   load [E] int32, may be NULL: the number of tokens that chose each expert is ADDED to it. */
 moe_status moe_router_fwd(const moe_router_config* cfg, const void* logits, const float* bias,
