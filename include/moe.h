@@ -384,7 +384,7 @@ moe_status moe_norm_fwd(const moe_norm_config* cfg, const void* x, const void* r
 
 /* Its gradients, from the stored h and rstd of forward.  With n = h * rstd:
  *   dx = dh + rstd * (dy * gain - n * mean(dy * gain * n));  dgain (+)= sum over tokens of dy * n,
- * in an order that depends on the sizes alone.  dx is the gradient of x and of residual alike.
+ * in an order that depends on the sizes and on whether dx is dy.  dx is the gradient of x and of residual alike.
  *   dy [T,M]; h [T,M]; gain as in forward; rstd [T]; dh [T,M]: what reaches h past the norm, may be NULL;
  *   dx [T,M] out, may be dy or dh themselves (with their stride); dgain [M] float, may be NULL;
  *   scratch: moe_norm_scratch_bytes(cfg) bytes, 4-byte aligned (needed with dgain only). */

@@ -255,15 +255,58 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(Nor
 
 struct NormBwdArgs {
     const void* dy; const void* h; const float* gain; const float* rstd; const void* dh; void* dx;
-    float* part;          // [gridDim.x, M] sums of the gain's gradient; one workgroup: the gradient itself
+    float* part;          // [row workgroups, M] sums of the gain's gradient; one workgroup: the gradient itself
+    float* dgain;         // of the column workgroups
     long long ldx, ldh, ldy;
-    int T, M, add;        // add: part is added to (one workgroup)
+    int T, M, add;        // add: what is there is added to (one workgroup, or column workgroups)
+    int col_blocks;       // the first workgroups have columns of the gain's gradient, the others rows
 };
+
+// The gain's gradient of 32 columns: four threads a row, eight columns each, the others every THREADS / 4-th row.
+constexpr int GAIN_UNITS = 4;
+template <typename T, int THREADS> __device__ __forceinline__ void gain_columns(const NormBwdArgs& a) {
+    __shared__ float s[THREADS / 64][GAIN_UNITS * 8];
+    const int unit = threadIdx.x % GAIN_UNITS, col = (blockIdx.x * GAIN_UNITS + unit) * 8, left = a.M - col;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (left > 0) {
+        const T* dy = reinterpret_cast<const T*>(a.dy) + col;
+        const T* h = reinterpret_cast<const T*>(a.h) + col;
+#pragma unroll 4
+        for (int row = threadIdx.x / GAIN_UNITS; row < a.T; row += THREADS / GAIN_UNITS) {
+            Unit8<T> ud, uh;
+            ud.load(dy + row * a.ldy, left);
+            uh.load(h + row * a.ldh, left);
+            const float rstd = a.rstd[row];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = fmaf(ud.at(i), uh.at(i) * rstd, v[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int away = GAIN_UNITS; away < 64; away *= 2) v[i] += __shfl_xor(v[i], away, 64);
+    if ((threadIdx.x & 63) < GAIN_UNITS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[threadIdx.x >> 6][unit * 8 + i] = v[i];
+    }
+    __syncthreads();
+    const int c = blockIdx.x * GAIN_UNITS * 8 + threadIdx.x;
+    if (threadIdx.x >= GAIN_UNITS * 8 || c >= a.M) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) sum += s[w][threadIdx.x];
+    a.dgain[c] = a.add ? a.dgain[c] + sum : sum;
+}
 
 // Each wavefront (WAVES = 1) or workgroup takes every gridDim-th row and keeps its sums of the gain's gradient in registers.
 template <typename T, int WAVES, int UNITS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_bwd_kernel(NormBwdArgs a) {
     constexpr int ROWS = WAVES == 1 ? 4 : 1, THREADS = WAVES * 64;
+    if ((int)blockIdx.x < a.col_blocks) {
+        gain_columns<T, WAVES == 1 ? 256 : THREADS>(a);
+        return;
+    }
+    const int block = blockIdx.x - a.col_blocks, blocks = gridDim.x - a.col_blocks;
     __shared__ float s_part[WAVES > 1 ? WAVES : 1];
     __shared__ float s_dg[WAVES == 1 ? 3 * UNITS * THREADS * 8 : 1];
     const int tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
@@ -273,7 +316,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_bwd_kernel
     for (int u = 0; u < UNITS; ++u)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dg[u][i] = 0.0f;
-    const long long step = (long long)gridDim.x * ROWS;
+    const long long step = (long long)blocks * ROWS;
     Unit8<T> ud[UNITS], uh[UNITS], ub[UNITS];
     float rstd = 0.0f;
     auto request = [&](long long row) {
@@ -292,7 +335,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_bwd_kernel
     };
     // Where the registers allow it the next row is on its way while one is summed up and stored.
     constexpr bool AHEAD = UNITS <= 2;
-    long long row = (long long)blockIdx.x * ROWS + sub;
+    long long row = (long long)block * ROWS + sub;
     if (AHEAD && row < a.T) request(row);
     for (; row < a.T; row += step) {
         if (!AHEAD) request(row);
@@ -350,7 +393,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_bwd_kernel
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dg[u][i] += s_dg[q * UNITS * THREADS * 8 + (u * 8 + i) * THREADS + tid];
     }
-    float* part = a.part + (long long)blockIdx.x * a.M;
+    float* part = a.part + (long long)block * a.M;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         const int col = (u * THREADS + tid) * 8, left = a.M - col;
@@ -445,7 +488,7 @@ template <typename T, bool E4M3> void norm_launch(const NormArgs& a, RowPlan p, 
 
 template <typename T> void norm_bwd_launch(const NormBwdArgs& a, RowPlan p, int blocks, hipStream_t s) {
 #define NORM_CASE(W, U) if (p.waves == W && p.units == U) { \
-        norm_bwd_kernel<T, W, U><<<blocks, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
+        norm_bwd_kernel<T, W, U><<<blocks + a.col_blocks, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
     NORM_CASE(1, 1) NORM_CASE(4, 1) NORM_CASE(4, 2) NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(16, 4)
 #undef NORM_CASE
 }
@@ -458,6 +501,11 @@ int norm_bwd_blocks(int T, int M, RowPlan p) {
     const int want = (T + rows - 1) / rows, fill = p.waves == 16 ? 512 : 1024, most = M > 1024 && T < 8192 ? fill / 2 : fill;
     return want < most ? want : most;
 }
+
+// Rows up to which the gain's gradient has workgroups of its own in the same launch, which read dy and h once more, from the caches
+// (so / with sums by the rows' workgroups and a second launch: 32 rows of 2048 in bfloat16 2.8 / 5.3 us, 256 3.1 / 7.7, 512 6.3 /
+// 8.9, 1024 10.0 / 10.3, 2048 17 / 13; float, 512 8.4 / 10, 1024 14.4 / 13.1).
+constexpr int GAIN_TOGETHER = 512;
 
 }  // namespace
 
@@ -505,17 +553,20 @@ extern "C" moe_status moe_norm_bwd(const moe_norm_config* cfg, const void* dy, c
     if (dgain && blocks > 1 && !scratch) return MOE_ERR_NULL;
     hipStream_t s = (hipStream_t)stream;
     const int add = !cfg->grad_overwrite;
+    // (rows that are overwritten are not there any more for other workgroups)
+    const bool together = dgain && blocks > 1 && d.T <= moe::GAIN_TOGETHER && dx != dy;
     if (d.T == 0 && (!dgain || add)) return MOE_OK;
     {
         moe::ProfScope prof(moe::PK_NORM_BWD, s);
         if (d.T > 0) {
             const bool direct = blocks == 1;
-            moe::NormBwdArgs a = {dy, h, gain, rstd, dh, dx, dgain ? (direct ? dgain : (float*)scratch) : nullptr, d.ldx, d.ldh, d.ldy,
-                                  d.T, d.M, direct && add};
+            moe::NormBwdArgs a = {dy, h, gain, rstd, dh, dx, dgain && !together ? (direct ? dgain : (float*)scratch) : nullptr, dgain,
+                                  d.ldx, d.ldh, d.ldy, d.T, d.M, (direct || together) && add,
+                                  together ? (d.M + 8 * moe::GAIN_UNITS - 1) / (8 * moe::GAIN_UNITS) : 0};
             if (cfg->dtype == MOE_F32) moe::norm_bwd_launch<float>(a, p, blocks, s); else moe::norm_bwd_launch<moe::bf16_t>(a, p, blocks, s);
             MOE_CHECK_LAUNCH();
         }
-        if (dgain && blocks != 1) {
+        if (dgain && blocks != 1 && !together) {
             moe::norm_dgain_kernel<<<(d.M + moe::DG_COLS - 1) / moe::DG_COLS, moe::DG_COLS * moe::DG_SPLIT, 0, s>>>(
                 (const float*)scratch, blocks, d.M, add, dgain);
             MOE_CHECK_LAUNCH();

@@ -262,3 +262,27 @@ def test_the_same_bits_every_time_on_another_stream_and_in_a_graph():
         both()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, first))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,M", [(2, 64), (5, 513), (40, 260), (512, 1031), (300, 2048), (37, 9000), (513, 88)])
+def test_backward_where_the_gradient_overwrites_dy(T, M, dtype):
+    """The gain's gradient is of dy as it was, whether dx is dy or not, stored and accumulated."""
+    g = torch.Generator().manual_seed(T + M)
+    h, dy = rows(g, T, M, dtype), rows(g, T, M, dtype)
+    gain = (1 + 0.3 * torch.randn(M, generator=g)).to(DEV)
+    rstd = (1.0 / torch.sqrt(h.double().square().mean(1) + 1e-6)).float()
+    n = h.double() * rstd.double()[:, None]
+    want, size = (dy.double() * n).sum(0), (dy.double() * n).abs().sum(0)
+    tol = (T / 64 + 100) * 2.0 ** -24
+    for overwrite in (1, 0):
+        cfg = B.make_norm_config(T, M, 1e-6, dtype, grad_overwrite=overwrite)
+        scratch = torch.empty(B.moe_norm_scratch_bytes(cfg) + 4, dtype=torch.uint8, device=DEV)
+        old = 0.0 if overwrite else 3.0
+        out, apart, same = torch.empty_like(h), torch.full((M,), 3.0, device=DEV), torch.full((M,), 3.0, device=DEV)
+        B.moe_norm_bwd(cfg, dy, h, gain, rstd, None, out, apart, scratch)
+        both = dy.clone()
+        B.moe_norm_bwd(cfg, both, h, gain, rstd, None, both, same, scratch)
+        assert torch.equal(both, out)
+        for got in (apart, same):
+            assert ((got.double() - old - want).abs() <= tol * (size + old)).all()
