@@ -5,8 +5,8 @@
 //
 // Few rows meet each expert's matrix, so what has to move is the matrix: K N (1/2 + 1/32) bytes for every expert that is
 // chosen, read once.  A wavefront multiplies 16 weight rows of 128 columns at a time: lane (r, q) holds 32 consecutive
-// columns of weight row r, which is one 16-byte load, one scale, and exactly what the matrix instructions take, so packed
-// weights go from memory into registers with no detour.  The weights are the left operand and the routed rows, padded to
+// columns of weight row r, 16 bytes and one scale, which is what the matrix instructions take (they get
+// there through LDS: Block16 says why).  The weights are the left operand and the routed rows, padded to
 // 16, the right one: an output's lanes then hold four neighbouring columns of one row.
 //   bfloat16 rows  the weights become bfloat16 (exact: the scale is a power of two) eight to an instruction of 16 x 16 x 32
 //   float rows     the same with each float cut into three bfloat16 parts, whose sum it is: every product is exact
