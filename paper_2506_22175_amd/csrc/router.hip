@@ -215,7 +215,9 @@ __device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, cons
     const int shift = (threadIdx.x & 63) & ~(LANES - 1);
     if (by_score) {
         // The lowest bits of a score give way to its place in the lane, so that the largest says by itself which it is and
-        // taking it out is one comparison; the error grows by as much.  k + 1 maxima: the last choice too is compared with the next.
+        // taking it out is one comparison.  k + 1 maxima: the last choice too is compared with the next, without the places:
+        // both scores are cut towards zero then, and what lies between them is off by less than one place's VALUES units (with
+        // the places in it, by twice as much).
         constexpr int PLACE = VALUES - 1;
         float before = NONE;
 #pragma unroll
@@ -225,9 +227,9 @@ __device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, cons
             float mine = rank[0];
 #pragma unroll
             for (int v = 1; v < VALUES; ++v) mine = larger(mine, rank[v]);
-            const float m = lanes_max(mine);
-            if (j > 0 && m > NONE) sure = sure && before - m > error + (0x1p-21f + 0x1p-23f * VALUES) * fabsf(before);
-            before = m;
+            const float m = lanes_max(mine), cut = __uint_as_float(__float_as_uint(m) & ~(unsigned)PLACE);
+            if (j > 0 && m > NONE) sure = sure && before - cut > error + (0x1p-21f + 0x1p-23f * VALUES) * fabsf(before);
+            before = cut;
             if (j == a.k) break;
             const unsigned owners = (unsigned)(__ballot(mine == m && m > NONE) >> shift) & 0xffffu;
             const int owner = __builtin_ctz(owners | 0x10000u);
