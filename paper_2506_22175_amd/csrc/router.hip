@@ -158,6 +158,7 @@ __device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, cons
     bool sure = true;
     if (a.groups > 1) {
         float mine = NONE;                            // this lane's group's score; the slow way: that of group number `lane`
+        float size = 0.0f;                            // the magnitudes of its two parts, which may nearly cancel
         if (a.group_lanes) {
             // a group is group_lanes (a power of two) whole lanes
             float first = NONE, second = NONE;
@@ -169,7 +170,9 @@ __device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, cons
             if (a.group_lanes > 1) join_two(first, second, from_lane<AWAY_1>(first), from_lane<AWAY_1>(second));
             if (a.group_lanes > 2) join_two(first, second, from_lane<AWAY_2>(first), from_lane<AWAY_2>(second));
             if (a.group_lanes > 4) join_two(first, second, from_lane<MIRROR_8>(first), from_lane<MIRROR_8>(second));
-            mine = a.group_top == 2 && second > NONE ? first + second : first;
+            const bool two = a.group_top == 2 && second > NONE;
+            mine = two ? first + second : first;
+            size = fabsf(first) + (two ? fabsf(second) : 0.0f);
         } else {
             for (int g = 0; g < a.groups; ++g) {
                 float first = NONE, second = NONE;
@@ -183,8 +186,11 @@ __device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, cons
                 join_two(first, second, from_lane<AWAY_2>(first), from_lane<AWAY_2>(second));
                 join_two(first, second, from_lane<MIRROR_8>(first), from_lane<MIRROR_8>(second));
                 join_two(first, second, from_lane<MIRROR_16>(first), from_lane<MIRROR_16>(second));
-                const float score = a.group_top == 2 && second > NONE ? first + second : first;
-                if (lane == g) mine = score;
+                const bool two = a.group_top == 2 && second > NONE;
+                if (lane == g) {
+                    mine = two ? first + second : first;
+                    size = fabsf(first) + (two ? fabsf(second) : 0.0f);
+                }
             }
         }
         // a group stays if fewer than group_k others are ahead of it; each lane meets all others by rotations
@@ -200,9 +206,11 @@ __device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, cons
         ROUTER_MEET(11); ROUTER_MEET(12); ROUTER_MEET(13); ROUTER_MEET(14); ROUTER_MEET(15);
 #undef ROUTER_MEET
         const bool in = ahead < a.group_k * lanes;
-        // the last that stays and the first that does not; their scores are sums of two
+        // The last that stays and the first that does not.  Their scores are sums of two, each part with the error of a score,
+        // rounded at its own size with its bias and once more with the other: four units of 2^-24 of the larger one's parts.
         const float last = -lanes_max(in && mine > NONE ? -mine : NONE), next = lanes_max(in ? NONE : mine);
-        sure = next == NONE || last - next > 2.0f * error + 0x1p-20f * fabsf(last);
+        const float parts = lanes_max(mine == (in ? last : next) ? size : 0.0f);
+        sure = next == NONE || last - next > 2.0f * error + 0x1p-21f * parts;
         const unsigned stays = (unsigned)(__ballot(in && group < a.groups) >> ((threadIdx.x & 63) & ~(LANES - 1))) & 0xffffu;
 #pragma unroll
         for (int v = 0; v < VALUES; ++v) {

@@ -57,3 +57,27 @@ def test_two_scores_around_a_multiple_of_a_lanes_values(E, values, base):
     assert clear.mean() > 0.9
     for k in (1, 2):
         assert np.array_equal(router(l, bias, k, scores=B.MOE_SIGMOID)[0][clear], want[clear, :k])
+
+
+@pytest.mark.parametrize("E,groups,size", [(16, 8, 1e4), (16, 8, 1e2), (64, 8, 1e4), (256, 8, 1e3), (512, 16, 1e4), (48, 16, 1e3), (33, 11, 1e4)])
+@pytest.mark.parametrize("sigmoid", [0, 1])
+def test_groups_whose_two_best_nearly_cancel(E, groups, size, sigmoid):
+    """Each group has one bias of + size and the others of - size: a group's score is some 1, and its parts are rounded as size."""
+    rng, T, per, stay = np.random.default_rng(E + groups), 20000, E // groups, 3
+    bias = np.full(E, -size, np.float32)
+    bias[np.arange(groups) * per + rng.integers(0, per, groups)] = size
+    l = (rng.standard_normal((T, E)) * 1.5).astype(np.float32)
+    v = scores(l, bias, sigmoid)
+    by_group = -np.sort(-v.reshape(T, groups, per), 2)[:, :, :2].sum(2)
+    kept, _ = first_k(by_group, groups)
+    ranked = np.take_along_axis(by_group, kept, 1)
+    # sums of the parts in 64 bits: good to 2^-52 of `size`
+    clear = ranked[:, stay - 1] - ranked[:, stay] > 2.0 ** -50 * size
+    inside = (np.arange(E)[None, :] // per == kept[:, :stay, None]).any(1)
+    # the one expert of each group with + size; the others are as far apart as rounding at `size` leaves them
+    want = np.where(inside & (bias > 0), v, NEG)
+    order, apart = first_k(want, stay)
+    clear &= apart
+    assert clear.mean() > 0.9
+    idx = router(l, bias, stay, scores=sigmoid, groups=groups, group_k=stay, group_top=2)[0]
+    assert np.array_equal(np.sort(idx[clear], 1), np.sort(order[clear], 1))
