@@ -101,18 +101,19 @@ template <typename F> struct Softmax { float m; F inv; };
 template <typename F> __device__ __forceinline__ F softmax_term(float l, float m) {
     return l == -__builtin_inff() ? F(0) : l == m ? F(1) : exp_of(F(l) - F(m));
 }
+template <typename F, int VALUES> __device__ __forceinline__ F in_pairs(const F* s) {
+    if constexpr (VALUES == 1) return s[0];
+    else return in_pairs<F, VALUES / 2>(s) + in_pairs<F, VALUES / 2>(s + VALUES / 2);
+}
+// A lane's terms are added in pairs: one after the other a largest term would swallow up to 31 small ones.
 template <typename F, int VALUES> __device__ __forceinline__ Softmax<F> softmax_of(const float* l, F* s) {
     float m = l[0];
 #pragma unroll
     for (int v = 1; v < VALUES; ++v) m = fmaxf(m, l[v]);
     m = lanes_max(m);
-    F sum = F(0);
 #pragma unroll
-    for (int v = 0; v < VALUES; ++v) {
-        s[v] = softmax_term<F>(l[v], m);
-        sum += s[v];
-    }
-    sum = lanes_sum(sum);
+    for (int v = 0; v < VALUES; ++v) s[v] = softmax_term<F>(l[v], m);
+    const F sum = lanes_sum(in_pairs<F, VALUES>(s));
     const F inv = sum > F(0) ? F(1) / sum : F(0);
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) s[v] *= inv;
@@ -133,9 +134,10 @@ __device__ __forceinline__ bool choose(const RouterArgs& a, const float* l, cons
     constexpr float NONE = -__builtin_inff();
     const int lane = threadIdx.x & (LANES - 1), e0 = lane * VALUES;
     const bool by_score = a.bias != nullptr, scored = by_score || a.groups > 1;
-    // How far apart two scores have to be.  A sigmoid is less than 2.5 units of 2^-24 off (the exponential's rounded argument,
-    // itself, the sum, the reciprocal), a softmax's part 11 of them times the largest part (its exponential, and the sum's
-    // error, which all parts share but the bias does not), the sum with the bias half a unit of its size.
+    // How far apart two scores have to be.  In units of 2^-24 a sigmoid is less than 3 off (the exponential's rounded argument,
+    // itself, the sum, the reciprocal), the sum with the bias one of its size.  A softmax's parts, in such units of the largest part:
+    // each its exponential's 3 and a product's 1; and what all share but the bias does not, the sum's error: 9 additions for 512
+    // experts, 11 of the terms' exponentials (the most that 511 terms of equal size can make), the reciprocal's 1.  29 for two.
     float rank[VALUES], error = 0x1p-21f;
     if (scored || !a.sigmoid) {                       // a softmax's parts are wanted for the weights in any case
         if (a.sigmoid) {

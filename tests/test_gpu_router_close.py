@@ -81,3 +81,34 @@ def test_groups_whose_two_best_nearly_cancel(E, groups, size, sigmoid):
     assert clear.mean() > 0.9
     idx = router(l, bias, stay, scores=sigmoid, groups=groups, group_k=stay, group_top=2)[0]
     assert np.array_equal(np.sort(idx[clear], 1), np.sort(order[clear], 1))
+
+
+def test_a_wide_softmax_adds_its_small_terms():
+    """Sixteen largest logits, each followed in its lane by terms of just under half a unit of 1: added to it one by one they
+    would all be lost, 31 units of 2^-24 of the sum.  Each term passes through at most log2(32) + 4 additions; the quotient,
+    a product and the smallest terms' own errors add three units more."""
+    E, T = 512, 8
+    l = np.full((T, E), np.log(0.9995 * 2.0 ** -24), np.float32)
+    l[:, ::32] = 0.0
+    idx, w = router(l, None, 16)
+    s = scores(l, np.zeros(E, np.float32), 0)
+    assert np.array_equal(idx, np.broadcast_to(np.arange(0, E, 32), (T, 16)))
+    assert (np.abs(w - s[:, ::32]) <= 12 * 2.0 ** -24 * s[:, ::32]).all()
+
+
+@pytest.mark.parametrize("E", [64, 128, 256, 512])
+def test_softmax_parts_that_a_bias_brings_together(E):
+    """A large part and one of nothing, whose bias makes up for it to some units of the sum's last place; many small terms."""
+    rng, T, values = np.random.default_rng(E), 20000, max(1, E // 16)
+    bias = np.zeros(E, np.float32)
+    a, b = 0, E - 1
+    l = (np.log(2.0 ** -24) - rng.random((T, E)) * 0.01).astype(np.float32)
+    l[:, ::values] = 0.0
+    l[:, b] = -60.0
+    bias[:] = -8.0
+    bias[a], bias[b] = -1.0 / 16, 0.0
+    l[:, a] = (rng.normal(0, 2e-6, T)).astype(np.float32)
+    v = scores(l, bias, 0)
+    want, clear = first_k(v, 2)
+    assert clear.mean() > 0.9 and 0.05 < (want[:, 0] == a).mean() < 0.95
+    assert np.array_equal(router(l, bias, 2)[0][clear], want[clear])
