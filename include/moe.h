@@ -446,7 +446,8 @@ typedef struct {
  *   x [T or T*k, K], 16-byte aligned; x_scales [its rows, ceil(K/128) or 1] float (MOE_E4M3 only);
  *   topk_idx [T,k] int32, NULL: expert 0 for all; topk_w [T,k] float, NULL: ones;
  *   Wq, Ws as above, Wq 16-byte aligned; y [T*k or T, N] out;
- *   scratch: moe_w4_scratch_bytes(cfg) bytes, 16-byte aligned (may be 0 bytes, then NULL will do).
+ *   scratch: moe_w4_scratch_bytes(cfg) bytes, 16-byte aligned (may be 0 bytes, then NULL will do; with NULL topk_idx and
+ *   without combine it always will).  More than 2048 choices are listed by expert in it.
  * x, Wq or scratch not 16-byte aligned: MOE_ERR_UNSUPPORTED. */
 moe_status moe_w4_product(const moe_w4_config* cfg, const void* x, const float* x_scales, const int32_t* topk_idx,
                           const float* topk_w, const uint8_t* Wq, const uint8_t* Ws, void* y, void* scratch, void* stream);

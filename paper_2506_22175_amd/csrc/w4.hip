@@ -30,6 +30,7 @@ typedef float f32x4_hw __attribute__((ext_vector_type(4)));
 struct W4Args {
     const void* x; const float* x_scales; const int* idx; const float* w; const uint8_t* Wq; const uint8_t* Ws;
     void* y;
+    const int* list; const int* begins;      // of many assignments: w4_list_kernel's, else NULL
     long long ldx, ldy;
     int n_rows;                      // T * k assignments
     int k, E, K, N, n_scales, per_choice, gelu, out_f32;
@@ -406,6 +407,68 @@ template <int WAVES> __device__ int collect_rows(const int* idx, int n, int e, i
     return total;
 }
 
+// Assignments in the order of their experts: list[begins[e] .. begins[e + 1] - 1] have expert e, ascending; behind the last
+// expert's those with none.  A workgroup has an expert, counts its assignments and those of the experts before it, and goes
+// through all of them again to write its own down: two readings for each expert, whatever the product's grid.
+constexpr int LIST_WAVES = 16;
+__global__ __launch_bounds__(LIST_WAVES * 64) void w4_list_kernel(const int* __restrict__ idx, int n, int E, int* __restrict__ begins,
+                                                                  int* __restrict__ list) {
+    constexpr int AT_ONCE = 8;                             // requests of a wavefront under way
+    __shared__ int s_mine[LIST_WAVES], s_before[LIST_WAVES];
+    const int e = blockIdx.x, wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int share = (n + LIST_WAVES * 64 - 1) / (LIST_WAVES * 64) * 64, begin = wid * share, end = begin + share < n ? begin + share : n;
+    int at = 0, before = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int base = begin; base < end; base += AT_ONCE * 64) {
+            int v[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = base + u * 64 + lane;
+                v[u] = idx[i < end ? i : end - 1];
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = base + u * 64 + lane;
+                const bool mine = i < end && (e < E ? v[u] == e : (unsigned)v[u] >= (unsigned)E);
+                const unsigned long long b = __ballot(mine);
+                if (pass == 1 && mine) list[at + __popcll(b & ((1ull << lane) - 1))] = i;
+                at += __popcll(b);
+                if (pass == 0) before += __popcll(__ballot(i < end && (unsigned)v[u] < (unsigned)e));
+            }
+        }
+        if (pass == 0) {
+            if (lane == 0) { s_mine[wid] = at; s_before[wid] = before; }
+            __syncthreads();
+            at = 0;
+#pragma unroll
+            for (int w = 0; w < LIST_WAVES; ++w) at += s_before[w] + (w < wid ? s_mine[w] : 0);
+            if (threadIdx.x == 0) {
+                begins[e] = at;
+                if (e == E) begins[E + 1] = n;
+            }
+        }
+    }
+}
+
+// The rows of a workgroup's expert (e < 0: of none) from number `from` on, up to CAP, into `s_list`; returns how many there are in
+// all.  Every thread of the workgroup calls it.
+template <int WAVES, int CAP> __device__ __forceinline__ int find_rows(const W4Args& a, int e, int from, int* s_list, int* s_count) {
+    static_assert(CAP <= WAVES * 64, "a thread to a row");
+    if (a.idx && !a.list) return collect_rows<WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
+    int first = 0, total = a.n_rows;
+    if (a.list) {
+        const int slot = e < 0 ? a.E : e;
+        first = a.begins[slot];
+        total = a.begins[slot + 1] - first;
+    }
+    if ((int)threadIdx.x < CAP && from + (int)threadIdx.x < total) {
+        const int at = first + from + (int)threadIdx.x;
+        s_list[threadIdx.x] = a.list ? a.list[at] : at;
+    }
+    __syncthreads();
+    return total;
+}
+
 // Few rows to an expert (up to 16 RT at a time): a wavefront has 64 weight rows and a share of K, which it streams by itself; `shares` of the
 // workgroup's wavefronts have the same weight rows and add up their sums at the end.  The routed rows come straight from the L2
 // cache, once for 64 weight rows.  There is no barrier on the way, and the next tile's requests are out while one is
@@ -575,16 +638,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void w4_few_kernel(W4Args a, int sha
     f.Wq = a.Wq + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 2);
     f.Ws = a.Ws + (long long)(e < 0 ? 0 : e) * a.N * (a.K / 32);
     for (int from = blockIdx.z * CAP;; from += gridDim.z * CAP) {
-        int total;
-        if (a.idx) {
-            total = collect_rows<WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
-            if (total <= from) return;
-        } else {
-            total = a.n_rows;
-            if (total <= from) return;
-            if (tid < CAP) s_list[tid] = from + tid;
-            __syncthreads();
-        }
+        const int total = find_rows<WAVES, CAP>(a, e, from, s_list, s_count);
+        if (total <= from) return;
         const int here = total - from < CAP ? total - from : CAP;
         float weight[RT];
 #pragma unroll
@@ -661,16 +716,8 @@ __global__ __launch_bounds__(W4_WAVES * 64) void w4_rows_kernel(W4Args a) {
     const uint8_t* Ws = a.Ws + ((long long)(e < 0 ? 0 : e) * a.N + scale_row) * (a.K / 32);
     const int tiles = (a.K + 127) / 128, per_share = ((tiles + WK - 1) / WK + TILES - 1) / TILES * TILES;
     for (int from = blockIdx.z * CAP;; from += gridDim.z * CAP) {
-        int total;
-        if (a.idx) {
-            total = collect_rows<W4_WAVES>(a.idx, a.n_rows, e, a.E, from, CAP, s_list, s_count);
-            if (total <= from) return;
-        } else {
-            total = a.n_rows;
-            if (total <= from) return;
-            if (tid < CAP) s_list[tid] = from + tid;
-            __syncthreads();
-        }
+        const int total = find_rows<W4_WAVES, CAP>(a, e, from, s_list, s_count);
+        if (total <= from) return;
         const int here = total - from < CAP ? total - from : CAP;
         if (e < 0) {
             const float zero[4] = {0, 0, 0, 0};
@@ -881,7 +928,14 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
 }
 
 // by_token: each token by itself (w4_token_kernel).  chosen: experts that may be expected to be chosen by T tokens.
-struct W4Plan { long long ldx, ldy; int n_scales; size_t scratch; bool by_token; double chosen; };
+// The scratch: rows to be joined (0 bytes where there are none), then the list of many assignments.
+struct W4Plan { long long ldx, ldy; int n_scales; size_t rows_bytes, list_bytes; bool by_token; double chosen; };
+
+// Up to so many assignments every workgroup looks for its rows itself.  What that reads grows with their number times the grid, which
+// grows with them too: T k = 2^24 would take hours.  Beyond that one launch lists them by expert (by themselves / listed: 1200
+// assignments to 4 experts of 128 x 256 7.1 / 10 us, 2048 to 64 of 512 x 64 15.0 / 16.1, of 1024 x 4096 83 / 73, to 16 of 2048 x 8192
+// 229 / 198; 4096 of these 470 / 354, to 8 of 512 x 2048 75 / 48; 65536 to 64 of 1024 x 4096 15 / 1.7 ms).
+constexpr int LIST_FROM = 2048;
 
 // Tokens by themselves read an expert's weights once for each of its rows, but have neither rows to collect nor shares of K to
 // add up between launches.  That is worth 20 MB of weights more than are chosen, whatever the sizes (by tokens / by experts: 2 tokens, 2
@@ -911,7 +965,8 @@ moe_status w4_plan(const moe_w4_config* c, W4Plan* p) {
     p->by_token = c->T == 1 || (c->T <= TOKENS_MOST && ((double)c->T * c->k - p->chosen) * c->K * c->N * (17.0 / 32.0) <= TOKEN_MORE);
     // Rows of several tokens' choices that are still to be added up.  Workgroups that have a token to themselves do that and need
     // none, but the size is to grow with T alone: a scratch for many tokens does for fewer.
-    p->scratch = c->combine && c->k > 1 && c->T > 1 ? (size_t)c->T * c->k * c->N * sizeof(float) : 0;
+    p->rows_bytes = c->combine && c->k > 1 && c->T > 1 ? (size_t)c->T * c->k * c->N * sizeof(float) : 0;
+    p->list_bytes = c->T * c->k > LIST_FROM ? ((size_t)c->T * c->k + c->E + 2) * sizeof(int) : 0;
     return MOE_OK;
 }
 
@@ -998,7 +1053,7 @@ extern "C" moe_status moe_w4_scratch_bytes(const moe_w4_config* cfg, size_t* byt
     moe::W4Plan p;
     MOE_TRY(moe::w4_plan(cfg, &p));
     if (!bytes) return MOE_ERR_NULL;
-    *bytes = p.scratch;
+    *bytes = p.rows_bytes + p.list_bytes;
     return MOE_OK;
 }
 
@@ -1007,15 +1062,23 @@ extern "C" moe_status moe_w4_product(const moe_w4_config* cfg, const void* x, co
     moe::W4Plan p;
     MOE_TRY(moe::w4_plan(cfg, &p));
     if (cfg->T == 0) return MOE_OK;
-    if (!x || !Wq || !Ws || !y || (cfg->dtype == MOE_E4M3 && !x_scales) || (p.scratch && !scratch)) return MOE_ERR_NULL;
+    if (!x || !Wq || !Ws || !y || (cfg->dtype == MOE_E4M3 && !x_scales)) return MOE_ERR_NULL;
+    const bool listed = p.list_bytes != 0 && topk_idx;
+    if ((p.rows_bytes || listed) && !scratch) return MOE_ERR_NULL;
     if (((uintptr_t)x | (uintptr_t)Wq | (uintptr_t)scratch) & 15) return MOE_ERR_UNSUPPORTED;
     hipStream_t s = (hipStream_t)stream;
     const int rows = cfg->T * cfg->k;
-    const bool join = p.scratch != 0 && !p.by_token;
-    moe::W4Args a = {x, x_scales, topk_idx, topk_w, Wq, Ws, join ? scratch : y, p.ldx, join ? cfg->N : p.ldy, rows,
+    const bool join = p.rows_bytes != 0 && !p.by_token;
+    int* const begins = listed ? (int*)((char*)scratch + p.rows_bytes) : nullptr;
+    int* const list = listed ? begins + cfg->E + 2 : nullptr;
+    moe::W4Args a = {x, x_scales, topk_idx, topk_w, Wq, Ws, join ? scratch : y, list, begins, p.ldx, join ? cfg->N : p.ldy, rows,
                      cfg->k, cfg->E, cfg->K, cfg->N, p.n_scales, cfg->per_choice, cfg->gelu, join || cfg->out == MOE_F32};
     {
         moe::ProfScope prof(moe::PK_W4, s);
+        if (listed) {
+            moe::w4_list_kernel<<<cfg->E + 1, moe::LIST_WAVES * 64, 0, s>>>(topk_idx, rows, cfg->E, begins, list);
+            MOE_CHECK_LAUNCH();
+        }
         if (cfg->dtype == MOE_F32) moe::w4_launch<MOE_F32>(a, p, cfg->T, join, cfg->combine, s);
         else if (cfg->dtype == MOE_BF16) moe::w4_launch<MOE_BF16>(a, p, cfg->T, join, cfg->combine, s);
         else moe::w4_launch<MOE_E4M3>(a, p, cfg->T, join, cfg->combine, s);
