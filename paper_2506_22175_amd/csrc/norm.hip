@@ -232,14 +232,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(Nor
             if (left <= 0) continue;
             const float scale = scale_of(a.group ? most[u] : row_most);
             if (a.group ? (tid & 15) == 0 : u == 0 && tid == 0) a.scales[row * a.n_scales + (a.group ? col >> 7 : 0)] = scale;
-            // y / scale as a product with the reciprocal: the quotient may be a unit in its 24th bit off, which moves a value
-            // only where it lies that close to the middle of two of the type's
-            const float inv = 1.0f / scale;
             Any8 o;
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                int w = __builtin_amdgcn_cvt_pk_fp8_f32(h[u][4 * q] * inv, h[u][4 * q + 1] * inv, 0, false);
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(h[u][4 * q + 2] * inv, h[u][4 * q + 3] * inv, w, true);
+                int w = __builtin_amdgcn_cvt_pk_fp8_f32(h[u][4 * q] / scale, h[u][4 * q + 1] / scale, 0, false);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(h[u][4 * q + 2] / scale, h[u][4 * q + 3] / scale, w, true);
                 o.w[q] = (unsigned)w;
             }
             if (left >= 8) {
