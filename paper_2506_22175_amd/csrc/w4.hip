@@ -927,7 +927,8 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
     Ws[(e * N + n) * (K / 32) + b] = (uint8_t)scale;
 }
 
-// by_token: each token by itself (w4_token_kernel).  chosen: experts that may be expected to be chosen by T tokens.
+// by_token: each token by itself (w4_token_kernel).  chosen: experts that may be expected to be chosen by T tokens, or the one
+// that all have without topk_idx.
 // The scratch: rows to be joined (0 bytes where there are none), then the list of many assignments.
 struct W4Plan { long long ldx, ldy; int n_scales; size_t rows_bytes, list_bytes; bool by_token; double chosen; };
 
@@ -942,11 +943,12 @@ constexpr int LIST_FROM = 2048;
 // of 16 experts of 2048 x 8192 10 / 16 us, 4 tokens 14 / 21, 8 tokens 23.5 / 24, 12 tokens 33 / 26; 4096 x 1024, joined, 2 of 8
 // experts, 4 tokens 6.1 / 11.7, 8 tokens 11.2 / 12.2, 12 tokens 15.2 / 12.5; 1024 x 4096, 8 of 64, 4 tokens 17 / 22, 6 tokens 23.5
 // / 22.6; one token, 2 of 16 experts of 2048 x 8192 6.4 / 23).  Beyond 16 tokens, small matrices: 512 x 2048, 2 of 8 experts, 12
-// tokens 6.2 / 6.4, 24 tokens 9.6 / 7.3.
-constexpr double TOKEN_MORE = 20e6;
+// tokens 6.2 / 6.4, 24 tokens 9.6 / 7.3.  Without topk_idx it is the same matrix every time, from the caches, and worth 30 MB: 2048 x
+// 8192, 4 tokens 6.4 / 7.6, 6 tokens 8.5 / 7.8; 8192 x 8192, 2 tokens 15.5 / 12.9.
+constexpr double TOKEN_MORE = 20e6, TOKEN_MORE_OF_ONE = 30e6;
 constexpr int TOKENS_MOST = 16;
 
-moe_status w4_plan(const moe_w4_config* c, W4Plan* p) {
+moe_status w4_plan(const moe_w4_config* c, bool routed, W4Plan* p) {
     if (!c) return MOE_ERR_NULL;
     if (c->T < 0 || c->k <= 0 || c->E <= 0 || c->K <= 0 || c->N <= 0 || c->k > c->E) return MOE_ERR_SHAPE;
     if (c->dtype != MOE_F32 && c->dtype != MOE_BF16 && c->dtype != MOE_E4M3) return MOE_ERR_UNSUPPORTED;
@@ -961,8 +963,9 @@ moe_status w4_plan(const moe_w4_config* c, W4Plan* p) {
     if ((long long)c->N * c->K > INT_MAX) return MOE_ERR_UNSUPPORTED;          // offsets within an expert are 32-bit
     if ((long long)c->T * c->k > (1 << 24) || (c->combine && c->T > 65535)) return MOE_ERR_UNSUPPORTED;
     p->n_scales = c->group ? (c->K + 127) / 128 : 1;
-    p->chosen = c->E * (1.0 - std::pow(1.0 - (double)c->k / c->E, (double)c->T));
-    p->by_token = c->T == 1 || (c->T <= TOKENS_MOST && ((double)c->T * c->k - p->chosen) * c->K * c->N * (17.0 / 32.0) <= TOKEN_MORE);
+    p->chosen = !routed ? 1.0 : c->E * (1.0 - std::pow(1.0 - (double)c->k / c->E, (double)c->T));
+    p->by_token = c->T == 1 || (c->T <= TOKENS_MOST && ((double)c->T * c->k - p->chosen) * c->K * c->N * (17.0 / 32.0) <=
+                                     (routed ? TOKEN_MORE : TOKEN_MORE_OF_ONE));
     // Rows of several tokens' choices that are still to be added up.  Workgroups that have a token to themselves do that and need
     // none, but the size is to grow with T alone: a scratch for many tokens does for fewer.
     p->rows_bytes = c->combine && c->k > 1 && c->T > 1 ? (size_t)c->T * c->k * c->N * sizeof(float) : 0;
@@ -1024,7 +1027,6 @@ template <int XT> void w4_launch(const W4Args& a, const W4Plan& p, int T, bool j
     // experts that may have rows, and how many each; and one more slot for rows of no expert
     const int experts = !a.idx ? 1 : a.n_rows < a.E ? a.n_rows : a.E, slots = !a.idx ? 1 : join ? a.E : a.E + 1;
     const int rows = (a.n_rows + experts - 1) / experts;
-    const double chosen = a.idx ? p.chosen : 1.0;
     // Two tiles of rows at a time and a workgroup for each 32 are as fast as four and one matrix read for 64 at some 40 rows each
     // (16 experts of 1024 x 4096: 16 rows 19 / 23 us, 32 rows 22 / 30, 40 rows 34 / 30).  Offsets in x are 32-bit in the kernel
     // for few rows.
@@ -1035,11 +1037,11 @@ template <int XT> void w4_launch(const W4Args& a, const W4Plan& p, int T, bool j
         // 45, 41; 8192 x 2048, 64 experts, mean 8: 194, 197.
         if constexpr (XT != MOE_F32) {
             if (rows > 4) {
-                w4_few_launch<XT, 2>(a, chosen, slots, rows, s);
+                w4_few_launch<XT, 2>(a, p.chosen, slots, rows, s);
                 return;
             }
         }
-        w4_few_launch<XT, 1>(a, chosen, slots, rows, s);
+        w4_few_launch<XT, 1>(a, p.chosen, slots, rows, s);
         return;
     }
     w4_rows_launch<XT, 4>(a, experts, slots, rows, s);
@@ -1051,7 +1053,7 @@ template <int XT> void w4_launch(const W4Args& a, const W4Plan& p, int T, bool j
 
 extern "C" moe_status moe_w4_scratch_bytes(const moe_w4_config* cfg, size_t* bytes) {
     moe::W4Plan p;
-    MOE_TRY(moe::w4_plan(cfg, &p));
+    MOE_TRY(moe::w4_plan(cfg, true, &p));                  // (the scratch is the same either way)
     if (!bytes) return MOE_ERR_NULL;
     *bytes = p.rows_bytes + p.list_bytes;
     return MOE_OK;
@@ -1060,7 +1062,7 @@ extern "C" moe_status moe_w4_scratch_bytes(const moe_w4_config* cfg, size_t* byt
 extern "C" moe_status moe_w4_product(const moe_w4_config* cfg, const void* x, const float* x_scales, const int32_t* topk_idx,
                                      const float* topk_w, const uint8_t* Wq, const uint8_t* Ws, void* y, void* scratch, void* stream) {
     moe::W4Plan p;
-    MOE_TRY(moe::w4_plan(cfg, &p));
+    MOE_TRY(moe::w4_plan(cfg, topk_idx != nullptr, &p));
     if (cfg->T == 0) return MOE_OK;
     if (!x || !Wq || !Ws || !y || (cfg->dtype == MOE_E4M3 && !x_scales)) return MOE_ERR_NULL;
     const bool listed = p.list_bytes != 0 && topk_idx;
