@@ -430,7 +430,7 @@ moe_status moe_router_bwd(const moe_router_config* cfg, const void* logits, cons
  * plus 127, of the powers of two that 32 columns share (byte 255: NaN). */
 typedef struct {
     int32_t T, k, E;        /* k <= 64, E <= 4096, T * k <= 2^24; with combine T <= 65535 */
-    int32_t K, N;           /* K a multiple of 32, N * K < 2^31 (E * N * K may be any) */
+    int32_t K, N;           /* K a multiple of 32, N * K < 2^31 (E * N * K may be any), N <= 2^26 - 16 */
     int32_t dtype;          /* of x: MOE_F32, MOE_BF16 or MOE_E4M3 */
     int32_t out;            /* of y: MOE_F32 or MOE_BF16 */
     int32_t group;          /* MOE_E4M3: 128 columns of x share a scale, or 0: the row */

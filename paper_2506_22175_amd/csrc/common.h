@@ -133,6 +133,9 @@ struct Dims {
 moe_status make_dims(const moe_config* cfg, Dims* d);
 moe_status check_part(const Dims& d, int part);
 
+// HIP takes fewer than 2^32 threads along a grid's direction; calls with more rows than that make several launches of so many.
+constexpr long long LAUNCH_THREADS = 1ll << 31;
+
 // Remembers where a HIP call failed; moe_last_error() returns the text.
 void note_hip_error(hipError_t e, const char* file, int line);
 #define MOE_CHECK_LAUNCH() do { hipError_t _e = hipGetLastError(); \

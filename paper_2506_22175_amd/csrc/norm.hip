@@ -124,7 +124,7 @@ template <int WAVES> __device__ __forceinline__ unsigned row_max(unsigned v, flo
 
 struct NormArgs {
     const void* x; const void* r; const float* gain; void* h; void* y; float* scales; float* rstd;
-    long long ldx, ldr, ldh, ldy;
+    long long ldx, ldr, ldh, ldy, first;     // first: row of the launch
     int T, M, group, n_scales;
     float eps;
 };
@@ -143,7 +143,7 @@ template <typename T, bool E4M3, int WAVES, int UNITS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(NormArgs a) {
     constexpr int ROWS = WAVES == 1 ? 4 : 1, THREADS = WAVES * 64;
     __shared__ float s_part[WAVES > 1 ? WAVES : 1];
-    const long long row = (long long)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
+    const long long row = a.first + (long long)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
     if (row >= a.T) return;                                // whole wavefronts, and only where a row is one
     const int tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
@@ -476,11 +476,15 @@ RowPlan norm_bwd_plan(int M) {
     return {16, 4};
 }
 
-template <typename T, bool E4M3> void norm_launch(const NormArgs& a, RowPlan p, hipStream_t s) {
-#define NORM_CASE(W, U) if (p.waves == W && p.units == U) { \
-        norm_kernel<T, E4M3, W, U><<<W == 1 ? (a.T + 3) / 4 : a.T, W == 1 ? 256 : W * 64, 0, s>>>(a); return; }
-    NORM_CASE(1, 1) NORM_CASE(2, 1) NORM_CASE(4, 1) NORM_CASE(8, 1) NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(16, 4)
+template <typename T, bool E4M3> void norm_launch(NormArgs a, RowPlan p, hipStream_t s) {
+    const long long most = LAUNCH_THREADS / (p.waves * 64);
+    for (a.first = 0; a.first < a.T; a.first += most) {
+        const int rows = (int)(a.T - a.first < most ? a.T - a.first : most);
+#define NORM_CASE(W, U) if (p.waves == W && p.units == U) \
+            norm_kernel<T, E4M3, W, U><<<W == 1 ? (rows + 3) / 4 : rows, W == 1 ? 256 : W * 64, 0, s>>>(a);
+        NORM_CASE(1, 1) NORM_CASE(2, 1) NORM_CASE(4, 1) NORM_CASE(8, 1) NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(16, 4)
 #undef NORM_CASE
+    }
 }
 
 template <typename T> void norm_bwd_launch(const NormBwdArgs& a, RowPlan p, int blocks, hipStream_t s) {
@@ -495,7 +499,7 @@ template <typename T> void norm_bwd_launch(const NormBwdArgs& a, RowPlan p, int 
 // 20 / 26; 4096 of 8192 56 / 61; 32768 of 2048 108 / 104; 4096 of 768, three quarters of the threads: 13.7 / 12.7).
 int norm_bwd_blocks(int T, int M, RowPlan p) {
     const int rows = p.waves == 1 ? 4 : 1;
-    const int want = (T + rows - 1) / rows, fill = p.waves == 16 ? 512 : 1024, most = M > 1024 && T < 8192 ? fill / 2 : fill;
+    const int want = T / rows + (T % rows != 0), fill = p.waves == 16 ? 512 : 1024, most = M > 1024 && T < 8192 ? fill / 2 : fill;
     return want < most ? want : most;
 }
 
@@ -514,7 +518,7 @@ extern "C" moe_status moe_norm_fwd(const moe_norm_config* cfg, const void* x, co
     MOE_TRY(moe::norm_dims(cfg, &d));
     if (d.T == 0) return MOE_OK;
     if (!x || !y || (cfg->out == MOE_E4M3 && !scales)) return MOE_ERR_NULL;
-    moe::NormArgs a = {x, residual, gain, h, y, scales, rstd, d.ldx, d.ldr, d.ldh, d.ldy, d.T, d.M, cfg->group, d.n_scales, cfg->eps};
+    moe::NormArgs a = {x, residual, gain, h, y, scales, rstd, d.ldx, d.ldr, d.ldh, d.ldy, 0, d.T, d.M, cfg->group, d.n_scales, cfg->eps};
     const moe::RowPlan p = moe::norm_plan(d.M);
     hipStream_t s = (hipStream_t)stream;
     {

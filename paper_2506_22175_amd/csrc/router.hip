@@ -22,7 +22,7 @@ namespace {
 
 struct RouterArgs {
     const void* logits; const float* bias; int* idx; float* w; int* load;
-    long long ld;
+    long long ld, first;             // first: token of the launch
     int T, E, k, sigmoid, groups, group_k, group_top, renorm;
     int group_lanes;                 // lanes that hold a group, if that is a whole number and a power of two, else 0
     int exact_lanes;                 // the same with a token dealt out to 64 lanes, up to 16
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(BLOCK, VALUES <= 16 ? 4 : 2) void router_kernel(Rou
         for (int e = threadIdx.x; e < a.E; e += BLOCK) hist[e] = 0;
         __syncthreads();
     }
-    const long long base = (long long)blockIdx.x * TOKENS, t = base + threadIdx.x / LANES;
+    const long long base = a.first + (long long)blockIdx.x * TOKENS, t = base + threadIdx.x / LANES;
     const bool there = t < a.T;
     const T* row = reinterpret_cast<const T*>(a.logits) + (there ? t : 0) * a.ld;
     float l[VALUES], bias[VALUES];
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(1024) void router_load_kernel(const int* __restrict
 
 struct RouterBwdArgs {
     const void* logits; const int* idx; const float* dw; void* dl;
-    long long ld;
+    long long ld, first;
     int T, E, k, sigmoid, renorm;
     float scale;
 };
@@ -483,7 +483,7 @@ template <typename T, int VALUES>
 __global__ __launch_bounds__(256) void router_bwd_kernel(RouterBwdArgs a) {
     constexpr int TOKENS = 256 / LANES;
     const int lane = threadIdx.x & (LANES - 1), e0 = lane * VALUES;
-    const long long t = (long long)blockIdx.x * TOKENS + threadIdx.x / LANES;
+    const long long t = a.first + (long long)blockIdx.x * TOKENS + threadIdx.x / LANES;
     const bool there = t < a.T;
     const T* row = reinterpret_cast<const T*>(a.logits) + (there ? t : 0) * a.ld;
     const bool full = !a.sigmoid && !a.renorm;
@@ -579,22 +579,35 @@ int router_values(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <=
 // experts 11.1 / 11.8; 8192 tokens, 64 experts 9.6 / 7.5); and the workgroups of the launch that counts instead.
 constexpr int OWN_COUNTS = 128, COUNT_BLOCKS = 32;
 
+// Tokens of a launch, and its workgroups from token `first` on.
+constexpr long long LAUNCH_TOKENS = LAUNCH_THREADS / LANES;
+int router_blocks(int T, long long first, int tokens) {
+    const long long here = T - first < LAUNCH_TOKENS ? T - first : LAUNCH_TOKENS;
+    return (int)((here + tokens - 1) / tokens);
+}
+
 template <typename T> void router_launch(RouterArgs a, hipStream_t s) {
-    const int tokens = BLOCK / LANES, blocks = (a.T + tokens - 1) / tokens;
+    const int tokens = BLOCK / LANES;
     int* const load = a.load;
-    if (blocks > OWN_COUNTS) a.load = nullptr;
+    if (a.T > OWN_COUNTS * tokens) a.load = nullptr;
+    for (a.first = 0; a.first < a.T; a.first += LAUNCH_TOKENS) {
+        const int blocks = router_blocks(a.T, a.first, tokens);
 #define ROUTER_LAUNCH(V) router_kernel<T, V><<<blocks, BLOCK, 0, s>>>(a)
-    ROUTER_BY_VALUES(a.E, ROUTER_LAUNCH);
+        ROUTER_BY_VALUES(a.E, ROUTER_LAUNCH);
 #undef ROUTER_LAUNCH
+    }
     if (load && !a.load) {
         const long long n = (long long)a.T * a.k, most = (n + 4095) / 4096;
         router_load_kernel<<<most < COUNT_BLOCKS ? (int)most : COUNT_BLOCKS, 1024, 0, s>>>(a.idx, n, a.E, load);
     }
 }
-template <typename T> void router_bwd_launch(const RouterBwdArgs& a, hipStream_t s) {
-#define ROUTER_LAUNCH(V) router_bwd_kernel<T, V><<<(a.T + 256 / LANES - 1) / (256 / LANES), 256, 0, s>>>(a)
-    ROUTER_BY_VALUES(a.E, ROUTER_LAUNCH);
+template <typename T> void router_bwd_launch(RouterBwdArgs a, hipStream_t s) {
+    for (a.first = 0; a.first < a.T; a.first += LAUNCH_TOKENS) {
+        const int blocks = router_blocks(a.T, a.first, 256 / LANES);
+#define ROUTER_LAUNCH(V) router_bwd_kernel<T, V><<<blocks, 256, 0, s>>>(a)
+        ROUTER_BY_VALUES(a.E, ROUTER_LAUNCH);
 #undef ROUTER_LAUNCH
+    }
 }
 
 }  // namespace
@@ -610,7 +623,7 @@ extern "C" moe_status moe_router_fwd(const moe_router_config* cfg, const void* l
     // lanes that hold a group, where that is a power of two
     auto whole = [per](int v) { return per % v == 0 && ((per / v) & (per / v - 1)) == 0 ? per / v : 0; };
     const int exact = whole((values + 3) / 4);
-    moe::RouterArgs a = {logits, bias, topk_idx, topk_w, load, cfg->ld ? (long long)cfg->ld : (long long)cfg->E, cfg->T, cfg->E, cfg->k,
+    moe::RouterArgs a = {logits, bias, topk_idx, topk_w, load, cfg->ld ? (long long)cfg->ld : (long long)cfg->E, 0, cfg->T, cfg->E, cfg->k,
                          cfg->scores == MOE_SIGMOID, cfg->groups, cfg->group_k, cfg->group_top, cfg->renormalize, whole(values),
                          exact <= 16 ? exact : 0,
                          ((1u << 20) + per - 1) / per, cfg->scale};
@@ -629,7 +642,7 @@ extern "C" moe_status moe_router_bwd(const moe_router_config* cfg, const void* l
     MOE_TRY(moe::router_check(cfg));
     if (cfg->T == 0) return MOE_OK;
     if (!logits || !topk_idx || !dw || !dlogits) return MOE_ERR_NULL;
-    moe::RouterBwdArgs a = {logits, topk_idx, dw, dlogits, cfg->ld ? (long long)cfg->ld : (long long)cfg->E, cfg->T, cfg->E, cfg->k,
+    moe::RouterBwdArgs a = {logits, topk_idx, dw, dlogits, cfg->ld ? (long long)cfg->ld : (long long)cfg->E, 0, cfg->T, cfg->E, cfg->k,
                             cfg->scores == MOE_SIGMOID, cfg->renormalize, cfg->scale};
     hipStream_t s = (hipStream_t)stream;
     {

@@ -961,6 +961,7 @@ moe_status w4_plan(const moe_w4_config* c, bool routed, W4Plan* p) {
     p->ldy = c->ldy ? (long long)c->ldy : (long long)c->N;
     if (p->ldx % (c->dtype == MOE_F32 ? 4 : c->dtype == MOE_BF16 ? 8 : 16) != 0) return MOE_ERR_UNSUPPORTED;
     if ((long long)c->N * c->K > INT_MAX) return MOE_ERR_UNSUPPORTED;          // offsets within an expert are 32-bit
+    if (c->N > (1 << 26) - 16) return MOE_ERR_UNSUPPORTED;       // 16 columns and up to 1024 threads to a workgroup: below 2^32 of these
     if ((long long)c->T * c->k > (1 << 24) || (c->combine && c->T > 65535)) return MOE_ERR_UNSUPPORTED;
     p->n_scales = c->group ? (c->K + 127) / 128 : 1;
     p->chosen = !routed ? 1.0 : c->E * (1.0 - std::pow(1.0 - (double)c->k / c->E, (double)c->T));

@@ -27,3 +27,13 @@ def test_the_list_needs_its_scratch(combine):
     args = [P] * 8
     args[7] = NONE
     assert B.lib().moe_w4_product(ctypes.byref(cfg), *args, None) == NULL
+
+
+def test_more_columns_than_a_launch_has_workgroups_for():
+    """2^26 columns with sixteen wavefronts for each 16 of them would be 2^32 threads, of which none would start."""
+    P8 = [P] * 8
+    most = (1 << 26) - 16
+    for N, status in ((most + 1, 3), ((1 << 26) - 1, 3)):
+        cfg = B.make_w4_config(1, 16, 16, 32, N, combine=1)
+        assert B.lib().moe_w4_product(ctypes.byref(cfg), *P8, None) == status
+    assert B.moe_w4_scratch_bytes(B.make_w4_config(1, 16, 16, 32, most, combine=1)) == 0
