@@ -232,6 +232,11 @@ moe_status moe_gate_bwd(const moe_config* cfg, int32_t part, const void* x, cons
                         const float* dw_part, float* dL, float* dWg, void* scratch, void* stream);
 moe_status moe_gate_scratch_bytes(const moe_config* cfg, size_t* bytes);
 
+/* The second half of moe_gate_bwd by itself, from a dL that is there already (moe_router_bwd's): dWg as above.
+ *   x [T,M]; dL [T,E] float in; scratch: moe_gate_scratch_bytes(cfg). */
+moe_status moe_gate_weight_grad(const moe_config* cfg, int32_t part, const void* x, const float* dL, float* dWg,
+                                void* scratch, void* stream);
+
 /* Inverse of the slot map: rows[p][slot[t,j]] = t for every kept assignment of
  * partition p (t counted over the whole batch).  Entries at or beyond
  * counts[p][e] inside expert e's C_p-entry segment are not written.
@@ -319,7 +324,7 @@ moe_status moe_layer_backward(const moe_config* cfg, const void* x, const void* 
 /* Counters of this process's work on the device since the last reset, by class:
  * out[0] GEMMs, out[1] permutations (dispatch, combine, dispatch-backward),
  * out[2] everything else (a gate 1, a slot assignment 2, a partition's gate
- * backward 3; of the operators around the layer a product on 4-bit weights counts in out[0],
+ * backward 3, with dL given or not; of the operators around the layer a product on 4-bit weights counts in out[0],
  * any other call 1 here).  Units of work and not kernels launched: a launch that does the
  * work of several counts as all of them, and a unit counts the same whether it
  * took a launch of its own, a part of one, or (slot assignment) one or two.

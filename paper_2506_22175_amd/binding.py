@@ -24,7 +24,7 @@ EXPORTS = [
     "moe_capacity", "moe_workspace_bytes", "moe_route", "moe_assign_slots", "moe_assign_slots_static", "moe_slot_scratch_bytes",
     "moe_dispatch", "moe_expert_ffn_fwd", "moe_expert_ffn_bwd", "moe_dw_parts", "moe_combine",
     "moe_slot_rows", "moe_expert_ffn_fwd_gather",
-    "moe_gate_bwd", "moe_gate_scratch_bytes", "moe_dispatch_bwd", "moe_layer_step",
+    "moe_gate_bwd", "moe_gate_scratch_bytes", "moe_gate_weight_grad", "moe_dispatch_bwd", "moe_layer_step",
     "moe_layer_forward", "moe_layer_backward", "moe_launch_counts", "moe_status_string",
     "moe_last_error", "moe_profile_enable", "moe_profile_read",
     "moe_gran_create", "moe_gran_destroy", "moe_gran_lookup", "moe_gran_record", "moe_gran_ranges",
@@ -252,6 +252,11 @@ def moe_combine(cfg, part, DO, slot, topk_w, y, stream=None):
 def moe_gate_bwd(cfg, part, x, logits, topk_idx, slot, dw, dw_part, dL, dWg, scratch, stream=None):
     _check(lib().moe_gate_bwd(_cfg(cfg), ctypes.c_int32(part), _p(x), _p(logits), _p(topk_idx), _p(slot),
                               _p(dw), _p(dw_part), _p(dL), _p(dWg), _p(scratch), _s(stream)), "moe_gate_bwd")
+
+
+def moe_gate_weight_grad(cfg, part, x, dL, dWg, scratch, stream=None):
+    _check(lib().moe_gate_weight_grad(_cfg(cfg), ctypes.c_int32(part), _p(x), _p(dL), _p(dWg), _p(scratch), _s(stream)),
+           "moe_gate_weight_grad")
 
 
 def moe_dispatch_bwd(cfg, part, dDI, slot, dL, Wg, dx, stream=None):

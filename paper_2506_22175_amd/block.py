@@ -46,6 +46,7 @@ class Block:
         self.dgain, self.dWg = new(M, dtype=f32), new(M, E, dtype=f32)
         self.dW1, self.dW2 = new(E, M, H, dtype=f32), new(E, H, M, dtype=f32)
         self.slot_scratch = new(B.moe_slot_scratch_bytes(self.layer), dtype=torch.uint8)
+        self.gate_scratch = new(B.moe_gate_scratch_bytes(self.layer), dtype=torch.uint8)
         self.norm_scratch = new(B.moe_norm_scratch_bytes(self.norm), dtype=torch.uint8)
 
     def forward(self, x, residual=None):
@@ -67,7 +68,7 @@ class Block:
         B.moe_expert_ffn_bwd(self.layer, 0, False, self.di, self.z, self.ddo, self.counts, self.slot_w, self.W1, self.W2,
                              self.dz, self.ddi, self.dW1, self.dW2, None)
         B.moe_router_bwd(self.router, self.logits, self.topk_idx, self.dw, self.dlogits)
-        torch.mm(self.y.float().t(), self.dlogits, out=self.dWg)
+        B.moe_gate_weight_grad(self.layer, 0, self.y, self.dlogits, self.dWg, self.gate_scratch)
         B.moe_dispatch_bwd(self.layer, 0, self.ddi, self.slot, self.dlogits, self.Wg, self.dy)
         B.moe_norm_bwd(self.norm, self.dy, self.h, self.gain, self.rstd, dh, self.dx, self.dgain, self.norm_scratch)
         return self.dx

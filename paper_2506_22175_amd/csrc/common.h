@@ -301,9 +301,9 @@ struct GateSums {
     float* dWg;
     int nblk, ME, np, store;             // blocks per partition, outputs, partitions; store: the first total is stored, not added
 };
-// Gate backward: dL (which may have been computed beside the last GEMMs, dl_done), then the gate-weight gradient.  dLt
-// (bfloat16): gate_dlt_bytes per partition, one behind the other; part: gate_part_bytes per partition, part_stride floats
-// apart.  sums != NULL: the partial sums are left for dispatch_bwd_rows to add up.
+// Gate backward: dL (which may have been computed beside the last GEMMs, dl_done, or given without logits), then the gate-weight
+// gradient.  dLt (bfloat16): gate_dlt_bytes per partition, one behind the other; part: gate_part_bytes per partition, part_stride
+// floats apart.  sums != NULL: the partial sums are left for dispatch_bwd_rows to add up.
 GateDlArgs gate_dl_args(const Dims& d, int p0, int np, const float* logits, const int* idx, const int* slot, const float* dw,
                         const float* dw_part, long long dw_part_stride, int parts, float* dL, void* dLt);
 moe_status gate_bwd_rows(const Dims& d, int np, const void* x, const GateDlArgs& dl, bool dl_done, float* dWg,

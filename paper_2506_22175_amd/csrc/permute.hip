@@ -718,6 +718,23 @@ __global__ __launch_bounds__(PERM_THREADS) void gate_dl_kernel(GateDlArgs a) {
     gate_dl(a, blockIdx.x, smem);
 }
 
+// dL that is there already, transposed and as two bfloat16 terms like gate_block_dl's: zeros in the columns of experts and tokens
+// that are not there.
+__global__ __launch_bounds__(PERM_THREADS) void gate_dlt_kernel(GateDlArgs a) {
+    __shared__ __attribute__((aligned(16))) float tile[DWG_TOK][DWG_LD];
+    const int tl0 = blockIdx.x * DWG_TOK, nt = min(DWG_TOK, a.Tp - tl0), E16 = (a.E + 15) & ~15;
+    gate_block_logits(tile, a.dL, a.p0 * a.Tp + tl0, nt, a.E);
+    __syncthreads();
+    for (int q = threadIdx.x; q < E16 * DWG_TOK; q += PERM_THREADS) {
+        const int e = q / DWG_TOK, ti = q % DWG_TOK;
+        const float v = ti < nt && e < a.E ? tile[ti][e] : 0.0f;
+        const bf16_t hi = f32_to_bf16(v), lo = f32_to_bf16(v - bf16_to_f32(hi));
+        bf16_t* col = a.dLt + ((size_t)((e >> 4) * 32 + (e & 15)) * a.tp_pad + tl0 + ti);
+        col[0] = hi;
+        col[(size_t)16 * a.tp_pad] = lo;
+    }
+}
+
 // part[s][d][e] = sum over the tokens of chunk s of x[t,d] * dL[t,e] on the matrix cores
 // (bfloat16 storage).  The tokens are the reduction dimension of v_mfma_f32_32x32x16_bf16, and
 // both operands want eight consecutive tokens in a lane: dL comes transposed from the kernel
@@ -1021,7 +1038,8 @@ moe_status gate_bwd_rows(const Dims& d, int np, const void* x, const GateDlArgs&
     t.part = part; t.part_stride = part_stride; t.dWg = dWg;
     t.ME = d.M * d.E; t.np = np; t.store = d.overwrite && p0 == 0;
     if (!dl_done) {
-        hipLaunchKernelGGL(gate_dl_kernel, dim3(dl.blocks), dim3(PERM_THREADS), 0, s, dl);
+        if (dl.logits) hipLaunchKernelGGL(gate_dl_kernel, dim3(dl.blocks), dim3(PERM_THREADS), 0, s, dl);
+        else if (dl.dLt) hipLaunchKernelGGL(gate_dlt_kernel, dim3(dl.blocks), dim3(PERM_THREADS), 0, s, dl);      // (one partition)
         MOE_CHECK_LAUNCH();
     }
     if (d.dtype == MOE_BF16) {
@@ -1112,5 +1130,16 @@ extern "C" moe_status moe_gate_bwd(const moe_config* cfg, int32_t part, const vo
     int parts = 0;
     MOE_TRY(moe_dw_parts(cfg, &parts));
     const GateDlArgs dl = gate_dl_args(d, part, 1, logits, topk_idx, slot, dw, dw_part, 0, parts, dL, (char*)scratch + gate_dlt_offset(d));
+    return gate_bwd_rows(d, 1, x, dl, false, dWg, (float*)scratch, 0, (hipStream_t)stream, nullptr);
+}
+
+extern "C" moe_status moe_gate_weight_grad(const moe_config* cfg, int32_t part, const void* x, const float* dL, float* dWg,
+                                           void* scratch, void* stream) {
+    Dims d;
+    MOE_TRY(make_dims(cfg, &d));
+    MOE_TRY(check_part(d, part));
+    if (!x || !dL || !dWg || !scratch) return MOE_ERR_NULL;
+    const GateDlArgs dl = gate_dl_args(d, part, 1, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, const_cast<float*>(dL),
+                                       (char*)scratch + gate_dlt_offset(d));
     return gate_bwd_rows(d, 1, x, dl, false, dWg, (float*)scratch, 0, (hipStream_t)stream, nullptr);
 }
