@@ -358,7 +358,7 @@ __device__ __forceinline__ int choose_exactly(const RouterArgs& a, const T* row)
             const double o = of_lane(mine, g);
             ahead += o > mine || (o == mine && g < lane);
         }
-        const unsigned stays = (unsigned)__ballot(lane < a.groups && ahead < a.group_k);
+        const unsigned long long stays = __ballot(lane < a.groups && ahead < a.group_k);       // (64 bits wide: lanes past E shift by up to 63)
 #pragma unroll
         for (int v = 0; v < VALUES; ++v)
             if (!(stays >> ((unsigned)(e0 + v) * a.group_mul >> 20) & 1)) s[v] = NONE;
