@@ -416,7 +416,7 @@ typedef struct {
  * Which comes first is decided as by 64-bit scores (closer than those can tell apart: either).  An expert whose logit
  * is NaN or -inf, or whose bias makes its sum -inf or NaN, is never chosen and has no share of a softmax if its logit is
  * the reason; where fewer than k are left the remaining choices are -1 with weight 0.  Infinite logits share a softmax
- * evenly.
+ * evenly.  topk_w is computed in float, to 32 units of 2^-24 of itself whatever the size of the logits.
  *   logits [T,E]; bias [E] float, may be NULL; topk_idx [T,k] int32, topk_w [T,k] float out;
  *   load [E] int32, may be NULL: the number of tokens that chose each expert is ADDED to it. */
 moe_status moe_router_fwd(const moe_router_config* cfg, const void* logits, const float* bias,

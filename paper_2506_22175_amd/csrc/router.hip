@@ -96,6 +96,14 @@ template <typename T, int VALUES> __device__ __forceinline__ void load_logits(co
     for (int v = 0; v < VALUES; ++v) l[v] = l[v] != l[v] ? -__builtin_inff() : l[v];
 }
 
+// exp(a - b), b finite or a smaller than it: what the difference's rounding leaves out is put back, as its share of the result grows
+// with the difference.  For weights, a value to a lane; the scores of all experts do with __expf, since small parts of a sum
+// need not be as exact as large ones.
+__device__ __forceinline__ float exp_of_difference(float a, float b) {
+    const float d = a - b, back = d - a, rest = (a - (d - back)) - (b + back), e = expf(d);
+    return d == -__builtin_inff() ? 0.0f : fmaf(e, rest, e);
+}
+
 // Of a softmax: the largest logit and 1 / the sum of exp(l - it).  Infinite logits share it evenly.
 template <typename F> struct Softmax { float m; F inv; };
 template <typename F> __device__ __forceinline__ F softmax_term(float l, float m) {
@@ -430,15 +438,15 @@ __global__ __launch_bounds__(BLOCK, VALUES <= 16 ? 4 : 2) void router_kernel(Rou
         const float m = lanes_max(z);
         if (a.sigmoid) {
             const float shift = fminf(m, 0.0f);
-            w = z >= 0.0f ? 1.0f / (1.0f + __expf(-z)) : __expf(z - shift) / (1.0f + __expf(z));
+            w = z >= 0.0f ? 1.0f / (1.0f + expf(-z)) : exp_of_difference(z, shift) / (1.0f + expf(z));
         } else {
-            w = z == m ? 1.0f : __expf(z - m);
+            w = z == m ? 1.0f : exp_of_difference(z, m);
         }
         if (chosen < 0) w = 0.0f;
         const float sum = lanes_sum(w);
         w = sum > 0.0f ? w / sum : 0.0f;
     } else {
-        w = a.sigmoid ? 1.0f / (1.0f + __expf(-z)) : softmax_term<float>(z, soft.m) * soft.inv;
+        w = a.sigmoid ? 1.0f / (1.0f + expf(-z)) : chosen < 0 ? 0.0f : (z == soft.m ? 1.0f : exp_of_difference(z, soft.m)) * soft.inv;
     }
     if (there && lane < a.k) {
         a.idx[t * a.k + lane] = chosen;
@@ -503,23 +511,23 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(RouterBwdArgs a) {
         const bool open = z > -__builtin_inff();
         if (!a.renorm) {
             // s (1 - s) = e / (1 + e)^2, e = exp(-|l|)
-            const float e = __expf(-fabsf(z)), q = 1.0f + e;
+            const float e = expf(-fabsf(z)), q = 1.0f + e;
             g = open ? d * (e / (q * q)) : 0.0f;
         } else {
             const float m = lanes_max(z);
             float w;
             if (a.sigmoid) {
                 const float shift = fminf(m, 0.0f);
-                w = z >= 0.0f ? 1.0f / (1.0f + __expf(-z)) : __expf(z - shift) / (1.0f + __expf(z));
+                w = z >= 0.0f ? 1.0f / (1.0f + expf(-z)) : exp_of_difference(z, shift) / (1.0f + expf(z));
             } else {
-                w = z == m ? 1.0f : __expf(z - m);
+                w = z == m ? 1.0f : exp_of_difference(z, m);
             }
             if (!open) w = 0.0f;
             const float sum = lanes_sum(w);
             w = sum > 0.0f ? w / sum : 0.0f;
             const float inner = lanes_sum(open ? w * d : 0.0f);
             g = open ? w * (d - inner) : 0.0f;
-            if (a.sigmoid) g *= 1.0f / (1.0f + __expf(z));             // ds/dl = s (1 - s)
+            if (a.sigmoid) g *= 1.0f / (1.0f + expf(z));             // ds/dl = s (1 - s)
             if (!open) g = 0.0f;
         }
     }
