@@ -446,7 +446,8 @@ typedef struct {
 } moe_w4_config;
 
 /* y[t,j] = f(x_row W[e]^T) * w[t,j] with e = topk_idx[t,j], or y[t] = their sum over j, in an order that depends
- * on the sizes alone; f is GeLU or nothing.  Products are exact or those of float, sums float; nothing is rounded but y.
+ * on the sizes alone; f is GeLU or nothing.  Products are exact or those of float, sums float; nothing is rounded but y (of float
+ * rows, what of a value lies below 2^-133 is cut off).
  * An expert outside 0..E-1 contributes zeros.
  *   x [T or T*k, K], 16-byte aligned; x_scales [its rows, ceil(K/128) or 1] float (MOE_E4M3 only);
  *   topk_idx [T,k] int32, NULL: expert 0 for all; topk_w [T,k] float, NULL: ones;

@@ -8,7 +8,7 @@
 // bytes of bfloat16), to a thread one (forward) or a few; a wavefront has a row of up to 512 columns to itself, a workgroup a
 // longer one.  Rows need the alignment of their elements only: the hardware does wide accesses
 // at any address, and a row's last unit, if it is not full, goes element by element.  32768 rows of 2048 in bfloat16 with h: 94 us
-// (5.7 TB/s; a copy of 1 GiB 4.7); 7001 rows of 4040 to e4m3 41 us (4.8 TB/s); backward, the first 103 us (5.2 TB/s).
+// (5.7 TB/s; a copy of 1 GiB 4.7); 7001 rows of 4040 to e4m3 42 us (4.8 TB/s); backward, the first 103 us (5.2 TB/s).
 #include "common.h"
 #include "lanes.h"
 #include "wide.h"
@@ -496,7 +496,7 @@ template <typename T> void norm_bwd_launch(const NormBwdArgs& a, RowPlan p, int 
 
 // Workgroups of the backward kernel.  Each leaves M floats of partial sums, which the second launch reads, so there are only as many
 // as fill the chip, and half of that where wide rows are fewer (bfloat16, half / all: 1024 rows of 2048 10.4 / 12.7 us, of 8192
-// 20 / 26; 4096 of 8192 56 / 61; 32768 of 2048 108 / 104; 4096 of 768, three quarters of the threads: 13.7 / 12.7).
+// 20 / 26; 4096 of 8192 56 / 61; 32768 of 2048 108 / 104; 4096 of 768, where 96 of 256 threads have columns: 13.7 / 12.7).
 int norm_bwd_blocks(int T, int M, RowPlan p) {
     const int rows = p.waves == 1 ? 4 : 1;
     const int want = T / rows + (T % rows != 0), fill = p.waves == 16 ? 512 : 1024, most = M > 1024 && T < 8192 ? fill / 2 : fill;

@@ -6,7 +6,7 @@
 // A token is dealt out to 16 neighbouring lanes of a wavefront, VALUES neighbouring logits to each, and its choice is one
 // maximum after another in registers: what a lane hands to the others goes through the vector unit's lane permutations,
 // without LDS or barriers.  What bounds it is that selection: for every choice a lane goes through its VALUES twice.  32768 tokens,
-// 2 of 64 experts: 6 us (1.4 TB/s); 16384 tokens, 8 of 256 experts in 8 groups: 18 us.  Backward has no selection: the first 5 us.
+// 2 of 64 experts: 6.3 us (1.4 TB/s); 16384 tokens, 8 of 256 experts in 8 groups: 18 us.  Backward has no selection: the first 5 us.
 //
 // Which of two experts comes first is defined by their exact scores, and float scores are some 2^-22 off.  So the scores
 // are compared in float, and where two that follow one another lie within that error (one token in a few hundred) the
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(BLOCK, VALUES <= 16 ? 4 : 2) void router_kernel(Rou
 
 // load[e] += how often e is in idx.  Many of the router's own workgroups adding their counts up would take longer than they
 // have taken to choose: what they add meets in a few cache lines, which take a request about every 5 ns (32768 tokens, 64
-// experts: 24 us with that, 9.7 us with this launch behind it, 3 of them this kernel's).
+// experts: 24 us with that, 9.9 us with this launch behind it, 3 of them this kernel's).
 __global__ __launch_bounds__(1024) void router_load_kernel(const int* __restrict__ idx, long long n, int E, int* __restrict__ load) {
     __shared__ int hist[512];
     for (int e = threadIdx.x; e < E; e += 1024) hist[e] = 0;

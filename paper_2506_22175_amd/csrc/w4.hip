@@ -9,7 +9,8 @@
 // there through LDS: Block16 says why).  The weights are the left operand and the routed rows, padded to
 // 16, the right one: an output's lanes then hold four neighbouring columns of one row.
 //   bfloat16 rows  the weights become bfloat16 (exact: the scale is a power of two) eight to an instruction of 16 x 16 x 32
-//   float rows     the same with each float cut into three bfloat16 parts, whose sum it is: every product is exact
+//   float rows     the same with each float cut into three bfloat16 parts, whose sum it is: every product is exact (what of a
+//                  value lies below 2^-133, the least bfloat16, is cut off)
 //   e4m3 rows      become bfloat16 as well (exact), and 128 columns' sum is multiplied by the rows' scale.  The 16 x 16 x 128
 //                  instruction that takes 4-bit and 8-bit operands as they are would save all the conversions, but among each
 //                  eight neighbouring products it drops what lies some 2^14 below the largest (measured: sums up to 2^-14 of
