@@ -324,8 +324,8 @@ moe_status moe_layer_backward(const moe_config* cfg, const void* x, const void* 
 /* Counters of this process's work on the device since the last reset, by class:
  * out[0] GEMMs, out[1] permutations (dispatch, combine, dispatch-backward),
  * out[2] everything else (a gate 1, a slot assignment 2, a partition's gate
- * backward 3, with dL given or not; of the operators around the layer a product on 4-bit weights counts in out[0],
- * any other call 1 here).  Units of work and not kernels launched: a launch that does the
+ * backward 3, with dL given or not; of the operators around the layer a product on 4-bit weights counts in out[0], the
+ * layer for a few tokens 2 there and 1 here, dense products there, clipping 2 here, any other call 1 here).  Units of work and not kernels launched: a launch that does the
  * work of several counts as all of them, and a unit counts the same whether it
  * took a launch of its own, a part of one, or (slot assignment) one or two.
  * Host only. */
@@ -344,7 +344,8 @@ moe_status moe_launch_counts(int64_t out[3], int32_t reset);
  * GeLU-backward epilogue, 3 input-gradient GEMM, 4 weight-gradient GEMMs,
  * 5 dispatch, 6 combine, 7 dispatch backward, 8 gate, 9 slot assignment,
  * 10 gate backward, 11 norm, 12 norm backward, 13 router, 14 router backward, 15 products on
- * 4-bit weights (each one whole call).  Arrays of `kinds` entries (at most 16).  Host only; not
+ * 4-bit weights, 16 the layer for a few tokens (each one whole call), 17 dense products (their input gradients count in 3, their
+ * weight gradients in 4), 18 activation backward, 19 gradients' norm and clipping.  Arrays of `kinds` entries (at most 20).  Host only; not
  * for use under stream capture. */
 moe_status moe_profile_enable(int32_t on);
 moe_status moe_profile_read(int32_t kinds, int64_t* launches, double* total_ms);
@@ -465,6 +466,89 @@ moe_status moe_w4_scratch_bytes(const moe_w4_config* cfg, size_t* bytes);
  * 16-byte aligned. */
 moe_status moe_w4_quantize(int32_t E, int32_t K, int32_t N, int32_t dtype, const void* W, uint8_t* Wq, uint8_t* Ws,
                            void* stream);
+
+/* ---- more operators around the layer -------------------------------------------------
+ * The whole layer for a few tokens, a dense product with its epilogue (a shared expert beside the routed ones), and the
+ * gradients' norm and clipping.  The conventions of the operators above hold, T = 0 included; and: rows, weights and scratch
+ * (not: float vectors, logits, weights and numbers of choices, y of moe_few_forward) begin at addresses that are multiples of 16,
+ * and dimensions and row strides are multiples of 8 elements, else MOE_ERR_UNSUPPORTED. */
+
+/* The whole layer, forward, for a few tokens: nothing has a capacity and no choice is dropped. */
+typedef struct {
+    int32_t T, M, H, E, k;  /* T <= 256; M, H <= 2^20; E, k and the next six as in moe_router_config */
+    int32_t scores, groups, group_k, group_top, renormalize;
+    float scale;
+    int32_t dtype;          /* MOE_F32 or MOE_BF16: x, Wg, W1, W2, y */
+    int64_t ldx, ldy;       /* row strides of x and y (ldy: any) */
+} moe_few_config;
+
+/* logits = x Wg + gate_bias, summed in 64 bits and rounded to float; topk_idx and topk_w from them as moe_router_fwd gives them;
+ * y[t] = sum over the token's choices of topk_w * gelu(x[t] W1[e]) W2[e], float sums in an order that depends on the sizes and on
+ * which experts are chosen; zero where a token has no choice.  Nothing is rounded to bfloat16 but y (of the rows between the products
+ * 16 bits of mantissa are kept).
+ *   x [T,M]; Wg [M,E]; gate_bias [E] float, may be NULL; bias [E] float, may be NULL: moves the choice as in moe_router_fwd;
+ *   W1 [E,M,H]; W2 [E,H,M]; y [T,M] out; logits [T,E] float, topk_idx [T,k] int32, topk_w [T,k] float out;
+ *   scratch: moe_few_scratch_bytes(cfg) bytes. */
+moe_status moe_few_forward(const moe_few_config* cfg, const void* x, const void* Wg, const float* gate_bias, const float* bias,
+                           const void* W1, const void* W2, void* y, float* logits, int32_t* topk_idx, float* topk_w,
+                           void* scratch, void* stream);
+moe_status moe_few_scratch_bytes(const moe_few_config* cfg, size_t* bytes);
+
+/* A dense product with bias, activation and residual, and its gradients. */
+typedef enum { MOE_ACT_NONE = 0, MOE_ACT_GELU = 1 /* erf form */, MOE_ACT_SILU = 2 /* z sigmoid(z) */ } moe_act;
+typedef struct {
+    int32_t T, K, N;        /* with m the largest of K, N and the strides: (max(K,N) + 1024) m <= 2^30, T m <= 2^35 */
+    int32_t dtype;          /* MOE_F32 or MOE_BF16: x, W, residual, z, y, dy, dz, dx */
+    int32_t act;            /* moe_act */
+    int32_t grad_overwrite; /* dW, dbias: 0 accumulated into, 1 stored */
+    int64_t ldx, ldy, ldr, ldz;  /* row strides of x and dx; y and dy; residual; z and dz */
+} moe_linear_config;
+
+/* z = x W + bias;  y = act(z) + residual.  Sums are float; the activation is taken of the float sum; z and y are rounded once.
+ *   x [T,K]; W [K,N]; bias [N] float, may be NULL; residual [T,N], may be NULL, may be y itself (with its stride);
+ *   z [T,N] out, may be NULL (kept for backward); y [T,N] out;
+ *   scratch: moe_linear_scratch_bytes(cfg) bytes, for this call and the two below, which may share it. */
+moe_status moe_linear_fwd(const moe_linear_config* cfg, const void* x, const void* W, const float* bias, const void* residual,
+                          void* z, void* y, void* scratch, void* stream);
+
+/* dz = dy act'(z), with the stored z;  dbias (+)= sum over rows of dz before its rounding, in an order that depends on the sizes.
+ * (The gradient of residual is dy itself.)
+ *   dy [T,N]; z [T,N], may be NULL with MOE_ACT_NONE; dz [T,N] out, may be NULL, may be dy or z themselves (with their stride);
+ *   dbias [N] float, may be NULL; scratch as above (needed with dbias only). */
+moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, const void* z, void* dz, float* dbias, void* scratch, void* stream);
+
+/* dx = dz W^T;  dW (+)= x^T dz, float, in an order that depends on the sizes.
+ *   dz [T,N]; x [T,K] (may be NULL without dW); W [K,N] (may be NULL without dx); dx [T,K] out, may be NULL; dW [K,N] float, may
+ *   be NULL; scratch as above. */
+moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, void* dx, float* dW,
+                          void* scratch, void* stream);
+moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, size_t* bytes);
+
+/* The norm of many tensors together, and clipping by it.  A list of tensors is laid out in device memory once (again when their
+ * addresses change) and serves any number of calls, one at a time: two calls that overlap on one table or scratch race. */
+typedef struct {
+    const void* grad;       /* n elements that lie together, aligned to their type only */
+    void* out;              /* where the clipped gradient goes, of the same type: grad itself, or memory that no tensor of the list
+                               shares; NULL: the list is for norms only */
+    int64_t n;              /* 0: no element, no address needed */
+    int32_t dtype;          /* MOE_F32 or MOE_BF16 */
+} moe_grad_tensor;
+typedef struct { void* table; int64_t chunks; int32_t tensors, outs; } moe_grad_list;      /* filled by moe_grad_table */
+
+/* Host only: bytes of the table and of the scratch for a list (count <= 65536; a host array). */
+moe_status moe_grad_bytes(const moe_grad_tensor* tensors, int32_t count, size_t* table, size_t* scratch);
+/* Writes the table (16-byte aligned) on `stream` and fills *list, a host struct that has to name the same table in every call.  The
+ * host array may go afterwards.  Outputs that overlap another tensor of the list, or their own input without being it: MOE_ERR_SHAPE.
+ * Not enough host memory to look: MOE_ERR_WORKSPACE. */
+moe_status moe_grad_table(const moe_grad_tensor* tensors, int32_t count, void* table, moe_grad_list* list, void* stream);
+/* norm[0] = the root of the sum of squares of all elements: squares and sum in 64 bits, in an order that depends on the sizes, rounded
+ * to float.  NaN or infinity where an element is, 0 without elements.   norm: float out; scratch: 8-byte aligned. */
+moe_status moe_grad_norm(const moe_grad_list* list, float* norm, void* scratch, void* stream);
+/* out = grad * (most / norm[0]) where norm[0] > most, rounded once, else grad.  A norm that is NaN or infinite scales nothing (its step is to
+ * be skipped).  norm: float in, of moe_grad_norm or of several processes' together; most: finite, not negative. */
+moe_status moe_grad_scale(const moe_grad_list* list, float most, const float* norm, void* stream);
+/* Both: norm out, then the scaling. */
+moe_status moe_grad_clip(const moe_grad_list* list, float most, float* norm, void* scratch, void* stream);
 
 /* ---- adaptive pipeline granularity (Algorithm 1, Section III-C) ------------------
  * Which n a batch of B tokens should be cut into, with as few timed searches as

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libmoe_hip.so")
 
 MOE_F32, MOE_BF16, MOE_E4M3 = 0, 1, 2
 MOE_SOFTMAX, MOE_SIGMOID = 0, 1
+MOE_ACT_NONE, MOE_ACT_GELU, MOE_ACT_SILU = 0, 1, 2
 MOE_REUSE_NONE, MOE_REUSE_BUFFERS, MOE_REUSE_RECOMPUTE = 0, 1, 2
 MOE_REUSE_S1, MOE_REUSE_S2, MOE_REUSE_S3 = 3, 4, 5
 
@@ -33,12 +34,15 @@ EXPORTS = [
     "moe_gemm_tile",
     "moe_norm_fwd", "moe_norm_bwd", "moe_norm_scratch_bytes", "moe_router_fwd", "moe_router_bwd",
     "moe_w4_product", "moe_w4_scratch_bytes", "moe_w4_quantize",
+    "moe_few_forward", "moe_few_scratch_bytes", "moe_linear_fwd", "moe_act_bwd", "moe_linear_bwd", "moe_linear_scratch_bytes",
+    "moe_grad_bytes", "moe_grad_table", "moe_grad_norm", "moe_grad_scale", "moe_grad_clip",
 ]
 
 
 # Calls that take nothing but pointers (the configuration's and the stream's among them): they are handed over as numbers,
 # a microsecond less per call than as objects, and a decoding step makes these calls one after the other.
-_POINTERS = {"moe_norm_fwd": 9, "moe_norm_bwd": 10, "moe_router_fwd": 7, "moe_router_bwd": 6, "moe_w4_product": 10}
+_POINTERS = {"moe_norm_fwd": 9, "moe_norm_bwd": 10, "moe_router_fwd": 7, "moe_router_bwd": 6, "moe_w4_product": 10,
+             "moe_few_forward": 13, "moe_linear_fwd": 9, "moe_act_bwd": 7, "moe_linear_bwd": 8, "moe_grad_norm": 4}
 
 
 class MoEError(RuntimeError):
@@ -185,7 +189,8 @@ def moe_launch_counts(reset: bool = False):
 
 
 PROFILE_KINDS = ["gemm_fwd1_gelu", "gemm_nn_store", "gemm_dgelu", "gemm_dgrad", "gemm_wgrad", "dispatch",
-                 "combine", "dispatch_bwd", "route", "slots", "gate_bwd", "norm", "norm_bwd", "router", "router_bwd", "w4"]
+                 "combine", "dispatch_bwd", "route", "slots", "gate_bwd", "norm", "norm_bwd", "router", "router_bwd", "w4",
+                 "few", "linear", "act_bwd", "grads"]
 
 
 def moe_profile_enable(on: bool):
@@ -502,3 +507,123 @@ def moe_w4_product(cfg, x, x_scales, topk_idx, topk_w, Wq, Ws, y, scratch=None, 
 def moe_w4_quantize(E, K, N, dtype, W, Wq, Ws, stream=None):
     _check(lib().moe_w4_quantize(ctypes.c_int32(E), ctypes.c_int32(K), ctypes.c_int32(N), ctypes.c_int32(dtype), _p(W),
                                  _p(Wq), _p(Ws), _s(stream)), "moe_w4_quantize")
+
+
+# ---- more operators around the layer ---------------------------------------------------------
+
+class MoEFewConfig(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("M", ctypes.c_int32), ("H", ctypes.c_int32), ("E", ctypes.c_int32),
+                ("k", ctypes.c_int32), ("scores", ctypes.c_int32), ("groups", ctypes.c_int32), ("group_k", ctypes.c_int32),
+                ("group_top", ctypes.c_int32), ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("dtype", ctypes.c_int32), ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64)]
+
+
+def make_few_config(T, M, H, E, k, dtype=MOE_BF16, scores=MOE_SOFTMAX, groups=1, group_k=1, group_top=2, renormalize=0,
+                    scale=1.0, ldx=0, ldy=0) -> MoEFewConfig:
+    return MoEFewConfig(int(T), int(M), int(H), int(E), int(k), int(scores), int(groups), int(group_k), int(group_top),
+                        int(renormalize), float(scale), int(dtype), int(ldx), int(ldy))
+
+
+def moe_few_scratch_bytes(cfg: MoEFewConfig) -> int:
+    v = ctypes.c_size_t(0)
+    _check(lib().moe_few_scratch_bytes(_cfg(cfg), ctypes.byref(v)), "moe_few_scratch_bytes")
+    return v.value
+
+
+def moe_few_forward(cfg, x, Wg, gate_bias, bias, W1, W2, y, logits, topk_idx, topk_w, scratch, stream=None):
+    _check(lib().moe_few_forward(_cfg(cfg), _a(x), _a(Wg), _a(gate_bias), _a(bias), _a(W1), _a(W2), _a(y), _a(logits),
+                                 _a(topk_idx), _a(topk_w), _a(scratch), _h(stream)), "moe_few_forward")
+
+
+class MoELinearConfig(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("K", ctypes.c_int32), ("N", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("grad_overwrite", ctypes.c_int32), ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64),
+                ("ldr", ctypes.c_int64), ("ldz", ctypes.c_int64)]
+
+
+def make_linear_config(T, K, N, dtype=MOE_BF16, act=MOE_ACT_NONE, grad_overwrite=0, ldx=0, ldy=0, ldr=0, ldz=0) -> MoELinearConfig:
+    return MoELinearConfig(int(T), int(K), int(N), int(dtype), int(act), int(grad_overwrite), int(ldx), int(ldy), int(ldr),
+                           int(ldz))
+
+
+def moe_linear_scratch_bytes(cfg: MoELinearConfig) -> int:
+    v = ctypes.c_size_t(0)
+    _check(lib().moe_linear_scratch_bytes(_cfg(cfg), ctypes.byref(v)), "moe_linear_scratch_bytes")
+    return v.value
+
+
+def moe_linear_fwd(cfg, x, W, bias, residual, z, y, scratch, stream=None):
+    _check(lib().moe_linear_fwd(_cfg(cfg), _a(x), _a(W), _a(bias), _a(residual), _a(z), _a(y), _a(scratch), _h(stream)),
+           "moe_linear_fwd")
+
+
+def moe_act_bwd(cfg, dy, z, dz, dbias, scratch, stream=None):
+    _check(lib().moe_act_bwd(_cfg(cfg), _a(dy), _a(z), _a(dz), _a(dbias), _a(scratch), _h(stream)), "moe_act_bwd")
+
+
+def moe_linear_bwd(cfg, dz, x, W, dx, dW, scratch, stream=None):
+    _check(lib().moe_linear_bwd(_cfg(cfg), _a(dz), _a(x), _a(W), _a(dx), _a(dW), _a(scratch), _h(stream)), "moe_linear_bwd")
+
+
+class MoEGradTensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class MoEGradList(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("tensors", ctypes.c_int32), ("outs", ctypes.c_int32)]
+
+
+def moe_grad_bytes(tensors) -> tuple:
+    """(table, scratch) bytes for an array of MoEGradTensor."""
+    t, s = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().moe_grad_bytes(tensors, ctypes.c_int32(len(tensors)), ctypes.byref(t), ctypes.byref(s)), "moe_grad_bytes")
+    return t.value, s.value
+
+
+def moe_grad_table(tensors, table, stream=None) -> MoEGradList:
+    out = MoEGradList()
+    _check(lib().moe_grad_table(tensors, ctypes.c_int32(len(tensors)), _p(table), ctypes.byref(out), _s(stream)), "moe_grad_table")
+    return out
+
+
+def make_grad_list(grads, outs=None, stream=None) -> MoEGradList:
+    """A list of gradient tensors (contiguous, float32 or bfloat16) with its table, which the returned object keeps alive; the
+    tensors are the caller's to keep.  outs: where the clipped ones go (the gradients themselves for clipping in place), or None."""
+    import torch
+    code = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}
+    outs = [None] * len(grads) if outs is None else outs
+    if len(outs) != len(grads):
+        raise ValueError(f"{len(grads)} gradients, {len(outs)} outputs")
+    tensors = (MoEGradTensor * len(grads))()
+    for t, g, o in zip(tensors, grads, outs):
+        if g.dtype not in code or not g.is_contiguous():
+            raise ValueError("gradients are contiguous tensors of float32 or bfloat16")
+        if o is not None and (o.dtype != g.dtype or o.numel() != g.numel() or not o.is_contiguous() or o.device != g.device):
+            raise ValueError("an output has its gradient's type, size and device, and is contiguous")
+        t.grad, t.out, t.n, t.dtype = g.data_ptr(), None if o is None else o.data_ptr(), g.numel(), code[g.dtype]
+    need, scratch = moe_grad_bytes(tensors)
+    device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+    if any(g.device != device for g in grads):
+        raise ValueError("gradients of one list are on one device")
+    with torch.cuda.device(device):
+        table = torch.empty(need, dtype=torch.uint8, device=device)
+        out = moe_grad_table(tensors, table, stream)
+    out.memory, out.scratch = table, scratch
+    return out
+
+
+def moe_grad_scratch_bytes(grads: MoEGradList) -> int:
+    """Of a list that make_grad_list made."""
+    return grads.scratch
+
+
+def moe_grad_norm(grads, norm, scratch, stream=None):
+    _check(lib().moe_grad_norm(_cfg(grads), _a(norm), _a(scratch), _h(stream)), "moe_grad_norm")
+
+
+def moe_grad_scale(grads, most, norm, stream=None):
+    _check(lib().moe_grad_scale(_cfg(grads), ctypes.c_float(most), _p(norm), _s(stream)), "moe_grad_scale")
+
+
+def moe_grad_clip(grads, most, norm, scratch, stream=None):
+    _check(lib().moe_grad_clip(_cfg(grads), ctypes.c_float(most), _p(norm), _p(scratch), _s(stream)), "moe_grad_clip")

@@ -1,0 +1,54 @@
+// The activations of the dense product and their derivatives, of values in float.
+#pragma once
+#include "common.h"
+
+namespace moe {
+
+// Phi(z), and exp(-z^2 / 2) on the way: erfc by the five-term rational approximation of Abramowitz & Stegun 7.1.26 (off by
+// at most 1.5e-7), taken as it is on the negative side, where 1 - erf would lose what is left.  For results that are
+// rounded to bfloat16.
+__device__ __forceinline__ float normal_cdf_fast(float z, float* ex) {
+    const float x = fabsf(z) * 0.70710678118654752440f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    *ex = __builtin_amdgcn_exp2f(-x * x * 1.44269504088896340736f);
+    float p = fmaf(t, 1.061405429f, -1.453152027f);
+    p = fmaf(t, p, 1.421413741f);
+    p = fmaf(t, p, -0.284496736f);
+    p = fmaf(t, p, 0.254829592f);
+    const float tail = 0.5f * p * t * *ex;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-0.70710678118654752440f * z); }
+
+// act(z); act is the same for a whole launch
+template <typename T> __device__ __forceinline__ float activate(float z, int act);
+template <> __device__ __forceinline__ float activate<bf16_t>(float z, int act) {
+    if (act == MOE_ACT_GELU) { float ex; return z * normal_cdf_fast(z, &ex); }
+    if (act == MOE_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z));
+    return z;
+}
+template <> __device__ __forceinline__ float activate<float>(float z, int act) {
+    if (act == MOE_ACT_GELU) return z * normal_cdf(z);
+    if (act == MOE_ACT_SILU) return z / (1.0f + expf(-z));
+    return z;
+}
+
+// act'(z) = Phi(z) + z phi(z), or s (1 + z (1 - s)) with s the sigmoid of z
+template <typename T> __device__ __forceinline__ float activation_slope(float z, int act) {
+    constexpr bool FAST = sizeof(T) == 2;
+    if (act == MOE_ACT_GELU) {
+        float ex, cdf;
+        if (FAST) cdf = normal_cdf_fast(z, &ex);
+        else { cdf = normal_cdf(z); ex = expf(-0.5f * z * z); }
+        return fmaf(z * 0.39894228040143267794f, ex, cdf);
+    }
+    if (act == MOE_ACT_SILU) {
+        const float e = FAST ? __builtin_amdgcn_exp2f(-1.44269504088896340736f * fabsf(z)) : expf(-fabsf(z));
+        const float q = FAST ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e);
+        const float s = z < 0.0f ? e * q : q, rest = z < 0.0f ? q : e * q;         // sigmoid(z), 1 - sigmoid(z)
+        return s * fmaf(z, rest, 1.0f);
+    }
+    return 1.0f;
+}
+
+}  // namespace moe

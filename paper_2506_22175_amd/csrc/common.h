@@ -160,7 +160,8 @@ enum ProfKind {
     PK_GEMM_WGRAD = 4,   // both weight gradients         (TN, float accumulate)
     PK_DISPATCH = 5, PK_COMBINE = 6, PK_DISPATCH_BWD = 7, PK_ROUTE = 8, PK_SLOTS = 9, PK_GATE_BWD = 10,
     PK_NORM = 11, PK_NORM_BWD = 12, PK_ROUTER = 13, PK_ROUTER_BWD = 14, PK_W4 = 15,
-    PK_COUNT = 16
+    PK_FEW = 16, PK_LINEAR = 17, PK_ACT_BWD = 18, PK_GRADS = 19,
+    PK_COUNT = 20
 };
 struct ProfScope {
     int idx; hipStream_t s;
@@ -181,7 +182,8 @@ enum GemmEpilogue {
     EPI_DGELU = 2,      // dZ = w*acc*gelu'(Z), Z <- w*gelu(Z), dw_part = <gelu(Z), acc>
     EPI_ACCUM_F32 = 3,  // C(float) += acc
     EPI_STORE_F32 = 4,  // C(float) = acc (also where the reduction is empty)
-    EPI_SCATTER = 5     // C[c_rows[row]] = slot_w[row] * acc: rows leave for one matrix of c_row_limit rows
+    EPI_SCATTER = 5,    // C[c_rows[row]] = slot_w[row] * acc: rows leave for one matrix of c_row_limit rows
+    EPI_LINEAR = 6      // z = acc + bias; Z = z (optional), C = act(z) + R; the "experts" are blocks of Cp of `rows` rows
 };
 
 struct GemmArgs {
@@ -214,7 +216,17 @@ struct GemmArgs {
     const float* slot_w;  // EPI_DGELU: [E*Cp] row weights
     float* dw_part;       // EPI_DGELU: [E*Cp, dw_parts] or NULL
     int dw_parts;
+    // EPI_LINEAR: no counts
+    const float* bias;    // [N], may be NULL
+    const void* R;        // rows like C's, may be NULL
+    int ldr, act;         // act: moe_act
+    long long rows;       // of all "experts" together, Cp each but the last
 };
+// Rows of an expert that has no count (EPI_LINEAR)
+__device__ __forceinline__ int block_rows(const GemmArgs& g, int e) {
+    const long long left = g.rows - (long long)e * g.Cp;
+    return left < 0 ? 0 : left < g.Cp ? (int)left : g.Cp;
+}
 
 // Experts of all partitions of a launch are numbered so that those that share their weights are neighbours:
 // number v is expert v / np of the launch's partition v % np.
@@ -231,6 +243,7 @@ inline int gemm_prof_kind(int lay, int epi) {
     if (epi == EPI_DGELU) return PK_GEMM_DGELU;
     if (epi == EPI_ACCUM_F32 || epi == EPI_STORE_F32) return PK_GEMM_WGRAD;
     if (epi == EPI_SCATTER) return PK_GEMM_NN;
+    if (epi == EPI_LINEAR) return PK_LINEAR;
     return lay == GEMM_NN ? PK_GEMM_NN : PK_GEMM_DGRAD;
 }
 
@@ -318,5 +331,10 @@ moe_status dispatch_bwd_rows(const Dims& d, int p0, int np, const void* dDI, lon
 // combine: rows of y of dropped tokens <- 0)
 moe_status assign_slots(const Dims& d, const int* topk_idx, const float* topk_w, int* slot, int* counts, float* slot_w,
                         int* rows, void* y, int* hist, hipStream_t s);
+
+// The router on logits that are there (router.hip): moe_router_fwd without its checks of pointers.
+moe_status router_run(const moe_router_config* cfg, const void* logits, const float* bias, int32_t* topk_idx, float* topk_w,
+                      int32_t* load, hipStream_t s);
+moe_status router_check(const moe_router_config* cfg);
 
 }  // namespace moe

@@ -5,6 +5,7 @@
 // activation as in place; Section III-D recomputes T_M from T_DI).
 #pragma once
 #include "common.h"
+#include "activation.h"
 
 namespace moe {
 
@@ -43,6 +44,9 @@ struct EpiCtx {
     const float* w;  // slot weights of this expert's rows
     int ldc, ldz;
     const int* out_rows;   // EPI_SCATTER: output row of each of this expert's rows; C is then the whole output
+    const float* bias;     // EPI_LINEAR: of the columns, may be null
+    const T* R;            // EPI_LINEAR: rows to add, may be null
+    int ldr, act;
 };
 
 // v: four accumulators of row r, columns n..n+3 (all in range).  Returns this
@@ -79,6 +83,23 @@ __device__ __forceinline__ float epilogue4(const EpiCtx<T>& c, int r, int n, con
         const float w = c.w[r];
         const float o[4] = {w * v[0], w * v[1], w * v[2], w * v[3]};
         Vec4<T>::store(c.C + (size_t)c.out_rows[r] * c.ldc + n, o);
+        return 0.0f;
+    } else if constexpr (EPI == EPI_LINEAR) {
+        // (the activation is taken of the sum as it is, not as Z stores it)
+        float z[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            z[i] = c.bias ? v[i] + c.bias[n + i] : v[i];
+            y[i] = activate<T>(z[i], c.act);
+        }
+        if (c.Z) Vec4<T>::store(c.Z + (size_t)r * c.ldz + n, z);
+        if (c.R) {
+            float o[4];
+            Vec4<T>::load(c.R + (size_t)r * c.ldr + n, o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += o[i];
+        }
+        Vec4<T>::store(c.C + (size_t)r * c.ldc + n, y);
         return 0.0f;
     } else if constexpr (EPI == EPI_STORE_F32) {
         *reinterpret_cast<float4*>(c.Cf + (size_t)r * c.ldc + n) = make_float4(v[0], v[1], v[2], v[3]);

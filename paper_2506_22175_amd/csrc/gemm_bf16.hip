@@ -505,7 +505,8 @@ __device__ __forceinline__ TileNumbers number_tiles(const GemmArgs& g, int tiles
             for (int sg = 0; sg < segs; ++sg) rows += g.counts[sg * g.E + lane];
         } else {
             const ExpertOf x = expert_of(g, lane);
-            rows = g.counts[x.q * g.E + x.e];
+            if constexpr (EPI == EPI_LINEAR) rows = block_rows(g, lane);
+            else rows = g.counts[x.q * g.E + x.e];
         }
         t.lane_rows = rows;
         if (LAY == GEMM_TN) t.lane_tm = (rows > 0 || EPI == EPI_STORE_F32) ? tiles_m : 0;   // a plain store still writes zeros
@@ -1383,8 +1384,8 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, int tiles_m, int t
         const float* wbase = g.slot_w ? g.slot_w + (size_t)er * g.Cp : nullptr;
         // What a pass reads from memory (the pre-activation and row weight for GeLU-backward, the old
         // sums for float accumulation) is requested one pass ahead.
-        constexpr bool READS = (EPI == EPI_DGELU || EPI == EPI_ACCUM_F32 || EPI == EPI_SCATTER);
-        struct PassIn { uint4 zin[NPIECE]; float4 cin0[NPIECE], cin1[NPIECE]; float wrow[NPIECE]; int crow[NPIECE]; };
+        constexpr bool READS = (EPI == EPI_DGELU || EPI == EPI_ACCUM_F32 || EPI == EPI_SCATTER || EPI == EPI_LINEAR);
+        struct PassIn { uint4 zin[NPIECE]; float4 cin0[NPIECE], cin1[NPIECE]; float wrow[NPIECE]; int crow[NPIECE]; float4 bias0, bias1; };
         // Piece t of a lane: row RSTEP*t + prow of the pass, columns 8*c8 .. 8*c8 + 7.  Addresses are one vector
         // offset per column block (out of range: past the descriptor, and it stays there with any step added) and a
         // wave-uniform step per pass and piece, added to the vector offset.  (Not handed over as the scalar offset of
@@ -1402,6 +1403,16 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, int tiles_m, int t
         auto row_of = [&](int ps, int t) __attribute__((always_inline)) { return block_row(ps / NCH) + RSTEP * t; };   // wave-uniform
         auto offC = [&](int ps, int t) __attribute__((always_inline)) { return baseC[ps % NCH] + (unsigned)(row_of(ps, t) * g.ldc) * CES; };
         auto offZ = [&](int ps, int t) __attribute__((always_inline)) { return baseZ[ps % NCH] + (unsigned)(row_of(ps, t) * g.ldz) * 2u; };
+        // EPI_LINEAR: rows to add and the columns' bias, zeros where there are none
+        const bf16_t* Rbase = EPI == EPI_LINEAR && g.R ? (const bf16_t*)g.R + ((size_t)e * g.Cp + m0) * g.ldr : nullptr;
+        const __amdgpu_buffer_rsrc_t rA = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<bf16_t*>(Rbase), 0, Rbase ? (unsigned)(((size_t)(trows - 1) * g.ldr + g.N) * 2) : 0u, 0x00020000);
+        const float* bias = EPI == EPI_LINEAR ? g.bias : nullptr;
+        const __amdgpu_buffer_rsrc_t rB = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(bias), 0, bias ? g.N * 4 : 0, 0x00020000);
+        auto offR = [&](int ps, int t) __attribute__((always_inline)) {
+            const int n = n0 + wn * WN + (ps % NCH) * CW + c8 * 8;
+            return n < g.N ? (unsigned)((row_of(ps, t) + prow) * g.ldr + n) * 2u : OOB_OFFSET;
+        };
         // row weights, output rows and row dots through descriptors too: nothing below branches on the row
         const unsigned row4 = (unsigned)(m0 + prow) * 4u;
         const __amdgpu_buffer_rsrc_t rW = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(wbase), 0, wbase ? Mdim * 4 : 0, 0x00020000);
@@ -1424,8 +1435,15 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, int tiles_m, int t
         };
         const unsigned ustep = (unsigned)(UROWS * g.ldc) * 4u;      // bytes from one unit of a lane to the next
         auto request_pass = [&](int ps, PassIn& in) {
+            if constexpr (EPI == EPI_LINEAR) {
+                const unsigned at = (unsigned)(n0 + wn * WN + (ps % NCH) * CW + c8 * 8) * 4u;      // (past N: past the descriptor)
+                in.bias0 = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(rB, at, 0, 0));
+                in.bias1 = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(rB, at + 16, 0, 0));
+            }
 #pragma unroll
             for (int t = 0; t < NPIECE; ++t) {
+                if constexpr (EPI == EPI_LINEAR)
+                    in.zin[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rA, offR(ps, t), 0, 0));
                 if constexpr (EPI == EPI_DGELU)
                     in.zin[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rZ, offZ(ps, t), 0, 0));
                 if constexpr (EPI == EPI_DGELU || EPI == EPI_SCATTER)
@@ -1522,6 +1540,22 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, int tiles_m, int t
                     uint4 oa = make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7]));
                     if (Zbase) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, oz), rZ, offZ(ps, t), 0, 0);
                     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, oa), rC, offC(ps, t), 0, 0);
+                } else if constexpr (EPI == EPI_LINEAR) {
+                    // (the activation is taken of the sum as it is, not as Z stores it)
+                    const float b[8] = {in.bias0.x, in.bias0.y, in.bias0.z, in.bias0.w, in.bias1.x, in.bias1.y, in.bias1.z, in.bias1.w};
+                    float add[8], y[8];
+                    Unit8::to_float(in.zin[t], add);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        v[q] += b[q];
+                        y[q] = activate<bf16_t>(v[q], g.act) + add[q];
+                    }
+                    if (Zbase) {
+                        const uint4 oz = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, oz), rZ, offZ(ps, t), 0, 0);
+                    }
+                    const uint4 oy = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, oy), rC, offC(ps, t), 0, 0);
                 } else if constexpr (EPI == EPI_DGELU) {
                     float z[8], dz[8], a[8];
                     Unit8::to_float(in.zin[t], z);
@@ -1804,7 +1838,7 @@ static bool few_tiles(const GemmArgs& a, int cus) {
 }
 // (one: a single tile's, not the launch's)
 static double tile_time(const TileCost& c, int lay, int epi, const GemmArgs& a, int cus, bool one = false) {
-    const int which = epi == EPI_GELU ? 1 : epi == EPI_DGELU ? 2 : epi == EPI_STORE_F32 ? 3 : epi == EPI_ACCUM_F32 ? 4 : 0;
+    const int which = epi == EPI_GELU || epi == EPI_LINEAR ? 1 : epi == EPI_DGELU ? 2 : epi == EPI_STORE_F32 ? 3 : epi == EPI_ACCUM_F32 ? 4 : 0;
     const int segs = a.k_segs > 1 ? a.k_segs : 1;
     const double kt = lay == GEMM_TN ? (double)((a.mean_rows + 63) / 64) * segs : (double)((a.K + 63) / 64);
     long long whole, tail = 0;                       // tiles; those of the experts' last, partly filled tile rows
@@ -1841,15 +1875,15 @@ static int tile_choice(int lay, int epi, const GemmArgs& a) {
     return best;
 }
 
-// Only the combinations the expert FFN uses are instantiated: NN with plain, GeLU and scattered stores
-// (both layers of forward, recomputation), NT with GeLU-backward and plain stores (the two input
+// Only the combinations in use are instantiated: NN with plain, GeLU and scattered stores
+// (both layers of forward, recomputation) and the dense product's, NT with GeLU-backward and plain stores (the two input
 // gradients), TN with float store and float accumulation (the weight gradients).
 template <int LAY, int EPI>
 static moe_status launch_cfg(const GemmArgs& a, hipStream_t s) {
     const int choice = tile_choice(LAY, EPI, a);
     if (choice == 2) return launch_one<LAY, EPI, CfgS>(a, s);
     if constexpr (LAY != GEMM_TN) { if (choice == 3) return launch_one<LAY, EPI, CfgT>(a, s); }
-    if constexpr (LAY == GEMM_NN && EPI != EPI_GELU) { if (choice == 4) return launch_one<LAY, EPI, CfgU>(a, s); }
+    if constexpr (LAY == GEMM_NN && (EPI == EPI_STORE || EPI == EPI_SCATTER)) { if (choice == 4) return launch_one<LAY, EPI, CfgU>(a, s); }
     if (choice == 1) return launch_one<LAY, EPI, CfgM>(a, s);
     return launch_one<LAY, EPI, typename CfgFor<LAY, EPI>::type>(a, s);
 }
@@ -1996,6 +2030,7 @@ moe_status gemm_bf16(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStr
     if (lay == GEMM_NN && epi == EPI_STORE) return launch_cfg<GEMM_NN, EPI_STORE>(a, s);
     if (lay == GEMM_NN && epi == EPI_GELU) return launch_cfg<GEMM_NN, EPI_GELU>(a, s);
     if (lay == GEMM_NN && epi == EPI_SCATTER) return launch_cfg<GEMM_NN, EPI_SCATTER>(a, s);
+    if (lay == GEMM_NN && epi == EPI_LINEAR) return launch_cfg<GEMM_NN, EPI_LINEAR>(a, s);
     if (lay == GEMM_NT && epi == EPI_STORE) return launch_cfg<GEMM_NT, EPI_STORE>(a, s);
     if (lay == GEMM_NT && epi == EPI_DGELU) return launch_cfg<GEMM_NT, EPI_DGELU>(a, s);
     if (lay == GEMM_TN && epi == EPI_STORE_F32) return launch_cfg<GEMM_TN, EPI_STORE_F32>(a, s);

@@ -103,7 +103,7 @@ template <int LAY, int EPI>
 __device__ __forceinline__ void gemm_f32_one(const GemmArgs& g, int v, int tm, int tn, char* smem) {
     const ExpertOf x = LAY == GEMM_TN ? ExpertOf{v, 0} : expert_of(g, v);
     const int e = x.e, er = x.q * g.E + e;
-    const int rows = g.counts[er];
+    const int rows = EPI == EPI_LINEAR ? block_rows(g, er) : g.counts[er];
     const int Mdim = LAY == GEMM_TN ? g.Mo : rows, Kdim = LAY == GEMM_TN ? rows : g.K;
     const int m0 = tm * F_BM, n0 = tn * F_BN;
     if (m0 >= Mdim) return;
@@ -162,6 +162,12 @@ __device__ __forceinline__ void gemm_f32_one(const GemmArgs& g, int v, int tm, i
     c.out_rows = g.c_rows ? g.c_rows + (size_t)er * g.Cp : nullptr;
     c.Z = g.Z ? (float*)g.Z + (size_t)e * g.Cp * g.ldz + x.q * g.z_pstride : nullptr;
     c.w = g.slot_w ? g.slot_w + (size_t)er * g.Cp : nullptr;
+    if constexpr (EPI == EPI_LINEAR) {
+        c.bias = g.bias;
+        c.R = g.R ? (const float*)g.R + (size_t)e * g.Cp * g.ldr : nullptr;
+        c.ldr = g.ldr;
+        c.act = g.act;
+    }
     const int r = m0 + wm * 32 + (lane & 31);
     float dot = 0.0f;
 #pragma unroll
@@ -279,6 +285,7 @@ moe_status gemm_f32(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStre
     if (lay == GEMM_NN && epi == EPI_STORE) return launch_f32<GEMM_NN, EPI_STORE>(a, s);
     if (lay == GEMM_NN && epi == EPI_GELU) return launch_f32<GEMM_NN, EPI_GELU>(a, s);
     if (lay == GEMM_NN && epi == EPI_SCATTER) return launch_f32<GEMM_NN, EPI_SCATTER>(a, s);
+    if (lay == GEMM_NN && epi == EPI_LINEAR) return launch_f32<GEMM_NN, EPI_LINEAR>(a, s);
     if (lay == GEMM_NT && epi == EPI_STORE) return launch_f32<GEMM_NT, EPI_STORE>(a, s);
     if (lay == GEMM_NT && epi == EPI_DGELU) return launch_f32<GEMM_NT, EPI_DGELU>(a, s);
     if (lay == GEMM_TN && epi == EPI_STORE_F32) return launch_f32<GEMM_TN, EPI_STORE_F32>(a, s);

@@ -1,0 +1,342 @@
+// A dense product with its epilogue, for what stands beside the routed experts (a shared expert, projections), and its gradients.
+//
+//   z = x W + bias;  y = act(z) + residual        W [K,N] as the layer's W1 and W2
+//   dz = dy act'(z);  dbias = sum over rows of dz;  dx = dz W^T;  dW = x^T dz
+//
+// Many rows are the layer's grouped GEMM's (gemm_bf16.hip, gemm_f32.hip) with blocks of rows for experts: one in forward unless 32-bit
+// offsets want more; in the weight gradient, whose sum is over the rows, as many as the chip needs to be full, which leave
+// partial sums.  Few rows are bound by reading W once and go through few_rows.h.
+#include "common.h"
+#include "activation.h"
+#include "few_rows.h"
+
+namespace moe {
+
+namespace {
+
+struct LinearDims {
+    int T, K, N, act, overwrite;
+    bool bf16;
+    long long ldx, ldy, ldr, ldz;
+    int block, blocks;                       // rows of a block of the GEMMs over rows, how many there are
+    int wblock, wblocks;                     // the same of the weight gradient
+    int slices;                              // few rows: workgroups that share a column block's K
+};
+
+constexpr int FEW_LINEAR_ROWS = 32;          // up to so many
+constexpr int FEW_WAVES = 8;
+constexpr int ACT_ROWS_LANES = 4, ACT_COLS = 512;       // of act_bwd_kernel: wavefronts, each a row of so many columns
+
+int up(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+int few_slices(int T, int K, int N, bool bf16) {
+    const int step = bf16 ? 64 : 32, columns = up(N, FEW_COLS), steps = up(K, step);
+    if (columns >= 256) return 1;
+    int s = up(512, columns);
+    const int most = up(steps, FEW_WAVES);
+    return s < most ? s : most;
+}
+
+moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
+    if (!c) return MOE_ERR_NULL;
+    if (c->T < 0 || c->K <= 0 || c->N <= 0) return MOE_ERR_SHAPE;
+    if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_UNSUPPORTED;
+    if (c->act != MOE_ACT_NONE && c->act != MOE_ACT_GELU && c->act != MOE_ACT_SILU) return MOE_ERR_UNSUPPORTED;
+    if (c->grad_overwrite != 0 && c->grad_overwrite != 1) return MOE_ERR_UNSUPPORTED;
+    if ((c->ldx && c->ldx < c->K) || (c->ldy && c->ldy < c->N) || (c->ldr && c->ldr < c->N) || (c->ldz && c->ldz < c->N)) return MOE_ERR_SHAPE;
+    if (c->K % 8 || c->N % 8 || c->ldx % 8 || c->ldy % 8 || c->ldr % 8 || c->ldz % 8) return MOE_ERR_UNSUPPORTED;
+    d->T = c->T; d->K = c->K; d->N = c->N; d->act = c->act; d->overwrite = c->grad_overwrite;
+    d->bf16 = c->dtype == MOE_BF16;
+    d->ldx = c->ldx ? c->ldx : c->K;
+    d->ldy = c->ldy ? c->ldy : c->N;
+    d->ldr = c->ldr ? c->ldr : c->N;
+    d->ldz = c->ldz ? c->ldz : c->N;
+    long long most = d->ldx;
+    for (long long l : {d->ldy, d->ldr, d->ldz, (long long)d->N, (long long)d->K})
+        if (l > most) most = l;
+    // What the GEMMs' 32-bit offsets allow: 2^30 elements from a matrix's first to its last, some rows more.
+    const long long rows = (1ll << 30) / most - 1024;
+    if (rows < 256 || (long long)(d->K > d->N ? d->K : d->N) + 1024 > rows) return MOE_ERR_UNSUPPORTED;
+    const int T = d->T > 0 ? d->T : 1;
+    d->block = (long long)T <= rows ? T : (int)(rows / 256 * 256);
+    d->blocks = up(T, d->block);
+    if (d->blocks > 64) return MOE_ERR_UNSUPPORTED;
+    // The weight gradient's sum is cut up until its 128 x 128 tiles fill the chip twice, but not below 1024 rows.
+    const long long tiles = (long long)up(d->K, 128) * up(d->N, 128);
+    long long parts = d->blocks, want = tiles < 512 ? 512 / tiles : 1;
+    if (want > up(T, 1024)) want = up(T, 1024);
+    if (want > 64) want = 64;
+    if (want > parts) parts = want;
+    d->wblock = up(up(T, parts), 64) * 64;
+    d->wblocks = up(T, d->wblock);
+    d->slices = few_slices(T, d->K, d->N, d->bf16);
+    return MOE_OK;
+}
+
+size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
+int act_blocks(const LinearDims& d) {
+    const int columns = up(d.N, ACT_COLS);
+    int blocks = up(2048, columns);
+    const int most = up(d.T > 0 ? d.T : 1, 2 * ACT_ROWS_LANES);
+    return blocks < most ? blocks : most;
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------
+struct FewLinearArgs {
+    const void* x; const void* W; const float* bias; const void* R; void* Z; void* y;
+    float* partial;                          // [slices][T][N], or NULL: the only slice finishes
+    long long ldx, ldy, ldr, ldz;
+    int T, K, N, act, steps;                 // steps of a slice
+};
+
+template <typename T> __device__ __forceinline__ void linear_finish(const FewLinearArgs& a, int t, int n, float z) {
+    if (a.bias) z += a.bias[n];
+    if (a.Z) Elem<T>::st(reinterpret_cast<T*>(a.Z) + t * a.ldz + n, z);
+    float y = activate<T>(z, a.act);
+    if (a.R) y += Elem<T>::ld(reinterpret_cast<const T*>(a.R) + t * a.ldr + n);
+    Elem<T>::st(reinterpret_cast<T*>(a.y) + t * a.ldy + n, y);
+}
+
+template <typename T, int GROUPS>
+__global__ __launch_bounds__(FEW_WAVES * 64) void few_linear_kernel(FewLinearArgs a) {
+    __shared__ FewSums<T, FEW_WAVES> sums;
+    const int n0 = blockIdx.x * FEW_COLS, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+    const int all = (a.K + Few<T>::STEP - 1) / Few<T>::STEP, begin = blockIdx.y * a.steps, end = begin + a.steps < all ? begin + a.steps : all;
+    const T* row[GROUPS];
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        const int t = g * Few<T>::ROWS + Few<T>::row(lane);
+        row[g] = reinterpret_cast<const T*>(a.x) + (t < a.T ? t : 0) * a.ldx;
+    }
+    few_acc acc[GROUPS][Few<T>::ACCS];
+    few_sums<T, GROUPS, 1, FEW_WAVES>(reinterpret_cast<const T*>(a.W) + n0, a.N, a.N - n0, row, 0, a.K, begin + wid, end, acc);
+    float* partial = a.partial ? a.partial + (long long)blockIdx.y * a.T * a.N : nullptr;
+    few_finish<T, GROUPS, FEW_WAVES>(sums, acc, a.T, a.N - n0, [&](int t, int n, float v) {
+        if (partial) partial[(long long)t * a.N + n0 + n] = v;
+        else linear_finish<T>(a, t, n0 + n, v);
+    });
+}
+template <typename T> __global__ __launch_bounds__(256) void few_linear_finish_kernel(FewLinearArgs a, int slices) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, size = (long long)a.T * a.N;
+    if (i >= size) return;
+    float v = 0.0f;
+    for (int s = 0; s < slices; ++s) v += a.partial[s * size + i];
+    linear_finish<T>(a, (int)(i / a.N), (int)(i % a.N), v);
+}
+
+template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a, hipStream_t s) {
+    const int steps = up(d.K, Few<T>::STEP);
+    a.steps = up(steps, d.slices);
+    const int slices = up(steps, a.steps);
+    if (slices == 1) a.partial = nullptr;
+    const dim3 grid(up(d.N, FEW_COLS), slices);
+    const int groups = up(d.T, Few<T>::ROWS);
+    if (groups <= 1) few_linear_kernel<T, 1><<<grid, FEW_WAVES * 64, 0, s>>>(a);
+    else if (groups <= 2) few_linear_kernel<T, 2><<<grid, FEW_WAVES * 64, 0, s>>>(a);
+    else if constexpr (sizeof(T) == 2) few_linear_kernel<T, 4><<<grid, FEW_WAVES * 64, 0, s>>>(a);
+    MOE_CHECK_LAUNCH();
+    if (slices > 1) {
+        few_linear_finish_kernel<T><<<up((long long)d.T * d.N, 256), 256, 0, s>>>(a, slices);
+        MOE_CHECK_LAUNCH();
+    }
+    return MOE_OK;
+}
+
+// ---- gradients --------------------------------------------------------------------------------------------
+struct ActBwdArgs {
+    const void* dy; const void* z; void* dz; float* part;       // part: [blocks][N], or NULL
+    long long ldy, ldz;
+    int T, N, act, rows;                                        // rows of a workgroup
+};
+
+// A wavefront has rows of 512 columns, eight to a lane.  The columns' sums stay in registers over the workgroup's rows, and its
+// wavefronts' are added in their order.
+template <typename T>
+__global__ __launch_bounds__(ACT_ROWS_LANES * 64) void act_bwd_kernel(ActBwdArgs a) {
+    __shared__ float sums[ACT_ROWS_LANES][ACT_COLS];
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+    const int n = blockIdx.x * ACT_COLS + lane * 8;
+    const int begin = blockIdx.y * a.rows, end = begin + a.rows < a.T ? begin + a.rows : a.T;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (n < a.N) {
+        const bool by_z = a.act != MOE_ACT_NONE;
+        for (int t = begin + wid; t < end; t += ACT_ROWS_LANES) {
+            Raw8<T> dy, z;
+            dy.load(reinterpret_cast<const T*>(a.dy) + t * a.ldy + n);
+            if (by_z) z.load(reinterpret_cast<const T*>(a.z) + t * a.ldz + n); else z.zero();
+            float d[8], v[8];
+            dy.to_float(d);
+            z.to_float(v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (by_z) d[i] *= activation_slope<T>(v[i], a.act);
+                sum[i] += d[i];
+            }
+            if (a.dz) {
+                T* o = reinterpret_cast<T*>(a.dz) + t * a.ldz + n;
+                if constexpr (sizeof(T) == 2) {
+                    *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
+                } else {
+                    reinterpret_cast<float4*>(o)[0] = make_float4(d[0], d[1], d[2], d[3]);
+                    reinterpret_cast<float4*>(o)[1] = make_float4(d[4], d[5], d[6], d[7]);
+                }
+            }
+        }
+    }
+    if (!a.part) return;
+    *reinterpret_cast<float4*>(&sums[wid][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    *reinterpret_cast<float4*>(&sums[wid][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+    __syncthreads();
+    for (int c = threadIdx.x; c < ACT_COLS; c += ACT_ROWS_LANES * 64) {
+        const int col = blockIdx.x * ACT_COLS + c;
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < ACT_ROWS_LANES; ++w) v += sums[w][c];
+        if (col < a.N) a.part[(long long)blockIdx.y * a.N + col] = v;
+    }
+}
+
+// out (+)= sum over p of part[p], in order
+__global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ part, int parts, long long size, float* __restrict__ out, int store) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= size) return;
+    float v = 0.0f;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) v += part[p * size + i];
+    out[i] = store ? v : out[i] + v;
+}
+moe_status join_parts(const float* part, int parts, long long size, float* out, int store, hipStream_t s) {
+    join_parts_kernel<<<up(size, 256), 256, 0, s>>>(part, parts, size, out, store);
+    MOE_CHECK_LAUNCH();
+    return MOE_OK;
+}
+
+// The rows of each block, for the GEMMs: of the input gradient's, and of the weight gradient's 64 further on.
+__global__ void block_counts_kernel(int* counts, int T, int block, int wblock) {
+    const int per = threadIdx.x < 64 ? block : wblock;
+    const long long left = T - (long long)(threadIdx.x & 63) * per;
+    counts[threadIdx.x] = left <= 0 ? 0 : left < per ? (int)left : per;
+}
+
+moe_status gemm(const LinearDims& d, GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStream_t s) {
+    return d.bf16 ? gemm_bf16(lay, epi, a, s) : gemm_f32(lay, epi, a, s);
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+}  // namespace
+
+}  // namespace moe
+
+extern "C" moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, size_t* bytes) {
+    moe::LinearDims d;
+    MOE_TRY(moe::linear_dims(cfg, &d));
+    if (!bytes) return MOE_ERR_NULL;
+    *bytes = 0;
+    if (d.T == 0) return MOE_OK;
+    size_t most = 512;                                                     // block_counts_kernel's
+    if (d.wblocks > 1) most += (size_t)d.wblocks * d.K * d.N * 4;
+    const size_t act = (size_t)moe::act_blocks(d) * d.N * 4;
+    if (act > most) most = act;
+    if (d.T <= moe::FEW_LINEAR_ROWS && d.slices > 1) {
+        const size_t few = (size_t)d.slices * d.T * d.N * 4;
+        if (few > most) most = few;
+    }
+    *bytes = moe::align16(most);
+    return MOE_OK;
+}
+
+extern "C" moe_status moe_linear_fwd(const moe_linear_config* cfg, const void* x, const void* W, const float* bias, const void* residual,
+                                     void* z, void* y, void* scratch, void* stream) {
+    moe::LinearDims d;
+    MOE_TRY(moe::linear_dims(cfg, &d));
+    if (d.T == 0) return MOE_OK;
+    if (!x || !W || !y || !scratch) return MOE_ERR_NULL;
+    if (!moe::aligned16(x) || !moe::aligned16(W) || !moe::aligned16(residual) || !moe::aligned16(z) || !moe::aligned16(y) || !moe::aligned16(scratch))
+        return MOE_ERR_UNSUPPORTED;
+    hipStream_t s = (hipStream_t)stream;
+    if (d.T <= moe::FEW_LINEAR_ROWS) {
+        moe::FewLinearArgs a = {x, W, bias, residual, z, y, (float*)scratch, d.ldx, d.ldy, d.ldr, d.ldz, d.T, d.K, d.N, d.act, 0};
+        {
+            moe::ProfScope prof(moe::PK_LINEAR, s);
+            MOE_TRY(d.bf16 ? moe::few_linear<moe::bf16_t>(d, a, s) : moe::few_linear<float>(d, a, s));
+        }
+        moe::count_launch(moe::LC_GEMM);
+        return MOE_OK;
+    }
+    moe::GemmArgs g = {};
+    g.A = x; g.B = W; g.C = y;
+    g.a_estride = d.block * d.ldx; g.b_estride = 0; g.c_estride = d.block * d.ldy;
+    g.lda = (int)d.ldx; g.ldb = d.N; g.ldc = (int)d.ldy;
+    g.E = d.blocks; g.Cp = d.block; g.mean_rows = moe::up(d.T, d.blocks);
+    g.N = d.N; g.K = d.K;
+    g.Z = z; g.ldz = (int)d.ldz;
+    g.bias = bias; g.R = residual; g.ldr = (int)d.ldr; g.act = d.act; g.rows = d.T;
+    return moe::gemm(d, moe::GEMM_NN, moe::EPI_LINEAR, g, s);
+}
+
+extern "C" moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, const void* z, void* dz, float* dbias, void* scratch, void* stream) {
+    moe::LinearDims d;
+    MOE_TRY(moe::linear_dims(cfg, &d));
+    hipStream_t s = (hipStream_t)stream;
+    if (d.T == 0) {
+        if (dbias && d.overwrite) MOE_TRY(moe::join_parts(nullptr, 0, d.N, dbias, 1, s));
+        return MOE_OK;
+    }
+    if (!dy || (!dz && !dbias) || (!z && d.act != MOE_ACT_NONE) || (dbias && !scratch)) return MOE_ERR_NULL;
+    if (!moe::aligned16(dy) || !moe::aligned16(z) || !moe::aligned16(dz) || !moe::aligned16(scratch)) return MOE_ERR_UNSUPPORTED;
+    const int blocks = moe::act_blocks(d);
+    moe::ActBwdArgs a = {dy, z, dz, dbias ? (float*)scratch : nullptr, d.ldy, d.ldz, d.T, d.N, d.act, moe::up(d.T, blocks)};
+    const int parts = moe::up(d.T, a.rows);
+    {
+        moe::ProfScope prof(moe::PK_ACT_BWD, s);
+        const dim3 grid(moe::up(d.N, moe::ACT_COLS), parts);
+        if (d.bf16) moe::act_bwd_kernel<moe::bf16_t><<<grid, moe::ACT_ROWS_LANES * 64, 0, s>>>(a);
+        else moe::act_bwd_kernel<float><<<grid, moe::ACT_ROWS_LANES * 64, 0, s>>>(a);
+        MOE_CHECK_LAUNCH();
+        if (dbias) MOE_TRY(moe::join_parts(a.part, parts, d.N, dbias, d.overwrite, s));
+    }
+    moe::count_launch(moe::LC_OTHER);
+    return MOE_OK;
+}
+
+extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, void* dx, float* dW,
+                                     void* scratch, void* stream) {
+    moe::LinearDims d;
+    MOE_TRY(moe::linear_dims(cfg, &d));
+    hipStream_t s = (hipStream_t)stream;
+    if (d.T == 0) {
+        if (dW && d.overwrite) MOE_TRY(moe::join_parts(nullptr, 0, (long long)d.K * d.N, dW, 1, s));
+        return MOE_OK;
+    }
+    if (!dz || (!dx && !dW) || (dx && !W) || (dW && !x) || !scratch) return MOE_ERR_NULL;
+    if (!moe::aligned16(dz) || !moe::aligned16(x) || !moe::aligned16(W) || !moe::aligned16(dx) || !moe::aligned16(dW) || !moe::aligned16(scratch))
+        return MOE_ERR_UNSUPPORTED;
+    int* counts = (int*)scratch;
+    float* parts = (float*)((char*)scratch + 512);
+    moe::block_counts_kernel<<<1, 128, 0, s>>>(counts, d.T, d.block, d.wblock);
+    MOE_CHECK_LAUNCH();
+    if (dx) {
+        moe::GemmArgs g = {};
+        g.A = dz; g.B = W; g.C = dx;
+        g.a_estride = d.block * d.ldz; g.b_estride = 0; g.c_estride = d.block * d.ldx;
+        g.lda = (int)d.ldz; g.ldb = d.N; g.ldc = (int)d.ldx;
+        g.counts = counts;
+        g.E = d.blocks; g.Cp = d.block; g.mean_rows = moe::up(d.T, d.blocks);
+        g.N = d.K; g.K = d.N;
+        MOE_TRY(moe::gemm(d, moe::GEMM_NT, moe::EPI_STORE, g, s));
+    }
+    if (dW) {
+        moe::GemmArgs g = {};
+        const bool split = d.wblocks > 1;
+        g.A = x; g.B = dz; g.C = split ? parts : dW;
+        g.a_estride = d.wblock * d.ldx; g.b_estride = d.wblock * d.ldz; g.c_estride = (long long)d.K * d.N;
+        g.lda = (int)d.ldx; g.ldb = (int)d.ldz; g.ldc = d.N;
+        g.counts = counts + 64;
+        g.E = d.wblocks; g.Cp = d.wblock; g.mean_rows = moe::up(d.T, d.wblocks);
+        g.Mo = d.K; g.N = d.N;
+        MOE_TRY(moe::gemm(d, moe::GEMM_TN, split || d.overwrite ? moe::EPI_STORE_F32 : moe::EPI_ACCUM_F32, g, s));
+        if (split) MOE_TRY(moe::join_parts(parts, d.wblocks, (long long)d.K * d.N, dW, d.overwrite, s));
+    }
+    return MOE_OK;
+}

@@ -563,6 +563,8 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(RouterBwdArgs a) {
     }
 }
 
+}  // namespace
+
 moe_status router_check(const moe_router_config* c) {
     if (!c) return MOE_ERR_NULL;
     if (c->T < 0 || c->E <= 0 || c->k <= 0 || c->groups <= 0 || c->group_k <= 0) return MOE_ERR_SHAPE;
@@ -576,6 +578,8 @@ moe_status router_check(const moe_router_config* c) {
     if (c->E % c->groups != 0 || c->group_k > c->groups || c->k > c->E / c->groups * c->group_k) return MOE_ERR_SHAPE;
     return MOE_OK;
 }
+
+namespace {
 
 // As many values to a lane as the experts need.
 int router_values(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <= 128 ? 8 : E <= 256 ? 16 : 32; }
@@ -620,6 +624,21 @@ template <typename T> void router_bwd_launch(RouterBwdArgs a, hipStream_t s) {
 
 }  // namespace
 
+moe_status router_run(const moe_router_config* cfg, const void* logits, const float* bias, int32_t* topk_idx, float* topk_w,
+                      int32_t* load, hipStream_t s) {
+    const int per = cfg->E / cfg->groups, values = router_values(cfg->E);
+    // lanes that hold a group, where that is a power of two
+    auto whole = [per](int v) { return per % v == 0 && ((per / v) & (per / v - 1)) == 0 ? per / v : 0; };
+    const int exact = whole((values + 3) / 4);
+    RouterArgs a = {logits, bias, topk_idx, topk_w, load, cfg->ld ? (long long)cfg->ld : (long long)cfg->E, 0, cfg->T, cfg->E, cfg->k,
+                    cfg->scores == MOE_SIGMOID, cfg->groups, cfg->group_k, cfg->group_top, cfg->renormalize, whole(values),
+                    exact <= 16 ? exact : 0,
+                    ((1u << 20) + per - 1) / per, cfg->scale};
+    if (cfg->dtype == MOE_F32) router_launch<float>(a, s); else router_launch<bf16_t>(a, s);
+    MOE_CHECK_LAUNCH();
+    return MOE_OK;
+}
+
 }  // namespace moe
 
 extern "C" moe_status moe_router_fwd(const moe_router_config* cfg, const void* logits, const float* bias, int32_t* topk_idx,
@@ -627,20 +646,11 @@ extern "C" moe_status moe_router_fwd(const moe_router_config* cfg, const void* l
     MOE_TRY(moe::router_check(cfg));
     if (cfg->T == 0) return MOE_OK;
     if (!logits || !topk_idx || !topk_w) return MOE_ERR_NULL;
-    const int per = cfg->E / cfg->groups, values = moe::router_values(cfg->E);
-    // lanes that hold a group, where that is a power of two
-    auto whole = [per](int v) { return per % v == 0 && ((per / v) & (per / v - 1)) == 0 ? per / v : 0; };
-    const int exact = whole((values + 3) / 4);
-    moe::RouterArgs a = {logits, bias, topk_idx, topk_w, load, cfg->ld ? (long long)cfg->ld : (long long)cfg->E, 0, cfg->T, cfg->E, cfg->k,
-                         cfg->scores == MOE_SIGMOID, cfg->groups, cfg->group_k, cfg->group_top, cfg->renormalize, whole(values),
-                         exact <= 16 ? exact : 0,
-                         ((1u << 20) + per - 1) / per, cfg->scale};
     hipStream_t s = (hipStream_t)stream;
     {
         moe::ProfScope prof(moe::PK_ROUTER, s);
-        if (cfg->dtype == MOE_F32) moe::router_launch<float>(a, s); else moe::router_launch<moe::bf16_t>(a, s);
+        MOE_TRY(moe::router_run(cfg, logits, bias, topk_idx, topk_w, load, s));
     }
-    MOE_CHECK_LAUNCH();
     moe::count_launch(moe::LC_OTHER);
     return MOE_OK;
 }

@@ -1,0 +1,214 @@
+"""The whole layer for a few tokens against 64 bits.
+
+u = 2^-24.  Sums of n products are off by at most n roundings of 2 u (a matrix instruction may cut where an addition would
+round) of the sum of magnitudes; GeLU has a slope below 1.13 and is off by 16 u of itself; rows between the products keep 16
+bits of mantissa where the weights are bfloat16; weights of choices are within 32 u."""
+import math
+
+import pytest
+import torch
+
+from paper_2506_22175_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+D = "cuda:0"
+DT = {B.MOE_F32: torch.float32, B.MOE_BF16: torch.bfloat16}
+HALF = {B.MOE_F32: 2.0 ** -24, B.MOE_BF16: 2.0 ** -8}
+KEPT = {B.MOE_F32: 2.0 ** -24, B.MOE_BF16: 2.0 ** -16}
+U = 2.0 ** -24
+
+
+def _choices(logits, bias, k, scores=B.MOE_SOFTMAX, groups=1, group_k=1, renormalize=0, scale=1.0, group_top=2):
+    """From float logits, in 64 bits: as the router defines them."""
+    l = logits.double()
+    l = torch.where(l.isnan(), -math.inf, l)
+    T, E = l.shape
+    s = torch.sigmoid(l) if scores == B.MOE_SIGMOID else torch.softmax(l, 1).nan_to_num(0.0)
+    v = s if bias is None else s + bias.double()
+    open_ = (l > -math.inf) & (v > -math.inf)
+    v = torch.where(open_, v, -math.inf)
+    rank = v if bias is not None else torch.where(open_, l, -math.inf)
+    if groups > 1:
+        top = v.reshape(T, groups, -1).sort(2, descending=True)[0][..., :group_top]
+        score = torch.where(top[..., 0] > -math.inf, torch.where(top > -math.inf, top, 0.0).sum(2), -math.inf)
+        best = score.sort(dim=1, descending=True, stable=True)[1][:, :group_k]
+        stays = torch.zeros_like(score, dtype=torch.bool).scatter(1, best, True)
+        rank = torch.where(stays.repeat_interleave(E // groups, 1), rank, -math.inf)
+    rank, idx = rank.sort(dim=1, descending=True, stable=True)
+    there = rank[:, :k] > -math.inf
+    idx = idx[:, :k]
+    w = torch.where(there, s.gather(1, idx), 0.0)
+    if renormalize:
+        w = w / w.sum(1, keepdim=True).clamp(min=1e-300)
+    return torch.where(there, idx, -1), w * scale
+
+
+def _weights(M, H, E, dtype, seed):
+    g = torch.Generator(device=D).manual_seed(seed)
+    return [(torch.randn(s, generator=g, device=D) * s[-2] ** -0.5).to(DT[dtype]) for s in ((M, E), (E, M, H), (E, H, M))]
+
+
+class Layer:
+    def __init__(self, T, M, H, E, k, dtype, seed=0, apart=0, **kw):
+        self.T, self.M, self.H, self.E, self.k, self.dtype = T, M, H, E, k, dtype
+        self.kw = kw
+        self.Wg, self.W1, self.W2 = _weights(M, H, E, dtype, seed)
+        g = torch.Generator(device=D).manual_seed(seed + 1)
+        dt = DT[dtype]
+        self.x = torch.as_strided(torch.full((T * (M + 8 * apart) + 8,), 5.0, device=D).to(dt), (T, M), (M + 8 * apart, 1), 8 if apart else 0)
+        self.x.copy_(torch.randn((T, M), generator=g, device=D))
+        self.flat = torch.full((T * (M + 3 * apart) + 8,), 7.0, device=D).to(dt)
+        self.y = torch.as_strided(self.flat, (T, M), (M + 3 * apart, 1), 1 if apart else 0)
+        self.gate_bias = self.bias = None
+        self.cfg = B.make_few_config(T, M, H, E, k, dtype, ldx=M + 8 * apart, ldy=M + 3 * apart, **kw)
+        self.need = B.moe_few_scratch_bytes(self.cfg)
+        self.scratch = torch.full((self.need + 64,), 0xAB, dtype=torch.uint8, device=D)
+        self.logits = torch.full((T, E), 9.0, device=D)
+        self.idx, self.w = torch.full((T, k), 99, dtype=torch.int32, device=D), torch.full((T, k), 9.0, device=D)
+
+    def run(self, stream=None):
+        B.moe_few_forward(self.cfg, self.x, self.Wg, self.gate_bias, self.bias, self.W1, self.W2, self.y, self.logits, self.idx, self.w,
+                          self.scratch, stream)
+
+    def check(self):
+        X = self.x.double()
+        logits = X @ self.Wg.double()
+        if self.gate_bias is not None:
+            logits = logits + self.gate_bias.double()
+        whole = logits.isfinite()
+        # sums in 64 bits, rounded once
+        assert ((self.logits.double() - logits).abs() <= U * (1 + 1e-6) * logits.abs() + 1e-12)[whole].all()
+        idx, w = _choices(self.logits, self.bias, self.k, **self.kw)
+        assert torch.equal(self.idx.long(), idx)
+        assert ((self.w.double() - w).abs() <= 32 * U * w).all()
+        want, err = torch.zeros(self.T, self.M, dtype=torch.float64, device=D), torch.zeros(self.T, self.M, dtype=torch.float64, device=D)
+        for e in range(self.E):
+            t, j = (idx == e).nonzero(as_tuple=True)
+            if t.numel() == 0:
+                continue
+            V1, V2 = self.W1[e].double(), self.W2[e].double()
+            z = X[t] @ V1
+            a = z * torch.special.ndtr(z)
+            da = 1.13 * 2 * (self.M + 20) * U * (X[t].abs() @ V1.abs()) + 16 * U * z.abs() + KEPT[self.dtype] * a.abs()
+            o = a @ V2
+            do = da @ V2.abs() + (2 * (self.H + 40) + 32 + 2 * self.k) * U * (a.abs() @ V2.abs())
+            want.index_add_(0, t, o * w[t, j, None])
+            err.index_add_(0, t, do * w[t, j, None].abs())
+        assert ((self.y.double() - want).abs() <= err + HALF[self.dtype] * (want.abs() + err)).all()
+        assert (self.scratch[self.need:] == 0xAB).all()
+        keep = self.y.clone()
+        self.y.fill_(7.0)
+        assert (self.flat == 7.0).all()
+        self.y.copy_(keep)
+
+
+SHAPES = [(1, 8, 8, 1, 1), (1, 64, 64, 4, 1), (1, 520, 1000, 16, 2), (2, 64, 128, 4, 4), (3, 72, 136, 8, 2), (8, 136, 264, 2, 1), (9, 136, 264, 2, 2),
+          (17, 520, 200, 33, 3), (5, 1024, 512, 64, 8), (33, 64, 72, 3, 2), (64, 128, 256, 4, 2), (70, 72, 64, 200, 16), (256, 64, 72, 3, 2),
+          (256, 128, 64, 512, 16), (4, 2056, 72, 100, 5)]
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("T,M,H,E,k", SHAPES)
+def test_shapes(T, M, H, E, k, dtype):
+    layer = Layer(T, M, H, E, k, dtype, seed=T + E, renormalize=T % 2)
+    layer.run()
+    layer.check()
+
+
+ROUTERS = {
+    "softmax": dict(), "renormalized": dict(renormalize=1, scale=1.5), "sigmoid": dict(scores=B.MOE_SIGMOID, scale=0.5),
+    "groups": dict(scores=B.MOE_SIGMOID, groups=4, group_k=2, renormalize=1, scale=2.5), "one of two groups": dict(groups=2, group_top=1),
+}
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("router", list(ROUTERS))
+@pytest.mark.parametrize("T", [1, 2, 13, 100])
+def test_routers_and_rows_that_lie_apart(T, router, dtype):
+    layer = Layer(T, 136, 200, 16, 3, dtype, seed=T, apart=1, **ROUTERS[router])
+    g = torch.Generator(device=D).manual_seed(T)
+    for gate_bias, bias in ((False, False), (True, False), (False, True), (True, True)):
+        layer.gate_bias = torch.randn(16, generator=g, device=D) if gate_bias else None
+        layer.bias = 0.2 * torch.randn(16, generator=g, device=D) if bias else None
+        layer.run()
+        layer.check()
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("T", [1, 11, 90])
+def test_tokens_and_experts_that_are_left_out(T, dtype):
+    layer = Layer(T, 72, 136, 8, 3, dtype, seed=T)
+    inf = float("inf")
+    for bias in ([0.0, -inf, 0.1, -inf, -inf, -inf, -inf, -inf], [-inf] * 8, [-inf] * 7 + [0.0]):
+        layer.bias = torch.tensor(bias, device=D)
+        layer.y.fill_(float("nan"))
+        layer.run()
+        assert (layer.idx[:, 2] == -1).all()
+        if bias[0] == bias[7] == -inf:
+            assert (layer.y == 0).all() and (layer.idx == -1).all()
+        layer.check()
+    # an unchosen expert's weights may be anything, as may what a gate closes
+    layer.bias = torch.tensor([0.0] * 4 + [-inf] * 4, device=D)
+    layer.run()
+    before = layer.y.clone()
+    layer.W1[4:].fill_(float("nan"))
+    layer.W2[4:].fill_(inf)
+    layer.run()
+    assert torch.equal(layer.y, before)
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("T", [2, 20, 120])
+def test_tokens_that_are_no_numbers_keep_it_to_themselves(T, dtype):
+    layer = Layer(T, 136, 72, 4, 2, dtype, seed=T)
+    layer.run()
+    before = layer.y.clone()
+    layer.x[1] = float("nan")
+    layer.run()
+    assert (layer.idx[1] == -1).all() and (layer.y[1] == 0).all() and layer.logits[1].isnan().all()
+    others = [t for t in range(T) if t != 1]
+    # (sums are the same; which rows share a launch's groups changes nothing but where they lie)
+    assert torch.equal(layer.y[others], before[others])
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+def test_equal_logits_go_to_the_lower_experts(dtype):
+    layer = Layer(3, 64, 64, 12, 4, dtype)
+    layer.Wg.copy_(layer.Wg[:, :1].expand(64, 12).contiguous())
+    layer.run()
+    assert layer.idx.tolist() == [[0, 1, 2, 3]] * 3
+    layer.check()
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("shape", [(1, 1024, 512, 16, 2), (4, 64, 256, 8, 2), (37, 264, 520, 16, 4)])
+def test_the_same_bits_every_time_and_from_graphs(shape, dtype):
+    layer = Layer(*shape, dtype, renormalize=1)
+    layer.run()
+    first = [t.clone() for t in (layer.y, layer.idx, layer.w, layer.logits)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.run()
+    for i in range(10):
+        for run in (graph.replay, layer.run):
+            layer.y.fill_(float("nan"))
+            layer.scratch[:layer.need].fill_(i)                  # nothing is expected in it
+            run()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(first, (layer.y, layer.idx, layer.w, layer.logits)))
+    layer.x.copy_(layer.x.flip(0) * 0.5)                         # other tokens at the same addresses
+    graph.replay()
+    layer.check()
+
+
+def test_two_layers_on_two_streams():
+    layers = [Layer(3 + 20 * i, 520, 1032, 16, 2, B.MOE_BF16, seed=i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in layers]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for layer, s in zip(layers, streams):
+            layer.run(s)
+    torch.cuda.synchronize()
+    for layer in layers:
+        layer.check()
