@@ -10,6 +10,7 @@
 // the storage type but y.
 #include "common.h"
 #include "few_rows.h"
+#include "wide.h"
 
 namespace moe {
 
@@ -23,15 +24,14 @@ struct FewArgs {
     float* logits; const int* idx; const float* w;
     void* a;                                 // [T*k, H] float, or twice that in bfloat16, the upper parts first
     float* partial;                          // [slices][T*k][M]
-    unsigned* arrived;                       // per column block of the second product: workgroups that are through
     long long ldx, ldy;
     int T, M, H, E, k, slices, steps;        // of the second product: slices of H, steps of a slice
 };
 
 // ---- gate -------------------------------------------------------------------------------------------------
-// A workgroup has GATE_TOKENS tokens and 64 experts: a lane eight of them (fewer lanes to a row of Wg where there are fewer experts),
+// A workgroup has one or two tokens and 64 experts: a lane eight of them (fewer lanes to a row of Wg where there are fewer experts),
 // the lanes and wavefronts share out the rows of Wg.
-constexpr int GATE_TOKENS = 4, GATE_WAVES = 16;
+constexpr int GATE_TOKENS = 2, GATE_WAVES = 16;
 
 template <typename T> __device__ __forceinline__ void load_eight(const T* p, int left, bool wide, float* o) {
     if (wide) {
@@ -44,48 +44,64 @@ template <typename T> __device__ __forceinline__ void load_eight(const T* p, int
     }
 }
 
-template <typename T>
+template <typename T, int TOKENS>
 __global__ __launch_bounds__(GATE_WAVES * 64) void few_gate_kernel(FewArgs a) {
-    __shared__ double s_sum[GATE_WAVES][GATE_TOKENS][64];
+    __shared__ double s_sum[GATE_WAVES][TOKENS][64];
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
     const int e_first = blockIdx.x * 64, experts = a.E - e_first < 64 ? a.E - e_first : 64;
     int chunks = 1;                                        // lanes to a row
     while (chunks * 8 < experts) chunks *= 2;
     const int chunk = lane & (chunks - 1), rows = 64 / chunks, e0 = e_first + chunk * 8, left = a.E - e0;
     const bool wide = a.E % 8 == 0 && left >= 8;
-    const int t0 = blockIdx.y * GATE_TOKENS;
-    double sum[GATE_TOKENS][8];
+    const int t0 = blockIdx.y * TOKENS;
+    double sum[TOKENS][8];
 #pragma unroll
-    for (int t = 0; t < GATE_TOKENS; ++t)
+    for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[t][i] = 0.0;
     if (left > 0) {
-#pragma unroll 2
-        for (int m = wid * rows + lane / chunks; m < a.M; m += GATE_WAVES * rows) {
-            float w[8];
-            load_eight(reinterpret_cast<const T*>(a.Wg) + (long long)m * a.E + e0, left, wide, w);
+        // so many rows of a lane are requested before the first is multiplied
+        constexpr int AT_ONCE = 4;
+        const int step = GATE_WAVES * rows;
+        for (int m0 = wid * rows + lane / chunks; m0 < a.M; m0 += AT_ONCE * step) {
+            float w[AT_ONCE][8], x[AT_ONCE][TOKENS];
 #pragma unroll
-            for (int t = 0; t < GATE_TOKENS; ++t) {
-                const double v = t0 + t < a.T ? (double)Elem<T>::ld(reinterpret_cast<const T*>(a.x) + (t0 + t) * a.ldx + m) : 0.0;
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int m = m0 + u * step;
+                if (m < a.M) {
+                    load_eight(reinterpret_cast<const T*>(a.Wg) + (long long)m * a.E + e0, left, wide, w[u]);
+                } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[t][i] = fma(v, (double)w[i], sum[t][i]);
+                    for (int i = 0; i < 8; ++i) w[u][i] = 0.0f;
+                }
+#pragma unroll
+                for (int t = 0; t < TOKENS; ++t)
+                    x[u][t] = m < a.M && t0 + t < a.T ? Elem<T>::ld(reinterpret_cast<const T*>(a.x) + (t0 + t) * a.ldx + m) : 0.0f;
             }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const double v = (double)w[u][i];
+#pragma unroll
+                    for (int t = 0; t < TOKENS; ++t) sum[t][i] = fma((double)x[u][t], v, sum[t][i]);
+                }
         }
     }
     for (int off = chunks; off < 64; off *= 2)
 #pragma unroll
-        for (int t = 0; t < GATE_TOKENS; ++t)
+        for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[t][i] += __shfl_xor(sum[t][i], off, 64);
     if (lane < chunks) {
 #pragma unroll
-        for (int t = 0; t < GATE_TOKENS; ++t)
+        for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
             for (int i = 0; i < 8; ++i) s_sum[wid][t][lane * 8 + i] = sum[t][i];
     }
     __syncthreads();
     const int t = threadIdx.x / 64, e = threadIdx.x & 63;
-    if (t < GATE_TOKENS && t0 + t < a.T && e < experts) {
+    if (t < TOKENS && t0 + t < a.T && e < experts) {
         double v = 0.0;
         for (int q = 0; q < GATE_WAVES; ++q) v += s_sum[q][t][e];
         if (a.gate_bias) v += (double)a.gate_bias[e_first + e];
@@ -152,8 +168,6 @@ __global__ __launch_bounds__(FEW_THREADS) void few_first_kernel(FewArgs a) {
     __shared__ FewSums<T, FEW_WAVES> sums;
     __shared__ FewPlan plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * FEW_COLS;
-    if (blockIdx.x == 0 && blockIdx.y == 0)                // for the second product's workgroups
-        for (int i = threadIdx.x; i < (a.M + FEW_COLS - 1) / FEW_COLS; i += FEW_THREADS) a.arrived[i] = 0;
     few_plan(a, blockIdx.y, plan);
     if (plan.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS;
@@ -185,20 +199,15 @@ __global__ __launch_bounds__(FEW_THREADS) void few_first_kernel(FewArgs a) {
 }
 
 // ---- second product ----------------------------------------------------------------------------------------------
-// Workgroups of the same columns, which have an expert and a slice of H each, leave their rows' sums, and the last one to be through
-// adds up the choices of every token, always in the same order.
+// A workgroup has 64 columns of an expert and a slice of H.  It leaves its rows' sums, which few_join_kernel adds up: a launch of its
+// own, since making sums visible from one workgroup to another of the same launch empties the caches of eight dies (the last
+// workgroup of a column block to finish, adding them up: 89 us for what takes 14 without).
 template <typename T, int GROUPS>
 __global__ __launch_bounds__(FEW_THREADS) void few_second_kernel(FewArgs a) {
     __shared__ FewSums<T, FEW_WAVES> sums;
     __shared__ FewPlan plan;
-    __shared__ bool last;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * FEW_COLS;
     few_plan(a, blockIdx.y, plan);
-    const int cols = a.M - n0 < FEW_COLS ? a.M - n0 : FEW_COLS;
-    if (plan.n_experts == 0 && blockIdx.y == 0 && blockIdx.z == 0) {          // no token has a choice
-        for (int i = threadIdx.x; i < a.T * FEW_COLS; i += FEW_THREADS)
-            if (i % FEW_COLS < cols) Elem<T>::st(reinterpret_cast<T*>(a.y) + i / FEW_COLS * a.ldy + n0 + i % FEW_COLS, 0.0f);
-    }
     if (plan.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS, PARTS = sizeof(T) == 2 ? 2 : 1;
     const T* W = reinterpret_cast<const T*>(a.W2) + (long long)plan.expert * a.H * a.M + n0;
@@ -217,32 +226,40 @@ __global__ __launch_bounds__(FEW_THREADS) void few_second_kernel(FewArgs a) {
         few_finish<T, GROUPS, FEW_WAVES>(sums, acc, plan.n_rows - r0, a.M - n0,
                                          [&](int r, int n, float v) { partial[(long long)plan.rows[r0 + r] * a.M + n0 + n] = v; });
     }
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0)
-        last = __hip_atomic_fetch_add(&a.arrived[blockIdx.x], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(plan.n_experts * a.slices) - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    for (int i = threadIdx.x; i < a.T * FEW_COLS; i += FEW_THREADS) {
-        const int t = i / FEW_COLS, n = i % FEW_COLS;
-        if (n >= cols) continue;
-        float y = 0.0f;
-        for (int j = 0; j < a.k; ++j) {
-            const int at = t * a.k + j;
-            if (plan.idx[at] < 0) continue;
-            float v = 0.0f;
-            for (int s = 0; s < a.slices; ++s) v += a.partial[((long long)s * a.T * a.k + at) * a.M + n0 + n];
-            y = fmaf(a.w[at], v, y);
+}
+
+// y[t] = sum over the choices of w times the sum of their slices; four columns to a thread, the slices' loads in eights
+constexpr int JOIN_THREADS = 64;
+template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void few_join_kernel(FewArgs a) {
+    const int t = blockIdx.y, n = (blockIdx.x * JOIN_THREADS + threadIdx.x) * 4;
+    if (n >= a.M) return;
+    const long long step = (long long)a.T * a.k * a.M;
+    float4 y = make_float4(0, 0, 0, 0);
+    for (int j = 0; j < a.k; ++j) {
+        const int at = t * a.k + j;
+        if (a.idx[at] < 0) continue;                      // (nothing was written for it)
+        const float w = a.w[at];
+        const float* p = a.partial + (long long)at * a.M + n;
+        float4 v = make_float4(0, 0, 0, 0);
+        for (int s0 = 0; s0 < a.slices; s0 += 8) {
+            float4 o[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (s0 + s < a.slices) o[s] = *reinterpret_cast<const float4*>(p + (s0 + s) * step);
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (s0 + s < a.slices) { v.x += o[s].x; v.y += o[s].y; v.z += o[s].z; v.w += o[s].w; }
         }
-        Elem<T>::st(reinterpret_cast<T*>(a.y) + t * a.ldy + n0 + n, y);
+        y.x = fmaf(w, v.x, y.x); y.y = fmaf(w, v.y, y.y); y.z = fmaf(w, v.z, y.z); y.w = fmaf(w, v.w, y.w);
     }
+    const float o[4] = {y.x, y.y, y.z, y.w};
+    store_columns(reinterpret_cast<T*>(a.y) + t * a.ldy + n, o, 4);
 }
 
 struct FewDims {
     moe_router_config router;
     int slots, slices, steps;                // experts that may be chosen; of the second product
-    size_t a_bytes, partial_bytes, arrived_bytes;
+    size_t a_bytes, partial_bytes;
 };
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
@@ -268,12 +285,12 @@ moe_status few_dims(const moe_few_config* c, FewDims* d) {
     d->slices = up(steps, d->steps);
     d->a_bytes = align16((size_t)n * c->H * 4);
     d->partial_bytes = align16((size_t)n * c->M * d->slices * 4);
-    d->arrived_bytes = align16((size_t)up(c->M, FEW_COLS) * 4);
     return MOE_OK;
 }
 
 template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, hipStream_t s, const float* bias, int* idx, float* w) {
-    few_gate_kernel<T><<<dim3(up(a.E, 64), up(a.T, GATE_TOKENS)), GATE_WAVES * 64, 0, s>>>(a);
+    if (a.T == 1) few_gate_kernel<T, 1><<<dim3(up(a.E, 64), 1), GATE_WAVES * 64, 0, s>>>(a);
+    else few_gate_kernel<T, GATE_TOKENS><<<dim3(up(a.E, 64), up(a.T, GATE_TOKENS)), GATE_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();
     MOE_TRY(router_run(&d.router, a.logits, bias, idx, w, nullptr, s));
     // Groups of rows that go through together: as many as an expert is expected to have, and some more.
@@ -290,6 +307,8 @@ template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, 
         few_second_kernel<T, 4><<<second, FEW_THREADS, 0, s>>>(a);
     }
     MOE_CHECK_LAUNCH();
+    few_join_kernel<T><<<dim3(up(a.M, 4 * JOIN_THREADS), a.T), JOIN_THREADS, 0, s>>>(a);
+    MOE_CHECK_LAUNCH();
     return MOE_OK;
 }
 
@@ -303,7 +322,7 @@ extern "C" moe_status moe_few_scratch_bytes(const moe_few_config* cfg, size_t* b
     moe::FewDims d;
     MOE_TRY(moe::few_dims(cfg, &d));
     if (!bytes) return MOE_ERR_NULL;
-    *bytes = cfg->T == 0 ? 0 : d.a_bytes + d.partial_bytes + d.arrived_bytes;
+    *bytes = cfg->T == 0 ? 0 : d.a_bytes + d.partial_bytes;
     return MOE_OK;
 }
 
@@ -317,7 +336,7 @@ extern "C" moe_status moe_few_forward(const moe_few_config* cfg, const void* x, 
     if (!moe::aligned16(x) || !moe::aligned16(Wg) || !moe::aligned16(W1) || !moe::aligned16(W2) || !moe::aligned16(scratch)) return MOE_ERR_UNSUPPORTED;
     char* p = (char*)scratch;
     moe::FewArgs a = {x, Wg, gate_bias, W1, W2, y, logits, topk_idx, topk_w, p, (float*)(p + d.a_bytes),
-                      (unsigned*)(p + d.a_bytes + d.partial_bytes), cfg->ldx ? (long long)cfg->ldx : cfg->M, cfg->ldy ? (long long)cfg->ldy : cfg->M,
+                      cfg->ldx ? (long long)cfg->ldx : cfg->M, cfg->ldy ? (long long)cfg->ldy : cfg->M,
                       cfg->T, cfg->M, cfg->H, cfg->E, cfg->k, d.slices, d.steps};
     hipStream_t s = (hipStream_t)stream;
     {

@@ -7,7 +7,10 @@
 //
 // The tensors' places are in a table in device memory, written once for a list of tensors, so that one launch covers any number
 // of them.  It cuts them into chunks of 32 KiB, of which a workgroup takes every so many-th; eight 16-byte loads of a thread are
-// a chunk.  The workgroups leave a partial sum each, and the last one to finish adds them up, always in the same order.
+// a chunk, and the next one's are requested before a chunk is worked on.  The workgroups leave a partial sum each.  Whoever needs
+// the norm adds those up: a workgroup of its own, or every workgroup of the scaling while its first chunk is on its way.  (The last
+// workgroup to finish cannot do it cheaply: what makes its neighbours' sums visible to it empties the caches of eight dies, and cost
+// 888 workgroups 25 us.)
 #include "common.h"
 #include "wide.h"
 #include <algorithm>
@@ -24,13 +27,10 @@ constexpr int GRAD_BLOCKS = 2048;                                  // workgroups
 constexpr int GRAD_MOST = 65536;                                   // tensors
 
 struct GradEntry { const void* grad; void* out; long long n; int first, bf16; };      // first: number of its first chunk
-struct GradHead { unsigned arrived; };
-constexpr size_t GRAD_HEAD_BYTES = 256;
-
 __host__ __device__ long long grad_chunk_elements(int bf16) { return bf16 ? GRAD_CHUNK / 2 : GRAD_CHUNK / 4; }
 
 // which tensor each chunk belongs to, behind the tensors
-__host__ __device__ size_t grad_map_offset(int count) { return GRAD_HEAD_BYTES + (size_t)count * sizeof(GradEntry); }
+__host__ __device__ size_t grad_map_offset(int count) { return (size_t)count * sizeof(GradEntry); }
 
 constexpr int GRAD_BATCH = 64;                                     // entries of a launch's arguments
 struct GradTableArgs { GradEntry e[GRAD_BATCH]; int from, here; };
@@ -38,143 +38,154 @@ struct GradTableArgs { GradEntry e[GRAD_BATCH]; int from, here; };
 __global__ __launch_bounds__(256) void grad_table_kernel(GradTableArgs a, char* table, int count) {
     const GradEntry e = a.e[blockIdx.x];
     const int number = a.from + blockIdx.x;
-    if (threadIdx.x == 0) {
-        if (number == 0) reinterpret_cast<GradHead*>(table)->arrived = 0;
-        if (number < count) reinterpret_cast<GradEntry*>(table + GRAD_HEAD_BYTES)[number] = e;
-    }
+    if (threadIdx.x == 0) reinterpret_cast<GradEntry*>(table)[number] = e;
     int* map = reinterpret_cast<int*>(table + grad_map_offset(count));
     const long long per = grad_chunk_elements(e.bf16), chunks = (e.n + per - 1) / per;
     for (long long i = threadIdx.x; i < chunks; i += 256) map[e.first + i] = number;
 }
 
-struct GradArgs { char* table; int count, chunks; double* partial; float* norm; float most; };
+struct GradArgs { const char* table; int count, chunks, partials; double* partial; float* norm; float most; };
 
-struct Chunk { GradEntry e; long long at; int left; };             // first element, elements
-__device__ __forceinline__ Chunk chunk_of(const GradArgs& a, int number) {
-    const int t = reinterpret_cast<const int*>(a.table + grad_map_offset(a.count))[number];
-    Chunk c;
-    c.e = reinterpret_cast<const GradEntry*>(a.table + GRAD_HEAD_BYTES)[t];
-    const long long per = grad_chunk_elements(c.e.bf16);
-    c.at = (number - c.e.first) * per;
-    const long long left = c.e.n - c.at;
-    c.left = (int)(left < per ? left : per);
-    return c;
-}
-
-// Elements of 16 bytes.
-template <typename T> struct Unit;
-template <> struct Unit<float> {
-    static constexpr int N = 4;
-    Anywhere<16, 4> u;
-    __device__ __forceinline__ float at(int i) const { return __uint_as_float(u.w[i]); }
-};
-template <> struct Unit<bf16_t> {
-    static constexpr int N = 8;
-    Anywhere<16, 2> u;
-    __device__ __forceinline__ float at(int i) const { return __uint_as_float((i & 1) ? u.w[i / 2] & 0xffff0000u : u.w[i / 2] << 16); }
-};
-
-template <typename T> __device__ __forceinline__ double chunk_squares(const Chunk& c) {
-    constexpr int N = Unit<T>::N;
-    const T* p = reinterpret_cast<const T*>(c.e.grad) + c.at;
-    double sum = 0.0;
-    Unit<T> v[GRAD_LOADS];
-    const int whole = c.left / N;
-#pragma unroll
-    for (int j = 0; j < GRAD_LOADS; ++j) {
-        const int i = j * GRAD_THREADS + threadIdx.x;
-        if (i < whole) v[j].u = *reinterpret_cast<const decltype(v[j].u)*>(p + i * N);
-        else v[j].u.w[0] = v[j].u.w[1] = v[j].u.w[2] = v[j].u.w[3] = 0;
+// A chunk and what a thread has of it: units of 16 bytes, and an element behind the last whole one.
+struct Chunk {
+    const char* grad; char* out;
+    int whole, rest;                                               // units, elements behind them
+    bool bf16;
+    Anywhere<16, 2> v[GRAD_LOADS];
+    float tail;
+    __device__ __forceinline__ bool has_tail() const { return (int)threadIdx.x < rest; }
+    __device__ __forceinline__ int unit(int j) const { return j * GRAD_THREADS + (int)threadIdx.x; }
+    __device__ __forceinline__ void find(const GradArgs& a, int number) {
+        const int t = reinterpret_cast<const int*>(a.table + grad_map_offset(a.count))[number];
+        const GradEntry e = reinterpret_cast<const GradEntry*>(a.table)[t];
+        const long long per = grad_chunk_elements(e.bf16), at = (number - e.first) * per, left = e.n - at;
+        const int here = (int)(left < per ? left : per), es = e.bf16 ? 2 : 4;
+        grad = reinterpret_cast<const char*>(e.grad) + at * es;
+        out = reinterpret_cast<char*>(e.out) + at * es;
+        bf16 = e.bf16;
+        whole = here * es / 16;
+        rest = here - whole * 16 / es;
     }
+    __device__ __forceinline__ void load() {
 #pragma unroll
-    for (int j = 0; j < GRAD_LOADS; ++j)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const double d = (double)v[j].at(i);
-            sum = fma(d, d, sum);
+        for (int j = 0; j < GRAD_LOADS; ++j)
+            if (unit(j) < whole) v[j] = *reinterpret_cast<const Anywhere<16, 2>*>(grad + unit(j) * 16);
+            else v[j].w[0] = v[j].w[1] = v[j].w[2] = v[j].w[3] = 0;
+        tail = 0.0f;
+        if (has_tail()) {
+            const char* p = grad + whole * 16;
+            tail = bf16 ? Elem<bf16_t>::ld(reinterpret_cast<const bf16_t*>(p) + threadIdx.x) : reinterpret_cast<const float*>(p)[threadIdx.x];
         }
-    const int rest = whole * N + threadIdx.x;
-    if (rest < c.left) {
-        const double d = (double)Elem<T>::ld(p + rest);
-        sum = fma(d, d, sum);
     }
-    return sum;
-}
+    __device__ __forceinline__ double squares() const {
+        double sum = (double)tail * (double)tail, more = 0.0;
+        auto add = [](double& s, float f) { const double d = (double)f; s = fma(d, d, s); };
+#pragma unroll
+        for (int j = 0; j < GRAD_LOADS; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const unsigned w = v[j].w[q];
+                if (bf16) {
+                    add(sum, __uint_as_float(w << 16));
+                    add(more, __uint_as_float(w & 0xffff0000u));
+                } else {
+                    add(q & 1 ? more : sum, __uint_as_float(w));
+                }
+            }
+        return sum + more;
+    }
+    __device__ __forceinline__ void store(double factor) const {
+        auto times = [factor](float f) { return (float)((double)f * factor); };
+#pragma unroll
+        for (int j = 0; j < GRAD_LOADS; ++j) {
+            if (unit(j) >= whole) continue;
+            Anywhere<16, 2> o;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const unsigned w = v[j].w[q];
+                o.w[q] = bf16 ? pack_bf16x2(times(__uint_as_float(w << 16)), times(__uint_as_float(w & 0xffff0000u)))
+                              : __float_as_uint(times(__uint_as_float(w)));
+            }
+            *reinterpret_cast<Anywhere<16, 2>*>(out + unit(j) * 16) = o;
+        }
+        if (has_tail()) {
+            char* p = out + whole * 16;
+            if (bf16) Elem<bf16_t>::st(reinterpret_cast<bf16_t*>(p) + threadIdx.x, times(tail));
+            else reinterpret_cast<float*>(p)[threadIdx.x] = times(tail);
+        }
+    }
+};
 
-// over a workgroup; thread 0 has the sum
+// over a workgroup; every thread has the sum
 __device__ __forceinline__ double block_sum(double v, double* lds) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_down(v, off, 64);
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     double sum = 0.0;
-    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) sum += lds[w];
-    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < GRAD_THREADS / 64; ++w) sum += lds[w];
     return sum;
 }
+// The norm of the partial sums, the same bits in every workgroup.
+__device__ __forceinline__ float norm_of(const double* partial, int n, double* lds) {
+    constexpr int AT_ONCE = GRAD_BLOCKS / GRAD_THREADS;
+    double v[AT_ONCE], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+        const int at = i * GRAD_THREADS + threadIdx.x;
+        v[i] = at < n ? partial[at] : 0.0;
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) sum += v[i];
+    return (float)sqrt(block_sum(sum, lds));
+}
 
-__global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(GradArgs a) {
+// ALONE: the only workgroup, which writes the norm itself
+template <bool ALONE> __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(GradArgs a) {
     __shared__ double lds[GRAD_THREADS / 64];
-    __shared__ bool last;
     double sum = 0.0;
-    for (int number = blockIdx.x; number < a.chunks; number += gridDim.x) {
-        const Chunk c = chunk_of(a, number);
-        sum += c.e.bf16 ? chunk_squares<bf16_t>(c) : chunk_squares<float>(c);
+    Chunk c, next;
+    int number = blockIdx.x;
+    if (number < a.chunks) { c.find(a, number); c.load(); }
+    while (number < a.chunks) {
+        number += gridDim.x;
+        if (number < a.chunks) { next.find(a, number); next.load(); }
+        sum += c.squares();
+        c = next;
     }
     sum = block_sum(sum, lds);
     if (threadIdx.x == 0) {
-        a.partial[blockIdx.x] = sum;
-        unsigned* arrived = &reinterpret_cast<GradHead*>(a.table)->arrived;
-        last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-        if (last) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next call
+        if (ALONE) *a.norm = (float)sqrt(sum); else a.partial[blockIdx.x] = sum;
     }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    double total = 0.0;
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += GRAD_THREADS) total += a.partial[i];
-    total = block_sum(total, lds);
-    if (threadIdx.x == 0) *a.norm = (float)sqrt(total);
+}
+__global__ __launch_bounds__(GRAD_THREADS) void grad_join_kernel(GradArgs a) {
+    __shared__ double lds[GRAD_THREADS / 64];
+    const float norm = norm_of(a.partial, a.partials, lds);
+    if (threadIdx.x == 0) *a.norm = norm;
 }
 
-template <typename T> __device__ __forceinline__ void chunk_scale(const Chunk& c, double factor) {
-    constexpr int N = Unit<T>::N;
-    const T* p = reinterpret_cast<const T*>(c.e.grad) + c.at;
-    T* o = reinterpret_cast<T*>(c.e.out) + c.at;
-    Unit<T> v[GRAD_LOADS];
-    const int whole = c.left / N;
-#pragma unroll
-    for (int j = 0; j < GRAD_LOADS; ++j) {
-        const int i = j * GRAD_THREADS + threadIdx.x;
-        if (i < whole) v[j].u = *reinterpret_cast<const decltype(v[j].u)*>(p + i * N);
-    }
-    const int rest = whole * N + threadIdx.x;
-    float tail = 0.0f;
-    if (rest < c.left) tail = Elem<T>::ld(p + rest);
-#pragma unroll
-    for (int j = 0; j < GRAD_LOADS; ++j) {
-        const int i = j * GRAD_THREADS + threadIdx.x;
-        if (i < whole) {
-            Unit<T> r;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if constexpr (sizeof(T) == 4) r.u.w[q] = __float_as_uint((float)((double)v[j].at(q) * factor));
-                else r.u.w[q] = pack_bf16x2((float)((double)v[j].at(2 * q) * factor), (float)((double)v[j].at(2 * q + 1) * factor));
-            }
-            *reinterpret_cast<decltype(r.u)*>(o + i * N) = r.u;
-        }
-    }
-    if (rest < c.left) Elem<T>::st(o + rest, (float)((double)tail * factor));
-}
-
+// The chunks that the norm read last are the first here: they are still in the memory-side cache.  a.partials: so many partial sums
+// are to be added up and their norm written down; 0: the norm is there.
 __global__ __launch_bounds__(GRAD_THREADS) void grad_scale_kernel(GradArgs a) {
-    const double norm = (double)*a.norm;
+    __shared__ double lds[GRAD_THREADS / 64];
+    Chunk c, next;
+    int back = blockIdx.x;
+    if (back < a.chunks) { c.find(a, a.chunks - 1 - back); c.load(); }
+    float norm;
+    if (a.partials > 0) {
+        norm = norm_of(a.partial, a.partials, lds);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
+    } else {
+        norm = *a.norm;
+    }
     // (NaN and infinity: nothing is scaled)
-    const double factor = norm > (double)a.most && norm < (double)__builtin_inff() ? (double)a.most / norm : 1.0;
-    for (int back = blockIdx.x; back < a.chunks; back += gridDim.x) {
-        const Chunk c = chunk_of(a, a.chunks - 1 - back);
-        if (factor == 1.0 && c.e.grad == c.e.out) continue;
-        if (c.e.bf16) chunk_scale<bf16_t>(c, factor); else chunk_scale<float>(c, factor);
+    const double factor = norm > a.most && norm < __builtin_inff() ? (double)a.most / (double)norm : 1.0;
+    while (back < a.chunks) {
+        back += gridDim.x;
+        if (back < a.chunks) { next.find(a, a.chunks - 1 - back); next.load(); }
+        if (factor != 1.0 || c.grad != c.out) c.store(factor);
+        c = next;
     }
 }
 
@@ -239,7 +250,7 @@ extern "C" moe_status moe_grad_bytes(const moe_grad_tensor* tensors, int32_t cou
     long long chunks;
     MOE_TRY(moe::grad_check(tensors, count, &chunks));
     if (!table || !scratch) return MOE_ERR_NULL;
-    *table = moe::grad_map_offset(count) + (size_t)chunks * 4;
+    *table = moe::grad_map_offset(count) + (size_t)chunks * 4 + 16;
     *scratch = (size_t)moe::grad_blocks(chunks) * 8;
     return MOE_OK;
 }
@@ -267,26 +278,46 @@ extern "C" moe_status moe_grad_table(const moe_grad_tensor* tensors, int32_t cou
             a.here = 0;
         }
     }
-    if (count == 0) {                                    // its head all the same
-        moe::grad_table_kernel<<<1, 256, 0, s>>>(a, (char*)table, count);
-        MOE_CHECK_LAUNCH();
-    }
     *list = l;
     moe::count_launch(moe::LC_OTHER);
     return MOE_OK;
 }
 
+namespace moe {
+namespace {
+
+// The partial sums, or (few chunks: a launch less) the norm itself, *partials = 0.
+constexpr int GRAD_ALONE = 4;
+moe_status grad_sums(const moe_grad_list* l, float* norm, void* scratch, hipStream_t s, GradArgs* a) {
+    const int blocks = grad_blocks(l->chunks);
+    *a = {(const char*)l->table, l->tensors, (int)l->chunks, 0, (double*)scratch, norm, 0.0f};
+    if (l->chunks <= GRAD_ALONE) {
+        grad_norm_kernel<true><<<1, GRAD_THREADS, 0, s>>>(*a);
+    } else {
+        grad_norm_kernel<false><<<blocks, GRAD_THREADS, 0, s>>>(*a);
+        a->partials = blocks;
+    }
+    MOE_CHECK_LAUNCH();
+    return MOE_OK;
+}
+
+}  // namespace
+}  // namespace moe
+
 extern "C" moe_status moe_grad_norm(const moe_grad_list* list, float* norm, void* scratch, void* stream) {
     MOE_TRY(moe::grad_list_check(list));
     if (!norm || !scratch) return MOE_ERR_NULL;
     if ((uintptr_t)scratch & 7) return MOE_ERR_UNSUPPORTED;
-    moe::GradArgs a = {(char*)list->table, list->tensors, (int)list->chunks, (double*)scratch, norm, 0.0f};
     hipStream_t s = (hipStream_t)stream;
     {
         moe::ProfScope prof(moe::PK_GRADS, s);
-        moe::grad_norm_kernel<<<moe::grad_blocks(list->chunks), moe::GRAD_THREADS, 0, s>>>(a);
+        moe::GradArgs a;
+        MOE_TRY(moe::grad_sums(list, norm, scratch, s, &a));
+        if (a.partials) {
+            moe::grad_join_kernel<<<1, moe::GRAD_THREADS, 0, s>>>(a);
+            MOE_CHECK_LAUNCH();
+        }
     }
-    MOE_CHECK_LAUNCH();
     moe::count_launch(moe::LC_OTHER);
     return MOE_OK;
 }
@@ -296,13 +327,13 @@ extern "C" moe_status moe_grad_scale(const moe_grad_list* list, float most, cons
     if (!(most >= 0.0f) || !std::isfinite(most)) return MOE_ERR_SHAPE;
     if (!norm || !list->outs) return MOE_ERR_NULL;
     if (list->chunks == 0) return MOE_OK;
-    moe::GradArgs a = {(char*)list->table, list->tensors, (int)list->chunks, nullptr, const_cast<float*>(norm), most};
+    moe::GradArgs a = {(const char*)list->table, list->tensors, (int)list->chunks, 0, nullptr, const_cast<float*>(norm), most};
     hipStream_t s = (hipStream_t)stream;
     {
         moe::ProfScope prof(moe::PK_GRADS, s);
         moe::grad_scale_kernel<<<moe::grad_blocks(list->chunks), moe::GRAD_THREADS, 0, s>>>(a);
+        MOE_CHECK_LAUNCH();
     }
-    MOE_CHECK_LAUNCH();
     moe::count_launch(moe::LC_OTHER);
     return MOE_OK;
 }
@@ -310,7 +341,19 @@ extern "C" moe_status moe_grad_scale(const moe_grad_list* list, float most, cons
 extern "C" moe_status moe_grad_clip(const moe_grad_list* list, float most, float* norm, void* scratch, void* stream) {
     MOE_TRY(moe::grad_list_check(list));
     if (!(most >= 0.0f) || !std::isfinite(most)) return MOE_ERR_SHAPE;
-    if (!list->outs) return MOE_ERR_NULL;
-    MOE_TRY(moe_grad_norm(list, norm, scratch, stream));
-    return moe_grad_scale(list, most, norm, stream);
+    if (!norm || !scratch || !list->outs) return MOE_ERR_NULL;
+    if ((uintptr_t)scratch & 7) return MOE_ERR_UNSUPPORTED;
+    hipStream_t s = (hipStream_t)stream;
+    {
+        moe::ProfScope prof(moe::PK_GRADS, s);
+        moe::GradArgs a;
+        MOE_TRY(moe::grad_sums(list, norm, scratch, s, &a));
+        if (list->chunks > 0) {
+            a.most = most;
+            moe::grad_scale_kernel<<<moe::grad_blocks(list->chunks), moe::GRAD_THREADS, 0, s>>>(a);
+            MOE_CHECK_LAUNCH();
+        }
+    }
+    moe::count_launch(moe::LC_OTHER, 2);
+    return MOE_OK;
 }

@@ -116,12 +116,20 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_linear_kernel(FewLinearArg
         else linear_finish<T>(a, t, n0 + n, v);
     });
 }
-template <typename T> __global__ __launch_bounds__(256) void few_linear_finish_kernel(FewLinearArgs a, int slices) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, size = (long long)a.T * a.N;
-    if (i >= size) return;
+template <typename T> __global__ __launch_bounds__(64) void few_linear_finish_kernel(FewLinearArgs a, int slices) {
+    const int t = blockIdx.y, n = blockIdx.x * 64 + threadIdx.x;
+    if (n >= a.N) return;
+    const long long size = (long long)a.T * a.N;
+    const float* p = a.partial + (long long)t * a.N + n;
     float v = 0.0f;
-    for (int s = 0; s < slices; ++s) v += a.partial[s * size + i];
-    linear_finish<T>(a, (int)(i / a.N), (int)(i % a.N), v);
+    for (int s0 = 0; s0 < slices; s0 += 16) {
+        float o[16];
+#pragma unroll
+        for (int s = 0; s < 16; ++s) o[s] = s0 + s < slices ? p[(s0 + s) * size] : 0.0f;
+#pragma unroll
+        for (int s = 0; s < 16; ++s) v += o[s];
+    }
+    linear_finish<T>(a, t, n, v);
 }
 
 template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a, hipStream_t s) {
@@ -136,7 +144,7 @@ template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a
     else if constexpr (sizeof(T) == 2) few_linear_kernel<T, 4><<<grid, FEW_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();
     if (slices > 1) {
-        few_linear_finish_kernel<T><<<up((long long)d.T * d.N, 256), 256, 0, s>>>(a, slices);
+        few_linear_finish_kernel<T><<<dim3(up(d.N, 64), d.T), 64, 0, s>>>(a, slices);
         MOE_CHECK_LAUNCH();
     }
     return MOE_OK;
