@@ -332,9 +332,6 @@ moe_status dispatch_bwd_rows(const Dims& d, int p0, int np, const void* dDI, lon
 moe_status assign_slots(const Dims& d, const int* topk_idx, const float* topk_w, int* slot, int* counts, float* slot_w,
                         int* rows, void* y, int* hist, hipStream_t s);
 
-// The router on logits that are there (router.hip): moe_router_fwd without its checks of pointers.
-moe_status router_run(const moe_router_config* cfg, const void* logits, const float* bias, int32_t* topk_idx, float* topk_w,
-                      int32_t* load, hipStream_t s);
-moe_status router_check(const moe_router_config* cfg);
+moe_status router_check(const moe_router_config* cfg);        // (router.hip)
 
 }  // namespace moe

@@ -10,6 +10,7 @@
 // the storage type but y.
 #include "common.h"
 #include "few_rows.h"
+#include "router_choose.h"
 #include "wide.h"
 
 namespace moe {
@@ -21,7 +22,10 @@ constexpr int FEW_WAVES = 8, FEW_THREADS = 64 * FEW_WAVES;
 
 struct FewArgs {
     const void* x; const void* Wg; const float* gate_bias; const void* W1; const void* W2; void* y;
-    float* logits; const int* idx; const float* w;
+    float* logits;
+    RouterArgs route;                        // where choices and weights go, among others
+    double* gate_part;                       // [gate_slices][T][E]
+    int gate_slices, gate_rows;              // slices of the rows of Wg, rows of each
     void* a;                                 // [T*k, H] float, or twice that in bfloat16, the upper parts first
     float* partial;                          // [slices][T*k][M]
     long long ldx, ldy;
@@ -29,10 +33,9 @@ struct FewArgs {
 };
 
 // ---- gate -------------------------------------------------------------------------------------------------
-// A workgroup has one or two tokens and 64 experts: a lane eight of them (fewer lanes to a row of Wg where there are fewer experts),
-// the lanes and wavefronts share out the rows of Wg.
-constexpr int GATE_TOKENS = 2, GATE_WAVES = 16;
-
+// TOKENS tokens' sums of x Wg over the rows [m0, m1), of 64 experts from e_first on, for each of WAVES wavefronts into `out`: a lane
+// has eight experts (there are fewer lanes to a row of Wg where there are fewer experts), and the lanes and wavefronts share out
+// the rows.  A lane's eight sums are dealt out to the lanes that have the same experts while they are added.
 template <typename T> __device__ __forceinline__ void load_eight(const T* p, int left, bool wide, float* o) {
     if (wide) {
         Raw8<T> r;
@@ -43,17 +46,14 @@ template <typename T> __device__ __forceinline__ void load_eight(const T* p, int
         for (int i = 0; i < 8; ++i) o[i] = i < left ? Elem<T>::ld(p + i) : 0.0f;
     }
 }
-
-template <typename T, int TOKENS>
-__global__ __launch_bounds__(GATE_WAVES * 64) void few_gate_kernel(FewArgs a) {
-    __shared__ double s_sum[GATE_WAVES][TOKENS][64];
+template <typename T, int TOKENS, int WAVES>
+__device__ __forceinline__ void gate_sums(const FewArgs& a, int t0, int e_first, int m0, int m1, double (&out)[WAVES][TOKENS][64]) {
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-    const int e_first = blockIdx.x * 64, experts = a.E - e_first < 64 ? a.E - e_first : 64;
+    const int experts = a.E - e_first < 64 ? a.E - e_first : 64;
     int chunks = 1;                                        // lanes to a row
     while (chunks * 8 < experts) chunks *= 2;
     const int chunk = lane & (chunks - 1), rows = 64 / chunks, e0 = e_first + chunk * 8, left = a.E - e0;
-    const bool wide = a.E % 8 == 0 && left >= 8;
-    const int t0 = blockIdx.y * TOKENS;
+    const bool wide = a.E % 8 == 0;
     double sum[TOKENS][8];
 #pragma unroll
     for (int t = 0; t < TOKENS; ++t)
@@ -62,13 +62,13 @@ __global__ __launch_bounds__(GATE_WAVES * 64) void few_gate_kernel(FewArgs a) {
     if (left > 0) {
         // so many rows of a lane are requested before the first is multiplied
         constexpr int AT_ONCE = 4;
-        const int step = GATE_WAVES * rows;
-        for (int m0 = wid * rows + lane / chunks; m0 < a.M; m0 += AT_ONCE * step) {
+        const int step = WAVES * rows;
+        for (int mm = m0 + wid * rows + lane / chunks; mm < m1; mm += AT_ONCE * step) {
             float w[AT_ONCE][8], x[AT_ONCE][TOKENS];
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                const int m = m0 + u * step;
-                if (m < a.M) {
+                const int m = mm + u * step;
+                if (m < m1) {
                     load_eight(reinterpret_cast<const T*>(a.Wg) + (long long)m * a.E + e0, left, wide, w[u]);
                 } else {
 #pragma unroll
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(GATE_WAVES * 64) void few_gate_kernel(FewArgs a) {
                 }
 #pragma unroll
                 for (int t = 0; t < TOKENS; ++t)
-                    x[u][t] = m < a.M && t0 + t < a.T ? Elem<T>::ld(reinterpret_cast<const T*>(a.x) + (t0 + t) * a.ldx + m) : 0.0f;
+                    x[u][t] = m < m1 && t0 + t < a.T ? Elem<T>::ld(reinterpret_cast<const T*>(a.x) + (t0 + t) * a.ldx + m) : 0.0f;
             }
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u)
@@ -88,25 +88,101 @@ __global__ __launch_bounds__(GATE_WAVES * 64) void few_gate_kernel(FewArgs a) {
                 }
         }
     }
-    for (int off = chunks; off < 64; off *= 2)
+    int mine = 0;                                          // which of the eight the lane ends up with
+#pragma unroll
+    for (int half = 4; half > 0; half >>= 1) {
+        const int off = chunks * (4 / half);
+        const bool up = (lane & off) != 0;
+        mine += up ? half : 0;
 #pragma unroll
         for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[t][i] += __shfl_xor(sum[t][i], off, 64);
-    if (lane < chunks) {
-#pragma unroll
-        for (int t = 0; t < TOKENS; ++t)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s_sum[wid][t][lane * 8 + i] = sum[t][i];
+            for (int i = 0; i < half; ++i) {
+                const double keep = up ? sum[t][half + i] : sum[t][i], give = up ? sum[t][i] : sum[t][half + i];
+                sum[t][i] = keep + __shfl_xor(give, off, 64);
+            }
     }
+    for (int off = chunks * 8; off < 64; off *= 2)
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) sum[t][0] += __shfl_xor(sum[t][0], off, 64);
+    if (lane < chunks * 8) {
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) out[wid][t][chunk * 8 + mine] = sum[t][0];
+    }
+}
+
+// By many workgroups: each has one or two tokens, 64 experts and a slice of the rows of Wg, whose sums it leaves in gate_part.
+constexpr int GATE_TOKENS = 2, GATE_WAVES = 8;
+template <typename T, int TOKENS>
+__global__ __launch_bounds__(GATE_WAVES * 64) void few_gate_kernel(FewArgs a) {
+    __shared__ double s_sum[GATE_WAVES][TOKENS][64];
+    const int e_first = blockIdx.x * 64, t0 = blockIdx.y * TOKENS, m0 = blockIdx.z * a.gate_rows;
+    gate_sums<T, TOKENS, GATE_WAVES>(a, t0, e_first, m0, m0 + a.gate_rows < a.M ? m0 + a.gate_rows : a.M, s_sum);
     __syncthreads();
     const int t = threadIdx.x / 64, e = threadIdx.x & 63;
-    if (t < TOKENS && t0 + t < a.T && e < experts) {
+    if (t < TOKENS && t0 + t < a.T && e_first + e < a.E) {
         double v = 0.0;
+#pragma unroll
         for (int q = 0; q < GATE_WAVES; ++q) v += s_sum[q][t][e];
-        if (a.gate_bias) v += (double)a.gate_bias[e_first + e];
-        a.logits[(long long)(t0 + t) * a.E + e_first + e] = (float)v;
+        a.gate_part[((long long)blockIdx.z * a.T + t0 + t) * a.E + e_first + e] = v;
     }
+}
+
+// ---- router -----------------------------------------------------------------------------------------------
+// A token's choices and weights by a wavefront whose lanes have its logits' sums, VALUES neighbouring experts each: lane j returns the
+// j-th in *weight and as its result.  `record`: logits, choices and weights are written down.
+template <int VALUES> __device__ __forceinline__ int route_token(const FewArgs& a, int t, const double* sum, bool record, float* weight) {
+    const int lane = threadIdx.x & 63, e0 = lane * VALUES;
+    float l[VALUES];
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        l[v] = -__builtin_inff();
+        if (e0 + v < a.E) {
+            l[v] = (float)(a.gate_bias ? sum[v] + (double)a.gate_bias[e0 + v] : sum[v]);
+            if (record) a.logits[(long long)t * a.E + e0 + v] = l[v];
+            if (l[v] != l[v]) l[v] = -__builtin_inff();
+        }
+    }
+    Softmax<double> soft = {0.0f, 0.0};
+    const int chosen = choose_exactly<VALUES>(a.route, l, &soft);
+    float z = -__builtin_inff();
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        const float o = __shfl(l[v], chosen < 0 ? 0 : chosen / VALUES, 64);
+        z = chosen >= 0 && chosen % VALUES == v ? o : z;
+    }
+    *weight = choice_weight(a.route, chosen, z, {soft.m, (float)soft.inv}) * a.route.scale;
+    if (record && lane < a.k) {
+        a.route.idx[t * a.k + lane] = chosen;
+        a.route.w[t * a.k + lane] = *weight;
+    }
+    return chosen;
+}
+// The sums of a lane's experts, from the gate's slices.
+template <int VALUES> __device__ __forceinline__ void gate_total(const FewArgs& a, int t, double* sum) {
+    const int e0 = (threadIdx.x & 63) * VALUES;
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) sum[v] = 0.0;
+    const double* p = a.gate_part + (long long)t * a.E + e0;
+    const long long step = (long long)a.T * a.E;
+    for (int s0 = 0; s0 < a.gate_slices; s0 += 4) {
+        double o[4][VALUES];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) o[s][v] = s0 + s < a.gate_slices && e0 + v < a.E ? p[(s0 + s) * step + v] : 0.0;
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) sum[v] += o[s][v];
+    }
+}
+// A wavefront to a token
+template <int VALUES> __global__ __launch_bounds__(64) void few_route_kernel(FewArgs a) {
+    double sum[VALUES];
+    float weight;
+    gate_total<VALUES>(a, blockIdx.x, sum);
+    route_token<VALUES>(a, blockIdx.x, sum, true, &weight);
 }
 
 // ---- which rows ---------------------------------------------------------------------------------------------
@@ -114,16 +190,53 @@ struct FewPlan {
     int idx[FEW_TOKENS * FEW_K];
     int rows[FEW_TOKENS];                    // assignments with the workgroup's expert, ascending
     unsigned there[FEW_E / 32];              // experts that are chosen
-    int expert, n_rows, n_experts;
+    int expert, n_rows;
 };
-// Fills `p` for the `slot`-th of the chosen experts (expert -1: there are fewer).  Every thread comes here.
+// Where the first product gets the choices from: they are there; or a workgroup routes for itself, which saves the launches between
+// it and the gate: from the gate's sums, or from x and Wg (one or two tokens).
+enum { FEW_ROUTED = 0, FEW_SUMMED = 1, FEW_ALONE = 2 };
+template <typename T, int MODE> __device__ __forceinline__ void few_choices(const FewArgs& a, bool record, FewPlan& p) {
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (MODE == FEW_ROUTED) {
+        for (int i = threadIdx.x; i < a.T * a.k; i += FEW_THREADS) p.idx[i] = a.route.idx[i];
+    } else {
+        __shared__ double s_sum[MODE == FEW_ALONE ? FEW_WAVES : 1][2][64];
+        if constexpr (MODE == FEW_ALONE) {
+            if (a.T == 1) gate_sums<T, 1, FEW_WAVES>(a, 0, 0, 0, a.M, reinterpret_cast<double (&)[FEW_WAVES][1][64]>(s_sum));
+            else gate_sums<T, 2, FEW_WAVES>(a, 0, 0, 0, a.M, s_sum);
+            __syncthreads();
+        }
+        for (int t = wid; t < a.T; t += FEW_WAVES) {
+            float weight;
+            int chosen;
+            if (a.E <= 64) {
+                double sum;
+                if constexpr (MODE == FEW_ALONE) {
+                    sum = 0.0;
+#pragma unroll
+                    for (int q = 0; q < FEW_WAVES; ++q) sum += a.T == 1 ? reinterpret_cast<double (&)[FEW_WAVES][1][64]>(s_sum)[q][0][lane] : s_sum[q][t][lane];
+                } else {
+                    gate_total<1>(a, t, &sum);
+                }
+                chosen = route_token<1>(a, t, &sum, record, &weight);
+            } else if constexpr (MODE == FEW_SUMMED) {
+                double sum[4];
+                gate_total<4>(a, t, sum);
+                chosen = route_token<4>(a, t, sum, record, &weight);
+            }
+            if (lane < a.k) p.idx[t * a.k + lane] = chosen;
+        }
+    }
+    __syncthreads();
+}
+
+// Fills `p`, whose choices are there, for the `slot`-th of the chosen experts (expert -1: there are fewer).  Every thread comes here.
 __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, FewPlan& p) {
     const int n = a.T * a.k, tid = threadIdx.x;
     if (tid < FEW_E / 32) p.there[tid] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += blockDim.x) {
-        const int e = a.idx[i];
-        p.idx[i] = e;
+    for (int i = tid; i < n; i += FEW_THREADS) {
+        const int e = p.idx[i];
         if (e >= 0) atomicOr(&p.there[e >> 5], 1u << (e & 31));
     }
     __syncthreads();
@@ -137,7 +250,6 @@ __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, FewPlan& p)
             const int o = __shfl_up(end, off, 64);
             if (tid >= off) end += o;
         }
-        const int all = __shfl(end, FEW_E / 32 - 1, 64);
         int expert = -1;
         if (tid < FEW_E / 32 && slot >= end - count && slot < end) {
             unsigned bits = mine;
@@ -155,7 +267,7 @@ __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, FewPlan& p)
                 rows += __popcll(b);
             }
         }
-        if (tid == 0) { p.expert = expert; p.n_rows = rows; p.n_experts = all; }
+        if (tid == 0) { p.expert = expert; p.n_rows = rows; }
     }
     __syncthreads();
 }
@@ -163,11 +275,12 @@ __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, FewPlan& p)
 __device__ __forceinline__ float gelu_of(float z) { return 0.5f * z * erfcf(-0.70710678118654752440f * z); }
 
 // ---- first product ----------------------------------------------------------------------------------------------
-template <typename T, int GROUPS>
+template <typename T, int GROUPS, int MODE>
 __global__ __launch_bounds__(FEW_THREADS) void few_first_kernel(FewArgs a) {
     __shared__ FewSums<T, FEW_WAVES> sums;
     __shared__ FewPlan plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * FEW_COLS;
+    few_choices<T, MODE>(a, blockIdx.x == 0 && blockIdx.y == 0, plan);
     few_plan(a, blockIdx.y, plan);
     if (plan.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS;
@@ -207,6 +320,7 @@ __global__ __launch_bounds__(FEW_THREADS) void few_second_kernel(FewArgs a) {
     __shared__ FewSums<T, FEW_WAVES> sums;
     __shared__ FewPlan plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * FEW_COLS;
+    few_choices<T, FEW_ROUTED>(a, false, plan);
     few_plan(a, blockIdx.y, plan);
     if (plan.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS, PARTS = sizeof(T) == 2 ? 2 : 1;
@@ -228,29 +342,39 @@ __global__ __launch_bounds__(FEW_THREADS) void few_second_kernel(FewArgs a) {
     }
 }
 
-// y[t] = sum over the choices of w times the sum of their slices; four columns to a thread, the slices' loads in eights
+// y[t] = sum over the choices of w times the sum of their slices; four columns to a thread.  Loads go out in eights, without a look at
+// whether there is a choice (nothing was written for one that is not).
 constexpr int JOIN_THREADS = 64;
 template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void few_join_kernel(FewArgs a) {
     const int t = blockIdx.y, n = (blockIdx.x * JOIN_THREADS + threadIdx.x) * 4;
     if (n >= a.M) return;
     const long long step = (long long)a.T * a.k * a.M;
-    float4 y = make_float4(0, 0, 0, 0);
-    for (int j = 0; j < a.k; ++j) {
-        const int at = t * a.k + j;
-        if (a.idx[at] < 0) continue;                      // (nothing was written for it)
-        const float w = a.w[at];
-        const float* p = a.partial + (long long)at * a.M + n;
-        float4 v = make_float4(0, 0, 0, 0);
-        for (int s0 = 0; s0 < a.slices; s0 += 8) {
-            float4 o[8];
+    const float* p = a.partial + (long long)t * a.k * a.M + n;
+    const int terms = a.k * a.slices;
+    float4 y = make_float4(0, 0, 0, 0), v = make_float4(0, 0, 0, 0);
+    for (int q0 = 0; q0 < terms; q0 += 8) {
+        float4 o[8];
+        float w[8];
+        int j[8], s[8];
+        bool there[8];
 #pragma unroll
-            for (int s = 0; s < 8; ++s)
-                if (s0 + s < a.slices) o[s] = *reinterpret_cast<const float4*>(p + (s0 + s) * step);
-#pragma unroll
-            for (int s = 0; s < 8; ++s)
-                if (s0 + s < a.slices) { v.x += o[s].x; v.y += o[s].y; v.z += o[s].z; v.w += o[s].w; }
+        for (int q = 0; q < 8; ++q) {
+            const int at = q0 + q < terms ? q0 + q : terms - 1;
+            j[q] = at / a.slices;
+            s[q] = at - j[q] * a.slices;
+            o[q] = *reinterpret_cast<const float4*>(p + s[q] * step + (long long)j[q] * a.M);
+            w[q] = a.route.w[t * a.k + j[q]];
+            there[q] = a.route.idx[t * a.k + j[q]] >= 0;
         }
-        y.x = fmaf(w, v.x, y.x); y.y = fmaf(w, v.y, y.y); y.z = fmaf(w, v.z, y.z); y.w = fmaf(w, v.w, y.w);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            if (q0 + q >= terms) break;
+            if (s[q] == 0) v = make_float4(0, 0, 0, 0);
+            v.x += o[q].x; v.y += o[q].y; v.z += o[q].z; v.w += o[q].w;
+            if (s[q] == a.slices - 1 && there[q]) {
+                y.x = fmaf(w[q], v.x, y.x); y.y = fmaf(w[q], v.y, y.y); y.z = fmaf(w[q], v.z, y.z); y.w = fmaf(w[q], v.w, y.w);
+            }
+        }
     }
     const float o[4] = {y.x, y.y, y.z, y.w};
     store_columns(reinterpret_cast<T*>(a.y) + t * a.ldy + n, o, 4);
@@ -259,7 +383,9 @@ template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void few_join_k
 struct FewDims {
     moe_router_config router;
     int slots, slices, steps;                // experts that may be chosen; of the second product
-    size_t a_bytes, partial_bytes;
+    int mode, exact_values, few_groups;
+    int gate_slices, gate_rows;
+    size_t a_bytes, partial_bytes, gate_bytes;
 };
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
@@ -283,27 +409,51 @@ moe_status few_dims(const moe_few_config* c, FewDims* d) {
     if (slices > most) slices = most;
     d->steps = up(steps, slices);
     d->slices = up(steps, d->steps);
+    // Who routes.  One or two tokens and a gate of up to 64 Ki elements: every workgroup of the first product by itself; up to 16 tokens:
+    // it does so from the gate's sums, which have a launch; more tokens: a launch of its own.
+    const int mean = up(n, c->E);
+    d->few_groups = up(mean + (mean > 1 ? up(mean, 2) : 0), bf16 ? Few<bf16_t>::ROWS : Few<float>::ROWS);
+    d->mode = c->T > 16 || c->E > 256 || d->few_groups > 1 ? FEW_ROUTED : c->T <= 2 && c->E <= 64 && (long long)c->M * c->E <= 65536 ? FEW_ALONE : FEW_SUMMED;
+    d->exact_values = d->mode != FEW_ROUTED && c->E > 64 ? 4 : c->E <= 64 ? 1 : c->E <= 128 ? 2 : c->E <= 256 ? 4 : 8;
+    // The gate's workgroups: enough for the chip, of 128 rows of Wg at least.
+    const int tiles = up(c->E, 64) * up(c->T > 0 ? c->T : 1, c->T == 1 ? 1 : GATE_TOKENS);
+    d->gate_slices = up(256, tiles);
+    if (d->gate_slices > 16) d->gate_slices = 16;
+    if (d->gate_slices > up(c->M, 128)) d->gate_slices = up(c->M, 128);
+    d->gate_rows = up(c->M, d->gate_slices);
+    d->gate_slices = up(c->M, d->gate_rows);
+    d->gate_bytes = align16((size_t)d->gate_slices * c->T * c->E * 8);
     d->a_bytes = align16((size_t)n * c->H * 4);
     d->partial_bytes = align16((size_t)n * c->M * d->slices * 4);
     return MOE_OK;
 }
 
-template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, hipStream_t s, const float* bias, int* idx, float* w) {
-    if (a.T == 1) few_gate_kernel<T, 1><<<dim3(up(a.E, 64), 1), GATE_WAVES * 64, 0, s>>>(a);
-    else few_gate_kernel<T, GATE_TOKENS><<<dim3(up(a.E, 64), up(a.T, GATE_TOKENS)), GATE_WAVES * 64, 0, s>>>(a);
-    MOE_CHECK_LAUNCH();
-    MOE_TRY(router_run(&d.router, a.logits, bias, idx, w, nullptr, s));
+template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, hipStream_t s) {
+    if (d.mode != FEW_ALONE) {
+        const dim3 grid(up(a.E, 64), up(a.T, a.T == 1 ? 1 : GATE_TOKENS), a.gate_slices);
+        if (a.T == 1) few_gate_kernel<T, 1><<<grid, GATE_WAVES * 64, 0, s>>>(a);
+        else few_gate_kernel<T, GATE_TOKENS><<<grid, GATE_WAVES * 64, 0, s>>>(a);
+        MOE_CHECK_LAUNCH();
+    }
+    if (d.mode == FEW_ROUTED) {
+        if (d.exact_values == 1) few_route_kernel<1><<<a.T, 64, 0, s>>>(a);
+        else if (d.exact_values == 2) few_route_kernel<2><<<a.T, 64, 0, s>>>(a);
+        else if (d.exact_values == 4) few_route_kernel<4><<<a.T, 64, 0, s>>>(a);
+        else few_route_kernel<8><<<a.T, 64, 0, s>>>(a);
+        MOE_CHECK_LAUNCH();
+    }
     // Groups of rows that go through together: as many as an expert is expected to have, and some more.
-    const int mean = up((long long)a.T * a.k, a.E), groups = up(mean + (mean > 1 ? up(mean, 2) : 0), Few<T>::ROWS);
     const dim3 first(up(a.H, FEW_COLS), d.slots), second(up(a.M, FEW_COLS), d.slots, a.slices);
-    if (groups <= 1) {
-        few_first_kernel<T, 1><<<first, FEW_THREADS, 0, s>>>(a);
+    if (d.few_groups <= 1) {
+        if (d.mode == FEW_ALONE) few_first_kernel<T, 1, FEW_ALONE><<<first, FEW_THREADS, 0, s>>>(a);
+        else if (d.mode == FEW_SUMMED) few_first_kernel<T, 1, FEW_SUMMED><<<first, FEW_THREADS, 0, s>>>(a);
+        else few_first_kernel<T, 1, FEW_ROUTED><<<first, FEW_THREADS, 0, s>>>(a);
         few_second_kernel<T, 1><<<second, FEW_THREADS, 0, s>>>(a);
-    } else if (groups <= 2) {
-        few_first_kernel<T, 2><<<first, FEW_THREADS, 0, s>>>(a);
+    } else if (d.few_groups <= 2) {
+        few_first_kernel<T, 2, FEW_ROUTED><<<first, FEW_THREADS, 0, s>>>(a);
         few_second_kernel<T, 2><<<second, FEW_THREADS, 0, s>>>(a);
     } else {
-        few_first_kernel<T, 4><<<first, FEW_THREADS, 0, s>>>(a);
+        few_first_kernel<T, 4, FEW_ROUTED><<<first, FEW_THREADS, 0, s>>>(a);
         few_second_kernel<T, 4><<<second, FEW_THREADS, 0, s>>>(a);
     }
     MOE_CHECK_LAUNCH();
@@ -322,7 +472,7 @@ extern "C" moe_status moe_few_scratch_bytes(const moe_few_config* cfg, size_t* b
     moe::FewDims d;
     MOE_TRY(moe::few_dims(cfg, &d));
     if (!bytes) return MOE_ERR_NULL;
-    *bytes = cfg->T == 0 ? 0 : d.a_bytes + d.partial_bytes;
+    *bytes = cfg->T == 0 ? 0 : d.a_bytes + d.partial_bytes + d.gate_bytes;
     return MOE_OK;
 }
 
@@ -335,14 +485,15 @@ extern "C" moe_status moe_few_forward(const moe_few_config* cfg, const void* x, 
     if (!x || !Wg || !W1 || !W2 || !y || !logits || !topk_idx || !topk_w || !scratch) return MOE_ERR_NULL;
     if (!moe::aligned16(x) || !moe::aligned16(Wg) || !moe::aligned16(W1) || !moe::aligned16(W2) || !moe::aligned16(scratch)) return MOE_ERR_UNSUPPORTED;
     char* p = (char*)scratch;
-    moe::FewArgs a = {x, Wg, gate_bias, W1, W2, y, logits, topk_idx, topk_w, p, (float*)(p + d.a_bytes),
+    moe::FewArgs a = {x, Wg, gate_bias, W1, W2, y, logits,
+                      moe::router_args(&d.router, logits, bias, topk_idx, topk_w, nullptr, d.exact_values, d.exact_values),
+                      (double*)(p + d.a_bytes + d.partial_bytes), d.gate_slices, d.gate_rows, p, (float*)(p + d.a_bytes),
                       cfg->ldx ? (long long)cfg->ldx : cfg->M, cfg->ldy ? (long long)cfg->ldy : cfg->M,
                       cfg->T, cfg->M, cfg->H, cfg->E, cfg->k, d.slices, d.steps};
     hipStream_t s = (hipStream_t)stream;
     {
         moe::ProfScope prof(moe::PK_FEW, s);
-        MOE_TRY(cfg->dtype == MOE_BF16 ? moe::few_launch<moe::bf16_t>(a, d, s, bias, topk_idx, topk_w)
-                                       : moe::few_launch<float>(a, d, s, bias, topk_idx, topk_w));
+        MOE_TRY(cfg->dtype == MOE_BF16 ? moe::few_launch<moe::bf16_t>(a, d, s) : moe::few_launch<float>(a, d, s));
     }
     moe::count_launch(moe::LC_GEMM, 2);
     moe::count_launch(moe::LC_OTHER);

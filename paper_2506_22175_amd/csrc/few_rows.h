@@ -43,11 +43,13 @@ template <> struct Few<float> {
 template <typename T, int GROUPS, int PARTS> struct FewStep;
 template <int GROUPS, int PARTS> struct FewStep<bf16_t, GROUPS, PARTS> {
     uint4 w[8], r[GROUPS][PARTS];
-    __device__ __forceinline__ void load(const bf16_t* W, long long ldw, const bf16_t* const (&row)[GROUPS], long long part, int k, int K) {
-        const int at = k < K ? k : 0;
-        const bf16_t* p = W + (long long)at * ldw;
+    __device__ __forceinline__ void load(const bf16_t* W, long long ldw, int k, int K) {
+        const bf16_t* p = W + (long long)(k < K ? k : 0) * ldw;
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const uint4*>(p + j * ldw);
+    }
+    __device__ __forceinline__ void load_rows(const bf16_t* const (&row)[GROUPS], long long part, int k, int K) {
+        const int at = k < K ? k : 0;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
@@ -82,11 +84,13 @@ template <int GROUPS, int PARTS> struct FewStep<bf16_t, GROUPS, PARTS> {
 template <int GROUPS, int PARTS> struct FewStep<float, GROUPS, PARTS> {
     static_assert(PARTS == 1, "a float is one part");
     float4 w[8], r[GROUPS][2];
-    __device__ __forceinline__ void load(const float* W, long long ldw, const float* const (&row)[GROUPS], long long, int k, int K) {
-        const int at = k < K ? k : 0;
-        const float* p = W + (long long)at * ldw;
+    __device__ __forceinline__ void load(const float* W, long long ldw, int k, int K) {
+        const float* p = W + (long long)(k < K ? k : 0) * ldw;
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const float4*>(p + j * ldw);
+    }
+    __device__ __forceinline__ void load_rows(const float* const (&row)[GROUPS], long long, int k, int K) {
+        const int at = k < K ? k : 0;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
             r[g][0] = *reinterpret_cast<const float4*>(row[g] + at);
@@ -129,12 +133,22 @@ __device__ __forceinline__ void few_sums(const T* W, long long ldw, int cols, co
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
         for (int i = 0; i < Few<T>::ACCS; ++i) acc[g][i] = few_acc{0, 0, 0, 0};
+    // The next step's loads are under way while one is multiplied; of eight fragments of rows (which come from the caches) there are no
+    // registers to hold two steps'.
+    constexpr bool EARLY = GROUPS * PARTS < 8;
     FewStep<T, GROUPS, PARTS> a, b;
     int s = __builtin_amdgcn_readfirstlane(first);
-    if (s < steps) a.load(W, ldw, row, part, s * Few<T>::STEP + k0, K);
+    if (s < steps) {
+        a.load(W, ldw, s * Few<T>::STEP + k0, K);
+        if (EARLY) a.load_rows(row, part, s * Few<T>::STEP + k0, K);
+    }
     while (s < steps) {
         const int next = s + WAVES;
-        if (next < steps) b.load(W, ldw, row, part, next * Few<T>::STEP + k0, K);
+        if (!EARLY) a.load_rows(row, part, s * Few<T>::STEP + k0, K);
+        if (next < steps) {
+            b.load(W, ldw, next * Few<T>::STEP + k0, K);
+            if (EARLY) b.load_rows(row, part, next * Few<T>::STEP + k0, K);
+        }
         if ((s + 1) * Few<T>::STEP > K && s * Few<T>::STEP + k0 >= K) a.zero();        // (nothing meets what was loaded in its place)
         a.multiply(acc);
         s = next;

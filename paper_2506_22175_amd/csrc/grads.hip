@@ -141,8 +141,7 @@ __device__ __forceinline__ float norm_of(const double* partial, int n, double* l
     return (float)sqrt(block_sum(sum, lds));
 }
 
-// ALONE: the only workgroup, which writes the norm itself
-template <bool ALONE> __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(GradArgs a) {
+__global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(GradArgs a) {
     __shared__ double lds[GRAD_THREADS / 64];
     double sum = 0.0;
     Chunk c, next;
@@ -155,9 +154,30 @@ template <bool ALONE> __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_
         c = next;
     }
     sum = block_sum(sum, lds);
-    if (threadIdx.x == 0) {
-        if (ALONE) *a.norm = (float)sqrt(sum); else a.partial[blockIdx.x] = sum;
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = sum;
+}
+// Few chunks: one workgroup, four of them at a time, and no second launch.  (Chunk takes its thread's number from threadIdx.x, which
+// counts the threads of a chunk here; y counts the chunks.)
+constexpr int GRAD_ALONE = 16, GRAD_AT_ONCE = 4;
+__global__ __launch_bounds__(GRAD_THREADS * GRAD_AT_ONCE) void grad_norm_alone_kernel(GradArgs a) {
+    __shared__ double lds[GRAD_AT_ONCE][GRAD_THREADS];
+    const int tid = threadIdx.x, q = threadIdx.y;
+    double sum = 0.0;
+    for (int number = q; number < a.chunks; number += GRAD_AT_ONCE) {
+        Chunk c;
+        c.find(a, number);
+        c.load();
+        sum += c.squares();
     }
+    lds[q][tid] = sum;
+    __syncthreads();
+    sum = (lds[0][tid] + lds[1][tid]) + (lds[2][tid] + lds[3][tid]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    __shared__ double waves[GRAD_THREADS / 64];
+    if (q == 0 && (tid & 63) == 0) waves[tid >> 6] = sum;
+    __syncthreads();
+    if (q == 0 && tid == 0) *a.norm = (float)sqrt((waves[0] + waves[1]) + (waves[2] + waves[3]));
 }
 __global__ __launch_bounds__(GRAD_THREADS) void grad_join_kernel(GradArgs a) {
     __shared__ double lds[GRAD_THREADS / 64];
@@ -287,14 +307,13 @@ namespace moe {
 namespace {
 
 // The partial sums, or (few chunks: a launch less) the norm itself, *partials = 0.
-constexpr int GRAD_ALONE = 4;
 moe_status grad_sums(const moe_grad_list* l, float* norm, void* scratch, hipStream_t s, GradArgs* a) {
     const int blocks = grad_blocks(l->chunks);
     *a = {(const char*)l->table, l->tensors, (int)l->chunks, 0, (double*)scratch, norm, 0.0f};
     if (l->chunks <= GRAD_ALONE) {
-        grad_norm_kernel<true><<<1, GRAD_THREADS, 0, s>>>(*a);
+        grad_norm_alone_kernel<<<1, dim3(GRAD_THREADS, GRAD_AT_ONCE), 0, s>>>(*a);
     } else {
-        grad_norm_kernel<false><<<blocks, GRAD_THREADS, 0, s>>>(*a);
+        grad_norm_kernel<<<blocks, GRAD_THREADS, 0, s>>>(*a);
         a->partials = blocks;
     }
     MOE_CHECK_LAUNCH();
