@@ -4,7 +4,7 @@
 //   a[t,j] = gelu(x[t] W1[e]),  y[t] = sum over j of w[t,j] a[t,j] W2[e],  e = topk_idx[t,j]
 //
 // What has to move are the chosen experts' weights, 2 M H elements each, once.  Both products go through few_rows.h: a
-// workgroup has 64 columns of one expert and all of the rows that chose it.  The logits are sums in 64 bits, rounded to float:
+// workgroup has 128 columns (float: 64) of one expert and all of the rows that chose it.  The logits are sums in 64 bits, rounded to float:
 // which expert is chosen hangs on their last bits.  The rows between the products are kept in float, or as two bfloat16 that add up
 // to 16 bits of mantissa, which costs the matrix pipe a second instruction where it waits for memory anyway: nothing is rounded to
 // the storage type but y.
@@ -18,7 +18,7 @@ namespace moe {
 namespace {
 
 constexpr int FEW_TOKENS = 256, FEW_K = 16, FEW_E = 512;
-constexpr int FEW_WAVES = 8, FEW_THREADS = 64 * FEW_WAVES;
+constexpr int FEW_WAVES = 8;
 
 struct FewArgs {
     const void* x; const void* Wg; const float* gate_bias; const void* W1; const void* W2; void* y;
@@ -61,7 +61,7 @@ __device__ __forceinline__ void gate_sums(const FewArgs& a, int t0, int e_first,
         for (int i = 0; i < 8; ++i) sum[t][i] = 0.0;
     if (left > 0) {
         // so many rows of a lane are requested before the first is multiplied
-        constexpr int AT_ONCE = 4;
+        constexpr int AT_ONCE = TOKENS == 1 && sizeof(T) == 2 ? 8 : 4;
         const int step = WAVES * rows;
         for (int mm = m0 + wid * rows + lane / chunks; mm < m1; mm += AT_ONCE * step) {
             float w[AT_ONCE][8], x[AT_ONCE][TOKENS];
@@ -143,7 +143,7 @@ template <int VALUES> __device__ __forceinline__ int route_token(const FewArgs& 
             if (l[v] != l[v]) l[v] = -__builtin_inff();
         }
     }
-    Softmax<double> soft = {0.0f, 0.0};
+    Softmax<float> soft = {0.0f, 0.0f};
     const int chosen = choose_exactly<VALUES>(a.route, l, &soft);
     float z = -__builtin_inff();
 #pragma unroll
@@ -151,7 +151,7 @@ template <int VALUES> __device__ __forceinline__ int route_token(const FewArgs& 
         const float o = __shfl(l[v], chosen < 0 ? 0 : chosen / VALUES, 64);
         z = chosen >= 0 && chosen % VALUES == v ? o : z;
     }
-    *weight = choice_weight(a.route, chosen, z, {soft.m, (float)soft.inv}) * a.route.scale;
+    *weight = choice_weight(a.route, chosen, z, soft) * a.route.scale;
     if (record && lane < a.k) {
         a.route.idx[t * a.k + lane] = chosen;
         a.route.w[t * a.k + lane] = *weight;
@@ -187,26 +187,30 @@ template <int VALUES> __global__ __launch_bounds__(64) void few_route_kernel(Few
 
 // ---- which rows ---------------------------------------------------------------------------------------------
 struct FewPlan {
-    int idx[FEW_TOKENS * FEW_K];
     int rows[FEW_TOKENS];                    // assignments with the workgroup's expert, ascending
     unsigned there[FEW_E / 32];              // experts that are chosen
     int expert, n_rows;
 };
+// What a workgroup has in LDS: the choices, which only the plan looks at, then the sums.
+template <typename T, int WAVES> struct FewLds {
+    FewPlan plan;
+    union { int idx[FEW_TOKENS * FEW_K]; FewSums<T, WAVES> sums; };
+};
 // Where the first product gets the choices from: they are there; or a workgroup routes for itself, which saves the launches between
 // it and the gate: from the gate's sums, or from x and Wg (one or two tokens).
 enum { FEW_ROUTED = 0, FEW_SUMMED = 1, FEW_ALONE = 2 };
-template <typename T, int MODE> __device__ __forceinline__ void few_choices(const FewArgs& a, bool record, FewPlan& p) {
+template <typename T, int MODE, int WAVES> __device__ __forceinline__ void few_choices(const FewArgs& a, bool record, int* idx) {
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if constexpr (MODE == FEW_ROUTED) {
-        for (int i = threadIdx.x; i < a.T * a.k; i += FEW_THREADS) p.idx[i] = a.route.idx[i];
+        for (int i = threadIdx.x; i < a.T * a.k; i += WAVES * 64) idx[i] = a.route.idx[i];
     } else {
-        __shared__ double s_sum[MODE == FEW_ALONE ? FEW_WAVES : 1][2][64];
+        __shared__ double s_sum[MODE == FEW_ALONE ? WAVES : 1][2][64];
         if constexpr (MODE == FEW_ALONE) {
-            if (a.T == 1) gate_sums<T, 1, FEW_WAVES>(a, 0, 0, 0, a.M, reinterpret_cast<double (&)[FEW_WAVES][1][64]>(s_sum));
-            else gate_sums<T, 2, FEW_WAVES>(a, 0, 0, 0, a.M, s_sum);
+            if (a.T == 1) gate_sums<T, 1, WAVES>(a, 0, 0, 0, a.M, reinterpret_cast<double (&)[WAVES][1][64]>(s_sum));
+            else gate_sums<T, 2, WAVES>(a, 0, 0, 0, a.M, s_sum);
             __syncthreads();
         }
-        for (int t = wid; t < a.T; t += FEW_WAVES) {
+        for (int t = wid; t < a.T; t += WAVES) {
             float weight;
             int chosen;
             if (a.E <= 64) {
@@ -214,7 +218,7 @@ template <typename T, int MODE> __device__ __forceinline__ void few_choices(cons
                 if constexpr (MODE == FEW_ALONE) {
                     sum = 0.0;
 #pragma unroll
-                    for (int q = 0; q < FEW_WAVES; ++q) sum += a.T == 1 ? reinterpret_cast<double (&)[FEW_WAVES][1][64]>(s_sum)[q][0][lane] : s_sum[q][t][lane];
+                    for (int q = 0; q < WAVES; ++q) sum += a.T == 1 ? reinterpret_cast<double (&)[WAVES][1][64]>(s_sum)[q][0][lane] : s_sum[q][t][lane];
                 } else {
                     gate_total<1>(a, t, &sum);
                 }
@@ -224,19 +228,19 @@ template <typename T, int MODE> __device__ __forceinline__ void few_choices(cons
                 gate_total<4>(a, t, sum);
                 chosen = route_token<4>(a, t, sum, record, &weight);
             }
-            if (lane < a.k) p.idx[t * a.k + lane] = chosen;
+            if (lane < a.k) idx[t * a.k + lane] = chosen;
         }
     }
     __syncthreads();
 }
 
-// Fills `p`, whose choices are there, for the `slot`-th of the chosen experts (expert -1: there are fewer).  Every thread comes here.
-__device__ __forceinline__ void few_plan(const FewArgs& a, int slot, FewPlan& p) {
+// Fills `p` from the choices in LDS for the `slot`-th of the chosen experts (expert -1: there are fewer).  Every thread comes here.
+__device__ __forceinline__ void few_plan(const FewArgs& a, int slot, const int* idx, FewPlan& p) {
     const int n = a.T * a.k, tid = threadIdx.x;
     if (tid < FEW_E / 32) p.there[tid] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += FEW_THREADS) {
-        const int e = p.idx[i];
+    for (int i = tid; i < n; i += blockDim.x) {
+        const int e = idx[i];
         if (e >= 0) atomicOr(&p.there[e >> 5], 1u << (e & 31));
     }
     __syncthreads();
@@ -261,7 +265,7 @@ __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, FewPlan& p)
         int rows = 0;
         if (expert >= 0) {
             for (int base = 0; base < n; base += 64) {
-                const bool is = base + tid < n && p.idx[base + tid] == expert;
+                const bool is = base + tid < n && idx[base + tid] == expert;
                 const unsigned long long b = __ballot(is);
                 if (is) p.rows[rows + __popcll(b & ((1ull << tid) - 1))] = base + tid;
                 rows += __popcll(b);
@@ -275,16 +279,17 @@ __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, FewPlan& p)
 __device__ __forceinline__ float gelu_of(float z) { return 0.5f * z * erfcf(-0.70710678118654752440f * z); }
 
 // ---- first product ----------------------------------------------------------------------------------------------
-template <typename T, int GROUPS, int MODE>
-__global__ __launch_bounds__(FEW_THREADS) void few_first_kernel(FewArgs a) {
-    __shared__ FewSums<T, FEW_WAVES> sums;
-    __shared__ FewPlan plan;
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * FEW_COLS;
-    few_choices<T, MODE>(a, blockIdx.x == 0 && blockIdx.y == 0, plan);
-    few_plan(a, blockIdx.y, plan);
-    if (plan.expert < 0) return;
+template <typename T, int GROUPS, int MODE, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, GROUPS > 1 ? 2 : 4) void few_first_kernel(FewArgs a) {
+    __shared__ FewLds<T, WAVES> lds;
+    const FewPlan& plan = lds.plan;
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
+    few_choices<T, MODE, WAVES>(a, blockIdx.x == 0 && blockIdx.y == 0, lds.idx);
+    few_plan(a, blockIdx.y, lds.idx, lds.plan);
+    const int expert = __builtin_amdgcn_readfirstlane(plan.expert);
+    if (expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS;
-    const T* W = reinterpret_cast<const T*>(a.W1) + (long long)plan.expert * a.M * a.H + n0;
+    const T* W = reinterpret_cast<const T*>(a.W1) + (long long)expert * a.M * a.H + n0;
     const long long size = (long long)a.T * a.k * a.H;
     for (int r0 = 0; r0 < plan.n_rows; r0 += GROUPS * ROWS) {
         const T* row[GROUPS];
@@ -294,8 +299,8 @@ __global__ __launch_bounds__(FEW_THREADS) void few_first_kernel(FewArgs a) {
             row[g] = reinterpret_cast<const T*>(a.x) + plan.rows[r < plan.n_rows ? r : r0] / a.k * a.ldx;
         }
         few_acc acc[GROUPS][Few<T>::ACCS];
-        few_sums<T, GROUPS, 1, FEW_WAVES>(W, a.H, a.H - n0, row, 0, a.M, wid, (a.M + Few<T>::STEP - 1) / Few<T>::STEP, acc);
-        few_finish<T, GROUPS, FEW_WAVES>(sums, acc, plan.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
+        few_sums<T, GROUPS, 1, WAVES>(W, a.H, a.H - n0, row, 0, a.M, wid, (a.M + Few<T>::STEP - 1) / Few<T>::STEP, acc);
+        few_finish<T, GROUPS, WAVES>(lds.sums, acc, plan.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
             const float v = gelu_of(z);
             const long long at = (long long)plan.rows[r0 + r] * a.H + n0 + n;
             if constexpr (sizeof(T) == 4) {
@@ -312,19 +317,20 @@ __global__ __launch_bounds__(FEW_THREADS) void few_first_kernel(FewArgs a) {
 }
 
 // ---- second product ----------------------------------------------------------------------------------------------
-// A workgroup has 64 columns of an expert and a slice of H.  It leaves its rows' sums, which few_join_kernel adds up: a launch of its
+// A workgroup has 128 columns (float: 64) of an expert and a slice of H.  It leaves its rows' sums, which few_join_kernel adds up: a launch of its
 // own, since making sums visible from one workgroup to another of the same launch empties the caches of eight dies (the last
 // workgroup of a column block to finish, adding them up: 89 us for what takes 14 without).
 template <typename T, int GROUPS>
-__global__ __launch_bounds__(FEW_THREADS) void few_second_kernel(FewArgs a) {
-    __shared__ FewSums<T, FEW_WAVES> sums;
-    __shared__ FewPlan plan;
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * FEW_COLS;
-    few_choices<T, FEW_ROUTED>(a, false, plan);
-    few_plan(a, blockIdx.y, plan);
-    if (plan.expert < 0) return;
+__global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 1 ? 2 : 4) void few_second_kernel(FewArgs a) {
+    __shared__ FewLds<T, FEW_WAVES> lds;
+    const FewPlan& plan = lds.plan;
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
+    few_choices<T, FEW_ROUTED, FEW_WAVES>(a, false, lds.idx);
+    few_plan(a, blockIdx.y, lds.idx, lds.plan);
+    const int expert = __builtin_amdgcn_readfirstlane(plan.expert);
+    if (expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS, PARTS = sizeof(T) == 2 ? 2 : 1;
-    const T* W = reinterpret_cast<const T*>(a.W2) + (long long)plan.expert * a.H * a.M + n0;
+    const T* W = reinterpret_cast<const T*>(a.W2) + (long long)expert * a.H * a.M + n0;
     const int all = (a.H + Few<T>::STEP - 1) / Few<T>::STEP, begin = blockIdx.z * a.steps, end = begin + a.steps < all ? begin + a.steps : all;
     const long long size = (long long)a.T * a.k * a.H;
     float* partial = a.partial + (long long)blockIdx.z * a.T * a.k * a.M;
@@ -337,7 +343,7 @@ __global__ __launch_bounds__(FEW_THREADS) void few_second_kernel(FewArgs a) {
         }
         few_acc acc[GROUPS][Few<T>::ACCS];
         few_sums<T, GROUPS, PARTS, FEW_WAVES>(W, a.M, a.M - n0, row, size, a.H, begin + wid, end, acc);
-        few_finish<T, GROUPS, FEW_WAVES>(sums, acc, plan.n_rows - r0, a.M - n0,
+        few_finish<T, GROUPS, FEW_WAVES>(lds.sums, acc, plan.n_rows - r0, a.M - n0,
                                          [&](int r, int n, float v) { partial[(long long)plan.rows[r0 + r] * a.M + n0 + n] = v; });
     }
 }
@@ -398,12 +404,12 @@ moe_status few_dims(const moe_few_config* c, FewDims* d) {
     if ((c->ldx && c->ldx < c->M) || (c->ldy && c->ldy < c->M)) return MOE_ERR_SHAPE;
     if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_UNSUPPORTED;
     if (c->T > FEW_TOKENS || c->M % 8 || c->H % 8 || c->ldx % 8) return MOE_ERR_UNSUPPORTED;
-    if (c->M > (1 << 20) || c->H > (1 << 20)) return MOE_ERR_UNSUPPORTED;
+    if ((long long)c->M * c->H > (1 << 30)) return MOE_ERR_UNSUPPORTED;
     const bool bf16 = c->dtype == MOE_BF16;
     const long long n = (long long)c->T * c->k;
     d->slots = (int)(n < c->E ? n : c->E);
     if (d->slots < 1) d->slots = 1;
-    const int step = bf16 ? 64 : 32, steps = up(c->H, step), blocks = up(c->M, FEW_COLS) * d->slots;
+    const int cols = bf16 ? Few<bf16_t>::COLS : Few<float>::COLS, steps = up(c->H, Few<float>::STEP), blocks = up(c->M, cols) * d->slots;
     int slices = blocks < 512 ? up(512, blocks) : 1;
     const int most = up(steps, FEW_WAVES);
     if (slices > most) slices = most;
@@ -412,7 +418,7 @@ moe_status few_dims(const moe_few_config* c, FewDims* d) {
     // Who routes.  One or two tokens and a gate of up to 64 Ki elements: every workgroup of the first product by itself; up to 16 tokens:
     // it does so from the gate's sums, which have a launch; more tokens: a launch of its own.
     const int mean = up(n, c->E);
-    d->few_groups = up(mean + (mean > 1 ? up(mean, 2) : 0), bf16 ? Few<bf16_t>::ROWS : Few<float>::ROWS);
+    d->few_groups = up(mean + (mean > 1 ? up(mean, 2) : 0), Few<float>::ROWS);
     d->mode = c->T > 16 || c->E > 256 || d->few_groups > 1 ? FEW_ROUTED : c->T <= 2 && c->E <= 64 && (long long)c->M * c->E <= 65536 ? FEW_ALONE : FEW_SUMMED;
     d->exact_values = d->mode != FEW_ROUTED && c->E > 64 ? 4 : c->E <= 64 ? 1 : c->E <= 128 ? 2 : c->E <= 256 ? 4 : 8;
     // The gate's workgroups: enough for the chip, of 128 rows of Wg at least.
@@ -442,20 +448,27 @@ template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, 
         else few_route_kernel<8><<<a.T, 64, 0, s>>>(a);
         MOE_CHECK_LAUNCH();
     }
-    // Groups of rows that go through together: as many as an expert is expected to have, and some more.
-    const dim3 first(up(a.H, FEW_COLS), d.slots), second(up(a.M, FEW_COLS), d.slots, a.slices);
+    // Groups of rows that go through together: as many as an expert is expected to have, and some more.  Where the first product has few
+    // workgroups, they have 16 wavefronts.
+    const dim3 first(up(a.H, Few<T>::COLS), d.slots), second(up(a.M, Few<T>::COLS), d.slots, a.slices);
+    const bool wide = first.x * first.y <= 256;
+#define FEW_FIRST(G, MODE) do { if (wide) few_first_kernel<T, G, MODE, 16><<<first, 1024, 0, s>>>(a); \
+        else few_first_kernel<T, G, MODE, FEW_WAVES><<<first, FEW_WAVES * 64, 0, s>>>(a); } while (0)
+#define FEW_SECOND(G) few_second_kernel<T, G><<<second, FEW_WAVES * 64, 0, s>>>(a)
     if (d.few_groups <= 1) {
-        if (d.mode == FEW_ALONE) few_first_kernel<T, 1, FEW_ALONE><<<first, FEW_THREADS, 0, s>>>(a);
-        else if (d.mode == FEW_SUMMED) few_first_kernel<T, 1, FEW_SUMMED><<<first, FEW_THREADS, 0, s>>>(a);
-        else few_first_kernel<T, 1, FEW_ROUTED><<<first, FEW_THREADS, 0, s>>>(a);
-        few_second_kernel<T, 1><<<second, FEW_THREADS, 0, s>>>(a);
+        if (d.mode == FEW_ALONE) FEW_FIRST(1, FEW_ALONE);
+        else if (d.mode == FEW_SUMMED) FEW_FIRST(1, FEW_SUMMED);
+        else FEW_FIRST(1, FEW_ROUTED);
+        FEW_SECOND(1);
     } else if (d.few_groups <= 2) {
-        few_first_kernel<T, 2, FEW_ROUTED><<<first, FEW_THREADS, 0, s>>>(a);
-        few_second_kernel<T, 2><<<second, FEW_THREADS, 0, s>>>(a);
+        few_first_kernel<T, 2, FEW_ROUTED, FEW_WAVES><<<first, FEW_WAVES * 64, 0, s>>>(a);
+        FEW_SECOND(2);
     } else {
-        few_first_kernel<T, 4, FEW_ROUTED><<<first, FEW_THREADS, 0, s>>>(a);
-        few_second_kernel<T, 4><<<second, FEW_THREADS, 0, s>>>(a);
+        few_first_kernel<T, 4, FEW_ROUTED, FEW_WAVES><<<first, FEW_WAVES * 64, 0, s>>>(a);
+        FEW_SECOND(4);
     }
+#undef FEW_FIRST
+#undef FEW_SECOND
     MOE_CHECK_LAUNCH();
     few_join_kernel<T><<<dim3(up(a.M, 4 * JOIN_THREADS), a.T), JOIN_THREADS, 0, s>>>(a);
     MOE_CHECK_LAUNCH();

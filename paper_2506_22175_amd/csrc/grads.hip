@@ -69,7 +69,7 @@ struct Chunk {
     __device__ __forceinline__ void load() {
 #pragma unroll
         for (int j = 0; j < GRAD_LOADS; ++j)
-            if (unit(j) < whole) v[j] = *reinterpret_cast<const Anywhere<16, 2>*>(grad + unit(j) * 16);
+            if (unit(j) < whole) v[j] = load_once_anywhere<Anywhere<16, 2>>(grad + unit(j) * 16);
             else v[j].w[0] = v[j].w[1] = v[j].w[2] = v[j].w[3] = 0;
         tail = 0.0f;
         if (has_tail()) {
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(GradArgs a) {
 }
 // Few chunks: one workgroup, four of them at a time, and no second launch.  (Chunk takes its thread's number from threadIdx.x, which
 // counts the threads of a chunk here; y counts the chunks.)
-constexpr int GRAD_ALONE = 16, GRAD_AT_ONCE = 4;
+constexpr int GRAD_ALONE = 4, GRAD_AT_ONCE = 4;
 __global__ __launch_bounds__(GRAD_THREADS * GRAD_AT_ONCE) void grad_norm_alone_kernel(GradArgs a) {
     __shared__ double lds[GRAD_AT_ONCE][GRAD_THREADS];
     const int tid = threadIdx.x, q = threadIdx.y;

@@ -30,7 +30,7 @@ constexpr int ACT_ROWS_LANES = 4, ACT_COLS = 512;       // of act_bwd_kernel: wa
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 int few_slices(int T, int K, int N, bool bf16) {
-    const int step = bf16 ? 64 : 32, columns = up(N, FEW_COLS), steps = up(K, step);
+    const int columns = up(N, bf16 ? Few<bf16_t>::COLS : Few<float>::COLS), steps = up(K, Few<float>::STEP);
     if (columns >= 256) return 1;
     int s = up(512, columns);
     const int most = up(steps, FEW_WAVES);
@@ -98,9 +98,9 @@ template <typename T> __device__ __forceinline__ void linear_finish(const FewLin
 }
 
 template <typename T, int GROUPS>
-__global__ __launch_bounds__(FEW_WAVES * 64) void few_linear_kernel(FewLinearArgs a) {
+__global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 1 ? 2 : 4) void few_linear_kernel(FewLinearArgs a) {
     __shared__ FewSums<T, FEW_WAVES> sums;
-    const int n0 = blockIdx.x * FEW_COLS, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+    const int n0 = blockIdx.x * Few<T>::COLS, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
     const int all = (a.K + Few<T>::STEP - 1) / Few<T>::STEP, begin = blockIdx.y * a.steps, end = begin + a.steps < all ? begin + a.steps : all;
     const T* row[GROUPS];
 #pragma unroll
@@ -137,11 +137,10 @@ template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a
     a.steps = up(steps, d.slices);
     const int slices = up(steps, a.steps);
     if (slices == 1) a.partial = nullptr;
-    const dim3 grid(up(d.N, FEW_COLS), slices);
+    const dim3 grid(up(d.N, Few<T>::COLS), slices);
     const int groups = up(d.T, Few<T>::ROWS);
     if (groups <= 1) few_linear_kernel<T, 1><<<grid, FEW_WAVES * 64, 0, s>>>(a);
-    else if (groups <= 2) few_linear_kernel<T, 2><<<grid, FEW_WAVES * 64, 0, s>>>(a);
-    else if constexpr (sizeof(T) == 2) few_linear_kernel<T, 4><<<grid, FEW_WAVES * 64, 0, s>>>(a);
+    else few_linear_kernel<T, 2><<<grid, FEW_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();
     if (slices > 1) {
         few_linear_finish_kernel<T><<<dim3(up(d.N, 64), d.T), 64, 0, s>>>(a, slices);
@@ -157,6 +156,9 @@ struct ActBwdArgs {
     int T, N, act, rows;                                        // rows of a workgroup
 };
 
+__device__ __forceinline__ void load_eight_once(Raw8<bf16_t>& r, const bf16_t* p) { r.u = load_once<uint4>(p); }
+__device__ __forceinline__ void load_eight_once(Raw8<float>& r, const float* p) { r.a = load_once<float4>(p); r.b = load_once<float4>(p + 4); }
+
 // A wavefront has rows of 512 columns, eight to a lane.  The columns' sums stay in registers over the workgroup's rows, and its
 // wavefronts' are added in their order.
 template <typename T>
@@ -170,8 +172,8 @@ __global__ __launch_bounds__(ACT_ROWS_LANES * 64) void act_bwd_kernel(ActBwdArgs
         const bool by_z = a.act != MOE_ACT_NONE;
         for (int t = begin + wid; t < end; t += ACT_ROWS_LANES) {
             Raw8<T> dy, z;
-            dy.load(reinterpret_cast<const T*>(a.dy) + t * a.ldy + n);
-            if (by_z) z.load(reinterpret_cast<const T*>(a.z) + t * a.ldz + n); else z.zero();
+            load_eight_once(dy, reinterpret_cast<const T*>(a.dy) + t * a.ldy + n);
+            if (by_z) load_eight_once(z, reinterpret_cast<const T*>(a.z) + t * a.ldz + n); else z.zero();
             float d[8], v[8];
             dy.to_float(d);
             z.to_float(v);

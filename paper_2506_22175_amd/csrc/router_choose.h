@@ -279,17 +279,30 @@ template <typename V> __device__ __forceinline__ V wave_max(V v) {
 // The choices of one token by 64-bit scores, by a whole wavefront, whose lanes have its logits (NaN counts as -inf), VALUES
 // neighbouring ones each: lane j returns the j-th.  *soft: of a softmax.  What counts is the length of the chain.
 template <int VALUES>
-__device__ __forceinline__ int choose_exactly(const RouterArgs& a, const float* l, Softmax<double>* soft) {
+__device__ __forceinline__ int choose_exactly(const RouterArgs& a, const float* l, Softmax<float>* soft) {
     constexpr double NONE = -__builtin_inf();
     const int lane = threadIdx.x & 63, e0 = lane * VALUES;
-    const bool by_score = a.bias != nullptr;
+    const bool by_score = a.bias != nullptr, scored = by_score || a.groups > 1;
     double s[VALUES];
     float bias[VALUES], m = -__builtin_inff();
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) bias[v] = by_score && e0 + v < a.E ? a.bias[e0 + v] : 0.0f;
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) m = fmaxf(m, l[v]);
-    if (a.sigmoid) {
+    if (!scored) {
+        // the logits decide; a softmax that is not renormalised still needs its sum
+        if (!a.sigmoid && !a.renorm) {
+            m = wave_max(m);
+            float terms[VALUES];
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) terms[v] = softmax_term<float>(l[v], m);
+            float sum = lanes_sum(in_pairs<float, VALUES>(terms));
+            sum = (of_lane(sum, 0) + of_lane(sum, 16)) + (of_lane(sum, 32) + of_lane(sum, 48));
+            *soft = {m, sum > 0.0f ? 1.0f / sum : 0.0f};
+        }
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) s[v] = 0.0;
+    } else if (a.sigmoid) {
 #pragma unroll
         for (int v = 0; v < VALUES; ++v) s[v] = 1.0 / (1.0 + exp(-(double)l[v]));
     } else {
@@ -302,7 +315,7 @@ __device__ __forceinline__ int choose_exactly(const RouterArgs& a, const float* 
         }
         sum = lanes_sum(sum);
         sum = (of_lane(sum, 0) + of_lane(sum, 16)) + (of_lane(sum, 32) + of_lane(sum, 48));
-        *soft = {m, sum > 0.0 ? 1.0 / sum : 0.0};
+        *soft = {m, sum > 0.0 ? (float)(1.0 / sum) : 0.0f};
 #pragma unroll
         for (int v = 0; v < VALUES; ++v) s[v] = sum > 0.0 ? s[v] / sum : 0.0;
     }
@@ -383,7 +396,7 @@ __device__ __forceinline__ int choose_exactly(const RouterArgs& a, const T* row)
     float l[VALUES];
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) l[v] = e0 + v < a.E ? load_logit(row + e0 + v) : -__builtin_inff();
-    Softmax<double> soft;
+    Softmax<float> soft;
     return choose_exactly<VALUES>(a, l, &soft);
 }
 

@@ -7,6 +7,19 @@ namespace moe {
 
 template <int BYTES, int ALIGN> struct __attribute__((packed, aligned(ALIGN))) Anywhere { unsigned w[BYTES / 4]; };
 
+// 16 bytes that nothing reads again: past the caches' keeping.  (Reading 512 MB and more: 7.0 TB/s so, 6.2 with an ordinary load.)
+typedef unsigned wide_u4 __attribute__((ext_vector_type(4)));
+template <typename V> __device__ __forceinline__ V load_once(const void* p) {
+    static_assert(sizeof(V) == 16, "16 bytes");
+    return __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const wide_u4*>(p)));
+}
+// the same at any multiple of two bytes
+typedef unsigned wide_u4_2 __attribute__((ext_vector_type(4), aligned(2)));
+template <typename V> __device__ __forceinline__ V load_once_anywhere(const void* p) {
+    static_assert(sizeof(V) == 16, "16 bytes");
+    return __builtin_bit_cast(V, (wide_u4)__builtin_nontemporal_load(reinterpret_cast<const wide_u4_2*>(p)));
+}
+
 // four neighbouring columns, `left` of which are in the row
 __device__ __forceinline__ void store_columns(float* p, const float* v, int left) {
     if (left >= 4) {
