@@ -33,6 +33,20 @@ template <> __device__ __forceinline__ float activate<float>(float z, int act) {
     return z;
 }
 
+// n values at once: which activation is asked once
+template <typename T, int N> __device__ __forceinline__ void activate_all(const float* z, float* y, int act) {
+    if (act == MOE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = activate<T>(z[i], MOE_ACT_GELU);
+    } else if (act == MOE_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = activate<T>(z[i], MOE_ACT_SILU);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = z[i];
+    }
+}
+
 // act'(z) = Phi(z) + z phi(z), or s (1 + z (1 - s)) with s the sigmoid of z
 template <typename T> __device__ __forceinline__ float activation_slope(float z, int act) {
     constexpr bool FAST = sizeof(T) == 2;

@@ -88,10 +88,8 @@ __device__ __forceinline__ float epilogue4(const EpiCtx<T>& c, int r, int n, con
         // (the activation is taken of the sum as it is, not as Z stores it)
         float z[4], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            z[i] = c.bias ? v[i] + c.bias[n + i] : v[i];
-            y[i] = activate<T>(z[i], c.act);
-        }
+        for (int i = 0; i < 4; ++i) z[i] = c.bias ? v[i] + c.bias[n + i] : v[i];
+        activate_all<T, 4>(z, y, c.act);
         if (c.Z) Vec4<T>::store(c.Z + (size_t)r * c.ldz + n, z);
         if (c.R) {
             float o[4];

@@ -348,42 +348,37 @@ __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 1 ? 2 : 4) void few_second
     }
 }
 
-// y[t] = sum over the choices of w times the sum of their slices; four columns to a thread.  Loads go out in eights, without a look at
-// whether there is a choice (nothing was written for one that is not).
-constexpr int JOIN_THREADS = 64;
-template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void few_join_kernel(FewArgs a) {
-    const int t = blockIdx.y, n = (blockIdx.x * JOIN_THREADS + threadIdx.x) * 4;
-    if (n >= a.M) return;
+// y[t] = sum over the choices of w times the sum of their slices.  Four columns to a thread; the wavefronts share out the choices and add
+// up in the choices' order.  Loads go out in eights, without a look at whether there is a choice (nothing was written for one that is not).
+constexpr int JOIN_WAVES = 4;
+template <typename T> __global__ __launch_bounds__(JOIN_WAVES * 64) void few_join_kernel(FewArgs a) {
+    __shared__ float4 part[FEW_K][64];
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+    const int t = blockIdx.y, n = (blockIdx.x * 64 + lane) * 4;
     const long long step = (long long)a.T * a.k * a.M;
-    const float* p = a.partial + (long long)t * a.k * a.M + n;
-    const int terms = a.k * a.slices;
-    float4 y = make_float4(0, 0, 0, 0), v = make_float4(0, 0, 0, 0);
-    for (int q0 = 0; q0 < terms; q0 += 8) {
-        float4 o[8];
-        float w[8];
-        int j[8], s[8];
-        bool there[8];
+    for (int j = wid; j < a.k; j += JOIN_WAVES) {
+        const float* p = a.partial + ((long long)t * a.k + j) * a.M + (n < a.M ? n : 0);
+        const int chosen = a.route.idx[t * a.k + j];
+        const float w = a.route.w[t * a.k + j];
+        float4 v = make_float4(0, 0, 0, 0);
+        for (int s0 = 0; s0 < a.slices; s0 += 8) {
+            float4 o[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int at = q0 + q < terms ? q0 + q : terms - 1;
-            j[q] = at / a.slices;
-            s[q] = at - j[q] * a.slices;
-            o[q] = *reinterpret_cast<const float4*>(p + s[q] * step + (long long)j[q] * a.M);
-            w[q] = a.route.w[t * a.k + j[q]];
-            there[q] = a.route.idx[t * a.k + j[q]] >= 0;
-        }
+            for (int s = 0; s < 8; ++s) o[s] = *reinterpret_cast<const float4*>(p + (s0 + s < a.slices ? s0 + s : 0) * step);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            if (q0 + q >= terms) break;
-            if (s[q] == 0) v = make_float4(0, 0, 0, 0);
-            v.x += o[q].x; v.y += o[q].y; v.z += o[q].z; v.w += o[q].w;
-            if (s[q] == a.slices - 1 && there[q]) {
-                y.x = fmaf(w[q], v.x, y.x); y.y = fmaf(w[q], v.y, y.y); y.z = fmaf(w[q], v.z, y.z); y.w = fmaf(w[q], v.w, y.w);
-            }
+            for (int s = 0; s < 8; ++s)
+                if (s0 + s < a.slices) { v.x += o[s].x; v.y += o[s].y; v.z += o[s].z; v.w += o[s].w; }
         }
+        part[j][lane] = chosen >= 0 ? make_float4(w * v.x, w * v.y, w * v.z, w * v.w) : make_float4(0, 0, 0, 0);
     }
-    const float o[4] = {y.x, y.y, y.z, y.w};
-    store_columns(reinterpret_cast<T*>(a.y) + t * a.ldy + n, o, 4);
+    __syncthreads();
+    if (wid > 0 || n >= a.M) return;
+    float y[4] = {0, 0, 0, 0};
+    for (int j = 0; j < a.k; ++j) {
+        const float4 v = part[j][lane];
+        y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
+    }
+    store_columns(reinterpret_cast<T*>(a.y) + t * a.ldy + n, y, 4);
 }
 
 struct FewDims {
@@ -470,7 +465,7 @@ template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, 
 #undef FEW_FIRST
 #undef FEW_SECOND
     MOE_CHECK_LAUNCH();
-    few_join_kernel<T><<<dim3(up(a.M, 4 * JOIN_THREADS), a.T), JOIN_THREADS, 0, s>>>(a);
+    few_join_kernel<T><<<dim3(up(a.M, 256), a.T), JOIN_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();
     return MOE_OK;
 }

@@ -1546,10 +1546,10 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, int tiles_m, int t
                     float add[8], y[8];
                     Unit8::to_float(in.zin[t], add);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        v[q] += b[q];
-                        y[q] = activate<bf16_t>(v[q], g.act) + add[q];
-                    }
+                    for (int q = 0; q < 8; ++q) v[q] += b[q];
+                    activate_all<bf16_t, 8>(v, y, g.act);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) y[q] += add[q];
                     if (Zbase) {
                         const uint4 oz = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
                         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, oz), rZ, offZ(ps, t), 0, 0);

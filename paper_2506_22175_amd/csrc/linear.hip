@@ -32,7 +32,7 @@ int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 int few_slices(int T, int K, int N, bool bf16) {
     const int columns = up(N, bf16 ? Few<bf16_t>::COLS : Few<float>::COLS), steps = up(K, Few<float>::STEP);
     if (columns >= 256) return 1;
-    int s = up(512, columns);
+    int s = up(256, columns);
     const int most = up(steps, FEW_WAVES);
     return s < most ? s : most;
 }
@@ -161,7 +161,7 @@ __device__ __forceinline__ void load_eight_once(Raw8<float>& r, const float* p) 
 
 // A wavefront has rows of 512 columns, eight to a lane.  The columns' sums stay in registers over the workgroup's rows, and its
 // wavefronts' are added in their order.
-template <typename T>
+template <typename T, int ACT>
 __global__ __launch_bounds__(ACT_ROWS_LANES * 64) void act_bwd_kernel(ActBwdArgs a) {
     __shared__ float sums[ACT_ROWS_LANES][ACT_COLS];
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
@@ -169,26 +169,38 @@ __global__ __launch_bounds__(ACT_ROWS_LANES * 64) void act_bwd_kernel(ActBwdArgs
     const int begin = blockIdx.y * a.rows, end = begin + a.rows < a.T ? begin + a.rows : a.T;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (n < a.N) {
-        const bool by_z = a.act != MOE_ACT_NONE;
-        for (int t = begin + wid; t < end; t += ACT_ROWS_LANES) {
-            Raw8<T> dy, z;
-            load_eight_once(dy, reinterpret_cast<const T*>(a.dy) + t * a.ldy + n);
-            if (by_z) load_eight_once(z, reinterpret_cast<const T*>(a.z) + t * a.ldz + n); else z.zero();
-            float d[8], v[8];
-            dy.to_float(d);
-            z.to_float(v);
+        constexpr bool by_z = ACT != MOE_ACT_NONE;
+        // so many rows of a wavefront are requested before the first is worked on
+        constexpr int AT_ONCE = sizeof(T) == 2 ? 4 : 2;
+        for (int t0 = begin + wid; t0 < end; t0 += AT_ONCE * ACT_ROWS_LANES) {
+            Raw8<T> dy[AT_ONCE], z[AT_ONCE];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (by_z) d[i] *= activation_slope<T>(v[i], a.act);
-                sum[i] += d[i];
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const long long t = t0 + u * ACT_ROWS_LANES;
+                if (t >= end) continue;
+                load_eight_once(dy[u], reinterpret_cast<const T*>(a.dy) + t * a.ldy + n);
+                if (by_z) load_eight_once(z[u], reinterpret_cast<const T*>(a.z) + t * a.ldz + n);
             }
-            if (a.dz) {
-                T* o = reinterpret_cast<T*>(a.dz) + t * a.ldz + n;
-                if constexpr (sizeof(T) == 2) {
-                    *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
-                } else {
-                    reinterpret_cast<float4*>(o)[0] = make_float4(d[0], d[1], d[2], d[3]);
-                    reinterpret_cast<float4*>(o)[1] = make_float4(d[4], d[5], d[6], d[7]);
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const long long t = t0 + u * ACT_ROWS_LANES;
+                if (t >= end) continue;
+                float d[8], v[8];
+                dy[u].to_float(d);
+                if (by_z) z[u].to_float(v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (by_z) d[i] *= activation_slope<T>(v[i], ACT);
+                    sum[i] += d[i];
+                }
+                if (a.dz) {
+                    T* o = reinterpret_cast<T*>(a.dz) + t * a.ldz + n;
+                    if constexpr (sizeof(T) == 2) {
+                        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
+                    } else {
+                        reinterpret_cast<float4*>(o)[0] = make_float4(d[0], d[1], d[2], d[3]);
+                        reinterpret_cast<float4*>(o)[1] = make_float4(d[4], d[5], d[6], d[7]);
+                    }
                 }
             }
         }
@@ -206,7 +218,32 @@ __global__ __launch_bounds__(ACT_ROWS_LANES * 64) void act_bwd_kernel(ActBwdArgs
     }
 }
 
-// out (+)= sum over p of part[p], in order
+template <typename T> moe_status act_bwd_launch(const ActBwdArgs& a, dim3 grid, hipStream_t s) {
+    if (a.act == MOE_ACT_GELU) act_bwd_kernel<T, MOE_ACT_GELU><<<grid, ACT_ROWS_LANES * 64, 0, s>>>(a);
+    else if (a.act == MOE_ACT_SILU) act_bwd_kernel<T, MOE_ACT_SILU><<<grid, ACT_ROWS_LANES * 64, 0, s>>>(a);
+    else act_bwd_kernel<T, MOE_ACT_NONE><<<grid, ACT_ROWS_LANES * 64, 0, s>>>(a);
+    MOE_CHECK_LAUNCH();
+    return MOE_OK;
+}
+
+// out (+)= sum over p of part[p].  A wavefront adds every 16th of them, in order, and the wavefronts' sums are added in theirs.
+__global__ __launch_bounds__(1024) void join_columns_kernel(const float* __restrict__ part, int parts, int size, float* __restrict__ out, int store) {
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
+    float v = 0.0f;
+    if (i < size) {
+#pragma unroll 8
+        for (int p = wid; p < parts; p += 16) v += part[(long long)p * size + i];
+    }
+    sums[wid][lane] = v;
+    __syncthreads();
+    if (wid > 0 || i >= size) return;
+    v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) v += sums[w][lane];
+    out[i] = store ? v : out[i] + v;
+}
+// The same for many columns, a thread to each
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ part, int parts, long long size, float* __restrict__ out, int store) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     if (i >= size) return;
@@ -301,10 +338,11 @@ extern "C" moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, 
     {
         moe::ProfScope prof(moe::PK_ACT_BWD, s);
         const dim3 grid(moe::up(d.N, moe::ACT_COLS), parts);
-        if (d.bf16) moe::act_bwd_kernel<moe::bf16_t><<<grid, moe::ACT_ROWS_LANES * 64, 0, s>>>(a);
-        else moe::act_bwd_kernel<float><<<grid, moe::ACT_ROWS_LANES * 64, 0, s>>>(a);
-        MOE_CHECK_LAUNCH();
-        if (dbias) MOE_TRY(moe::join_parts(a.part, parts, d.N, dbias, d.overwrite, s));
+        MOE_TRY(d.bf16 ? moe::act_bwd_launch<moe::bf16_t>(a, grid, s) : moe::act_bwd_launch<float>(a, grid, s));
+        if (dbias) {
+            moe::join_columns_kernel<<<moe::up(d.N, 64), 1024, 0, s>>>(a.part, parts, d.N, dbias, d.overwrite);
+            MOE_CHECK_LAUNCH();
+        }
     }
     moe::count_launch(moe::LC_OTHER);
     return MOE_OK;
