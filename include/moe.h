@@ -475,7 +475,7 @@ moe_status moe_w4_quantize(int32_t E, int32_t K, int32_t N, int32_t dtype, const
 
 /* The whole layer, forward, for a few tokens: nothing has a capacity and no choice is dropped. */
 typedef struct {
-    int32_t T, M, H, E, k;  /* T <= 256; M * H <= 2^30; E, k and the next six as in moe_router_config */
+    int32_t T, M, H, E, k;  /* T <= 256; M H, T k H and 256 ldx below 2^30; E, k and the next six as in moe_router_config */
     int32_t scores, groups, group_k, group_top, renormalize;
     float scale;
     int32_t dtype;          /* MOE_F32 or MOE_BF16: x, Wg, W1, W2, y */

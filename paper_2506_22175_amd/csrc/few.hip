@@ -189,53 +189,37 @@ template <int VALUES> __global__ __launch_bounds__(64) void few_route_kernel(Few
 struct FewPlan {
     int rows[FEW_TOKENS];                    // assignments with the workgroup's expert, ascending
     unsigned there[FEW_E / 32];              // experts that are chosen
-    int expert, n_rows;
+    int expert, n_rows, n_experts;
 };
 // What a workgroup has in LDS: the choices, which only the plan looks at, then the sums.
 template <typename T, int WAVES> struct FewLds {
     FewPlan plan;
     union { int idx[FEW_TOKENS * FEW_K]; FewSums<T, WAVES> sums; };
 };
-// Where the first product gets the choices from: they are there; or a workgroup routes for itself, which saves the launches between
-// it and the gate: from the gate's sums, or from x and Wg (one or two tokens).
-enum { FEW_ROUTED = 0, FEW_SUMMED = 1, FEW_ALONE = 2 };
-template <typename T, int MODE, int WAVES> __device__ __forceinline__ void few_choices(const FewArgs& a, bool record, int* idx) {
-    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if constexpr (MODE == FEW_ROUTED) {
-        for (int i = threadIdx.x; i < a.T * a.k; i += WAVES * 64) idx[i] = a.route.idx[i];
-    } else {
-        __shared__ double s_sum[MODE == FEW_ALONE ? WAVES : 1][2][64];
-        if constexpr (MODE == FEW_ALONE) {
-            if (a.T == 1) gate_sums<T, 1, WAVES>(a, 0, 0, 0, a.M, reinterpret_cast<double (&)[WAVES][1][64]>(s_sum));
-            else gate_sums<T, 2, WAVES>(a, 0, 0, 0, a.M, s_sum);
-            __syncthreads();
-        }
-        for (int t = wid; t < a.T; t += WAVES) {
-            float weight;
-            int chosen;
-            if (a.E <= 64) {
-                double sum;
-                if constexpr (MODE == FEW_ALONE) {
-                    sum = 0.0;
-#pragma unroll
-                    for (int q = 0; q < WAVES; ++q) sum += a.T == 1 ? reinterpret_cast<double (&)[WAVES][1][64]>(s_sum)[q][0][lane] : s_sum[q][t][lane];
-                } else {
-                    gate_total<1>(a, t, &sum);
-                }
-                chosen = route_token<1>(a, t, &sum, record, &weight);
-            } else if constexpr (MODE == FEW_SUMMED) {
-                double sum[4];
-                gate_total<4>(a, t, sum);
-                chosen = route_token<4>(a, t, sum, record, &weight);
-            }
-            if (lane < a.k) idx[t * a.k + lane] = chosen;
-        }
-    }
-    __syncthreads();
-}
+// The workgroup's expert, the slot-th of those that are chosen (-1: there are fewer), how many are, and how many assignments it has,
+// which are in FewPlan::rows.
+struct FewPick { int expert, n_rows, n_experts; };
 
-// Fills `p` from the choices in LDS for the `slot`-th of the chosen experts (expert -1: there are fewer).  Every thread comes here.
-__device__ __forceinline__ void few_plan(const FewArgs& a, int slot, const int* idx, FewPlan& p) {
+// Up to 32 assignments, whose choices the lanes of every wavefront have: each finds out by itself, and writes down the same.
+constexpr int FEW_IN_LANES = 32;
+__device__ __forceinline__ FewPick few_pick(int e, int slot, FewPlan& p) {
+    const int lane = threadIdx.x & 63;
+    FewPick pick = {-1, 0, 0};
+    unsigned long long left = __ballot(e >= 0), rows = 0;
+    while (left) {
+        const int one = __builtin_amdgcn_readlane(e, __builtin_ctzll(left));
+        const unsigned long long same = __ballot(e == one);
+        if (pick.n_experts == slot) { pick.expert = one; rows = same; }
+        ++pick.n_experts;
+        left &= ~same;
+    }
+    pick.n_rows = __popcll(rows);
+    if (rows >> lane & 1) p.rows[__popcll(rows & ((1ull << lane) - 1))] = lane;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return pick;
+}
+// More of them, from the choices in LDS.  Every thread comes here.
+__device__ __forceinline__ FewPick few_plan(const FewArgs& a, int slot, const int* idx, FewPlan& p) {
     const int n = a.T * a.k, tid = threadIdx.x;
     if (tid < FEW_E / 32) p.there[tid] = 0;
     __syncthreads();
@@ -254,6 +238,7 @@ __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, const int* 
             const int o = __shfl_up(end, off, 64);
             if (tid >= off) end += o;
         }
+        const int all = __shfl(end, FEW_E / 32 - 1, 64);
         int expert = -1;
         if (tid < FEW_E / 32 && slot >= end - count && slot < end) {
             unsigned bits = mine;
@@ -271,36 +256,91 @@ __device__ __forceinline__ void few_plan(const FewArgs& a, int slot, const int* 
                 rows += __popcll(b);
             }
         }
-        if (tid == 0) { p.expert = expert; p.n_rows = rows; }
+        if (tid == 0) { p.expert = expert; p.n_rows = rows; p.n_experts = all; }
     }
     __syncthreads();
+    return {__builtin_amdgcn_readfirstlane(p.expert), __builtin_amdgcn_readfirstlane(p.n_rows), __builtin_amdgcn_readfirstlane(p.n_experts)};
+}
+
+// Where the choices come from: they are there; or, in the first product, a workgroup routes for itself, which saves the launches between
+// it and the gate: from the gate's sums, or from x and Wg (one or two tokens).
+enum { FEW_ROUTED = 0, FEW_SUMMED = 1, FEW_ALONE = 2 };
+template <typename T, int MODE, int WAVES> __device__ __forceinline__ FewPick few_choices(const FewArgs& a, int slot, bool record, FewLds<T, WAVES>& lds) {
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.T * a.k;
+    if constexpr (MODE == FEW_ROUTED) {
+        if (n <= FEW_IN_LANES) return few_pick(lane < n ? a.route.idx[lane] : -1, slot, lds.plan);
+        for (int i = threadIdx.x; i < n; i += WAVES * 64) lds.idx[i] = a.route.idx[i];
+    } else {
+        __shared__ double s_sum[MODE == FEW_ALONE ? WAVES : 1][2][64];
+        if constexpr (MODE == FEW_ALONE) {
+            if (a.T == 1) {
+                auto& sums = reinterpret_cast<double (&)[WAVES][1][64]>(s_sum);
+                gate_sums<T, 1, WAVES>(a, 0, 0, 0, a.M, sums);
+                __syncthreads();
+                double sum = 0.0;
+#pragma unroll
+                for (int q = 0; q < WAVES; ++q) sum += sums[q][0][lane];
+                float weight;
+                return few_pick(route_token<1>(a, 0, &sum, record && wid == 0, &weight), slot, lds.plan);
+            }
+            gate_sums<T, 2, WAVES>(a, 0, 0, 0, a.M, s_sum);
+            __syncthreads();
+        }
+        for (int t = wid; t < a.T; t += WAVES) {
+            float weight;
+            int chosen;
+            if (a.E <= 64) {
+                double sum;
+                if constexpr (MODE == FEW_ALONE) {
+                    sum = 0.0;
+#pragma unroll
+                    for (int q = 0; q < WAVES; ++q) sum += s_sum[q][t][lane];
+                } else {
+                    gate_total<1>(a, t, &sum);
+                }
+                chosen = route_token<1>(a, t, &sum, record, &weight);
+            } else if constexpr (MODE == FEW_SUMMED) {
+                double sum[4];
+                gate_total<4>(a, t, sum);
+                chosen = route_token<4>(a, t, sum, record, &weight);
+            }
+            if (lane < a.k) lds.idx[t * a.k + lane] = chosen;
+        }
+        if (n <= FEW_IN_LANES) {
+            __syncthreads();
+            const int e = lane < n ? lds.idx[lane] : -1;
+            __syncthreads();                               // (the sums will lie there)
+            return few_pick(e, slot, lds.plan);
+        }
+    }
+    __syncthreads();
+    return few_plan(a, slot, lds.idx, lds.plan);
 }
 
 __device__ __forceinline__ float gelu_of(float z) { return 0.5f * z * erfcf(-0.70710678118654752440f * z); }
 
 // ---- first product ----------------------------------------------------------------------------------------------
 template <typename T, int GROUPS, int MODE, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, GROUPS > 1 ? 2 : 4) void few_first_kernel(FewArgs a) {
+__global__ __launch_bounds__(WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_kernel(FewArgs a) {
     __shared__ FewLds<T, WAVES> lds;
     const FewPlan& plan = lds.plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
-    few_choices<T, MODE, WAVES>(a, blockIdx.x == 0 && blockIdx.y == 0, lds.idx);
-    few_plan(a, blockIdx.y, lds.idx, lds.plan);
-    const int expert = __builtin_amdgcn_readfirstlane(plan.expert);
-    if (expert < 0) return;
+    const FewPick pick = few_choices<T, MODE, WAVES>(a, blockIdx.y, blockIdx.x == 0 && blockIdx.y == 0, lds);
+    if (pick.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS;
-    const T* W = reinterpret_cast<const T*>(a.W1) + (long long)expert * a.M * a.H + n0;
+    const T* W = reinterpret_cast<const T*>(a.W1) + (long long)pick.expert * a.M * a.H + n0;
     const long long size = (long long)a.T * a.k * a.H;
-    for (int r0 = 0; r0 < plan.n_rows; r0 += GROUPS * ROWS) {
-        const T* row[GROUPS];
+    for (int r0 = 0; r0 < pick.n_rows; r0 += GROUPS * ROWS) {
+        const T* const rows[1] = {reinterpret_cast<const T*>(a.x)};
+        unsigned row[GROUPS];
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
             const int r = r0 + g * ROWS + Few<T>::row(lane);
-            row[g] = reinterpret_cast<const T*>(a.x) + plan.rows[r < plan.n_rows ? r : r0] / a.k * a.ldx;
+            row[g] = (unsigned)(plan.rows[r < pick.n_rows ? r : r0] / a.k) * (unsigned)a.ldx * (unsigned)sizeof(T);
         }
         few_acc acc[GROUPS][Few<T>::ACCS];
-        few_sums<T, GROUPS, 1, WAVES>(W, a.H, a.H - n0, row, 0, a.M, wid, (a.M + Few<T>::STEP - 1) / Few<T>::STEP, acc);
-        few_finish<T, GROUPS, WAVES>(lds.sums, acc, plan.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
+        few_sums<T, GROUPS, 1, WAVES>(W, a.H, a.H - n0, rows, row, a.M, wid, (a.M + Few<T>::STEP - 1) / Few<T>::STEP, acc);
+        few_finish<T, GROUPS, WAVES>(lds.sums, acc, pick.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
             const float v = gelu_of(z);
             const long long at = (long long)plan.rows[r0 + r] * a.H + n0 + n;
             if constexpr (sizeof(T) == 4) {
@@ -317,33 +357,34 @@ __global__ __launch_bounds__(WAVES * 64, GROUPS > 1 ? 2 : 4) void few_first_kern
 }
 
 // ---- second product ----------------------------------------------------------------------------------------------
-// A workgroup has 128 columns (float: 64) of an expert and a slice of H.  It leaves its rows' sums, which few_join_kernel adds up: a launch of its
-// own, since making sums visible from one workgroup to another of the same launch empties the caches of eight dies (the last
-// workgroup of a column block to finish, adding them up: 89 us for what takes 14 without).
+// A workgroup has 128 columns (float: 64) of an expert and a slice of H.  It leaves its rows' sums, which few_join_kernel adds up: a launch of
+// its own.  (The last workgroup of a column block to finish, adding them up: with fences, which write back and empty the caches of
+// eight dies, 89 us for what takes 14 without; with stores and loads that go past the caches 44.5 us for the whole of one token, 2048/8192,
+// and 37.5 for seven of 520/1000 in float, against 45.1 and 35.5 with the launch.)
 template <typename T, int GROUPS>
-__global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 1 ? 2 : 4) void few_second_kernel(FewArgs a) {
+__global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_second_kernel(FewArgs a) {
     __shared__ FewLds<T, FEW_WAVES> lds;
     const FewPlan& plan = lds.plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
-    few_choices<T, FEW_ROUTED, FEW_WAVES>(a, false, lds.idx);
-    few_plan(a, blockIdx.y, lds.idx, lds.plan);
-    const int expert = __builtin_amdgcn_readfirstlane(plan.expert);
-    if (expert < 0) return;
+    const FewPick pick = few_choices<T, FEW_ROUTED, FEW_WAVES>(a, blockIdx.y, false, lds);
+    if (pick.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS, PARTS = sizeof(T) == 2 ? 2 : 1;
-    const T* W = reinterpret_cast<const T*>(a.W2) + (long long)expert * a.H * a.M + n0;
+    const T* W = reinterpret_cast<const T*>(a.W2) + (long long)pick.expert * a.H * a.M + n0;
     const int all = (a.H + Few<T>::STEP - 1) / Few<T>::STEP, begin = blockIdx.z * a.steps, end = begin + a.steps < all ? begin + a.steps : all;
-    const long long size = (long long)a.T * a.k * a.H;
+    const T* rows[PARTS];
+#pragma unroll
+    for (int c = 0; c < PARTS; ++c) rows[c] = reinterpret_cast<const T*>(a.a) + (long long)c * a.T * a.k * a.H;
     float* partial = a.partial + (long long)blockIdx.z * a.T * a.k * a.M;
-    for (int r0 = 0; r0 < plan.n_rows; r0 += GROUPS * ROWS) {
-        const T* row[GROUPS];
+    for (int r0 = 0; r0 < pick.n_rows; r0 += GROUPS * ROWS) {
+        unsigned row[GROUPS];
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
             const int r = r0 + g * ROWS + Few<T>::row(lane);
-            row[g] = reinterpret_cast<const T*>(a.a) + (long long)plan.rows[r < plan.n_rows ? r : r0] * a.H;
+            row[g] = (unsigned)plan.rows[r < pick.n_rows ? r : r0] * (unsigned)a.H * (unsigned)sizeof(T);
         }
         few_acc acc[GROUPS][Few<T>::ACCS];
-        few_sums<T, GROUPS, PARTS, FEW_WAVES>(W, a.M, a.M - n0, row, size, a.H, begin + wid, end, acc);
-        few_finish<T, GROUPS, FEW_WAVES>(lds.sums, acc, plan.n_rows - r0, a.M - n0,
+        few_sums<T, GROUPS, PARTS, FEW_WAVES>(W, a.M, a.M - n0, rows, row, a.H, begin + wid, end, acc);
+        few_finish<T, GROUPS, FEW_WAVES>(lds.sums, acc, pick.n_rows - r0, a.M - n0,
                                          [&](int r, int n, float v) { partial[(long long)plan.rows[r0 + r] * a.M + n0 + n] = v; });
     }
 }
@@ -399,7 +440,8 @@ moe_status few_dims(const moe_few_config* c, FewDims* d) {
     if ((c->ldx && c->ldx < c->M) || (c->ldy && c->ldy < c->M)) return MOE_ERR_SHAPE;
     if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_UNSUPPORTED;
     if (c->T > FEW_TOKENS || c->M % 8 || c->H % 8 || c->ldx % 8) return MOE_ERR_UNSUPPORTED;
-    if ((long long)c->M * c->H > (1 << 30)) return MOE_ERR_UNSUPPORTED;
+    const long long limit = 1 << 30;                       // of offsets in elements
+    if ((long long)c->M * c->H >= limit || (long long)c->T * c->k * c->H >= limit || (c->ldx ? c->ldx : c->M) >= limit / FEW_TOKENS) return MOE_ERR_UNSUPPORTED;
     const bool bf16 = c->dtype == MOE_BF16;
     const long long n = (long long)c->T * c->k;
     d->slots = (int)(n < c->E ? n : c->E);

@@ -41,12 +41,12 @@ template <int GROUPS, int PARTS> struct FewStep<bf16_t, GROUPS, PARTS> {
 #pragma unroll
         for (int j = 0; j < 8; ++j, at += ldw * 2u) w[j] = load_once<uint4>(p + at);
     }
-    __device__ __forceinline__ void load_rows(const bf16_t* const (&row)[GROUPS], long long part, int k, int K) {
-        const int at = k < K ? k : 0;
+    __device__ __forceinline__ void load_rows(const bf16_t* const (&rows)[PARTS], const unsigned (&row)[GROUPS], int k, int K) {
+        const unsigned at = (k < K ? k : 0) * 2u;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-            for (int c = 0; c < PARTS; ++c) r[g][c] = *reinterpret_cast<const uint4*>(row[g] + c * part + at);
+            for (int c = 0; c < PARTS; ++c) r[g][c] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(rows[c]) + (row[g] + at));
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll
@@ -83,12 +83,13 @@ template <int GROUPS, int PARTS> struct FewStep<float, GROUPS, PARTS> {
 #pragma unroll
         for (int j = 0; j < 8; ++j, at += ldw * 4u) w[j] = load_once<float4>(p + at);
     }
-    __device__ __forceinline__ void load_rows(const float* const (&row)[GROUPS], long long, int k, int K) {
-        const int at = k < K ? k : 0;
+    __device__ __forceinline__ void load_rows(const float* const (&rows)[1], const unsigned (&row)[GROUPS], int k, int K) {
+        const char* p = reinterpret_cast<const char*>(rows[0]);
+        const unsigned at = (k < K ? k : 0) * 4u;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-            r[g][0] = *reinterpret_cast<const float4*>(row[g] + at);
-            r[g][1] = *reinterpret_cast<const float4*>(row[g] + at + 4);
+            r[g][0] = *reinterpret_cast<const float4*>(p + (row[g] + at));
+            r[g][1] = *reinterpret_cast<const float4*>(p + (row[g] + at + 16u));
         }
     }
     __device__ __forceinline__ void zero() {
@@ -113,11 +114,14 @@ template <int GROUPS, int PARTS> struct FewStep<float, GROUPS, PARTS> {
 constexpr int FEW_PASS = 8;
 template <typename T, int WAVES> struct FewSums { float v[WAVES][FEW_PASS][Few<T>::COLS + 4]; };
 
-// Offsets in W are 32 bits wide: K N elements below 2^30.
 // Sums over the steps first, first + WAVES, ... below `steps` of K (a multiple of 8), each wavefront its own.  W: the workgroup's
-// first column; cols: columns there are from it on; row: the lane's row of each group (any row will do where there is none).
+// first column; cols: columns there are from it on; rows: the rows' parts, row: where the lane's row of each group begins, in bytes (any
+// row will do where there is none).  Offsets are 32 bits wide: a matrix has less than 2^32 bytes.
+// A wavefront waits for a step's loads and has no others under way meanwhile: registers for two steps would leave a CU half the wavefronts
+// (and the compiler waits for both where it copies one's to the other's), and sixteen of them have 128 KiB under way, twice what the memory's
+// latency asks of a CU.
 template <typename T, int GROUPS, int PARTS, int WAVES>
-__device__ __forceinline__ void few_sums(const T* W, unsigned ldw, int cols, const T* const (&row)[GROUPS], long long part, int K, int first,
+__device__ __forceinline__ void few_sums(const T* W, unsigned ldw, int cols, const T* const (&rows)[PARTS], const unsigned (&row)[GROUPS], int K, int first,
                                          int steps, few_acc (&acc)[GROUPS][Few<T>::ACCS]) {
     const int lane = threadIdx.x & 63;
     // columns past the last are the first ones again, and not looked at
@@ -128,26 +132,16 @@ __device__ __forceinline__ void few_sums(const T* W, unsigned ldw, int cols, con
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
         for (int i = 0; i < Few<T>::ACCS; ++i) acc[g][i] = few_acc{0, 0, 0, 0};
-    // The next step's loads are under way while one is multiplied; of eight fragments of rows (which come from the caches) there are no
-    // registers to hold two steps'.
-    constexpr bool EARLY = GROUPS * PARTS < 8;
-    FewStep<T, GROUPS, PARTS> a, b;
-    int s = __builtin_amdgcn_readfirstlane(first);
-    if (s < steps) {
-        a.load(W, ldw, col, s * Few<T>::STEP + k0, K);
-        if (EARLY) a.load_rows(row, part, s * Few<T>::STEP + k0, K);
-    }
-    while (s < steps) {
-        const int next = s + WAVES;
-        if (!EARLY) a.load_rows(row, part, s * Few<T>::STEP + k0, K);
-        if (next < steps) {
-            b.load(W, ldw, col, next * Few<T>::STEP + k0, K);
-            if (EARLY) b.load_rows(row, part, next * Few<T>::STEP + k0, K);
+#pragma unroll 1
+    for (int s = __builtin_amdgcn_readfirstlane(first); s < steps; s += WAVES) {
+        FewStep<T, GROUPS, PARTS> x;
+        const int k = s * Few<T>::STEP + k0;
+        x.load(W, ldw, col, k, K);
+        x.load_rows(rows, row, k, K);
+        if ((s + 1) * Few<T>::STEP > K) {                  // (nothing meets what was loaded in the place of what is not there)
+            if (k >= K) x.zero();
         }
-        if ((s + 1) * Few<T>::STEP > K && s * Few<T>::STEP + k0 >= K) a.zero();        // (nothing meets what was loaded in its place)
-        a.multiply(acc);
-        s = next;
-        a = b;
+        x.multiply(acc);
     }
 }
 

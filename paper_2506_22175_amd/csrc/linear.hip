@@ -25,7 +25,7 @@ struct LinearDims {
 
 constexpr int FEW_LINEAR_ROWS = 32;          // up to so many
 constexpr int FEW_WAVES = 8;
-constexpr int ACT_ROWS_LANES = 4, ACT_COLS = 512;       // of act_bwd_kernel: wavefronts, each a row of so many columns
+constexpr int ACT_WAVES = 4, ACT_COLS = 512; // of act_bwd_kernel: wavefronts, columns of each
 
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
@@ -74,10 +74,11 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
 }
 
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
+// Wavefronts side by side, and blocks of rows: enough for the chip, of two rows to a wavefront at least.
+int act_beside(const LinearDims& d) { return d.N > 2 * ACT_COLS ? 4 : d.N > ACT_COLS ? 2 : 1; }
 int act_blocks(const LinearDims& d) {
-    const int columns = up(d.N, ACT_COLS);
-    int blocks = up(2048, columns);
-    const int most = up(d.T > 0 ? d.T : 1, 2 * ACT_ROWS_LANES);
+    const int beside = act_beside(d), columns = up(d.N, beside * ACT_COLS);
+    const int blocks = up(1024, columns), most = up(d.T > 0 ? d.T : 1, 2 * (ACT_WAVES / beside));
     return blocks < most ? blocks : most;
 }
 
@@ -98,18 +99,19 @@ template <typename T> __device__ __forceinline__ void linear_finish(const FewLin
 }
 
 template <typename T, int GROUPS>
-__global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 1 ? 2 : 4) void few_linear_kernel(FewLinearArgs a) {
+__global__ __launch_bounds__(FEW_WAVES * 64, 4) void few_linear_kernel(FewLinearArgs a) {
     __shared__ FewSums<T, FEW_WAVES> sums;
     const int n0 = blockIdx.x * Few<T>::COLS, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
     const int all = (a.K + Few<T>::STEP - 1) / Few<T>::STEP, begin = blockIdx.y * a.steps, end = begin + a.steps < all ? begin + a.steps : all;
-    const T* row[GROUPS];
+    const T* const rows[1] = {reinterpret_cast<const T*>(a.x)};
+    unsigned row[GROUPS];
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
         const int t = g * Few<T>::ROWS + Few<T>::row(lane);
-        row[g] = reinterpret_cast<const T*>(a.x) + (t < a.T ? t : 0) * a.ldx;
+        row[g] = (unsigned)(t < a.T ? t : 0) * (unsigned)a.ldx * (unsigned)sizeof(T);
     }
     few_acc acc[GROUPS][Few<T>::ACCS];
-    few_sums<T, GROUPS, 1, FEW_WAVES>(reinterpret_cast<const T*>(a.W) + n0, a.N, a.N - n0, row, 0, a.K, begin + wid, end, acc);
+    few_sums<T, GROUPS, 1, FEW_WAVES>(reinterpret_cast<const T*>(a.W) + n0, a.N, a.N - n0, rows, row, a.K, begin + wid, end, acc);
     float* partial = a.partial ? a.partial + (long long)blockIdx.y * a.T * a.N : nullptr;
     few_finish<T, GROUPS, FEW_WAVES>(sums, acc, a.T, a.N - n0, [&](int t, int n, float v) {
         if (partial) partial[(long long)t * a.N + n0 + n] = v;
@@ -153,37 +155,37 @@ template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a
 struct ActBwdArgs {
     const void* dy; const void* z; void* dz; float* part;       // part: [blocks][N], or NULL
     long long ldy, ldz;
-    int T, N, act, rows;                                        // rows of a workgroup
+    int T, N, act, rows, beside;                                // rows of a workgroup; wavefronts side by side
 };
 
 __device__ __forceinline__ void load_eight_once(Raw8<bf16_t>& r, const bf16_t* p) { r.u = load_once<uint4>(p); }
 __device__ __forceinline__ void load_eight_once(Raw8<float>& r, const float* p) { r.a = load_once<float4>(p); r.b = load_once<float4>(p + 4); }
 
-// A wavefront has rows of 512 columns, eight to a lane.  The columns' sums stay in registers over the workgroup's rows, and its
-// wavefronts' are added in their order.
+// A wavefront has 512 columns, eight to a lane, and some of the workgroup's rows; as many of the wavefronts as there are columns for
+// stand side by side in a row, the others have other rows.  The columns' sums stay in registers over the rows.
 template <typename T, int ACT>
-__global__ __launch_bounds__(ACT_ROWS_LANES * 64) void act_bwd_kernel(ActBwdArgs a) {
-    __shared__ float sums[ACT_ROWS_LANES][ACT_COLS];
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-    const int n = blockIdx.x * ACT_COLS + lane * 8;
+__global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(ActBwdArgs a) {
+    __shared__ float sums[ACT_WAVES][ACT_COLS];
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, beside = wid % a.beside, below = wid / a.beside, rows = ACT_WAVES / a.beside;
+    const int n = (blockIdx.x * a.beside + beside) * ACT_COLS + lane * 8;
     const int begin = blockIdx.y * a.rows, end = begin + a.rows < a.T ? begin + a.rows : a.T;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (n < a.N) {
         constexpr bool by_z = ACT != MOE_ACT_NONE;
         // so many rows of a wavefront are requested before the first is worked on
-        constexpr int AT_ONCE = sizeof(T) == 2 ? 4 : 2;
-        for (int t0 = begin + wid; t0 < end; t0 += AT_ONCE * ACT_ROWS_LANES) {
+        constexpr int AT_ONCE = 2;
+        for (int t0 = begin + below; t0 < end; t0 += AT_ONCE * rows) {
             Raw8<T> dy[AT_ONCE], z[AT_ONCE];
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                const long long t = t0 + u * ACT_ROWS_LANES;
+                const long long t = t0 + u * rows;
                 if (t >= end) continue;
                 load_eight_once(dy[u], reinterpret_cast<const T*>(a.dy) + t * a.ldy + n);
                 if (by_z) load_eight_once(z[u], reinterpret_cast<const T*>(a.z) + t * a.ldz + n);
             }
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                const long long t = t0 + u * ACT_ROWS_LANES;
+                const long long t = t0 + u * rows;
                 if (t >= end) continue;
                 float d[8], v[8];
                 dy[u].to_float(d);
@@ -209,19 +211,18 @@ __global__ __launch_bounds__(ACT_ROWS_LANES * 64) void act_bwd_kernel(ActBwdArgs
     *reinterpret_cast<float4*>(&sums[wid][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
     *reinterpret_cast<float4*>(&sums[wid][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
     __syncthreads();
-    for (int c = threadIdx.x; c < ACT_COLS; c += ACT_ROWS_LANES * 64) {
-        const int col = blockIdx.x * ACT_COLS + c;
+    for (int c = threadIdx.x; c < a.beside * ACT_COLS; c += ACT_WAVES * 64) {
+        const int col = blockIdx.x * a.beside * ACT_COLS + c;
         float v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < ACT_ROWS_LANES; ++w) v += sums[w][c];
+        for (int r = 0; r < rows; ++r) v += sums[r * a.beside + c / ACT_COLS][c % ACT_COLS];
         if (col < a.N) a.part[(long long)blockIdx.y * a.N + col] = v;
     }
 }
 
 template <typename T> moe_status act_bwd_launch(const ActBwdArgs& a, dim3 grid, hipStream_t s) {
-    if (a.act == MOE_ACT_GELU) act_bwd_kernel<T, MOE_ACT_GELU><<<grid, ACT_ROWS_LANES * 64, 0, s>>>(a);
-    else if (a.act == MOE_ACT_SILU) act_bwd_kernel<T, MOE_ACT_SILU><<<grid, ACT_ROWS_LANES * 64, 0, s>>>(a);
-    else act_bwd_kernel<T, MOE_ACT_NONE><<<grid, ACT_ROWS_LANES * 64, 0, s>>>(a);
+    if (a.act == MOE_ACT_GELU) act_bwd_kernel<T, MOE_ACT_GELU><<<grid, ACT_WAVES * 64, 0, s>>>(a);
+    else if (a.act == MOE_ACT_SILU) act_bwd_kernel<T, MOE_ACT_SILU><<<grid, ACT_WAVES * 64, 0, s>>>(a);
+    else act_bwd_kernel<T, MOE_ACT_NONE><<<grid, ACT_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();
     return MOE_OK;
 }
@@ -333,11 +334,11 @@ extern "C" moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, 
     if (!dy || (!dz && !dbias) || (!z && d.act != MOE_ACT_NONE) || (dbias && !scratch)) return MOE_ERR_NULL;
     if (!moe::aligned16(dy) || !moe::aligned16(z) || !moe::aligned16(dz) || !moe::aligned16(scratch)) return MOE_ERR_UNSUPPORTED;
     const int blocks = moe::act_blocks(d);
-    moe::ActBwdArgs a = {dy, z, dz, dbias ? (float*)scratch : nullptr, d.ldy, d.ldz, d.T, d.N, d.act, moe::up(d.T, blocks)};
+    moe::ActBwdArgs a = {dy, z, dz, dbias ? (float*)scratch : nullptr, d.ldy, d.ldz, d.T, d.N, d.act, moe::up(d.T, blocks), moe::act_beside(d)};
     const int parts = moe::up(d.T, a.rows);
     {
         moe::ProfScope prof(moe::PK_ACT_BWD, s);
-        const dim3 grid(moe::up(d.N, moe::ACT_COLS), parts);
+        const dim3 grid(moe::up(d.N, a.beside * moe::ACT_COLS), parts);
         MOE_TRY(d.bf16 ? moe::act_bwd_launch<moe::bf16_t>(a, grid, s) : moe::act_bwd_launch<float>(a, grid, s));
         if (dbias) {
             moe::join_columns_kernel<<<moe::up(d.N, 64), 1024, 0, s>>>(a.part, parts, d.N, dbias, d.overwrite);

@@ -25,7 +25,8 @@ OK = dict(T=2, M=64, H=64, E=8, k=2)
     (dict(T=257), UNSUPPORTED), (dict(M=60), UNSUPPORTED), (dict(H=68), UNSUPPORTED), (dict(ldx=68), UNSUPPORTED),
     (dict(E=513), UNSUPPORTED), (dict(E=64, k=17), UNSUPPORTED), (dict(dtype=E4M3), UNSUPPORTED), (dict(dtype=9), UNSUPPORTED),
     (dict(scores=2), UNSUPPORTED), (dict(renormalize=2), UNSUPPORTED), (dict(group_top=0), UNSUPPORTED),
-    (dict(M=1 << 15, H=(1 << 15) + 8), UNSUPPORTED), (dict(M=1 << 30), UNSUPPORTED),
+    (dict(M=1 << 15, H=1 << 15), UNSUPPORTED), (dict(M=1 << 30), UNSUPPORTED), (dict(T=256, k=8, H=1 << 19), UNSUPPORTED),
+    (dict(ldx=1 << 22), UNSUPPORTED),
 ])
 def test_few_refuses(kw, status):
     cfg = B.make_few_config(**{**OK, **kw})
