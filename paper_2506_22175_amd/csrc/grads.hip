@@ -5,9 +5,9 @@
 // Nothing but memory bounds either: the norm reads every element once, clipping reads it again and writes it.  Squares and sums
 // are in 64 bits, which the vector unit does in the shadow of the loads and in which nothing overflows or vanishes.
 //
-// The tensors' places are in a table in device memory, written once for a list of tensors, so that one launch covers any number
-// of them.  It cuts them into chunks of 32 KiB, of which a workgroup takes every so many-th; eight 16-byte loads of a thread are
-// a chunk, and the next one's are requested before a chunk is worked on.  The workgroups leave a partial sum each.  Whoever needs
+// The tensors' chunks of 32 KiB are in a table in device memory, written once for a list of tensors, so that one launch covers any number
+// of them, and a workgroup needs one look at the table for a chunk.  Of the chunks a workgroup takes every so many-th; eight 16-byte loads of a thread are
+// a chunk, and there are enough workgroups for some to wait while others add.  The workgroups leave a partial sum each.  Whoever needs
 // the norm adds those up: a workgroup of its own, or every workgroup of the scaling while its first chunk is on its way.  (The last
 // workgroup to finish cannot do it cheaply: what makes its neighbours' sums visible to it empties the caches of eight dies, and cost
 // 888 workgroups 25 us.)
@@ -27,24 +27,34 @@ constexpr int GRAD_BLOCKS = 2048;                                  // workgroups
 constexpr int GRAD_MOST = 65536;                                   // tensors
 
 struct GradEntry { const void* grad; void* out; long long n; int first, bf16; };      // first: number of its first chunk
+struct alignas(16) GradChunk { const char* grad; char* out; int whole, rest, bf16, unused; };        // units of 16 bytes, elements behind them
+
 __host__ __device__ long long grad_chunk_elements(int bf16) { return bf16 ? GRAD_CHUNK / 2 : GRAD_CHUNK / 4; }
 
-// which tensor each chunk belongs to, behind the tensors
-__host__ __device__ size_t grad_map_offset(int count) { return (size_t)count * sizeof(GradEntry); }
-
 constexpr int GRAD_BATCH = 64;                                     // entries of a launch's arguments
-struct GradTableArgs { GradEntry e[GRAD_BATCH]; int from, here; };
+struct GradTableArgs { GradEntry e[GRAD_BATCH]; };
 
-__global__ __launch_bounds__(256) void grad_table_kernel(GradTableArgs a, char* table, int count) {
+__global__ __launch_bounds__(256) void grad_table_kernel(GradTableArgs a, GradChunk* table) {
     const GradEntry e = a.e[blockIdx.x];
-    const int number = a.from + blockIdx.x;
-    if (threadIdx.x == 0) reinterpret_cast<GradEntry*>(table)[number] = e;
-    int* map = reinterpret_cast<int*>(table + grad_map_offset(count));
     const long long per = grad_chunk_elements(e.bf16), chunks = (e.n + per - 1) / per;
-    for (long long i = threadIdx.x; i < chunks; i += 256) map[e.first + i] = number;
+    const int es = e.bf16 ? 2 : 4;
+    for (long long i = threadIdx.x; i < chunks; i += 256) {
+        const long long left = e.n - i * per, here = left < per ? left : per;
+        GradChunk c;
+        c.grad = reinterpret_cast<const char*>(e.grad) + i * GRAD_CHUNK;
+        c.out = e.out ? reinterpret_cast<char*>(e.out) + i * GRAD_CHUNK : nullptr;
+        c.whole = (int)(here * es / 16);
+        c.rest = (int)(here - (long long)c.whole * 16 / es);
+        c.bf16 = e.bf16;
+        c.unused = 0;
+        table[e.first + i] = c;
+    }
 }
 
-struct GradArgs { const char* table; int count, chunks, partials; double* partial; float* norm; float most; };
+// kept: the list is small enough to stay in the memory-side cache from the norm to the scaling, and is read in a way that leaves it there;
+// larger ones are read past it.
+constexpr long long GRAD_KEPT = 128 * 1024 * 1024 / GRAD_CHUNK;
+struct GradArgs { const GradChunk* table; int chunks, kept, partials; double* partial; float* norm; float most; };
 
 // A chunk and what a thread has of it: units of 16 bytes, and an element behind the last whole one.
 struct Chunk {
@@ -56,20 +66,18 @@ struct Chunk {
     __device__ __forceinline__ bool has_tail() const { return (int)threadIdx.x < rest; }
     __device__ __forceinline__ int unit(int j) const { return j * GRAD_THREADS + (int)threadIdx.x; }
     __device__ __forceinline__ void find(const GradArgs& a, int number) {
-        const int t = reinterpret_cast<const int*>(a.table + grad_map_offset(a.count))[number];
-        const GradEntry e = reinterpret_cast<const GradEntry*>(a.table)[t];
-        const long long per = grad_chunk_elements(e.bf16), at = (number - e.first) * per, left = e.n - at;
-        const int here = (int)(left < per ? left : per), es = e.bf16 ? 2 : 4;
-        grad = reinterpret_cast<const char*>(e.grad) + at * es;
-        out = reinterpret_cast<char*>(e.out) + at * es;
-        bf16 = e.bf16;
-        whole = here * es / 16;
-        rest = here - whole * 16 / es;
+        const GradChunk c = a.table[number];
+        grad = c.grad;
+        out = c.out;
+        whole = c.whole;
+        rest = c.rest;
+        bf16 = c.bf16 != 0;
     }
-    __device__ __forceinline__ void load() {
+    __device__ __forceinline__ void place(const Chunk& o) { grad = o.grad; out = o.out; whole = o.whole; rest = o.rest; bf16 = o.bf16; }
+    template <bool ONCE> __device__ __forceinline__ void load() {
 #pragma unroll
         for (int j = 0; j < GRAD_LOADS; ++j)
-            if (unit(j) < whole) v[j] = load_once_anywhere<Anywhere<16, 2>>(grad + unit(j) * 16);
+            if (unit(j) < whole) v[j] = ONCE ? load_once_anywhere<Anywhere<16, 2>>(grad + unit(j) * 16) : *reinterpret_cast<const Anywhere<16, 2>*>(grad + unit(j) * 16);
             else v[j].w[0] = v[j].w[1] = v[j].w[2] = v[j].w[3] = 0;
         tail = 0.0f;
         if (has_tail()) {
@@ -94,7 +102,7 @@ struct Chunk {
             }
         return sum + more;
     }
-    __device__ __forceinline__ void store(double factor) const {
+    template <bool ONCE> __device__ __forceinline__ void store(double factor) const {
         auto times = [factor](float f) { return (float)((double)f * factor); };
 #pragma unroll
         for (int j = 0; j < GRAD_LOADS; ++j) {
@@ -106,7 +114,7 @@ struct Chunk {
                 o.w[q] = bf16 ? pack_bf16x2(times(__uint_as_float(w << 16)), times(__uint_as_float(w & 0xffff0000u)))
                               : __float_as_uint(times(__uint_as_float(w)));
             }
-            *reinterpret_cast<Anywhere<16, 2>*>(out + unit(j) * 16) = o;
+            if (ONCE) store_once_anywhere(out + unit(j) * 16, o); else *reinterpret_cast<Anywhere<16, 2>*>(out + unit(j) * 16) = o;
         }
         if (has_tail()) {
             char* p = out + whole * 16;
@@ -144,14 +152,17 @@ __device__ __forceinline__ float norm_of(const double* partial, int n, double* l
 __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(GradArgs a) {
     __shared__ double lds[GRAD_THREADS / 64];
     double sum = 0.0;
-    Chunk c, next;
+    Chunk c;
     int number = blockIdx.x;
-    if (number < a.chunks) { c.find(a, number); c.load(); }
+    c.find(a, number);
     while (number < a.chunks) {
-        number += gridDim.x;
-        if (number < a.chunks) { next.find(a, number); next.load(); }
+        if (a.kept) c.load<false>(); else c.load<true>();
+        const int next = number + gridDim.x;
+        Chunk n;
+        n.find(a, next < a.chunks ? next : number);
         sum += c.squares();
-        c = next;
+        c.place(n);
+        number = next;
     }
     sum = block_sum(sum, lds);
     if (threadIdx.x == 0) a.partial[blockIdx.x] = sum;
@@ -166,7 +177,7 @@ __global__ __launch_bounds__(GRAD_THREADS * GRAD_AT_ONCE) void grad_norm_alone_k
     for (int number = q; number < a.chunks; number += GRAD_AT_ONCE) {
         Chunk c;
         c.find(a, number);
-        c.load();
+        c.load<true>();
         sum += c.squares();
     }
     lds[q][tid] = sum;
@@ -185,13 +196,14 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_join_kernel(GradArgs a) {
     if (threadIdx.x == 0) *a.norm = norm;
 }
 
-// The chunks that the norm read last are the first here: they are still in the memory-side cache.  a.partials: so many partial sums
+// a.partials: so many partial sums
 // are to be added up and their norm written down; 0: the norm is there.
 __global__ __launch_bounds__(GRAD_THREADS) void grad_scale_kernel(GradArgs a) {
     __shared__ double lds[GRAD_THREADS / 64];
-    Chunk c, next;
+    Chunk c;
     int back = blockIdx.x;
-    if (back < a.chunks) { c.find(a, a.chunks - 1 - back); c.load(); }
+    c.find(a, a.chunks - 1 - back);
+    if (a.kept) c.load<false>(); else c.load<true>();
     float norm;
     if (a.partials > 0) {
         norm = norm_of(a.partial, a.partials, lds);
@@ -201,11 +213,17 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_scale_kernel(GradArgs a) {
     }
     // (NaN and infinity: nothing is scaled)
     const double factor = norm > a.most && norm < __builtin_inff() ? (double)a.most / (double)norm : 1.0;
-    while (back < a.chunks) {
-        back += gridDim.x;
-        if (back < a.chunks) { next.find(a, a.chunks - 1 - back); next.load(); }
-        if (factor != 1.0 || c.grad != c.out) c.store(factor);
-        c = next;
+    while (true) {
+        const int next = back + gridDim.x;
+        Chunk n;
+        n.find(a, a.chunks - 1 - (next < a.chunks ? next : back));
+        if (factor != 1.0 || c.grad != c.out) {
+            if (a.kept) c.store<false>(factor); else c.store<true>(factor);
+        }
+        if (next >= a.chunks) break;
+        back = next;
+        c.place(n);
+        if (a.kept) c.load<false>(); else c.load<true>();
     }
 }
 
@@ -270,7 +288,7 @@ extern "C" moe_status moe_grad_bytes(const moe_grad_tensor* tensors, int32_t cou
     long long chunks;
     MOE_TRY(moe::grad_check(tensors, count, &chunks));
     if (!table || !scratch) return MOE_ERR_NULL;
-    *table = moe::grad_map_offset(count) + (size_t)chunks * 4 + 16;
+    *table = ((size_t)chunks + 1) * sizeof(moe::GradChunk);
     *scratch = (size_t)moe::grad_blocks(chunks) * 8;
     return MOE_OK;
 }
@@ -283,19 +301,19 @@ extern "C" moe_status moe_grad_table(const moe_grad_tensor* tensors, int32_t cou
     MOE_TRY(moe::grad_overlaps(tensors, count));
     moe_grad_list l = {table, chunks, count, 1};
     hipStream_t s = (hipStream_t)stream;
-    int first = 0;
+    int first = 0, here = 0;
     moe::GradTableArgs a = {};
     for (int i = 0; i < count; ++i) {
-        moe::GradEntry& e = a.e[a.here++];
-        e = {tensors[i].grad, tensors[i].out, (long long)tensors[i].n, first, tensors[i].dtype == MOE_BF16};
-        const long long per = moe::grad_chunk_elements(e.bf16);
-        first += (int)((e.n + per - 1) / per);
-        if (e.n > 0 && !e.out) l.outs = 0;
-        if (a.here == moe::GRAD_BATCH || i == count - 1) {
-            moe::grad_table_kernel<<<a.here, 256, 0, s>>>(a, (char*)table, count);
+        const long long per = moe::grad_chunk_elements(tensors[i].dtype == MOE_BF16);
+        if (tensors[i].n > 0) {
+            a.e[here++] = {tensors[i].grad, tensors[i].out, (long long)tensors[i].n, first, tensors[i].dtype == MOE_BF16};
+            first += (int)((tensors[i].n + per - 1) / per);
+            if (!tensors[i].out) l.outs = 0;
+        }
+        if (here == moe::GRAD_BATCH || (here > 0 && i == count - 1)) {
+            moe::grad_table_kernel<<<here, 256, 0, s>>>(a, (moe::GradChunk*)table);
             MOE_CHECK_LAUNCH();
-            a.from += a.here;
-            a.here = 0;
+            here = 0;
         }
     }
     *list = l;
@@ -307,9 +325,9 @@ namespace moe {
 namespace {
 
 // The partial sums, or (few chunks: a launch less) the norm itself, *partials = 0.
-moe_status grad_sums(const moe_grad_list* l, float* norm, void* scratch, hipStream_t s, GradArgs* a) {
+moe_status grad_sums(const moe_grad_list* l, int kept, float* norm, void* scratch, hipStream_t s, GradArgs* a) {
     const int blocks = grad_blocks(l->chunks);
-    *a = {(const char*)l->table, l->tensors, (int)l->chunks, 0, (double*)scratch, norm, 0.0f};
+    *a = {(const GradChunk*)l->table, (int)l->chunks, kept, 0, (double*)scratch, norm, 0.0f};
     if (l->chunks <= GRAD_ALONE) {
         grad_norm_alone_kernel<<<1, dim3(GRAD_THREADS, GRAD_AT_ONCE), 0, s>>>(*a);
     } else {
@@ -331,7 +349,7 @@ extern "C" moe_status moe_grad_norm(const moe_grad_list* list, float* norm, void
     {
         moe::ProfScope prof(moe::PK_GRADS, s);
         moe::GradArgs a;
-        MOE_TRY(moe::grad_sums(list, norm, scratch, s, &a));
+        MOE_TRY(moe::grad_sums(list, 0, norm, scratch, s, &a));
         if (a.partials) {
             moe::grad_join_kernel<<<1, moe::GRAD_THREADS, 0, s>>>(a);
             MOE_CHECK_LAUNCH();
@@ -346,7 +364,7 @@ extern "C" moe_status moe_grad_scale(const moe_grad_list* list, float most, cons
     if (!(most >= 0.0f) || !std::isfinite(most)) return MOE_ERR_SHAPE;
     if (!norm || !list->outs) return MOE_ERR_NULL;
     if (list->chunks == 0) return MOE_OK;
-    moe::GradArgs a = {(const char*)list->table, list->tensors, (int)list->chunks, 0, nullptr, const_cast<float*>(norm), most};
+    moe::GradArgs a = {(const moe::GradChunk*)list->table, (int)list->chunks, 0, 0, nullptr, const_cast<float*>(norm), most};
     hipStream_t s = (hipStream_t)stream;
     {
         moe::ProfScope prof(moe::PK_GRADS, s);
@@ -366,7 +384,7 @@ extern "C" moe_status moe_grad_clip(const moe_grad_list* list, float most, float
     {
         moe::ProfScope prof(moe::PK_GRADS, s);
         moe::GradArgs a;
-        MOE_TRY(moe::grad_sums(list, norm, scratch, s, &a));
+        MOE_TRY(moe::grad_sums(list, list->chunks <= moe::GRAD_KEPT, norm, scratch, s, &a));
         if (list->chunks > 0) {
             a.most = most;
             moe::grad_scale_kernel<<<moe::grad_blocks(list->chunks), moe::GRAD_THREADS, 0, s>>>(a);

@@ -276,6 +276,31 @@ template <typename V> __device__ __forceinline__ V wave_max(V v) {
     return larger(larger(of_lane(v, 0), of_lane(v, 16)), larger(of_lane(v, 32), of_lane(v, 48)));
 }
 
+// The k largest of what a wavefront's lanes have, VALUES neighbouring experts' each: lane j returns the j-th, -1 where nothing above -inf is left.
+template <int VALUES, typename F> __device__ __forceinline__ int choose_largest(const RouterArgs& a, const F* values) {
+    constexpr F NONE = -(F)__builtin_inf();
+    const int lane = threadIdx.x & 63, e0 = lane * VALUES;
+    F s[VALUES];
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) s[v] = values[v];
+    int chosen = -1;
+    for (int j = 0; j < a.k; ++j) {
+        F mine = s[0];
+#pragma unroll
+        for (int v = 1; v < VALUES; ++v) mine = larger(mine, s[v]);
+        const F most = wave_max(mine);
+        if (!(most > NONE)) break;
+        int at = 0;
+#pragma unroll
+        for (int v = VALUES - 1; v >= 0; --v) at = s[v] == most ? e0 + v : at;
+        at = of_lane(at, __builtin_ctzll(__ballot(mine == most)));       // the lowest lane has the lowest experts
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) s[v] = at == e0 + v ? NONE : s[v];
+        if (lane == j) chosen = at;
+    }
+    return chosen;
+}
+
 // The choices of one token by 64-bit scores, by a whole wavefront, whose lanes have its logits (NaN counts as -inf), VALUES
 // neighbouring ones each: lane j returns the j-th.  *soft: of a softmax.  What counts is the length of the chain.
 template <int VALUES>
@@ -300,8 +325,7 @@ __device__ __forceinline__ int choose_exactly(const RouterArgs& a, const float* 
             sum = (of_lane(sum, 0) + of_lane(sum, 16)) + (of_lane(sum, 32) + of_lane(sum, 48));
             *soft = {m, sum > 0.0f ? 1.0f / sum : 0.0f};
         }
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) s[v] = 0.0;
+        return choose_largest<VALUES>(a, l);
     } else if (a.sigmoid) {
 #pragma unroll
         for (int v = 0; v < VALUES; ++v) s[v] = 1.0 / (1.0 + exp(-(double)l[v]));
@@ -373,22 +397,7 @@ __device__ __forceinline__ int choose_exactly(const RouterArgs& a, const float* 
 #pragma unroll
     for (int v = 0; v < VALUES; ++v)
         if (!by_score && s[v] > NONE) s[v] = (double)l[v];
-    int chosen = -1;
-    for (int j = 0; j < a.k; ++j) {
-        double mine = s[0];
-#pragma unroll
-        for (int v = 1; v < VALUES; ++v) mine = larger(mine, s[v]);
-        const double most = wave_max(mine);
-        if (!(most > NONE)) break;
-        int at = 0;
-#pragma unroll
-        for (int v = VALUES - 1; v >= 0; --v) at = s[v] == most ? e0 + v : at;
-        at = of_lane(at, __builtin_ctzll(__ballot(mine == most)));       // the lowest lane has the lowest experts
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) s[v] = at == e0 + v ? NONE : s[v];
-        if (lane == j) chosen = at;
-    }
-    return chosen;
+    return choose_largest<VALUES>(a, s);
 }
 template <typename T, int VALUES>
 __device__ __forceinline__ int choose_exactly(const RouterArgs& a, const T* row) {

@@ -20,6 +20,11 @@ template <typename V> __device__ __forceinline__ V load_once_anywhere(const void
     return __builtin_bit_cast(V, (wide_u4)__builtin_nontemporal_load(reinterpret_cast<const wide_u4_2*>(p)));
 }
 
+template <typename V> __device__ __forceinline__ void store_once_anywhere(void* p, const V& v) {
+    static_assert(sizeof(V) == 16, "16 bytes");
+    __builtin_nontemporal_store((wide_u4_2)__builtin_bit_cast(wide_u4, v), reinterpret_cast<wide_u4_2*>(p));
+}
+
 // four neighbouring columns, `left` of which are in the row
 __device__ __forceinline__ void store_columns(float* p, const float* v, int left) {
     if (left >= 4) {
