@@ -344,8 +344,8 @@ moe_status moe_launch_counts(int64_t out[3], int32_t reset);
  * GeLU-backward epilogue, 3 input-gradient GEMM, 4 weight-gradient GEMMs,
  * 5 dispatch, 6 combine, 7 dispatch backward, 8 gate, 9 slot assignment,
  * 10 gate backward, 11 norm, 12 norm backward, 13 router, 14 router backward, 15 products on
- * 4-bit weights, 16 the layer for a few tokens (each one whole call), 17 dense products (their input gradients count in 3, their
- * weight gradients in 4), 18 activation backward, 19 gradients' norm and clipping.  Arrays of `kinds` entries (at most 20).  Host only; not
+ * 4-bit weights, 16 the layer for a few tokens (each one whole call), 17 dense products and their input gradients (their weight
+ * gradients count in 4), 18 activation backward, 19 gradients' norm and clipping.  Arrays of `kinds` entries (at most 20).  Host only; not
  * for use under stream capture. */
 moe_status moe_profile_enable(int32_t on);
 moe_status moe_profile_read(int32_t kinds, int64_t* launches, double* total_ms);
@@ -517,11 +517,12 @@ moe_status moe_linear_fwd(const moe_linear_config* cfg, const void* x, const voi
  *   dbias [N] float, may be NULL; scratch as above (needed with dbias only). */
 moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, const void* z, void* dz, float* dbias, void* scratch, void* stream);
 
-/* dx = dz W^T;  dW (+)= x^T dz, float, in an order that depends on the sizes.
- *   dz [T,N]; x [T,K] (may be NULL without dW); W [K,N] (may be NULL without dx); dx [T,K] out, may be NULL; dW [K,N] float, may
- *   be NULL; scratch as above. */
-moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, void* dx, float* dW,
-                          void* scratch, void* stream);
+/* dx = dz W^T + add;  dW (+)= x^T dz, float, in an order that depends on the sizes.
+ *   dz [T,N]; x [T,K] (may be NULL without dW); W [K,N] (may be NULL without dx); add [T,K]: what reaches x past the product, may be
+ *   NULL, may be dx itself, with its stride in any case; dx [T,K] out, may be NULL; dW [K,N] float, may be NULL; scratch as above
+ *   (needed with dW only). */
+moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, const void* add, void* dx,
+                          float* dW, void* scratch, void* stream);
 moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, size_t* bytes);
 
 /* The norm of many tensors together, and clipping by it.  A list of tensors is laid out in device memory once (again when their

@@ -42,7 +42,7 @@ EXPORTS = [
 # Calls that take nothing but pointers (the configuration's and the stream's among them): they are handed over as numbers,
 # a microsecond less per call than as objects, and a decoding step makes these calls one after the other.
 _POINTERS = {"moe_norm_fwd": 9, "moe_norm_bwd": 10, "moe_router_fwd": 7, "moe_router_bwd": 6, "moe_w4_product": 10,
-             "moe_few_forward": 13, "moe_linear_fwd": 9, "moe_act_bwd": 7, "moe_linear_bwd": 8, "moe_grad_norm": 4}
+             "moe_few_forward": 13, "moe_linear_fwd": 9, "moe_act_bwd": 7, "moe_linear_bwd": 9, "moe_grad_norm": 4}
 
 
 class MoEError(RuntimeError):
@@ -561,8 +561,8 @@ def moe_act_bwd(cfg, dy, z, dz, dbias, scratch, stream=None):
     _check(lib().moe_act_bwd(_cfg(cfg), _a(dy), _a(z), _a(dz), _a(dbias), _a(scratch), _h(stream)), "moe_act_bwd")
 
 
-def moe_linear_bwd(cfg, dz, x, W, dx, dW, scratch, stream=None):
-    _check(lib().moe_linear_bwd(_cfg(cfg), _a(dz), _a(x), _a(W), _a(dx), _a(dW), _a(scratch), _h(stream)), "moe_linear_bwd")
+def moe_linear_bwd(cfg, dz, x, W, dx, dW, scratch, add=None, stream=None):
+    _check(lib().moe_linear_bwd(_cfg(cfg), _a(dz), _a(x), _a(W), _a(add), _a(dx), _a(dW), _a(scratch), _h(stream)), "moe_linear_bwd")
 
 
 class MoEGradTensor(ctypes.Structure):

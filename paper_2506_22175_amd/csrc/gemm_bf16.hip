@@ -1838,7 +1838,7 @@ static bool few_tiles(const GemmArgs& a, int cus) {
 }
 // (one: a single tile's, not the launch's)
 static double tile_time(const TileCost& c, int lay, int epi, const GemmArgs& a, int cus, bool one = false) {
-    const int which = epi == EPI_GELU || epi == EPI_LINEAR ? 1 : epi == EPI_DGELU ? 2 : epi == EPI_STORE_F32 ? 3 : epi == EPI_ACCUM_F32 ? 4 : 0;
+    const int which = epi == EPI_GELU || (epi == EPI_LINEAR && a.act != MOE_ACT_NONE) ? 1 : epi == EPI_DGELU ? 2 : epi == EPI_STORE_F32 ? 3 : epi == EPI_ACCUM_F32 ? 4 : 0;
     const int segs = a.k_segs > 1 ? a.k_segs : 1;
     const double kt = lay == GEMM_TN ? (double)((a.mean_rows + 63) / 64) * segs : (double)((a.K + 63) / 64);
     long long whole, tail = 0;                       // tiles; those of the experts' last, partly filled tile rows
@@ -2031,6 +2031,7 @@ moe_status gemm_bf16(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStr
     if (lay == GEMM_NN && epi == EPI_GELU) return launch_cfg<GEMM_NN, EPI_GELU>(a, s);
     if (lay == GEMM_NN && epi == EPI_SCATTER) return launch_cfg<GEMM_NN, EPI_SCATTER>(a, s);
     if (lay == GEMM_NN && epi == EPI_LINEAR) return launch_cfg<GEMM_NN, EPI_LINEAR>(a, s);
+    if (lay == GEMM_NT && epi == EPI_LINEAR) return launch_cfg<GEMM_NT, EPI_LINEAR>(a, s);
     if (lay == GEMM_NT && epi == EPI_STORE) return launch_cfg<GEMM_NT, EPI_STORE>(a, s);
     if (lay == GEMM_NT && epi == EPI_DGELU) return launch_cfg<GEMM_NT, EPI_DGELU>(a, s);
     if (lay == GEMM_TN && epi == EPI_STORE_F32) return launch_cfg<GEMM_TN, EPI_STORE_F32>(a, s);

@@ -286,6 +286,7 @@ moe_status gemm_f32(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStre
     if (lay == GEMM_NN && epi == EPI_GELU) return launch_f32<GEMM_NN, EPI_GELU>(a, s);
     if (lay == GEMM_NN && epi == EPI_SCATTER) return launch_f32<GEMM_NN, EPI_SCATTER>(a, s);
     if (lay == GEMM_NN && epi == EPI_LINEAR) return launch_f32<GEMM_NN, EPI_LINEAR>(a, s);
+    if (lay == GEMM_NT && epi == EPI_LINEAR) return launch_f32<GEMM_NT, EPI_LINEAR>(a, s);
     if (lay == GEMM_NT && epi == EPI_STORE) return launch_f32<GEMM_NT, EPI_STORE>(a, s);
     if (lay == GEMM_NT && epi == EPI_DGELU) return launch_f32<GEMM_NT, EPI_DGELU>(a, s);
     if (lay == GEMM_TN && epi == EPI_STORE_F32) return launch_f32<GEMM_TN, EPI_STORE_F32>(a, s);

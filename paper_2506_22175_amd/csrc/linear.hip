@@ -74,6 +74,9 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
 }
 
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
+// A dz of more bytes than this, which would not be found in the memory-side cache by the products behind it anyway, is written past the caches
+// (268 MB: 153 us so, 164 with ordinary stores).
+constexpr long long ACT_PAST = 128ll << 20;
 // Wavefronts side by side, and blocks of rows: enough for the chip, of two rows to a wavefront at least.
 int act_beside(const LinearDims& d) { return d.N > 2 * ACT_COLS ? 4 : d.N > ACT_COLS ? 2 : 1; }
 int act_blocks(const LinearDims& d) {
@@ -156,6 +159,7 @@ struct ActBwdArgs {
     const void* dy; const void* z; void* dz; float* part;       // part: [blocks][N], or NULL
     long long ldy, ldz;
     int T, N, act, rows, beside;                                // rows of a workgroup; wavefronts side by side
+    int past;                                                   // dz goes past the caches
 };
 
 __device__ __forceinline__ void load_eight_once(Raw8<bf16_t>& r, const bf16_t* p) { r.u = load_once<uint4>(p); }
@@ -198,10 +202,17 @@ __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(ActBwdArgs a) {
                 if (a.dz) {
                     T* o = reinterpret_cast<T*>(a.dz) + t * a.ldz + n;
                     if constexpr (sizeof(T) == 2) {
-                        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
+                        const uint4 w = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
+                        if (a.past) store_once_anywhere(o, w); else *reinterpret_cast<uint4*>(o) = w;
                     } else {
-                        reinterpret_cast<float4*>(o)[0] = make_float4(d[0], d[1], d[2], d[3]);
-                        reinterpret_cast<float4*>(o)[1] = make_float4(d[4], d[5], d[6], d[7]);
+                        const float4 lo = make_float4(d[0], d[1], d[2], d[3]), hi = make_float4(d[4], d[5], d[6], d[7]);
+                        if (a.past) {
+                            store_once_anywhere(o, lo);
+                            store_once_anywhere(o + 4, hi);
+                        } else {
+                            reinterpret_cast<float4*>(o)[0] = lo;
+                            reinterpret_cast<float4*>(o)[1] = hi;
+                        }
                     }
                 }
             }
@@ -259,10 +270,9 @@ moe_status join_parts(const float* part, int parts, long long size, float* out, 
     return MOE_OK;
 }
 
-// The rows of each block, for the GEMMs: of the input gradient's, and of the weight gradient's 64 further on.
-__global__ void block_counts_kernel(int* counts, int T, int block, int wblock) {
-    const int per = threadIdx.x < 64 ? block : wblock;
-    const long long left = T - (long long)(threadIdx.x & 63) * per;
+// The rows of each block, for the weight gradient's GEMM.
+__global__ void block_counts_kernel(int* counts, int T, int per) {
+    const long long left = T - (long long)threadIdx.x * per;
     counts[threadIdx.x] = left <= 0 ? 0 : left < per ? (int)left : per;
 }
 
@@ -282,7 +292,7 @@ extern "C" moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, siz
     if (!bytes) return MOE_ERR_NULL;
     *bytes = 0;
     if (d.T == 0) return MOE_OK;
-    size_t most = 512;                                                     // block_counts_kernel's
+    size_t most = 256;                                                     // block_counts_kernel's
     if (d.wblocks > 1) most += (size_t)d.wblocks * d.K * d.N * 4;
     const size_t act = (size_t)moe::act_blocks(d) * d.N * 4;
     if (act > most) most = act;
@@ -334,7 +344,8 @@ extern "C" moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, 
     if (!dy || (!dz && !dbias) || (!z && d.act != MOE_ACT_NONE) || (dbias && !scratch)) return MOE_ERR_NULL;
     if (!moe::aligned16(dy) || !moe::aligned16(z) || !moe::aligned16(dz) || !moe::aligned16(scratch)) return MOE_ERR_UNSUPPORTED;
     const int blocks = moe::act_blocks(d);
-    moe::ActBwdArgs a = {dy, z, dz, dbias ? (float*)scratch : nullptr, d.ldy, d.ldz, d.T, d.N, d.act, moe::up(d.T, blocks), moe::act_beside(d)};
+    moe::ActBwdArgs a = {dy, z, dz, dbias ? (float*)scratch : nullptr, d.ldy, d.ldz, d.T, d.N, d.act, moe::up(d.T, blocks), moe::act_beside(d),
+                         (long long)d.T * d.N * (d.bf16 ? 2 : 4) > moe::ACT_PAST};
     const int parts = moe::up(d.T, a.rows);
     {
         moe::ProfScope prof(moe::PK_ACT_BWD, s);
@@ -349,8 +360,8 @@ extern "C" moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, 
     return MOE_OK;
 }
 
-extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, void* dx, float* dW,
-                                     void* scratch, void* stream) {
+extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, const void* add, void* dx,
+                                     float* dW, void* scratch, void* stream) {
     moe::LinearDims d;
     MOE_TRY(moe::linear_dims(cfg, &d));
     hipStream_t s = (hipStream_t)stream;
@@ -358,30 +369,31 @@ extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* d
         if (dW && d.overwrite) MOE_TRY(moe::join_parts(nullptr, 0, (long long)d.K * d.N, dW, 1, s));
         return MOE_OK;
     }
-    if (!dz || (!dx && !dW) || (dx && !W) || (dW && !x) || !scratch) return MOE_ERR_NULL;
-    if (!moe::aligned16(dz) || !moe::aligned16(x) || !moe::aligned16(W) || !moe::aligned16(dx) || !moe::aligned16(dW) || !moe::aligned16(scratch))
+    if (!dz || (!dx && !dW) || (dx && !W) || (dW && (!x || !scratch))) return MOE_ERR_NULL;
+    if (!moe::aligned16(dz) || !moe::aligned16(x) || !moe::aligned16(W) || !moe::aligned16(add) || !moe::aligned16(dx) || !moe::aligned16(dW) ||
+        !moe::aligned16(scratch))
         return MOE_ERR_UNSUPPORTED;
-    int* counts = (int*)scratch;
-    float* parts = (float*)((char*)scratch + 512);
-    moe::block_counts_kernel<<<1, 128, 0, s>>>(counts, d.T, d.block, d.wblock);
-    MOE_CHECK_LAUNCH();
     if (dx) {
         moe::GemmArgs g = {};
         g.A = dz; g.B = W; g.C = dx;
         g.a_estride = d.block * d.ldz; g.b_estride = 0; g.c_estride = d.block * d.ldx;
         g.lda = (int)d.ldz; g.ldb = d.N; g.ldc = (int)d.ldx;
-        g.counts = counts;
         g.E = d.blocks; g.Cp = d.block; g.mean_rows = moe::up(d.T, d.blocks);
         g.N = d.K; g.K = d.N;
-        MOE_TRY(moe::gemm(d, moe::GEMM_NT, moe::EPI_STORE, g, s));
+        g.R = add; g.ldr = (int)d.ldx; g.act = MOE_ACT_NONE; g.rows = d.T;
+        MOE_TRY(moe::gemm(d, moe::GEMM_NT, moe::EPI_LINEAR, g, s));
     }
     if (dW) {
+        int* counts = (int*)scratch;
+        float* parts = (float*)((char*)scratch + 256);
+        moe::block_counts_kernel<<<1, 64, 0, s>>>(counts, d.T, d.wblock);
+        MOE_CHECK_LAUNCH();
         moe::GemmArgs g = {};
         const bool split = d.wblocks > 1;
         g.A = x; g.B = dz; g.C = split ? parts : dW;
         g.a_estride = d.wblock * d.ldx; g.b_estride = d.wblock * d.ldz; g.c_estride = (long long)d.K * d.N;
         g.lda = (int)d.ldx; g.ldb = (int)d.ldz; g.ldc = d.N;
-        g.counts = counts + 64;
+        g.counts = counts;
         g.E = d.wblocks; g.Cp = d.wblock; g.mean_rows = moe::up(d.T, d.wblocks);
         g.Mo = d.K; g.N = d.N;
         MOE_TRY(moe::gemm(d, moe::GEMM_TN, split || d.overwrite ? moe::EPI_STORE_F32 : moe::EPI_ACCUM_F32, g, s));

@@ -224,6 +224,14 @@ def test_product_backward(T, K, N, dtype):
         B.moe_linear_bwd(cfg, dz, None, W, dx2, None, scratch)
         B.moe_linear_bwd(cfg, dz, x, None, None, dW2, scratch)
         assert torch.equal(dx2, dx) and torch.equal(dW2, dW)
+        # with what reaches x past the product, in its place or another
+        add = _apart(T, K, K + apart, DT[dtype], g, 9.0)[1]
+        A = add.double()
+        B.moe_linear_bwd(cfg, dz, None, W, dx2, None, None, add=add)
+        want, err = Z @ V.t() + A, 2 * (N + 20) * U * (Z.abs() @ V.abs().t() + A.abs())
+        assert ((dx2.double() - want).abs() <= err + HALF[dtype] * (want.abs() + err)).all()
+        B.moe_linear_bwd(cfg, dz, None, W, add, None, None, add=add)
+        assert torch.equal(add, dx2)
 
 
 def test_no_rows_have_no_gradient():

@@ -44,7 +44,7 @@ def test_few_needs_its_pointers_and_their_alignment():
     assert B.moe_few_scratch_bytes(cfg) > 0
 
 
-def _linear(cfg, fwd=(P,) * 7, act=(P,) * 5, bwd=(P,) * 6):
+def _linear(cfg, fwd=(P,) * 7, act=(P,) * 5, bwd=(P,) * 7):
     c, lib = ctypes.byref(cfg), B.lib()
     return lib.moe_linear_fwd(c, *fwd, None), lib.moe_act_bwd(c, *act, None), lib.moe_linear_bwd(c, *bwd, None)
 
@@ -71,18 +71,18 @@ def test_linear_needs_its_pointers_and_their_alignment():
             assert _linear(cfg, act=[NONE if i == missing else P for i in range(5)])[1] == NULL
         assert _linear(cfg, act=(P, P, NONE, NONE, P))[1] == NULL          # nothing to compute
         assert _linear(cfg, act=(P, P, P, P, NONE))[1] == NULL             # a bias gradient without scratch
-        for missing in (0, 1, 2, 5):                             # dz, x, W, scratch
-            assert _linear(cfg, bwd=[NONE if i == missing else P for i in range(6)])[2] == NULL
-        assert _linear(cfg, bwd=(P, P, P, NONE, NONE, P))[2] == NULL
+        for missing in (0, 1, 2, 6):                             # dz, x, W, scratch
+            assert _linear(cfg, bwd=[NONE if i == missing else P for i in range(7)])[2] == NULL
+        assert _linear(cfg, bwd=(P, P, P, P, NONE, NONE, P))[2] == NULL
         for odd in (0, 1, 3, 4, 5, 6):                           # all but the bias
             assert _linear(cfg, fwd=[ODD if i == odd else P for i in range(7)])[0] == UNSUPPORTED
         for odd in (0, 1, 2, 4):
             assert _linear(cfg, act=[ODD if i == odd else P for i in range(5)])[1] == UNSUPPORTED
-        for odd in range(6):
-            assert _linear(cfg, bwd=[ODD if i == odd else P for i in range(6)])[2] == UNSUPPORTED
+        for odd in range(7):
+            assert _linear(cfg, bwd=[ODD if i == odd else P for i in range(7)])[2] == UNSUPPORTED
     lib = B.lib()
     assert lib.moe_linear_fwd(None, *(P,) * 7, None) == NULL and lib.moe_act_bwd(None, *(P,) * 5, None) == NULL
-    assert lib.moe_linear_bwd(None, *(P,) * 6, None) == NULL
+    assert lib.moe_linear_bwd(None, *(P,) * 7, None) == NULL
 
 
 def _tensors(*entries):
@@ -156,7 +156,7 @@ def test_grad_table_has_room_for_every_chunk():
 def test_a_batch_without_tokens_is_no_error_and_launches_nothing():
     before = B.moe_launch_counts()
     assert _few(B.make_few_config(**{**OK, "T": 0}), (NONE,) * 11) == 0
-    assert _linear(B.make_linear_config(0, 64, 64), (NONE,) * 7, (NONE,) * 5, (NONE,) * 6) == (0, 0, 0)
+    assert _linear(B.make_linear_config(0, 64, 64), (NONE,) * 7, (NONE,) * 5, (NONE,) * 7) == (0, 0, 0)
     assert B.moe_few_scratch_bytes(B.make_few_config(**{**OK, "T": 0})) == 0
     assert B.moe_linear_scratch_bytes(B.make_linear_config(0, 64, 64)) == 0
     assert B.moe_launch_counts() == before
