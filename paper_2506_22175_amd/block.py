@@ -2,10 +2,12 @@
 the norm, the gate's logits, the router, the experts, the weighted sum; and the same block serving, its experts in 4 bits.
 
     h = x + residual;  y = h / sqrt(mean(h^2) + eps) * gain;  logits = y Wg;  idx, w = router(logits, bias)
-    out[t] = sum over j of w[t,j] * gelu(y[t] W1[idx[t,j]]) W2[idx[t,j]]
+    out[t] = sum over j of w[t,j] * gelu(y[t] W1[idx[t,j]]) W2[idx[t,j]]  [+ gelu(y[t] V1 + b1) V2 + b2]
 
-out and h are what the next block adds up.  Training (`Block`) has a capacity per expert and drops what is beyond; serving
-(`Served`) drops nothing.  All buffers are made once, so that each pass may be captured into a HIP graph after it has run once.
+out and h are what the next block adds up; V1, b1, V2, b2 are a shared expert that every token goes through, if there is one.
+Training (`Block`) has a capacity per expert and drops what is beyond, and ends with the gradients clipped by their norm; serving
+drops nothing: from 4-bit weights (`Served`), or a few tokens at a time from the trained weights as they are (`Few`).  All buffers are
+made once, so that each pass may be captured into a HIP graph after it has run once.
 
     python -m paper_2506_22175_amd.block          # times both on the GPU
 """
@@ -20,12 +22,48 @@ from . import binding as B
 _TORCH = {B.MOE_F32: torch.float32, B.MOE_BF16: torch.bfloat16}
 
 
+class Shared:
+    """The shared expert's two products for T rows of M: weights V1 [M,N], V2 [N,M] of `dtype`, biases float or None.  With `training`
+    its gradients dV1, dV2, db1, db2 (float) are overwritten by backward."""
+
+    def __init__(self, T, V1, V2, b1=None, b2=None, training=False, device="cuda:0"):
+        (M, N), dtype = V1.shape, B.MOE_F32 if V1.dtype == torch.float32 else B.MOE_BF16
+        self.V1, self.V2, self.b1, self.b2 = V1, V2, b1, b2
+        self.first = B.make_linear_config(T, M, N, dtype, B.MOE_ACT_GELU, 1)
+        self.second = B.make_linear_config(T, N, M, dtype, B.MOE_ACT_NONE, 1)
+        self.a = torch.empty((T, N), dtype=V1.dtype, device=device)
+        self.z = self.da = None
+        if training:
+            self.z, self.da = torch.empty_like(self.a), torch.empty_like(self.a)
+            self.dV1, self.dV2 = (torch.empty(V.shape, dtype=torch.float32, device=device) for V in (V1, V2))
+            self.db1, self.db2 = (None if b is None else torch.empty_like(b) for b in (b1, b2))
+        need = max(B.moe_linear_scratch_bytes(c) for c in (self.first, self.second))
+        self.scratch = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+
+    def forward(self, y, out):
+        """out += the expert's rows for y."""
+        B.moe_linear_fwd(self.first, y, self.V1, self.b1, None, self.z, self.a, self.scratch)
+        B.moe_linear_fwd(self.second, self.a, self.V2, self.b2, out, None, out, self.scratch)
+
+    def backward(self, y, dout, dy):
+        """dy += the gradient of y."""
+        if self.b2 is not None:
+            B.moe_act_bwd(self.second, dout, None, None, self.db2, self.scratch)
+        B.moe_linear_bwd(self.second, dout, self.a, self.V2, self.da, self.dV2, self.scratch)
+        B.moe_act_bwd(self.first, self.da, self.z, self.da, self.db1, self.scratch)
+        B.moe_linear_bwd(self.first, self.da, y, self.V1, dy, self.dV1, self.scratch, add=dy)
+
+    def gradients(self):
+        return [g for g in (self.dV1, self.db1, self.dV2, self.db2) if g is not None]
+
+
 class Block:
     """Training.  Weights: gain [M] float, Wg [M,E], W1 [E,M,H], W2 [E,H,M] of `dtype`; bias [E] float or None moves the
-    router's choice and not its weights (its gradient is none: it is set from `load`, the tokens counted per expert)."""
+    router's choice and not its weights (its gradient is none: it is set from `load`, the tokens counted per expert).
+    shared: (V1, V2, b1, b2) of a shared expert, biases or None, or None."""
 
     def __init__(self, T, M, H, E, k, gain, Wg, W1, W2, bias=None, capacity_factor=1.25, dtype=B.MOE_BF16, eps=1e-6,
-                 scores=B.MOE_SOFTMAX, renormalize=0, groups=1, group_k=1, scale=1.0, device="cuda:0"):
+                 scores=B.MOE_SOFTMAX, renormalize=0, groups=1, group_k=1, scale=1.0, device="cuda:0", shared=None):
         self.gain, self.Wg, self.W1, self.W2, self.bias = gain, Wg, W1, W2, bias
         self.layer = B.make_config(T, M, H, E, k, capacity_factor, 1, dtype, 0, 1)
         self.norm = B.make_norm_config(T, M, eps, dtype, grad_overwrite=1)
@@ -48,6 +86,12 @@ class Block:
         self.slot_scratch = new(B.moe_slot_scratch_bytes(self.layer), dtype=torch.uint8)
         self.gate_scratch = new(B.moe_gate_scratch_bytes(self.layer), dtype=torch.uint8)
         self.norm_scratch = new(B.moe_norm_scratch_bytes(self.norm), dtype=torch.uint8)
+        self.shared = None if shared is None else Shared(T, *shared, training=True, device=device)
+        # the gradients' list is laid out once: backward writes to the same memory every time
+        self.gradients = [self.dgain, self.dWg, self.dW1, self.dW2] + ([] if shared is None else self.shared.gradients())
+        self.grad_list = B.make_grad_list(self.gradients, self.gradients)
+        self.grad_norm = new(1, dtype=f32)
+        self.grad_scratch = new(B.moe_grad_scratch_bytes(self.grad_list), dtype=torch.uint8)
 
     def forward(self, x, residual=None):
         """(out, h); `load` counts on."""
@@ -59,19 +103,27 @@ class Block:
         B.moe_dispatch(self.layer, 0, self.y, self.slot, self.di)
         B.moe_expert_ffn_fwd(self.layer, 0, self.di, self.counts, self.W1, self.W2, self.z, self.a, self.do)
         B.moe_combine(self.layer, 0, self.do, self.slot, self.topk_w, self.out)
+        if self.shared:
+            self.shared.forward(self.y, self.out)
         return self.out, self.h
 
     def backward(self, dout, dh=None):
-        """From the gradients of out and h that of x (and of residual alike); dgain, dWg, dW1, dW2 are overwritten.  Once
-        per forward: what forward kept of the experts' inner rows is used up."""
+        """From the gradients of out and h that of x (and of residual alike); `gradients` are overwritten.  Once per forward: what forward kept of the experts' inner rows is used up."""
         B.moe_dispatch(self.layer, 0, dout, self.slot, self.ddo, self.do, self.dw)
         B.moe_expert_ffn_bwd(self.layer, 0, False, self.di, self.z, self.ddo, self.counts, self.slot_w, self.W1, self.W2,
                              self.dz, self.ddi, self.dW1, self.dW2, None)
         B.moe_router_bwd(self.router, self.logits, self.topk_idx, self.dw, self.dlogits)
         B.moe_gate_weight_grad(self.layer, 0, self.y, self.dlogits, self.dWg, self.gate_scratch)
         B.moe_dispatch_bwd(self.layer, 0, self.ddi, self.slot, self.dlogits, self.Wg, self.dy)
+        if self.shared:
+            self.shared.backward(self.y, dout, self.dy)
         B.moe_norm_bwd(self.norm, self.dy, self.h, self.gain, self.rstd, dh, self.dx, self.dgain, self.norm_scratch)
         return self.dx
+
+    def clip(self, most):
+        """Scales all gradients together so that their norm is at most `most`; the norm they had, a float on the GPU."""
+        B.moe_grad_clip(self.grad_list, most, self.grad_norm, self.grad_scratch)
+        return self.grad_norm
 
 
 class Packed:
@@ -131,6 +183,32 @@ class Served:
         return self.out, self.h
 
 
+class Few:
+    """Serving up to 256 tokens at a time from the trained weights as they are (`Block`'s); `shared` as there."""
+
+    def __init__(self, T, k, gain, Wg, W1, W2, bias=None, eps=1e-6, scores=B.MOE_SOFTMAX, renormalize=0, groups=1, group_k=1,
+                 scale=1.0, device="cuda:0", shared=None):
+        E, M, H = W1.shape
+        dtype = B.MOE_F32 if W1.dtype == torch.float32 else B.MOE_BF16
+        self.gain, self.Wg, self.W1, self.W2, self.bias = gain, Wg, W1, W2, bias
+        self.norm = B.make_norm_config(T, M, eps, dtype)
+        self.layer = B.make_few_config(T, M, H, E, k, dtype, scores, groups, group_k, 2, renormalize, scale)
+        self.shared = None if shared is None else Shared(T, *shared, device=device)
+        self.h, self.y, self.out = (torch.empty((T, M), dtype=W1.dtype, device=device) for _ in range(3))
+        self.logits, self.topk_w = (torch.empty((T, n), dtype=torch.float32, device=device) for n in (E, k))
+        self.topk_idx = torch.empty((T, k), dtype=torch.int32, device=device)
+        self.scratch = torch.empty(B.moe_few_scratch_bytes(self.layer), dtype=torch.uint8, device=device)
+
+    def forward(self, x, residual=None):
+        """(out, h)."""
+        B.moe_norm_fwd(self.norm, x, residual, self.gain, self.h, self.y)
+        B.moe_few_forward(self.layer, self.y, self.Wg, None, self.bias, self.W1, self.W2, self.out, self.logits, self.topk_idx,
+                          self.topk_w, self.scratch)
+        if self.shared:
+            self.shared.forward(self.y, self.out)
+        return self.out, self.h
+
+
 def _timed(f, passes):
     f()
     torch.cuda.synchronize()
@@ -149,26 +227,34 @@ def main():
         return (torch.randn(shape, generator=g, device="cuda:0") * std).to(dtype)
 
     weights = (torch.ones(M, device="cuda:0"), normal(M, E, std=0.02), normal(E, M, H, std=0.02), normal(E, H, M, std=0.02))
+    shared = (normal(M, H, std=0.02), normal(H, M, std=0.02), torch.zeros(H, device="cuda:0"), torch.zeros(M, device="cuda:0"))
     T = 4096
-    block, x, residual = Block(T, M, H, E, k, *weights, renormalize=1), normal(T, M), normal(T, M)
-    dout, dh = normal(T, M), normal(T, M)
+    x, residual, dout, dh = (normal(T, M) for _ in range(4))
+    for beside in (None, shared):
+        block = Block(T, M, H, E, k, *weights, renormalize=1, shared=beside)
 
-    def step():
-        block.forward(x, residual)
-        block.backward(dout, dh)
+        def step():
+            block.forward(x, residual)
+            block.backward(dout, dh)
 
-    print(f"training, {T} tokens of {M}/{H}, {E} experts, {k} choices: {_timed(step, 20):.0f} us per step", flush=True)
+        def clipped():
+            step()
+            block.clip(1.0)
+
+        print(f"training, {T} tokens of {M}/{H}, {E} experts{', a shared one' if beside else ''}, {k} choices: {_timed(step, 20):.0f} us "
+              f"per step, {_timed(clipped, 20):.0f} us with its gradients clipped", flush=True)
     packed = Packed(block.W1, block.W2)
     for T in (1, 16):
-        for eight_bits in (False, True):
-            served = Served(T, k, weights[0], weights[1], packed, renormalize=1, eight_bits=eight_bits)
-            x, residual = normal(T, M), normal(T, M)
+        x, residual = normal(T, M), normal(T, M)
+        passes = [(f"4-bit weights, {'e4m3' if eight else 'bf16'} rows", Served(T, k, weights[0], weights[1], packed, renormalize=1, eight_bits=eight))
+                  for eight in (False, True)]
+        passes += [(f"bf16 weights{', a shared expert' if beside else ''}", Few(T, k, *weights, renormalize=1, shared=beside)) for beside in (None, shared)]
+        for name, served in passes:
             eager = _timed(lambda: served.forward(x, residual), 200)
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph):
                 served.forward(x, residual)
-            print(f"serving, {T} tokens, {'e4m3' if eight_bits else 'bf16'} rows: {eager:.1f} us, as a graph "
-                  f"{_timed(graph.replay, 200):.1f} us", flush=True)
+            print(f"serving, {T} tokens, {name}: {eager:.1f} us, as a graph {_timed(graph.replay, 200):.1f} us", flush=True)
 
 
 if __name__ == "__main__":
