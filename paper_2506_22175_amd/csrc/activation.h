@@ -20,10 +20,23 @@ __device__ __forceinline__ float normal_cdf_fast(float z, float* ex) {
 }
 __device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-0.70710678118654752440f * z); }
 
+// z Phi(z) = max(z, 0) - |z| Phi(-|z|), the same form with as few instructions as it takes: with 256 values to a lane they are a tenth of
+// a GEMM's time over K = 2048.  (The maximum is a sum, which keeps a NaN; beyond 32 there is nothing to subtract, and an infinity stays one.)
+__device__ __forceinline__ float gelu_tail_f(float z) {
+    const float a = fminf(fabsf(z), 32.0f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752440f, a, 1.0f));
+    const float ex = __builtin_amdgcn_exp2f(a * (a * (-0.5f * 1.44269504088896340736f)));
+    float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    p = fmaf(t, p, 0.5f * 1.421413741f);
+    p = fmaf(t, p, 0.5f * -0.284496736f);
+    p = fmaf(t, p, 0.5f * 0.254829592f);
+    return fmaf(-a, p * (t * ex), fmaf(0.5f, fabsf(z), 0.5f * z));
+}
+
 // act(z); act is the same for a whole launch
 template <typename T> __device__ __forceinline__ float activate(float z, int act);
 template <> __device__ __forceinline__ float activate<bf16_t>(float z, int act) {
-    if (act == MOE_ACT_GELU) { float ex; return z * normal_cdf_fast(z, &ex); }
+    if (act == MOE_ACT_GELU) return gelu_tail_f(z);
     if (act == MOE_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z));
     return z;
 }
