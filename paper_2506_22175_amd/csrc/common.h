@@ -183,8 +183,13 @@ enum GemmEpilogue {
     EPI_ACCUM_F32 = 3,  // C(float) += acc
     EPI_STORE_F32 = 4,  // C(float) = acc (also where the reduction is empty)
     EPI_SCATTER = 5,    // C[c_rows[row]] = slot_w[row] * acc: rows leave for one matrix of c_row_limit rows
-    EPI_LINEAR = 6      // z = acc + bias; Z = z (optional), C = act(z) + R; the "experts" are blocks of Cp of `rows` rows
+    EPI_LINEAR = 6,     // z = acc + bias; Z = z (optional), C = act(z) + R
+    // EPI_LINEAR, and the others with this added (plain and float stores, float sums): there are no counts, the "experts" are blocks of
+    // Cp of `rows` rows
+    EPI_BLOCKS = 8
 };
+constexpr int epi_of(int epi) { return epi & ~EPI_BLOCKS; }
+constexpr bool epi_blocks(int epi) { return epi == EPI_LINEAR || (epi & EPI_BLOCKS) != 0; }
 
 struct GemmArgs {
     const void* A; const void* B; void* C;
@@ -216,13 +221,13 @@ struct GemmArgs {
     const float* slot_w;  // EPI_DGELU: [E*Cp] row weights
     float* dw_part;       // EPI_DGELU: [E*Cp, dw_parts] or NULL
     int dw_parts;
-    // EPI_LINEAR: no counts
+    // EPI_LINEAR
     const float* bias;    // [N], may be NULL
     const void* R;        // rows like C's, may be NULL
     int ldr, act;         // act: moe_act
-    long long rows;       // of all "experts" together, Cp each but the last
+    long long rows;       // no counts: of all "experts" together, Cp each but the last
 };
-// Rows of an expert that has no count (EPI_LINEAR)
+// Rows of an expert that has no count
 __device__ __forceinline__ int block_rows(const GemmArgs& g, int e) {
     const long long left = g.rows - (long long)e * g.Cp;
     return left < 0 ? 0 : left < g.Cp ? (int)left : g.Cp;
@@ -239,6 +244,7 @@ __device__ __forceinline__ ExpertOf expert_of(const GemmArgs& g, int v) {
 }
 
 inline int gemm_prof_kind(int lay, int epi) {
+    epi = epi_of(epi);
     if (epi == EPI_GELU) return PK_GEMM_FWD1;
     if (epi == EPI_DGELU) return PK_GEMM_DGELU;
     if (epi == EPI_ACCUM_F32 || epi == EPI_STORE_F32) return PK_GEMM_WGRAD;
@@ -247,8 +253,8 @@ inline int gemm_prof_kind(int lay, int epi) {
     return lay == GEMM_NN ? PK_GEMM_NN : PK_GEMM_DGRAD;
 }
 
-moe_status gemm_bf16(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStream_t s);
-moe_status gemm_f32(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStream_t s);
+moe_status gemm_bf16(GemmLayout lay, int epi, const GemmArgs& a, hipStream_t s);       // epi: GemmEpilogue, with EPI_BLOCKS or without
+moe_status gemm_f32(GemmLayout lay, int epi, const GemmArgs& a, hipStream_t s);
 // dL of np partitions' gates, blocks of 64 tokens (gate_bwd.h)
 struct GateDlArgs {
     const float* logits; const int* topk_idx; const int* slot;

@@ -447,6 +447,7 @@ moe_status few_dims(const moe_few_config* c, FewDims* d) {
     d->slots = (int)(n < c->E ? n : c->E);
     if (d->slots < 1) d->slots = 1;
     const int cols = bf16 ? Few<bf16_t>::COLS : Few<float>::COLS, steps = up(c->H, Few<float>::STEP), blocks = up(c->M, cols) * d->slots;
+    // (two workgroups fit a compute unit: slices of H until the 512 places are taken)
     int slices = blocks < 512 ? up(512, blocks) : 1;
     const int most = up(steps, FEW_WAVES);
     if (slices > most) slices = most;

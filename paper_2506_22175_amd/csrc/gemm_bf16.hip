@@ -492,21 +492,23 @@ struct TileNumbers {
     int lane_end, tail_end;              // numbers of whole tiles / of last tile rows up to and including this expert
     int nwhole, nblocks;                 // whole tiles; all tiles
 };
-template <int LAY, int EPI, typename C>
+template <int LAY, int EPILOGUE, typename C>
 __device__ __forceinline__ TileNumbers number_tiles(const GemmArgs& g, int tiles_m, int tiles_n, int lane) {
-    constexpr int BM = C::BM;
+    constexpr int BM = C::BM, EPI = epi_of(EPILOGUE);
+    constexpr bool BLOCKS = epi_blocks(EPILOGUE);
     TileNumbers t;
     t.lane_rows = t.lane_tm = 0;
     int lane_tail = 0;                   // whether a last tile row with fewer rows follows
     if (lane < (LAY == GEMM_TN ? g.E : launch_experts(g))) {
         int rows = 0;
-        if constexpr (LAY == GEMM_TN) {
+        if constexpr (BLOCKS) {
+            rows = block_rows(g, lane);
+        } else if constexpr (LAY == GEMM_TN) {
             const int segs = g.k_segs > 1 ? g.k_segs : 1;
             for (int sg = 0; sg < segs; ++sg) rows += g.counts[sg * g.E + lane];
         } else {
             const ExpertOf x = expert_of(g, lane);
-            if constexpr (EPI == EPI_LINEAR) rows = block_rows(g, lane);
-            else rows = g.counts[x.q * g.E + x.e];
+            rows = g.counts[x.q * g.E + x.e];
         }
         t.lane_rows = rows;
         if (LAY == GEMM_TN) t.lane_tm = (rows > 0 || EPI == EPI_STORE_F32) ? tiles_m : 0;   // a plain store still writes zeros
@@ -532,8 +534,9 @@ __device__ __forceinline__ TileNumbers number_tiles(const GemmArgs& g, int tiles
 // tile are already on their way into the rest of the ring, so neither the launch of a new
 // workgroup nor the first trip to memory stands between two main loops.
 // ONE: tile b0 only.
-template <int LAY, int EPI, typename C, bool ONE>
+template <int LAY, int EPILOGUE, typename C, bool ONE>
 __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, int tiles_m, int tiles_n, const TileNumbers& tiles, int b0, int step) {
+    constexpr int EPI = epi_of(EPILOGUE);
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, TM = C::TM, RB = C::RB, NB = C::NB;
     constexpr int STAGE = C::STAGE_BYTES, BK = C::BK, NS = C::NS;
@@ -1880,7 +1883,7 @@ static int tile_choice(int lay, int epi, const GemmArgs& a) {
 // gradients), TN with float store and float accumulation (the weight gradients).
 template <int LAY, int EPI>
 static moe_status launch_cfg(const GemmArgs& a, hipStream_t s) {
-    const int choice = tile_choice(LAY, EPI, a);
+    const int choice = tile_choice(LAY, epi_of(EPI), a);
     if (choice == 2) return launch_one<LAY, EPI, CfgS>(a, s);
     if constexpr (LAY != GEMM_TN) { if (choice == 3) return launch_one<LAY, EPI, CfgT>(a, s); }
     if constexpr (LAY == GEMM_NN && (EPI == EPI_STORE || EPI == EPI_SCATTER)) { if (choice == 4) return launch_one<LAY, EPI, CfgU>(a, s); }
@@ -2025,8 +2028,11 @@ moe_status gemm_bf16_backward(const GemmArgs* dgrad, const GemmArgs& w2, const G
                                 : backward_cfg<EPI_ACCUM_F32>(dgrad, w2, w1, gate, s, done);
 }
 
-moe_status gemm_bf16(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStream_t s) {
-    MOE_TRY(check_args(lay, epi, a));
+moe_status gemm_bf16(GemmLayout lay, int epi, const GemmArgs& a, hipStream_t s) {
+    MOE_TRY(check_args(lay, (GemmEpilogue)epi_of(epi), a));
+    if (lay == GEMM_NT && epi == (EPI_STORE | EPI_BLOCKS)) return launch_cfg<GEMM_NT, EPI_STORE | EPI_BLOCKS>(a, s);
+    if (lay == GEMM_TN && epi == (EPI_STORE_F32 | EPI_BLOCKS)) return launch_cfg<GEMM_TN, EPI_STORE_F32 | EPI_BLOCKS>(a, s);
+    if (lay == GEMM_TN && epi == (EPI_ACCUM_F32 | EPI_BLOCKS)) return launch_cfg<GEMM_TN, EPI_ACCUM_F32 | EPI_BLOCKS>(a, s);
     if (lay == GEMM_NN && epi == EPI_STORE) return launch_cfg<GEMM_NN, EPI_STORE>(a, s);
     if (lay == GEMM_NN && epi == EPI_GELU) return launch_cfg<GEMM_NN, EPI_GELU>(a, s);
     if (lay == GEMM_NN && epi == EPI_SCATTER) return launch_cfg<GEMM_NN, EPI_SCATTER>(a, s);

@@ -99,11 +99,12 @@ template <bool KC> struct FOperand {
 };
 
 // Tile (tm, tn) of expert number v
-template <int LAY, int EPI>
+template <int LAY, int EPILOGUE>
 __device__ __forceinline__ void gemm_f32_one(const GemmArgs& g, int v, int tm, int tn, char* smem) {
+    constexpr int EPI = epi_of(EPILOGUE);
     const ExpertOf x = LAY == GEMM_TN ? ExpertOf{v, 0} : expert_of(g, v);
     const int e = x.e, er = x.q * g.E + e;
-    const int rows = EPI == EPI_LINEAR ? block_rows(g, er) : g.counts[er];
+    const int rows = epi_blocks(EPILOGUE) ? block_rows(g, er) : g.counts[er];
     const int Mdim = LAY == GEMM_TN ? g.Mo : rows, Kdim = LAY == GEMM_TN ? rows : g.K;
     const int m0 = tm * F_BM, n0 = tn * F_BN;
     if (m0 >= Mdim) return;
@@ -278,13 +279,16 @@ moe_status gemm_f32_backward(const GemmArgs* dgrad, const GemmArgs& w2, const Ge
     return MOE_OK;
 }
 
-moe_status gemm_f32(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, hipStream_t s) {
+moe_status gemm_f32(GemmLayout lay, int epi, const GemmArgs& a, hipStream_t s) {
     if (a.dw_part && a.dw_parts != gemm_f32_dw_parts(a.N)) return MOE_ERR_SHAPE;
     if (a.a_rows && (lay == GEMM_TN || a.a_row_limit <= 0)) return MOE_ERR_UNSUPPORTED;
     if (epi == EPI_SCATTER && (lay == GEMM_TN || !a.c_rows || !a.slot_w || a.c_row_limit <= 0)) return MOE_ERR_UNSUPPORTED;
     if (lay == GEMM_NN && epi == EPI_STORE) return launch_f32<GEMM_NN, EPI_STORE>(a, s);
     if (lay == GEMM_NN && epi == EPI_GELU) return launch_f32<GEMM_NN, EPI_GELU>(a, s);
     if (lay == GEMM_NN && epi == EPI_SCATTER) return launch_f32<GEMM_NN, EPI_SCATTER>(a, s);
+    if (lay == GEMM_NT && epi == (EPI_STORE | EPI_BLOCKS)) return launch_f32<GEMM_NT, EPI_STORE | EPI_BLOCKS>(a, s);
+    if (lay == GEMM_TN && epi == (EPI_STORE_F32 | EPI_BLOCKS)) return launch_f32<GEMM_TN, EPI_STORE_F32 | EPI_BLOCKS>(a, s);
+    if (lay == GEMM_TN && epi == (EPI_ACCUM_F32 | EPI_BLOCKS)) return launch_f32<GEMM_TN, EPI_ACCUM_F32 | EPI_BLOCKS>(a, s);
     if (lay == GEMM_NN && epi == EPI_LINEAR) return launch_f32<GEMM_NN, EPI_LINEAR>(a, s);
     if (lay == GEMM_NT && epi == EPI_LINEAR) return launch_f32<GEMM_NT, EPI_LINEAR>(a, s);
     if (lay == GEMM_NT && epi == EPI_STORE) return launch_f32<GEMM_NT, EPI_STORE>(a, s);
