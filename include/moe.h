@@ -519,8 +519,7 @@ moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, const void*
 
 /* dx = dz W^T + add;  dW (+)= x^T dz, float, in an order that depends on the sizes.
  *   dz [T,N]; x [T,K] (may be NULL without dW); W [K,N] (may be NULL without dx); add [T,K]: what reaches x past the product, may be
- *   NULL, may be dx itself, with its stride in any case; dx [T,K] out, may be NULL; dW [K,N] float, may be NULL; scratch as above
- *   (needed with dW only). */
+ *   NULL, may be dx itself, with its stride in any case; dx [T,K] out, may be NULL; dW [K,N] float, may be NULL; scratch as above. */
 moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, const void* add, void* dx,
                           float* dW, void* scratch, void* stream);
 moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, size_t* bytes);

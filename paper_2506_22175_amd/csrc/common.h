@@ -186,9 +186,11 @@ enum GemmEpilogue {
     EPI_LINEAR = 6,     // z = acc + bias; Z = z (optional), C = act(z) + R
     // EPI_LINEAR, and the others with this added (plain and float stores, float sums): there are no counts, the "experts" are blocks of
     // Cp of `rows` rows
-    EPI_BLOCKS = 8
+    EPI_BLOCKS = 8,
+    // (NN, NT with a float store:) the "experts" are slices of K, all of Cp rows, and leave partial sums: K columns each of k_total, the last fewer
+    EPI_SLICES = 16
 };
-constexpr int epi_of(int epi) { return epi & ~EPI_BLOCKS; }
+constexpr int epi_of(int epi) { return epi & ~(EPI_BLOCKS | EPI_SLICES); }
 constexpr bool epi_blocks(int epi) { return epi == EPI_LINEAR || (epi & EPI_BLOCKS) != 0; }
 
 struct GemmArgs {
@@ -226,6 +228,7 @@ struct GemmArgs {
     const void* R;        // rows like C's, may be NULL
     int ldr, act;         // act: moe_act
     long long rows;       // no counts: of all "experts" together, Cp each but the last
+    int k_total;          // EPI_SLICES
 };
 // Rows of an expert that has no count
 __device__ __forceinline__ int block_rows(const GemmArgs& g, int e) {
@@ -275,6 +278,9 @@ moe_status gemm_bf16_backward(const GemmArgs* dgrad, const GemmArgs& w2, const G
                               const GateDlArgs* gate, hipStream_t s, bool* done);
 moe_status gemm_f32_backward(const GemmArgs* dgrad, const GemmArgs& w2, const GemmArgs& w1, GemmEpilogue epi,
                              const GateDlArgs* gate, hipStream_t s, bool* done);
+// Slices of K (at least `least` columns each) in which a store of one "expert" is fastest, the partial sums' joining included.
+int gemm_bf16_slices(GemmLayout lay, const GemmArgs& a, int least);
+int gemm_f32_slices(const GemmArgs& a, int least);
 int gemm_bf16_dw_parts(int H);   // column blocks the DGELU epilogue reports per row
 int gemm_f32_dw_parts(int H);
 void gemm_bf16_tile(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, int* rows, int* cols);   // of a launch; host only

@@ -495,13 +495,15 @@ struct TileNumbers {
 template <int LAY, int EPILOGUE, typename C>
 __device__ __forceinline__ TileNumbers number_tiles(const GemmArgs& g, int tiles_m, int tiles_n, int lane) {
     constexpr int BM = C::BM, EPI = epi_of(EPILOGUE);
-    constexpr bool BLOCKS = epi_blocks(EPILOGUE);
+    constexpr bool BLOCKS = epi_blocks(EPILOGUE), SLICES = (EPILOGUE & EPI_SLICES) != 0;
     TileNumbers t;
     t.lane_rows = t.lane_tm = 0;
     int lane_tail = 0;                   // whether a last tile row with fewer rows follows
     if (lane < (LAY == GEMM_TN ? g.E : launch_experts(g))) {
         int rows = 0;
-        if constexpr (BLOCKS) {
+        if constexpr (SLICES) {
+            rows = g.Cp;
+        } else if constexpr (BLOCKS) {
             rows = block_rows(g, lane);
         } else if constexpr (LAY == GEMM_TN) {
             const int segs = g.k_segs > 1 ? g.k_segs : 1;
@@ -657,6 +659,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, int tiles_m, int t
         t.er = x.q * g.E + x.e;
         const int rows = __builtin_amdgcn_readlane(tiles.lane_rows, e);
         if (LAY == GEMM_TN) { t.Mdim = g.Mo; t.Kdim = rows; } else { t.Mdim = rows; t.Kdim = g.K; }
+        if constexpr ((EPILOGUE & EPI_SLICES) != 0) t.Kdim = min(g.K, g.k_total - e * g.K);
         t.e = x.e;
         t.q = x.q;
         t.m0 = tm * BM;
@@ -1891,6 +1894,44 @@ static moe_status launch_cfg(const GemmArgs& a, hipStream_t s) {
     return launch_one<LAY, EPI, typename CfgFor<LAY, EPI>::type>(a, s);
 }
 
+// Slices of K: in the smaller tiles (a launch that fills the chip with larger ones has none), of which the two-ring loop is not one.
+template <int LAY>
+static int slice_choice(const GemmArgs& a) {
+    int best = 2;
+    for (int c = 3; c < (LAY == GEMM_NN ? 5 : 4); ++c)
+        if (tile_time(TILE_COSTS[c], LAY, EPI_STORE, a, compute_units()) < tile_time(TILE_COSTS[best], LAY, EPI_STORE, a, compute_units())) best = c;
+    return best;
+}
+template <int LAY>
+static moe_status launch_slices(const GemmArgs& a, hipStream_t s) {
+    constexpr int EPI = EPI_STORE_F32 | EPI_SLICES;
+    const int choice = slice_choice<LAY>(a);
+    if (choice == 2) return launch_one<LAY, EPI, CfgS>(a, s);
+    if constexpr (LAY == GEMM_NN) { if (choice == 4) return launch_one<LAY, EPI, CfgU>(a, s); }
+    return launch_one<LAY, EPI, CfgT>(a, s);
+}
+int gemm_bf16_slices(GemmLayout lay, const GemmArgs& a, int least) {
+    const int cus = compute_units();
+    double fastest = 0.0;
+    int slices = 1;
+    if ((long long)((a.Cp + 63) / 64) * ((a.N + 127) / 128) >= cus) return 1;
+    for (int n = 1; n <= 32 && (n == 1 || a.K >= n * least); n = n < 4 ? n + 1 : n + n / 4) {
+        GemmArgs g = a;
+        g.K = ((a.K + n - 1) / n + 63) / 64 * 64;
+        g.E = (a.K + g.K - 1) / g.K;
+        double t;
+        if (n == 1) {
+            t = tile_time(TILE_COSTS[tile_choice(lay, EPI_STORE, a)], lay, EPI_STORE, a, cus);
+        } else {
+            const int c = lay == GEMM_NN ? slice_choice<GEMM_NN>(g) : slice_choice<GEMM_NT>(g);
+            // (the partial sums are written and read at some 4 TB/s, their launch takes 3 us)
+            t = tile_time(TILE_COSTS[c], lay, EPI_STORE, g, cus) + 3.0 + (double)g.E * g.Cp * g.N * 8.0 / 4e6;
+        }
+        if (n == 1 || t < 0.9 * fastest) { fastest = t; slices = g.E; }
+    }
+    return slices;
+}
+
 void gemm_bf16_tile(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, int* rows, int* cols) {
     const TileCost& c = TILE_COSTS[tile_choice(lay, epi, a)];
     *rows = c.bm;
@@ -2030,6 +2071,8 @@ moe_status gemm_bf16_backward(const GemmArgs* dgrad, const GemmArgs& w2, const G
 
 moe_status gemm_bf16(GemmLayout lay, int epi, const GemmArgs& a, hipStream_t s) {
     MOE_TRY(check_args(lay, (GemmEpilogue)epi_of(epi), a));
+    if (lay == GEMM_NN && epi == (EPI_STORE_F32 | EPI_SLICES)) return launch_slices<GEMM_NN>(a, s);
+    if (lay == GEMM_NT && epi == (EPI_STORE_F32 | EPI_SLICES)) return launch_slices<GEMM_NT>(a, s);
     if (lay == GEMM_NT && epi == (EPI_STORE | EPI_BLOCKS)) return launch_cfg<GEMM_NT, EPI_STORE | EPI_BLOCKS>(a, s);
     if (lay == GEMM_TN && epi == (EPI_STORE_F32 | EPI_BLOCKS)) return launch_cfg<GEMM_TN, EPI_STORE_F32 | EPI_BLOCKS>(a, s);
     if (lay == GEMM_TN && epi == (EPI_ACCUM_F32 | EPI_BLOCKS)) return launch_cfg<GEMM_TN, EPI_ACCUM_F32 | EPI_BLOCKS>(a, s);

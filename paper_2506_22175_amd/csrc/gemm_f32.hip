@@ -104,8 +104,9 @@ __device__ __forceinline__ void gemm_f32_one(const GemmArgs& g, int v, int tm, i
     constexpr int EPI = epi_of(EPILOGUE);
     const ExpertOf x = LAY == GEMM_TN ? ExpertOf{v, 0} : expert_of(g, v);
     const int e = x.e, er = x.q * g.E + e;
-    const int rows = epi_blocks(EPILOGUE) ? block_rows(g, er) : g.counts[er];
-    const int Mdim = LAY == GEMM_TN ? g.Mo : rows, Kdim = LAY == GEMM_TN ? rows : g.K;
+    constexpr bool SLICES = (EPILOGUE & EPI_SLICES) != 0;
+    const int rows = SLICES ? g.Cp : epi_blocks(EPILOGUE) ? block_rows(g, er) : g.counts[er];
+    const int Mdim = LAY == GEMM_TN ? g.Mo : rows, Kdim = LAY == GEMM_TN ? rows : SLICES ? min(g.K, g.k_total - e * g.K) : g.K;
     const int m0 = tm * F_BM, n0 = tn * F_BN;
     if (m0 >= Mdim) return;
     if (EPI == EPI_ACCUM_F32 && Kdim <= 0) return;            // nothing to add
@@ -279,6 +280,21 @@ moe_status gemm_f32_backward(const GemmArgs* dgrad, const GemmArgs& w2, const Ge
     return MOE_OK;
 }
 
+int gemm_f32_slices(const GemmArgs& a, int least) {
+    const int tiles = (a.Cp + F_BM - 1) / F_BM * ((a.N + F_BN - 1) / F_BN), cus = compute_units();
+    double fastest = 0.0;
+    int slices = 1;
+    if (tiles >= 2 * cus) return 1;
+    for (int n = 1; n <= 32 && (n == 1 || a.K >= n * least); n = n < 4 ? n + 1 : n + n / 4) {
+        const int k = ((a.K + n - 1) / n + 63) / 64 * 64, here = (a.K + k - 1) / k;
+        // a step of 32 k takes a tile 0.45 us of its CU's matrix pipes, and alone some more (the first loads 3 us)
+        double t = ((long long)tiles * here + cus - 1) / cus * ((k + 31) / 32) * 0.45 + 3.0;
+        if (n > 1) t += 3.0 + (double)here * a.Cp * a.N * 8.0 / 4e6;
+        if (n == 1 || t < 0.9 * fastest) { fastest = t; slices = here; }
+    }
+    return slices;
+}
+
 moe_status gemm_f32(GemmLayout lay, int epi, const GemmArgs& a, hipStream_t s) {
     if (a.dw_part && a.dw_parts != gemm_f32_dw_parts(a.N)) return MOE_ERR_SHAPE;
     if (a.a_rows && (lay == GEMM_TN || a.a_row_limit <= 0)) return MOE_ERR_UNSUPPORTED;
@@ -286,6 +302,8 @@ moe_status gemm_f32(GemmLayout lay, int epi, const GemmArgs& a, hipStream_t s) {
     if (lay == GEMM_NN && epi == EPI_STORE) return launch_f32<GEMM_NN, EPI_STORE>(a, s);
     if (lay == GEMM_NN && epi == EPI_GELU) return launch_f32<GEMM_NN, EPI_GELU>(a, s);
     if (lay == GEMM_NN && epi == EPI_SCATTER) return launch_f32<GEMM_NN, EPI_SCATTER>(a, s);
+    if (lay == GEMM_NN && epi == (EPI_STORE_F32 | EPI_SLICES)) return launch_f32<GEMM_NN, EPI_STORE_F32 | EPI_SLICES>(a, s);
+    if (lay == GEMM_NT && epi == (EPI_STORE_F32 | EPI_SLICES)) return launch_f32<GEMM_NT, EPI_STORE_F32 | EPI_SLICES>(a, s);
     if (lay == GEMM_NT && epi == (EPI_STORE | EPI_BLOCKS)) return launch_f32<GEMM_NT, EPI_STORE | EPI_BLOCKS>(a, s);
     if (lay == GEMM_TN && epi == (EPI_STORE_F32 | EPI_BLOCKS)) return launch_f32<GEMM_TN, EPI_STORE_F32 | EPI_BLOCKS>(a, s);
     if (lay == GEMM_TN && epi == (EPI_ACCUM_F32 | EPI_BLOCKS)) return launch_f32<GEMM_TN, EPI_ACCUM_F32 | EPI_BLOCKS>(a, s);

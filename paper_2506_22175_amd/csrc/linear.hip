@@ -9,6 +9,7 @@
 #include "common.h"
 #include "activation.h"
 #include "few_rows.h"
+#include "wide.h"
 
 namespace moe {
 
@@ -73,6 +74,15 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
     return MOE_OK;
 }
 
+// Slices of the sum in which a GEMM over the rows goes (few tiles, long sums).
+int gemm_slices(const LinearDims& d, GemmLayout lay, int N, int K) {
+    GemmArgs g = {};
+    g.E = 1; g.Cp = d.block; g.mean_rows = d.block; g.N = N; g.K = K;
+    return d.blocks > 1 ? 1 : d.bf16 ? gemm_bf16_slices(lay, g, 256) : gemm_f32_slices(g, 128);
+}
+int fwd_slices(const LinearDims& d) { return gemm_slices(d, GEMM_NN, d.N, d.K); }
+int dx_slices(const LinearDims& d) { return gemm_slices(d, GEMM_NT, d.K, d.N); }
+
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
 // A dz of more bytes than this, which would not be found in the memory-side cache by the products behind it anyway, is written past the caches
 // (268 MB: 153 us so, 164 with ordinary stores).
@@ -121,20 +131,38 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 4) void few_linear_kernel(FewLinear
         else linear_finish<T>(a, t, n0 + n, v);
     });
 }
-template <typename T> __global__ __launch_bounds__(64) void few_linear_finish_kernel(FewLinearArgs a, int slices) {
-    const int t = blockIdx.y, n = blockIdx.x * 64 + threadIdx.x;
+// The slices' partial sums and the epilogue, four columns to a thread; sixteen slices are requested at a time.
+template <typename T> __global__ __launch_bounds__(64) void linear_finish_kernel(FewLinearArgs a, int slices) {
+    const int t = blockIdx.x, n = (blockIdx.y * 64 + threadIdx.x) * 4;
     if (n >= a.N) return;
     const long long size = (long long)a.T * a.N;
     const float* p = a.partial + (long long)t * a.N + n;
-    float v = 0.0f;
+    float z[4] = {0, 0, 0, 0}, y[4];
     for (int s0 = 0; s0 < slices; s0 += 16) {
-        float o[16];
+        float4 o[16];
 #pragma unroll
-        for (int s = 0; s < 16; ++s) o[s] = s0 + s < slices ? p[(s0 + s) * size] : 0.0f;
+        for (int s = 0; s < 16; ++s)
+            if (s0 + s < slices) o[s] = *reinterpret_cast<const float4*>(p + (s0 + s) * size);
 #pragma unroll
-        for (int s = 0; s < 16; ++s) v += o[s];
+        for (int s = 0; s < 16; ++s)
+            if (s0 + s < slices) { z[0] += o[s].x; z[1] += o[s].y; z[2] += o[s].z; z[3] += o[s].w; }
     }
-    linear_finish<T>(a, t, n, v);
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += a.bias[n + i];
+    }
+    if (a.Z) store_columns(reinterpret_cast<T*>(a.Z) + t * a.ldz + n, z, 4);
+    activate_all<T, 4>(z, y, a.act);
+    if (a.R) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += Elem<T>::ld(reinterpret_cast<const T*>(a.R) + t * a.ldr + n + i);
+    }
+    store_columns(reinterpret_cast<T*>(a.y) + t * a.ldy + n, y, 4);
+}
+template <typename T> moe_status linear_finish_launch(const FewLinearArgs& a, int slices, hipStream_t s) {
+    linear_finish_kernel<T><<<dim3(a.T, up(a.N, 256)), 64, 0, s>>>(a, slices);
+    MOE_CHECK_LAUNCH();
+    return MOE_OK;
 }
 
 template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a, hipStream_t s) {
@@ -147,11 +175,7 @@ template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a
     if (groups <= 1) few_linear_kernel<T, 1><<<grid, FEW_WAVES * 64, 0, s>>>(a);
     else few_linear_kernel<T, 2><<<grid, FEW_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();
-    if (slices > 1) {
-        few_linear_finish_kernel<T><<<dim3(up(d.N, 64), d.T), 64, 0, s>>>(a, slices);
-        MOE_CHECK_LAUNCH();
-    }
-    return MOE_OK;
+    return slices > 1 ? linear_finish_launch<T>(a, slices, s) : MOE_OK;
 }
 
 // ---- gradients --------------------------------------------------------------------------------------------
@@ -274,6 +298,22 @@ moe_status gemm(const LinearDims& d, GemmLayout lay, int epi, const GemmArgs& a,
     return d.bf16 ? gemm_bf16(lay, epi, a, s) : gemm_f32(lay, epi, a, s);
 }
 
+// A product of one block of rows in slices of its sum, whose partial sums the epilogue adds up.  g: A, B, their strides, N, K.
+moe_status sliced(const LinearDims& d, GemmLayout lay, int slices, GemmArgs g, const FewLinearArgs& a, hipStream_t s) {
+    const int total = g.K;
+    g.K = up(up(total, slices), 64) * 64;
+    g.k_total = total;
+    g.E = up(total, g.K);
+    g.Cp = g.mean_rows = d.T;
+    g.a_estride = g.K;
+    g.b_estride = lay == GEMM_NN ? (long long)g.K * g.ldb : g.K;
+    g.C = a.partial;
+    g.c_estride = (long long)d.T * g.N;
+    g.ldc = g.N;
+    MOE_TRY(gemm(d, lay, EPI_STORE_F32 | EPI_SLICES, g, s));
+    return d.bf16 ? linear_finish_launch<bf16_t>(a, g.E, s) : linear_finish_launch<float>(a, g.E, s);
+}
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace
@@ -294,6 +334,9 @@ extern "C" moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, siz
         const size_t few = (size_t)d.slices * d.T * d.N * 4;
         if (few > most) most = few;
     }
+    const size_t fwd = (size_t)moe::fwd_slices(d) * d.T * d.N * 4, dx = (size_t)moe::dx_slices(d) * d.T * d.K * 4;
+    if (moe::fwd_slices(d) > 1 && fwd > most) most = fwd;
+    if (moe::dx_slices(d) > 1 && dx > most) most = dx;
     *bytes = moe::align16(most);
     return MOE_OK;
 }
@@ -324,6 +367,10 @@ extern "C" moe_status moe_linear_fwd(const moe_linear_config* cfg, const void* x
     g.N = d.N; g.K = d.K;
     g.Z = z; g.ldz = (int)d.ldz;
     g.bias = bias; g.R = residual; g.ldr = (int)d.ldr; g.act = d.act; g.rows = d.T;
+    const int slices = moe::fwd_slices(d);
+    if (slices > 1)
+        return moe::sliced(d, moe::GEMM_NN, slices, g,
+                           {x, W, bias, residual, z, y, (float*)scratch, d.ldx, d.ldy, d.ldr, d.ldz, d.T, d.K, d.N, d.act, 0}, s);
     return moe::gemm(d, moe::GEMM_NN, moe::EPI_LINEAR, g, s);
 }
 
@@ -363,7 +410,7 @@ extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* d
         if (dW && d.overwrite) MOE_TRY(moe::join_parts(nullptr, 0, (long long)d.K * d.N, dW, 1, s));
         return MOE_OK;
     }
-    if (!dz || (!dx && !dW) || (dx && !W) || (dW && (!x || !scratch))) return MOE_ERR_NULL;
+    if (!dz || (!dx && !dW) || (dx && !W) || (dW && !x) || !scratch) return MOE_ERR_NULL;
     if (!moe::aligned16(dz) || !moe::aligned16(x) || !moe::aligned16(W) || !moe::aligned16(add) || !moe::aligned16(dx) || !moe::aligned16(dW) ||
         !moe::aligned16(scratch))
         return MOE_ERR_UNSUPPORTED;
@@ -375,8 +422,14 @@ extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* d
         g.E = d.blocks; g.Cp = d.block; g.mean_rows = moe::up(d.T, d.blocks);
         g.N = d.K; g.K = d.N;
         g.R = add; g.ldr = (int)d.ldx; g.act = MOE_ACT_NONE; g.rows = d.T;
-        // (with nothing to add, the plain store's epilogue: 30011 rows, 520 x 1000 59 us against 71)
-        MOE_TRY(moe::gemm(d, moe::GEMM_NT, add ? moe::EPI_LINEAR : moe::EPI_STORE | moe::EPI_BLOCKS, g, s));
+        const int slices = moe::dx_slices(d);
+        if (slices > 1) {
+            MOE_TRY(moe::sliced(d, moe::GEMM_NT, slices, g,
+                                {dz, W, nullptr, add, nullptr, dx, (float*)scratch, d.ldz, d.ldx, d.ldx, 0, d.T, d.N, d.K, MOE_ACT_NONE, 0}, s));
+        } else {
+            // (with nothing to add, the plain store's epilogue: 30011 rows, 520 x 1000 59 us against 71)
+            MOE_TRY(moe::gemm(d, moe::GEMM_NT, add ? moe::EPI_LINEAR : moe::EPI_STORE | moe::EPI_BLOCKS, g, s));
+        }
     }
     if (dW) {
         moe::GemmArgs g = {};

@@ -86,7 +86,8 @@ def test_forward_epilogues_with_rows_that_lie_apart(T, act, parts, dtype):
 
 
 @pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
-@pytest.mark.parametrize("T,K,N", [(1, 8192, 2048), (3, 2048, 8192), (32, 4096, 512), (1, 20000, 64), (1500, 512, 2048), (5000, 264, 520)])
+@pytest.mark.parametrize("T,K,N", [(1, 8192, 2048), (3, 2048, 8192), (32, 4096, 512), (1, 20000, 64), (1500, 512, 2048), (5000, 264, 520), (40, 8192, 264), (100, 5000, 72),
+                                   (64, 2048, 2048), (130, 4104, 520)])
 def test_forward_of_long_sums_and_many_rows(T, K, N, dtype):
     _forward(T, K, N, dtype, B.MOE_ACT_GELU, True, True, True)
 
@@ -201,7 +202,7 @@ def test_activations_far_from_zero(act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
-@pytest.mark.parametrize("T,K,N", [(1, 8, 8), (3, 64, 72), (40, 136, 64), (300, 520, 264), (1025, 64, 128), (5000, 72, 136), (2049, 1096, 72)])
+@pytest.mark.parametrize("T,K,N", [(1, 8, 8), (3, 64, 72), (40, 136, 64), (300, 520, 264), (1025, 64, 128), (5000, 72, 136), (2049, 1096, 72), (40, 72, 8192), (1, 264, 4104), (200, 64, 3000)])
 def test_product_backward(T, K, N, dtype):
     g = torch.Generator(device=D).manual_seed(T + K + N)
     for apart, overwrite in ((0, 1), (8, 0)):
@@ -227,10 +228,10 @@ def test_product_backward(T, K, N, dtype):
         # with what reaches x past the product, in its place or another
         add = _apart(T, K, K + apart, DT[dtype], g, 9.0)[1]
         A = add.double()
-        B.moe_linear_bwd(cfg, dz, None, W, dx2, None, None, add=add)
+        B.moe_linear_bwd(cfg, dz, None, W, dx2, None, scratch, add=add)
         want, err = Z @ V.t() + A, 2 * (N + 20) * U * (Z.abs() @ V.abs().t() + A.abs())
         assert ((dx2.double() - want).abs() <= err + HALF[dtype] * (want.abs() + err)).all()
-        B.moe_linear_bwd(cfg, dz, None, W, add, None, None, add=add)
+        B.moe_linear_bwd(cfg, dz, None, W, add, None, scratch, add=add)
         assert torch.equal(add, dx2)
 
 
