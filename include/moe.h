@@ -344,8 +344,8 @@ moe_status moe_launch_counts(int64_t out[3], int32_t reset);
  * GeLU-backward epilogue, 3 input-gradient GEMM, 4 weight-gradient GEMMs,
  * 5 dispatch, 6 combine, 7 dispatch backward, 8 gate, 9 slot assignment,
  * 10 gate backward, 11 norm, 12 norm backward, 13 router, 14 router backward, 15 products on
- * 4-bit weights, 16 the layer for a few tokens (each one whole call), 17 dense products and their input gradients (their weight
- * gradients count in 4), 18 activation backward, 19 gradients' norm and clipping.  Arrays of `kinds` entries (at most 20).  Host only; not
+ * 4-bit weights, 16 the layer for a few tokens (each one whole call), 17 dense products and their input gradients (without the
+ * joining of partial sums; their weight gradients count in 4), 18 activation backward, 19 gradients' norm and clipping.  Arrays of `kinds` entries (at most 20).  Host only; not
  * for use under stream capture. */
 moe_status moe_profile_enable(int32_t on);
 moe_status moe_profile_read(int32_t kinds, int64_t* launches, double* total_ms);
@@ -497,7 +497,7 @@ moe_status moe_few_scratch_bytes(const moe_few_config* cfg, size_t* bytes);
 /* A dense product with bias, activation and residual, and its gradients. */
 typedef enum { MOE_ACT_NONE = 0, MOE_ACT_GELU = 1 /* erf form */, MOE_ACT_SILU = 2 /* z sigmoid(z) */ } moe_act;
 typedef struct {
-    int32_t T, K, N;        /* with m the largest of K, N and the strides: (max(K,N) + 1024) m <= 2^30, T m <= 2^35 */
+    int32_t T, K, N;        /* T <= 2^27; with m the largest of K, N and the strides: m <= 2^18, (max(K,N) + 1024) m <= 2^30, T m <= 2^35 */
     int32_t dtype;          /* MOE_F32 or MOE_BF16: x, W, residual, z, y, dy, dz, dx */
     int32_t act;            /* moe_act */
     int32_t grad_overwrite; /* dW, dbias: 0 accumulated into, 1 stored */

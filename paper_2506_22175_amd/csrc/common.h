@@ -247,6 +247,7 @@ __device__ __forceinline__ ExpertOf expert_of(const GemmArgs& g, int v) {
 }
 
 inline int gemm_prof_kind(int lay, int epi) {
+    if ((epi & EPI_SLICES) || epi == (EPI_STORE | EPI_BLOCKS)) return PK_LINEAR;
     epi = epi_of(epi);
     if (epi == EPI_GELU) return PK_GEMM_FWD1;
     if (epi == EPI_DGELU) return PK_GEMM_DGELU;

@@ -3,9 +3,11 @@
 //   z = x W + bias;  y = act(z) + residual        W [K,N] as the layer's W1 and W2
 //   dz = dy act'(z);  dbias = sum over rows of dz;  dx = dz W^T;  dW = x^T dz
 //
-// Many rows are the layer's grouped GEMM's (gemm_bf16.hip, gemm_f32.hip) with blocks of rows for experts: one in forward unless 32-bit
-// offsets want more; in the weight gradient, whose sum is over the rows, as many as the chip needs to be full, which leave
-// partial sums.  Few rows are bound by reading W once and go through few_rows.h.
+// Many rows are the layer's grouped GEMM's (gemm_bf16.hip, gemm_f32.hip) with blocks of rows for experts: one unless 32-bit offsets want more.
+// Where the output has too few tiles for the chip, the sum is cut into slices whose partial sums a second launch adds up: rows in the
+// weight gradient, columns of x or dz in the others (64 rows, 8192 x 2048: 15 us, 41 without; float 31 and 177).  8192 rows of 2048 x 8192
+// take 255 us with GeLU and z kept (1.08 PFLOP/s; a library's product of 8192^3 1.10), back 380 us (1.45).  Up to 32 rows are bound by reading
+// W once and go through few_rows.h: one of 8192 x 2048 10 to 11 us, of which the second launch and what lies between are half.
 #include "common.h"
 #include "activation.h"
 #include "few_rows.h"
@@ -30,11 +32,10 @@ constexpr int ACT_WAVES = 4, ACT_COLS = 512; // of act_bwd_kernel: wavefronts, c
 
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-int few_slices(int T, int K, int N, bool bf16) {
+int few_slices(int K, int N, bool bf16) {
     const int columns = up(N, bf16 ? Few<bf16_t>::COLS : Few<float>::COLS), steps = up(K, Few<float>::STEP);
     if (columns >= 256) return 1;
-    int s = 256 / columns;
-    const int most = up(steps, FEW_WAVES);
+    const int s = 256 / columns, most = up(steps, FEW_WAVES);
     return s < most ? s : most;
 }
 
@@ -55,13 +56,15 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
     long long most = d->ldx;
     for (long long l : {d->ldy, d->ldr, d->ldz, (long long)d->N, (long long)d->K})
         if (l > most) most = l;
-    // What the GEMMs' 32-bit offsets allow: 2^30 elements from a matrix's first to its last, some rows more.
-    const long long rows = (1ll << 30) / most - 1024;
-    if (rows < 256 || (long long)(d->K > d->N ? d->K : d->N) + 1024 > rows) return MOE_ERR_UNSUPPORTED;
+    // What the GEMMs' 32-bit offsets allow: 2^30 elements from a matrix's first to its last, some rows more; longer calls go in up to 64
+    // blocks of rows, of which a launch of the float GEMM takes no more than 65535 tiles each.
+    const long long widest = d->K > d->N ? d->K : d->N;
+    if (most > (1 << 18) || (widest + 1024) * most > (1ll << 30) || c->T > (1 << 27) || c->T * most > (1ll << 35)) return MOE_ERR_UNSUPPORTED;
+    long long rows = ((1ll << 30) / most - 1024) / 256 * 256;
+    if (!d->bf16 && rows > 65535 / 4 * 256) rows = 65535 / 4 * 256;
     const int T = d->T > 0 ? d->T : 1;
-    d->block = (long long)T <= rows ? T : (int)(rows / 256 * 256);
+    d->block = T <= rows ? T : (int)rows;
     d->blocks = up(T, d->block);
-    if (d->blocks > 64) return MOE_ERR_UNSUPPORTED;
     // The weight gradient's sum is cut up until its 128 x 128 tiles fill the chip twice, but not below 1024 rows.
     const long long tiles = (long long)up(d->K, 128) * up(d->N, 128);
     long long parts = d->blocks, want = tiles < 512 ? 512 / tiles : 1;
@@ -70,7 +73,7 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
     if (want > parts) parts = want;
     d->wblock = up(up(T, parts), 64) * 64;
     d->wblocks = up(T, d->wblock);
-    d->slices = few_slices(T, d->K, d->N, d->bf16);
+    d->slices = few_slices(d->K, d->N, d->bf16);
     return MOE_OK;
 }
 

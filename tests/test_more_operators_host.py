@@ -55,6 +55,7 @@ def _linear(cfg, fwd=(P,) * 7, act=(P,) * 5, bwd=(P,) * 7):
     (dict(ldz=70), UNSUPPORTED), (dict(dtype=E4M3), UNSUPPORTED), (dict(act=3), UNSUPPORTED), (dict(act=-1), UNSUPPORTED),
     (dict(grad_overwrite=2), UNSUPPORTED), (dict(N=40000), UNSUPPORTED), (dict(K=32768), UNSUPPORTED),
     (dict(ldy=1 << 22), UNSUPPORTED), (dict(ldx=1 << 40), UNSUPPORTED), (dict(T=1 << 30, K=2048, N=2048), UNSUPPORTED),
+    (dict(T=(1 << 27) + 1, K=8, N=8), UNSUPPORTED), (dict(T=1 << 25, K=2048, N=8), UNSUPPORTED), (dict(ldr=(1 << 18) + 8), UNSUPPORTED),
 ])
 def test_linear_refuses(kw, status):
     cfg = B.make_linear_config(**{**dict(T=4, K=64, N=64), **kw})
@@ -144,6 +145,14 @@ def test_grad_calls_need_their_pointers():
     size = ctypes.c_size_t()
     assert lib.moe_grad_bytes(t, ctypes.c_int32(65537), ctypes.byref(size), ctypes.byref(size)) == UNSUPPORTED
     assert lib.moe_grad_bytes(t, ctypes.c_int32(1), None, ctypes.byref(size)) == NULL
+
+
+def test_linear_takes_what_it_says():
+    """The largest rows, dimensions and strides, and their scratch; a weight gradient has at most 64 partial sums."""
+    for kw in (dict(T=1 << 27, K=8, N=8), dict(T=1 << 17, K=64, N=64, ldz=1 << 18), dict(T=1 << 20, K=31000, N=64), dict(T=5, K=8, N=31736)):
+        for dtype in (F32, BF16):
+            cfg = B.make_linear_config(dtype=dtype, **kw)
+            assert 0 < B.moe_linear_scratch_bytes(cfg) <= 64 * 4 * max(kw["K"] * kw["N"], kw["T"] * kw["K"], kw["T"] * kw["N"], 1024 * kw["N"])
 
 
 def test_grad_table_has_room_for_every_chunk():
