@@ -606,8 +606,13 @@ def make_grad_list(grads, outs=None, stream=None) -> MoEGradList:
     if any(g.device != device for g in grads):
         raise ValueError("gradients of one list are on one device")
     with torch.cuda.device(device):
-        table = torch.empty(need, dtype=torch.uint8, device=device)
-        out = moe_grad_table(tensors, table, stream)
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        elif isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream)
+        with torch.cuda.stream(stream):          # (memory of the stream that writes it: another's may still be in use there)
+            table = torch.empty(need, dtype=torch.uint8, device=device)
+            out = moe_grad_table(tensors, table, stream)
     out.memory, out.scratch = table, scratch
     return out
 

@@ -171,3 +171,22 @@ def test_lists_refuse_what_they_cannot_hold():
         B.make_grad_list([t, t], [t, t])
     assert e.value.status == 2
     B.make_grad_list([t, t])                                     # norms of the same tensor twice are no race
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_the_table_belongs_to_the_stream_that_writes_it(handle):
+    """Memory that the current stream still uses is not handed to another one."""
+    grads = [torch.full((1000,), 2.0, device=D)]
+    need = B.make_grad_list(grads).memory.numel()
+    torch.cuda.synchronize()
+    freed = [torch.empty(need, dtype=torch.uint8, device=D) for _ in range(4)]
+    places = {t.data_ptr() for t in freed}
+    freed.clear()
+    side = torch.cuda.Stream()
+    lst = B.make_grad_list(grads, stream=side.cuda_stream if handle else side)
+    assert lst.memory.data_ptr() not in places
+    norm, scratch = torch.zeros(1, device=D), _scratch(lst)
+    side.wait_stream(torch.cuda.current_stream())
+    B.moe_grad_norm(lst, norm, scratch, side)
+    side.synchronize()
+    assert float(norm) == float(torch.tensor(math.sqrt(4000.0)))
