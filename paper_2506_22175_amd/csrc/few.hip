@@ -192,15 +192,16 @@ struct FewPlan {
     int expert, n_rows, n_experts;
 };
 // What a workgroup has in LDS: the choices, which only the plan looks at, then the sums.
-template <typename T, int WAVES> struct FewLds {
+template <typename T> struct FewLds {
     FewPlan plan;
-    union { int idx[FEW_TOKENS * FEW_K]; FewSums<T, WAVES> sums; };
+    union { int idx[FEW_TOKENS * FEW_K]; FewSums<T, FEW_WAVES> sums; };
 };
 // The workgroup's expert, the slot-th of those that are chosen (-1: there are fewer), how many are, and how many assignments it has,
 // which are in FewPlan::rows.
 struct FewPick { int expert, n_rows, n_experts; };
 
-// Up to 32 assignments, whose choices the lanes of every wavefront have: each finds out by itself, and writes down the same.
+// Up to 32 assignments, whose choices the lanes of every wavefront have: each finds out by itself, and writes down the same (0.6 to 0.9 us of
+// the call sooner than through LDS).
 constexpr int FEW_IN_LANES = 32;
 __device__ __forceinline__ FewPick few_pick(int e, int slot, FewPlan& p) {
     const int lane = threadIdx.x & 63;
@@ -265,45 +266,37 @@ __device__ __forceinline__ FewPick few_plan(const FewArgs& a, int slot, const in
 // Where the choices come from: they are there; or, in the first product, a workgroup routes for itself, which saves the launches between
 // it and the gate: from the gate's sums, or from x and Wg (one or two tokens).
 enum { FEW_ROUTED = 0, FEW_SUMMED = 1, FEW_ALONE = 2 };
-template <typename T, int MODE, int WAVES> __device__ __forceinline__ FewPick few_choices(const FewArgs& a, int slot, bool record, FewLds<T, WAVES>& lds) {
+template <typename T, int MODE> __device__ __forceinline__ FewPick few_choices(const FewArgs& a, int slot, bool record, FewLds<T>& lds) {
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.T * a.k;
     if constexpr (MODE == FEW_ROUTED) {
         if (n <= FEW_IN_LANES) return few_pick(lane < n ? a.route.idx[lane] : -1, slot, lds.plan);
-        for (int i = threadIdx.x; i < n; i += WAVES * 64) lds.idx[i] = a.route.idx[i];
+        for (int i = threadIdx.x; i < n; i += FEW_WAVES * 64) lds.idx[i] = a.route.idx[i];
     } else {
-        __shared__ double s_sum[MODE == FEW_ALONE ? WAVES : 1][2][64];
+        __shared__ double s_sum[MODE == FEW_ALONE ? FEW_WAVES : 1][2][64];
         if constexpr (MODE == FEW_ALONE) {
             if (a.T == 1) {
-                auto& sums = reinterpret_cast<double (&)[WAVES][1][64]>(s_sum);
-                gate_sums<T, 1, WAVES>(a, 0, 0, 0, a.M, sums);
+                auto& sums = reinterpret_cast<double (&)[FEW_WAVES][1][64]>(s_sum);
+                gate_sums<T, 1, FEW_WAVES>(a, 0, 0, 0, a.M, sums);
                 __syncthreads();
                 double sum = 0.0;
 #pragma unroll
-                for (int q = 0; q < WAVES; ++q) sum += sums[q][0][lane];
+                for (int q = 0; q < FEW_WAVES; ++q) sum += sums[q][0][lane];
                 float weight;
                 return few_pick(route_token<1>(a, 0, &sum, record && wid == 0, &weight), slot, lds.plan);
             }
-            gate_sums<T, 2, WAVES>(a, 0, 0, 0, a.M, s_sum);
+            gate_sums<T, 2, FEW_WAVES>(a, 0, 0, 0, a.M, s_sum);
             __syncthreads();
         }
-        for (int t = wid; t < a.T; t += WAVES) {
+        for (int t = wid; t < a.T; t += FEW_WAVES) {
             float weight;
-            int chosen;
-            if (a.E <= 64) {
-                double sum;
-                if constexpr (MODE == FEW_ALONE) {
-                    sum = 0.0;
+            double sum = 0.0;
+            if constexpr (MODE == FEW_ALONE) {
 #pragma unroll
-                    for (int q = 0; q < WAVES; ++q) sum += s_sum[q][t][lane];
-                } else {
-                    gate_total<1>(a, t, &sum);
-                }
-                chosen = route_token<1>(a, t, &sum, record, &weight);
-            } else if constexpr (MODE == FEW_SUMMED) {
-                double sum[4];
-                gate_total<4>(a, t, sum);
-                chosen = route_token<4>(a, t, sum, record, &weight);
+                for (int q = 0; q < FEW_WAVES; ++q) sum += s_sum[q][t][lane];
+            } else {
+                gate_total<1>(a, t, &sum);
             }
+            const int chosen = route_token<1>(a, t, &sum, record, &weight);
             if (lane < a.k) lds.idx[t * a.k + lane] = chosen;
         }
         if (n <= FEW_IN_LANES) {
@@ -320,12 +313,12 @@ template <typename T, int MODE, int WAVES> __device__ __forceinline__ FewPick fe
 __device__ __forceinline__ float gelu_of(float z) { return 0.5f * z * erfcf(-0.70710678118654752440f * z); }
 
 // ---- first product ----------------------------------------------------------------------------------------------
-template <typename T, int GROUPS, int MODE, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_kernel(FewArgs a) {
-    __shared__ FewLds<T, WAVES> lds;
+template <typename T, int GROUPS, int MODE>
+__global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_kernel(FewArgs a) {
+    __shared__ FewLds<T> lds;
     const FewPlan& plan = lds.plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
-    const FewPick pick = few_choices<T, MODE, WAVES>(a, blockIdx.y, blockIdx.x == 0 && blockIdx.y == 0, lds);
+    const FewPick pick = few_choices<T, MODE>(a, blockIdx.y, blockIdx.x == 0 && blockIdx.y == 0, lds);
     if (pick.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS;
     const T* W = reinterpret_cast<const T*>(a.W1) + (long long)pick.expert * a.M * a.H + n0;
@@ -339,8 +332,8 @@ __global__ __launch_bounds__(WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_kern
             row[g] = (unsigned)(plan.rows[r < pick.n_rows ? r : r0] / a.k) * (unsigned)a.ldx * (unsigned)sizeof(T);
         }
         few_acc acc[GROUPS][Few<T>::ACCS];
-        few_sums<T, GROUPS, 1, WAVES>(W, a.H, a.H - n0, rows, row, a.M, wid, (a.M + Few<T>::STEP - 1) / Few<T>::STEP, acc);
-        few_finish<T, GROUPS, WAVES>(lds.sums, acc, pick.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
+        few_sums<T, GROUPS, 1, FEW_WAVES>(W, a.H, a.H - n0, rows, row, a.M, wid, (a.M + Few<T>::STEP - 1) / Few<T>::STEP, acc);
+        few_finish<T, GROUPS, FEW_WAVES>(lds.sums, acc, pick.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
             const float v = gelu_of(z);
             const long long at = (long long)plan.rows[r0 + r] * a.H + n0 + n;
             if constexpr (sizeof(T) == 4) {
@@ -363,10 +356,10 @@ __global__ __launch_bounds__(WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_kern
 // and 37.5 for seven of 520/1000 in float, against 45.1 and 35.5 with the launch.)
 template <typename T, int GROUPS>
 __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_second_kernel(FewArgs a) {
-    __shared__ FewLds<T, FEW_WAVES> lds;
+    __shared__ FewLds<T> lds;
     const FewPlan& plan = lds.plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
-    const FewPick pick = few_choices<T, FEW_ROUTED, FEW_WAVES>(a, blockIdx.y, false, lds);
+    const FewPick pick = few_choices<T, FEW_ROUTED>(a, blockIdx.y, false, lds);
     if (pick.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS, PARTS = sizeof(T) == 2 ? 2 : 1;
     const T* W = reinterpret_cast<const T*>(a.W2) + (long long)pick.expert * a.H * a.M + n0;
@@ -447,19 +440,24 @@ moe_status few_dims(const moe_few_config* c, FewDims* d) {
     d->slots = (int)(n < c->E ? n : c->E);
     if (d->slots < 1) d->slots = 1;
     const int cols = bf16 ? Few<bf16_t>::COLS : Few<float>::COLS, steps = up(c->H, Few<float>::STEP), blocks = up(c->M, cols) * d->slots;
-    // (two workgroups fit a compute unit: slices of H until the 512 places are taken)
+    // (two workgroups fit a compute unit: slices of H until the 512 places are taken; 256 of them: 3 x 16 of 2048/8192 92 us instead of 85,
+    // 7 x 33 of 520/1000 in float 35.8 and 35.3, but 1 x 8 of 2048/8192 37.9 and 39.2; 1024: 84.5, 33.8 and 41.6)
     int slices = blocks < 512 ? up(512, blocks) : 1;
     const int most = up(steps, FEW_WAVES);
     if (slices > most) slices = most;
     d->steps = up(steps, slices);
     d->slices = up(steps, d->steps);
-    // Who routes.  One or two tokens and a gate of up to 64 Ki elements: every workgroup of the first product by itself; up to 16 tokens:
-    // it does so from the gate's sums, which have a launch; more tokens: a launch of its own.
+    // Who routes (tokens x experts of M/H, us).  Little gate in all: every workgroup of the first product by itself, which saves two launches
+    // (1 x 16 of 1024/4096 22.2, 24.0 with the gate's launch, 24.5 with both; 2 x 16 25.2, 26.2, 27.0; 2 x 64, which is too much, 31.8, 28.2,
+    // 29.1).  Up to four tokens and 64 experts: it does so from the gate's sums (4 x 64 of 1024/1024 28.6, 29.3 with a launch for it).  More: a launch of
+    // its own (16 x 16 of 1024/4096 56.4 and 57.8 without; 64 x 64 of 1024/1024 55.4 and 67.6).
+    // Groups of rows that go through together: as many as an expert is expected to have, and half as many again (8 experts of 1024/4096,
+    // choices 2: 64 tokens, two groups, 51.7, one 63.5; 128 tokens, four, 74.4, two 78.5, one 97.8; 48 x 64 of four, one, 150.7, two 156.2).
     const int mean = up(n, c->E);
     d->few_groups = up(mean + (mean > 1 ? up(mean, 2) : 0), Few<float>::ROWS);
-    d->mode = c->T > 16 || c->E > 256 || d->few_groups > 1 ? FEW_ROUTED : c->T <= 2 && c->E <= 64 && (long long)c->M * c->E <= 65536 ? FEW_ALONE : FEW_SUMMED;
-    d->exact_values = d->mode != FEW_ROUTED && c->E > 64 ? 4 : c->E <= 64 ? 1 : c->E <= 128 ? 2 : c->E <= 256 ? 4 : 8;
-    // The gate's workgroups: enough for the chip, of 128 rows of Wg at least.
+    d->mode = c->T > 4 || c->E > 64 ? FEW_ROUTED : c->T <= 2 && (long long)c->T * c->M * c->E <= 65536 ? FEW_ALONE : FEW_SUMMED;
+    d->exact_values = c->E <= 64 ? 1 : c->E <= 128 ? 2 : c->E <= 256 ? 4 : 8;
+    // The gate's workgroups: enough for the chip, of 128 rows of Wg at least (64 or 256: the same within 3 %).
     const int tiles = up(c->E, 64) * up(c->T > 0 ? c->T : 1, c->T == 1 ? 1 : GATE_TOKENS);
     d->gate_slices = up(256, tiles);
     if (d->gate_slices > 16) d->gate_slices = 16;
@@ -486,27 +484,15 @@ template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, 
         else few_route_kernel<8><<<a.T, 64, 0, s>>>(a);
         MOE_CHECK_LAUNCH();
     }
-    // Groups of rows that go through together: as many as an expert is expected to have, and some more.  Where the first product has few
-    // workgroups, they have 16 wavefronts.
     const dim3 first(up(a.H, Few<T>::COLS), d.slots), second(up(a.M, Few<T>::COLS), d.slots, a.slices);
-    const bool wide = first.x * first.y <= 256;
-#define FEW_FIRST(G, MODE) do { if (wide) few_first_kernel<T, G, MODE, 16><<<first, 1024, 0, s>>>(a); \
-        else few_first_kernel<T, G, MODE, FEW_WAVES><<<first, FEW_WAVES * 64, 0, s>>>(a); } while (0)
-#define FEW_SECOND(G) few_second_kernel<T, G><<<second, FEW_WAVES * 64, 0, s>>>(a)
-    if (d.few_groups <= 1) {
-        if (d.mode == FEW_ALONE) FEW_FIRST(1, FEW_ALONE);
-        else if (d.mode == FEW_SUMMED) FEW_FIRST(1, FEW_SUMMED);
-        else FEW_FIRST(1, FEW_ROUTED);
-        FEW_SECOND(1);
-    } else if (d.few_groups <= 2) {
-        few_first_kernel<T, 2, FEW_ROUTED, FEW_WAVES><<<first, FEW_WAVES * 64, 0, s>>>(a);
-        FEW_SECOND(2);
-    } else {
-        few_first_kernel<T, 4, FEW_ROUTED, FEW_WAVES><<<first, FEW_WAVES * 64, 0, s>>>(a);
-        FEW_SECOND(4);
-    }
-#undef FEW_FIRST
-#undef FEW_SECOND
+#define FEW_BOTH(G, MODE) do { few_first_kernel<T, G, MODE><<<first, FEW_WAVES * 64, 0, s>>>(a); \
+        few_second_kernel<T, G><<<second, FEW_WAVES * 64, 0, s>>>(a); } while (0)
+    if (d.mode == FEW_ALONE) FEW_BOTH(1, FEW_ALONE);
+    else if (d.mode == FEW_SUMMED) FEW_BOTH(1, FEW_SUMMED);
+    else if (d.few_groups <= 1) FEW_BOTH(1, FEW_ROUTED);
+    else if (d.few_groups <= 2) FEW_BOTH(2, FEW_ROUTED);
+    else FEW_BOTH(4, FEW_ROUTED);
+#undef FEW_BOTH
     MOE_CHECK_LAUNCH();
     few_join_kernel<T><<<dim3(up(a.M, 256), a.T), JOIN_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();

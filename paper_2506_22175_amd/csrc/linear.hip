@@ -26,12 +26,14 @@ struct LinearDims {
     int slices;                              // few rows: workgroups that share a column block's K
 };
 
-constexpr int FEW_LINEAR_ROWS = 32;          // up to so many
+// Up to so many rows (2048 x 8192: 16 rows 11.7 us, 15.5 through the GEMM; 32 rows 15.6 and 15.6; 48 rows 19.8 and 15.8).
+constexpr int FEW_LINEAR_ROWS = 32;
 constexpr int FEW_WAVES = 8;
 constexpr int ACT_WAVES = 4, ACT_COLS = 512; // of act_bwd_kernel: wavefronts, columns of each
 
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
+// Workgroups that share a column block's K: 256 in all (one row, 8192 x 2048: 11.7 us, with 128 12.7, with 512 12.4; 2048 x 8192 11.0, 12.4, 10.9).
 int few_slices(int K, int N, bool bf16) {
     const int columns = up(N, bf16 ? Few<bf16_t>::COLS : Few<float>::COLS), steps = up(K, Few<float>::STEP);
     if (columns >= 256) return 1;
@@ -65,7 +67,8 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
     const int T = d->T > 0 ? d->T : 1;
     d->block = T <= rows ? T : (int)rows;
     d->blocks = up(T, d->block);
-    // The weight gradient's sum is cut up until its 128 x 128 tiles fill the chip twice, but not below 1024 rows.
+    // The weight gradient's sum is cut up until its 128 x 128 tiles fill the chip twice, but not below 1024 rows (30011 rows, 520 x 1000: 125 us;
+    // once or four times 139 and 140; 512 or 2048 rows 123 and 124, but 4096 rows, 1024 x 1024, 36, 44 and 40).
     const long long tiles = (long long)up(d->K, 128) * up(d->N, 128);
     long long parts = d->blocks, want = tiles < 512 ? 512 / tiles : 1;
     if (want > up(T, 1024)) want = up(T, 1024);
@@ -90,7 +93,8 @@ size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
 // A dz of more bytes than this, which would not be found in the memory-side cache by the products behind it anyway, is written past the caches
 // (268 MB: 153 us so, 164 with ordinary stores).
 constexpr long long ACT_PAST = 128ll << 20;
-// Wavefronts side by side, and blocks of rows: enough for the chip, of two rows to a wavefront at least.
+// Wavefronts side by side, and blocks of rows: enough for the chip, of two rows to a wavefront at least.  (1024 workgroups: 16384 x 8192
+// 156 us, 4096 x 4096 25; 512 of them 160 and 26, 2048 157 and 26.)
 int act_beside(const LinearDims& d) { return d.N > 2 * ACT_COLS ? 4 : d.N > ACT_COLS ? 2 : 1; }
 int act_blocks(const LinearDims& d) {
     const int beside = act_beside(d), columns = up(d.N, beside * ACT_COLS);
