@@ -68,10 +68,20 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
     d->block = T <= rows ? T : (int)rows;
     d->blocks = up(T, d->block);
     // The weight gradient's sum is cut up until its 128 x 128 tiles fill the chip twice, but not below 1024 rows (30011 rows, 520 x 1000: 125 us;
-    // once or four times 139 and 140; 512 or 2048 rows 123 and 124, but 4096 rows, 1024 x 1024, 36, 44 and 40).
-    const long long tiles = (long long)up(d->K, 128) * up(d->N, 128);
-    long long parts = d->blocks, want = tiles < 512 ? 512 / tiles : 1;
-    if (want > up(T, 1024)) want = up(T, 1024);
+    // once or four times 139 and 140; 512 or 2048 rows 123 and 124, but 4096 rows, 1024 x 1024, 36, 44 and 40), or 256 where the partial sums
+    // are small (2480 rows, 72 x 1144, with the input gradient: 20.8 us and 23.8; 1688 rows, 152 x 664: 19.8 and 22.1; 8192 rows, 512 x 512,
+    // which is too much: 29.4 and 26.4).  Float has smaller tiles and its own reckoning (the first two: 32.5 us and 38, 26 and 36), which is too
+    // careful with many rows (8192 rows, 512 x 512: 92.6 us and 89.4).
+    const long long tiles = (long long)up(d->K, 128) * up(d->N, 128), fill = tiles < 512 ? 512 / tiles : 1, size = (long long)d->K * d->N;
+    long long parts = d->blocks, want = fill < up(T, 1024) ? fill : up(T, 1024);
+    const long long more = fill < up(T, 256) ? fill : up(T, 256);
+    if (more * size <= 1 << 20) want = more;
+    if (!d->bf16) {
+        GemmArgs g = {};
+        g.Cp = d->K; g.N = d->N; g.K = T;
+        const int slices = gemm_f32_slices(g, 128);
+        if (want < slices) want = slices;
+    }
     if (want > 64) want = 64;
     if (want > parts) parts = want;
     d->wblock = up(up(T, parts), 64) * 64;
