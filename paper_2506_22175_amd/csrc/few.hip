@@ -8,6 +8,11 @@
 // which expert is chosen hangs on their last bits.  The rows between the products are kept in float, or as two bfloat16 that add up
 // to 16 bits of mantissa, which costs the matrix pipe a second instruction where it waits for memory anyway: nothing is rounded to
 // the storage type but y.
+//
+// One token, 2 of 16 experts of 2048/8192 in bfloat16 (134 MB, at the 7 TB/s of a read 19 us): 39 us, of which the first product 20.7
+// (3.9 of gate and router in front of its 67 MB), the second 14.8, the join 4.  48 tokens, 4 of 64 experts of 1024/4096 (1.03 GB): 151 us,
+// 6.8 TB/s; the products alone 55 to 61 and 71 to 77.  Seven tokens of 520/1000 in float (67 MB): 35 us, two steps to a wavefront and the way to
+// the first of them, five times over.
 #include "common.h"
 #include "few_rows.h"
 #include "router_choose.h"
@@ -35,7 +40,7 @@ struct FewArgs {
 // ---- gate -------------------------------------------------------------------------------------------------
 // TOKENS tokens' sums of x Wg over the rows [m0, m1), of 64 experts from e_first on, for each of WAVES wavefronts into `out`: a lane
 // has eight experts (there are fewer lanes to a row of Wg where there are fewer experts), and the lanes and wavefronts share out
-// the rows.  A lane's eight sums are dealt out to the lanes that have the same experts while they are added.
+// the rows.  Bound by the way to Wg, which the next caches have after the first workgroup: eight rows of a lane are under way at once.  A lane's eight sums are dealt out to the lanes that have the same experts while they are added.
 template <typename T> __device__ __forceinline__ void load_eight(const T* p, int left, bool wide, float* o) {
     if (wide) {
         Raw8<T> r;
@@ -111,7 +116,9 @@ __device__ __forceinline__ void gate_sums(const FewArgs& a, int t0, int e_first,
     }
 }
 
-// By many workgroups: each has one or two tokens, 64 experts and a slice of the rows of Wg, whose sums it leaves in gate_part.
+// By many workgroups: each has one or two tokens, 64 experts and a slice of the rows of Wg, whose sums it leaves in gate_part.  (48 tokens,
+// 1024 x 64: 4.9 us, and the router's launch 4.7.  Both in one, a workgroup of 16 wavefronts to a token: the whole call 151 us either way, 1 to 3 us
+// less for 256 tokens, but 37.9 us instead of 35.5 for 7 x 33 of 520/1000, and 74.6 instead of 65.0 where Wg is 4096 x 64.)
 constexpr int GATE_TOKENS = 2, GATE_WAVES = 8;
 template <typename T, int TOKENS>
 __global__ __launch_bounds__(GATE_WAVES * 64) void few_gate_kernel(FewArgs a) {
@@ -313,6 +320,8 @@ template <typename T, int MODE> __device__ __forceinline__ FewPick few_choices(c
 __device__ __forceinline__ float gelu_of(float z) { return 0.5f * z * erfcf(-0.70710678118654752440f * z); }
 
 // ---- first product ----------------------------------------------------------------------------------------------
+// Bound by the weights' way from memory.  A workgroup has 128 columns (float: 64) of an expert and all of M, as nothing may be added up
+// between here and the activation.
 template <typename T, int GROUPS, int MODE>
 __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_kernel(FewArgs a) {
     __shared__ FewLds<T> lds;

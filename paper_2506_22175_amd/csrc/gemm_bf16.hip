@@ -1910,6 +1910,8 @@ static moe_status launch_slices(const GemmArgs& a, hipStream_t s) {
     if constexpr (LAY == GEMM_NN) { if (choice == 4) return launch_one<LAY, EPI, CfgU>(a, s); }
     return launch_one<LAY, EPI, CfgT>(a, s);
 }
+// How many slices of K a product of one block of rows goes in, whose partial sums a second launch adds up (1: none).  64 rows, K = 8192,
+// N = 2048: 15.5 us, 41 in one piece.
 int gemm_bf16_slices(GemmLayout lay, const GemmArgs& a, int least) {
     const int cus = compute_units();
     double fastest = 0.0;

@@ -280,6 +280,7 @@ moe_status gemm_f32_backward(const GemmArgs* dgrad, const GemmArgs& w2, const Ge
     return MOE_OK;
 }
 
+// How many slices of K a product of one block of rows goes in (1: none): 64 rows, K = 8192, N = 2048 31 us, 177 in one piece.
 int gemm_f32_slices(const GemmArgs& a, int least) {
     const int tiles = (a.Cp + F_BM - 1) / F_BM * ((a.N + F_BN - 1) / F_BN), cus = compute_units();
     double fastest = 0.0;

@@ -2,7 +2,8 @@
 //
 //   norm = sqrt(sum over all tensors of g^2);  out = g * min(1, most / norm)
 //
-// Nothing but memory bounds either: the norm reads every element once, clipping reads it again and writes it.  Squares and sums
+// Nothing but memory bounds either: the norm reads every element once, clipping reads it again and writes it (537 MB of a block's gradients:
+// 80 us, 6.7 TB/s, and 183 us, 5.9 TB/s, the reads and writes of a copy of as much 207; 300 tensors with 23 MB: 17 us in all).  Squares and sums
 // are in 64 bits, which the vector unit does in the shadow of the loads and in which nothing overflows or vanishes.
 //
 // The tensors' chunks of 32 KiB are in a table in device memory, written once for a list of tensors, so that one launch covers any number
@@ -191,14 +192,15 @@ __global__ __launch_bounds__(GRAD_THREADS * GRAD_AT_ONCE) void grad_norm_alone_k
     __syncthreads();
     if (q == 0 && tid == 0) *a.norm = (float)sqrt((waves[0] + waves[1]) + (waves[2] + waves[3]));
 }
+// (1.7 us beside the norm's 3.6 for 14 chunks; between them, 2 us of a launch)
 __global__ __launch_bounds__(GRAD_THREADS) void grad_join_kernel(GradArgs a) {
     __shared__ double lds[GRAD_THREADS / 64];
     const float norm = norm_of(a.partial, a.partials, lds);
     if (threadIdx.x == 0) *a.norm = norm;
 }
 
-// a.partials: so many partial sums
-// are to be added up and their norm written down; 0: the norm is there.
+// a.partials: so many partial sums are to be added up and their norm written down; 0: the norm is there.  The chunks are taken from
+// the last on, which are the likeliest to be in the caches still.
 __global__ __launch_bounds__(GRAD_THREADS) void grad_scale_kernel(GradArgs a) {
     __shared__ double lds[GRAD_THREADS / 64];
     Chunk c;
