@@ -33,10 +33,12 @@ constexpr int ACT_WAVES = 4, ACT_COLS = 512; // of act_bwd_kernel: wavefronts, c
 
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Workgroups that share a column block's K: 256 in all (one row, 8192 x 2048: 11.7 us, with 128 12.7, with 512 12.4; 2048 x 8192 11.0, 12.4, 10.9).
+// Workgroups that share a column block's K: 256 in all (one row, 8192 x 2048: 11.7 us, with 128 12.7, with 512 12.4; 2048 x 8192 11.0, 12.4, 10.9),
+// or one, which finishes by itself, where K is three steps to a wavefront (one row, 520 x 1000: 4.7 us, 7.3 with a second launch; 1024 x 4096, which is
+// too much, 8.5 and 7.6).
 int few_slices(int K, int N, bool bf16) {
     const int columns = up(N, bf16 ? Few<bf16_t>::COLS : Few<float>::COLS), steps = up(K, Few<float>::STEP);
-    if (columns >= 256) return 1;
+    if (columns >= 256 || steps <= 3 * FEW_WAVES) return 1;
     const int s = 256 / columns, most = up(steps, FEW_WAVES);
     return s < most ? s : most;
 }
@@ -201,6 +203,7 @@ template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a
 // ---- gradients --------------------------------------------------------------------------------------------
 struct ActBwdArgs {
     const void* dy; const void* z; void* dz; float* part;       // part: [blocks][N], or NULL
+    float* dbias; int store;                                    // of few rows
     long long ldy, ldz;
     int T, N, act, rows, beside;                                // rows of a workgroup; wavefronts side by side
     int past;                                                   // dz goes past the caches
@@ -209,10 +212,38 @@ struct ActBwdArgs {
 __device__ __forceinline__ void load_eight_once(Raw8<bf16_t>& r, const bf16_t* p) { r.u = load_once<uint4>(p); }
 __device__ __forceinline__ void load_eight_once(Raw8<float>& r, const float* p) { r.a = load_once<float4>(p); r.b = load_once<float4>(p + 4); }
 
+// Eight columns of a row from n on: dz, which is added to sum.
+template <typename T, int ACT> __device__ __forceinline__ void act_row(const ActBwdArgs& a, const Raw8<T>& dy, const Raw8<T>& z, long long t, int n, float* sum) {
+    constexpr bool by_z = ACT != MOE_ACT_NONE;
+    float d[8], v[8];
+    dy.to_float(d);
+    if (by_z) z.to_float(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (by_z) d[i] *= activation_slope<T>(v[i], ACT);
+        sum[i] += d[i];
+    }
+    if (a.dz) {
+        T* o = reinterpret_cast<T*>(a.dz) + t * a.ldz + n;
+        if constexpr (sizeof(T) == 2) {
+            const uint4 w = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
+            if (a.past) store_once_anywhere(o, w); else *reinterpret_cast<uint4*>(o) = w;
+        } else {
+            const float4 lo = make_float4(d[0], d[1], d[2], d[3]), hi = make_float4(d[4], d[5], d[6], d[7]);
+            if (a.past) {
+                store_once_anywhere(o, lo);
+                store_once_anywhere(o + 4, hi);
+            } else {
+                reinterpret_cast<float4*>(o)[0] = lo;
+                reinterpret_cast<float4*>(o)[1] = hi;
+            }
+        }
+    }
+}
+
 // A wavefront has 512 columns, eight to a lane, and some of the workgroup's rows; as many of the wavefronts as there are columns for
 // stand side by side in a row, the others have other rows.  The columns' sums stay in registers over the rows.  Bound by memory: 16384 x 8192,
-// GeLU, bfloat16 148 us, 5.4 TB/s (a copy of as much 155), and 4.6 us of the sums' launch.  (Few rows in one workgroup of 16 wavefronts to 512
-// columns, which needs no such launch: 64 rows of 3648 floats 19 us instead of 8.2, 29 of 1136 9.1 instead of 7.7.)
+// GeLU, bfloat16 148 us, 5.4 TB/s (a copy of as much 155), and 4.6 us of the sums' launch.
 template <typename T, int ACT>
 __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(ActBwdArgs a) {
     __shared__ float sums[ACT_WAVES][ACT_COLS];
@@ -237,30 +268,7 @@ __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(ActBwdArgs a) {
             for (int u = 0; u < AT_ONCE; ++u) {
                 const long long t = t0 + u * rows;
                 if (t >= end) continue;
-                float d[8], v[8];
-                dy[u].to_float(d);
-                if (by_z) z[u].to_float(v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (by_z) d[i] *= activation_slope<T>(v[i], ACT);
-                    sum[i] += d[i];
-                }
-                if (a.dz) {
-                    T* o = reinterpret_cast<T*>(a.dz) + t * a.ldz + n;
-                    if constexpr (sizeof(T) == 2) {
-                        const uint4 w = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
-                        if (a.past) store_once_anywhere(o, w); else *reinterpret_cast<uint4*>(o) = w;
-                    } else {
-                        const float4 lo = make_float4(d[0], d[1], d[2], d[3]), hi = make_float4(d[4], d[5], d[6], d[7]);
-                        if (a.past) {
-                            store_once_anywhere(o, lo);
-                            store_once_anywhere(o + 4, hi);
-                        } else {
-                            reinterpret_cast<float4*>(o)[0] = lo;
-                            reinterpret_cast<float4*>(o)[1] = hi;
-                        }
-                    }
-                }
+                act_row<T, ACT>(a, dy[u], z[u], t, n, sum);
             }
         }
     }
@@ -276,10 +284,60 @@ __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(ActBwdArgs a) {
     }
 }
 
+// Few rows: a workgroup has 64 columns of all of them, eight threads to a row, and with them the whole of the bias's gradient, which saves the
+// second launch (us so / otherwise, with the bias's gradient: 64 rows of 3648 floats 4.8 / 7.0; 64 x 8192 floats, GeLU 5.2 / 8.5; 256 x 8192, SiLU 6.2 / 8.9;
+// but 200 x 512 floats, GeLU, whose float form is a few hundred instructions, 11.6 / 7.3).
+constexpr int ACT_FEW_COLS = 64, ACT_FEW_THREADS = 256;
+int act_few(const LinearDims& d) { return d.bf16 || d.act == MOE_ACT_NONE ? 256 : 64; }
+template <typename T, int ACT>
+__global__ __launch_bounds__(ACT_FEW_THREADS) void act_bwd_few_kernel(ActBwdArgs a) {
+    __shared__ float sums[ACT_FEW_THREADS / 64][ACT_FEW_COLS];
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, c = (lane & 7) * 8, n = blockIdx.x * ACT_FEW_COLS + c;
+    constexpr int ROWS = ACT_FEW_THREADS / 8, AT_ONCE = 2;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (n < a.N) {
+        for (int t0 = threadIdx.x / 8; t0 < a.T; t0 += AT_ONCE * ROWS) {
+            Raw8<T> dy[AT_ONCE], z[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const long long t = t0 + u * ROWS;
+                if (t >= a.T) continue;
+                load_eight_once(dy[u], reinterpret_cast<const T*>(a.dy) + t * a.ldy + n);
+                if (ACT != MOE_ACT_NONE) load_eight_once(z[u], reinterpret_cast<const T*>(a.z) + t * a.ldz + n);
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const long long t = t0 + u * ROWS;
+                if (t < a.T) act_row<T, ACT>(a, dy[u], z[u], t, n, sum);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int off = 8; off < 64; off <<= 1) sum[i] += __shfl_xor(sum[i], off, 64);
+    }
+    if (lane < 8) {
+        *reinterpret_cast<float4*>(&sums[wid][c]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        *reinterpret_cast<float4*>(&sums[wid][c + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+    }
+    __syncthreads();
+    const int col = blockIdx.x * ACT_FEW_COLS + threadIdx.x;
+    if (threadIdx.x >= ACT_FEW_COLS || col >= a.N) return;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < ACT_FEW_THREADS / 64; ++w) v += sums[w][threadIdx.x];
+    a.dbias[col] = a.store ? v : a.dbias[col] + v;
+}
+
+template <typename T, int ACT> void act_bwd_launch(const ActBwdArgs& a, dim3 grid, hipStream_t s) {
+    if (a.dbias) act_bwd_few_kernel<T, ACT><<<up(a.N, ACT_FEW_COLS), ACT_FEW_THREADS, 0, s>>>(a);
+    else act_bwd_kernel<T, ACT><<<grid, ACT_WAVES * 64, 0, s>>>(a);
+}
 template <typename T> moe_status act_bwd_launch(const ActBwdArgs& a, dim3 grid, hipStream_t s) {
-    if (a.act == MOE_ACT_GELU) act_bwd_kernel<T, MOE_ACT_GELU><<<grid, ACT_WAVES * 64, 0, s>>>(a);
-    else if (a.act == MOE_ACT_SILU) act_bwd_kernel<T, MOE_ACT_SILU><<<grid, ACT_WAVES * 64, 0, s>>>(a);
-    else act_bwd_kernel<T, MOE_ACT_NONE><<<grid, ACT_WAVES * 64, 0, s>>>(a);
+    if (a.act == MOE_ACT_GELU) act_bwd_launch<T, MOE_ACT_GELU>(a, grid, s);
+    else if (a.act == MOE_ACT_SILU) act_bwd_launch<T, MOE_ACT_SILU>(a, grid, s);
+    else act_bwd_launch<T, MOE_ACT_NONE>(a, grid, s);
     MOE_CHECK_LAUNCH();
     return MOE_OK;
 }
@@ -407,14 +465,15 @@ extern "C" moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, 
     if (!dy || (!dz && !dbias) || (!z && d.act != MOE_ACT_NONE) || (dbias && !scratch)) return MOE_ERR_NULL;
     if (!moe::aligned16(dy) || !moe::aligned16(z) || !moe::aligned16(dz) || !moe::aligned16(scratch)) return MOE_ERR_UNSUPPORTED;
     const int blocks = moe::act_blocks(d);
-    moe::ActBwdArgs a = {dy, z, dz, dbias ? (float*)scratch : nullptr, d.ldy, d.ldz, d.T, d.N, d.act, moe::up(d.T, blocks), moe::act_beside(d),
+    const bool few = dbias && d.T <= moe::act_few(d);
+    moe::ActBwdArgs a = {dy, z, dz, dbias && !few ? (float*)scratch : nullptr, few ? dbias : nullptr, d.overwrite, d.ldy, d.ldz, d.T, d.N, d.act, moe::up(d.T, blocks), moe::act_beside(d),
                          (long long)d.T * d.N * (d.bf16 ? 2 : 4) > moe::ACT_PAST};
     const int parts = moe::up(d.T, a.rows);
     {
         moe::ProfScope prof(moe::PK_ACT_BWD, s);
         const dim3 grid(moe::up(d.N, a.beside * moe::ACT_COLS), parts);
         MOE_TRY(d.bf16 ? moe::act_bwd_launch<moe::bf16_t>(a, grid, s) : moe::act_bwd_launch<float>(a, grid, s));
-        if (dbias) {
+        if (a.part) {
             moe::join_columns_kernel<<<moe::up(d.N, 64), 1024, 0, s>>>(a.part, parts, d.N, dbias, d.overwrite);
             MOE_CHECK_LAUNCH();
         }

@@ -188,6 +188,21 @@ def test_activation_backward(T, N, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("T,N", [(31, 56), (64, 136), (65, 136), (256, 1032), (257, 72)])
+@pytest.mark.parametrize("act", list(ACTS))
+def test_activation_backward_of_few_rows(T, N, act, dtype):
+    """About the numbers of rows up to which one workgroup has all of a column."""
+    test_activation_backward(T, N, act, dtype)
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("T,K,N", [(1, 520, 1000), (32, 768, 136), (17, 776, 136), (32, 8, 8)])
+def test_forward_about_one_slice(T, K, N, dtype):
+    """About the sums that go in one slice, with a last step that is not full."""
+    _forward(T, K, N, dtype, B.MOE_ACT_SILU, True, True, True, apart=8)
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
 @pytest.mark.parametrize("act", [B.MOE_ACT_GELU, B.MOE_ACT_SILU])
 def test_activations_far_from_zero(act, dtype):
     """Exactly z or nothing far out, never NaN, whatever overflows on the way."""
