@@ -145,6 +145,27 @@ def test_more_rows_than_32_bit_offsets_reach():
     assert ((dW[:, cols].double() - want).abs() <= 2 * T * U * size).all()
 
 
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+def test_more_rows_than_a_launch_of_floats_takes(dtype):
+    T, K, N = 65535 // 4 * 256 + 70, 8, 16
+    g = torch.Generator(device=D).manual_seed(2)
+    x, dz = (torch.randn((T, n), generator=g, device=D).to(DT[dtype]) for n in (K, N))
+    W = torch.randn((K, N), generator=g, device=D).to(DT[dtype])
+    y, dx = torch.full((T, N), float("nan"), device=D, dtype=DT[dtype]), torch.full((T, K), float("nan"), device=D, dtype=DT[dtype])
+    dW, db = torch.full((K, N), float("nan"), device=D), torch.full((N,), float("nan"), device=D)
+    cfg = B.make_linear_config(T, K, N, dtype, grad_overwrite=1)
+    scratch = _scratch(cfg)
+    B.moe_linear_fwd(cfg, x, W, None, None, None, y, scratch)
+    B.moe_linear_bwd(cfg, dz, x, W, dx, dW, scratch)
+    B.moe_act_bwd(cfg, dz, None, None, db, scratch)
+    X, Z, V = x.double(), dz.double(), W.double()
+    for got, want, size in ((y, X @ V, X.abs() @ V.abs()), (dx, Z @ V.t(), Z.abs() @ V.t().abs())):
+        err = 2 * (N + 20) * U * size
+        assert ((got.double() - want).abs() <= err + HALF[dtype] * (want.abs() + err)).all()
+    assert ((dW.double() - X.t() @ Z).abs() <= 2 * T * U * (X.abs().t() @ Z.abs())).all()
+    assert ((db.double() - Z.sum(0)).abs() <= 2 * T * U * Z.abs().sum(0)).all()
+
+
 # ---- gradients ---------------------------------------------------------------------------------
 
 def _slope(act, z):
