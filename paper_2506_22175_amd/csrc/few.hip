@@ -4,12 +4,12 @@
 //   a[t,j] = gelu(x[t] W1[e]),  y[t] = sum over j of w[t,j] a[t,j] W2[e],  e = topk_idx[t,j]
 //
 // What has to move are the chosen experts' weights, 2 M H elements each, once.  Both products go through few_rows.h: a
-// workgroup has 128 columns (float: 64) of one expert and all of the rows that chose it.  The logits are sums in 64 bits, rounded to float:
+// workgroup has 128 columns (float: 64) of one expert, or half as many, and all of the rows that chose it.  The logits are sums in 64 bits, rounded to float:
 // which expert is chosen hangs on their last bits.  The rows between the products are kept in float, or as two bfloat16 that add up
 // to 16 bits of mantissa, which costs the matrix pipe a second instruction where it waits for memory anyway: nothing is rounded to
 // the storage type but y.
 //
-// One token, 2 of 16 experts of 2048/8192 in bfloat16 (134 MB, at the 7 TB/s of a read 19 us): 39 us, of which the first product 20.7
+// One token, 2 of 16 experts of 2048/8192 in bfloat16 (134 MB, at the 7 TB/s of a read 19 us): 38 us, of which the first product 20
 // (3.9 of gate and router in front of its 67 MB), the second 14.8, the join 4.  48 tokens, 4 of 64 experts of 1024/4096 (1.03 GB): 151 us,
 // 6.8 TB/s; the products alone 55 to 61 and 71 to 77.  Seven tokens of 520/1000 in float (67 MB): 35 us, two steps to a wavefront and the way to
 // the first of them, five times over.
@@ -199,9 +199,9 @@ struct FewPlan {
     int expert, n_rows, n_experts;
 };
 // What a workgroup has in LDS: the choices, which only the plan looks at, then the sums.
-template <typename T> struct FewLds {
+template <typename T, bool NARROW = false> struct FewLds {
     FewPlan plan;
-    union { int idx[FEW_TOKENS * FEW_K]; FewSums<T, FEW_WAVES> sums; };
+    union { int idx[FEW_TOKENS * FEW_K]; FewSums<T, FEW_WAVES, NARROW> sums; };
 };
 // The workgroup's expert, the slot-th of those that are chosen (-1: there are fewer), how many are, and how many assignments it has,
 // which are in FewPlan::rows.
@@ -273,7 +273,7 @@ __device__ __forceinline__ FewPick few_plan(const FewArgs& a, int slot, const in
 // Where the choices come from: they are there; or, in the first product, a workgroup routes for itself, which saves the launches between
 // it and the gate: from the gate's sums, or from x and Wg (one or two tokens).
 enum { FEW_ROUTED = 0, FEW_SUMMED = 1, FEW_ALONE = 2 };
-template <typename T, int MODE> __device__ __forceinline__ FewPick few_choices(const FewArgs& a, int slot, bool record, FewLds<T>& lds) {
+template <typename T, int MODE, bool NARROW> __device__ __forceinline__ FewPick few_choices(const FewArgs& a, int slot, bool record, FewLds<T, NARROW>& lds) {
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.T * a.k;
     if constexpr (MODE == FEW_ROUTED) {
         if (n <= FEW_IN_LANES) return few_pick(lane < n ? a.route.idx[lane] : -1, slot, lds.plan);
@@ -320,16 +320,16 @@ template <typename T, int MODE> __device__ __forceinline__ FewPick few_choices(c
 __device__ __forceinline__ float gelu_of(float z) { return 0.5f * z * erfcf(-0.70710678118654752440f * z); }
 
 // ---- first product ----------------------------------------------------------------------------------------------
-// Bound by the weights' way from memory.  A workgroup has 128 columns (float: 64) of an expert and all of M, as nothing may be added up
+// Bound by the weights' way from memory.  A workgroup has 128 columns (float: 64) of an expert, or with few workgroups half as many, and all of M, as nothing may be added up
 // between here and the activation.
-template <typename T, int GROUPS, int MODE>
+template <typename T, int GROUPS, int MODE, bool NARROW>
 __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_kernel(FewArgs a) {
-    __shared__ FewLds<T> lds;
+    __shared__ FewLds<T, NARROW> lds;
     const FewPlan& plan = lds.plan;
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
-    const FewPick pick = few_choices<T, MODE>(a, blockIdx.y, blockIdx.x == 0 && blockIdx.y == 0, lds);
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T, NARROW>::COLS;
+    const FewPick pick = few_choices<T, MODE, NARROW>(a, blockIdx.y, blockIdx.x == 0 && blockIdx.y == 0, lds);
     if (pick.expert < 0) return;
-    constexpr int ROWS = Few<T>::ROWS;
+    constexpr int ROWS = Few<T, NARROW>::ROWS;
     const T* W = reinterpret_cast<const T*>(a.W1) + (long long)pick.expert * a.M * a.H + n0;
     const long long size = (long long)a.T * a.k * a.H;
     for (int r0 = 0; r0 < pick.n_rows; r0 += GROUPS * ROWS) {
@@ -337,12 +337,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_
         unsigned row[GROUPS];
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-            const int r = r0 + g * ROWS + Few<T>::row(lane);
+            const int r = r0 + g * ROWS + Few<T, NARROW>::row(lane);
             row[g] = (unsigned)(plan.rows[r < pick.n_rows ? r : r0] / a.k) * (unsigned)a.ldx * (unsigned)sizeof(T);
         }
         few_acc acc[GROUPS][Few<T>::ACCS];
-        few_sums<T, GROUPS, 1, FEW_WAVES>(W, a.H, a.H - n0, rows, row, a.M, wid, (a.M + Few<T>::STEP - 1) / Few<T>::STEP, acc);
-        few_finish<T, GROUPS, FEW_WAVES>(lds.sums, acc, pick.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
+        few_sums<T, GROUPS, 1, FEW_WAVES, NARROW>(W, a.H, a.H - n0, rows, row, a.M, wid, (a.M + Few<T, NARROW>::STEP - 1) / Few<T, NARROW>::STEP, acc);
+        few_finish<T, GROUPS, FEW_WAVES, NARROW>(lds.sums, acc, pick.n_rows - r0, a.H - n0, [&](int r, int n, float z) {
             const float v = gelu_of(z);
             const long long at = (long long)plan.rows[r0 + r] * a.H + n0 + n;
             if constexpr (sizeof(T) == 4) {
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_second
     __shared__ FewLds<T> lds;
     const FewPlan& plan = lds.plan;
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, n0 = blockIdx.x * Few<T>::COLS;
-    const FewPick pick = few_choices<T, FEW_ROUTED>(a, blockIdx.y, false, lds);
+    const FewPick pick = few_choices<T, FEW_ROUTED, false>(a, blockIdx.y, false, lds);
     if (pick.expert < 0) return;
     constexpr int ROWS = Few<T>::ROWS, PARTS = sizeof(T) == 2 ? 2 : 1;
     const T* W = reinterpret_cast<const T*>(a.W2) + (long long)pick.expert * a.H * a.M + n0;
@@ -493,15 +493,27 @@ template <typename T> moe_status few_launch(const FewArgs& a, const FewDims& d, 
         else few_route_kernel<8><<<a.T, 64, 0, s>>>(a);
         MOE_CHECK_LAUNCH();
     }
-    const dim3 first(up(a.H, Few<T>::COLS), d.slots), second(up(a.M, Few<T>::COLS), d.slots, a.slices);
-#define FEW_BOTH(G, MODE) do { few_first_kernel<T, G, MODE><<<first, FEW_WAVES * 64, 0, s>>>(a); \
-        few_second_kernel<T, G><<<second, FEW_WAVES * 64, 0, s>>>(a); } while (0)
-    if (d.mode == FEW_ALONE) FEW_BOTH(1, FEW_ALONE);
-    else if (d.mode == FEW_SUMMED) FEW_BOTH(1, FEW_SUMMED);
-    else if (d.few_groups <= 1) FEW_BOTH(1, FEW_ROUTED);
-    else if (d.few_groups <= 2) FEW_BOTH(2, FEW_ROUTED);
-    else FEW_BOTH(4, FEW_ROUTED);
-#undef FEW_BOTH
+    // The first product in pieces of half the columns: up to eight tokens, and twice the workgroups are no more than the chip has room for at once
+    // (tokens x experts of M/H, us so / otherwise: 1 x 16 of 1024/4096 20.3 / 21.9; 1 x 64 of 2048/1024, four choices, 26.3 / 30.1; 1 x 16 of 2048/8192
+    // 38.1 / 39.0; too many: 4 x 33 of 520/1000 in float 29.4 / 27.2, 4 x 16 of 1024/4096 34.0 / 32.7).
+    const bool narrow = a.T <= Few<T, true>::ROWS && up(a.H, Few<T>::COLS) * d.slots <= 128;
+    const dim3 first(up(a.H, narrow ? Few<T, true>::COLS : Few<T>::COLS), d.slots), second(up(a.M, Few<T>::COLS), d.slots, a.slices);
+#define FEW_FIRST(G, MODE, NARROW) few_first_kernel<T, G, MODE, NARROW><<<first, FEW_WAVES * 64, 0, s>>>(a)
+#define FEW_SECOND(G) few_second_kernel<T, G><<<second, FEW_WAVES * 64, 0, s>>>(a)
+    if (d.few_groups <= 1) {
+        if (d.mode == FEW_ALONE) { if (narrow) FEW_FIRST(1, FEW_ALONE, true); else FEW_FIRST(1, FEW_ALONE, false); }
+        else if (d.mode == FEW_SUMMED) { if (narrow) FEW_FIRST(1, FEW_SUMMED, true); else FEW_FIRST(1, FEW_SUMMED, false); }
+        else { if (narrow) FEW_FIRST(1, FEW_ROUTED, true); else FEW_FIRST(1, FEW_ROUTED, false); }
+        FEW_SECOND(1);
+    } else if (d.few_groups <= 2) {
+        FEW_FIRST(2, FEW_ROUTED, false);
+        FEW_SECOND(2);
+    } else {
+        FEW_FIRST(4, FEW_ROUTED, false);
+        FEW_SECOND(4);
+    }
+#undef FEW_FIRST
+#undef FEW_SECOND
     MOE_CHECK_LAUNCH();
     few_join_kernel<T><<<dim3(up(a.M, 256), a.T), JOIN_WAVES * 64, 0, s>>>(a);
     MOE_CHECK_LAUNCH();

@@ -12,6 +12,10 @@
 // Rows are read in pieces of 256 bytes, past the caches (537 MB in 64 matrices: pieces of 128 bytes 5.9 TB/s, of 256 6.6, 512 7.1, and
 // 10 % less with ordinary loads; wider pieces would leave a single matrix too few workgroups).
 // The workgroup's wavefronts take the steps in turn and add up their sums through LDS, in their order.
+// Up to eight rows may go in pieces of 128 bytes (NARROW), which is twice the workgroups where there are too few for the chip: a step is twice
+// the k of half the columns.  Lanes l and l + 8 have the same columns and other k, each with its row number l % 8 of the right operand
+// at its own k; of the instruction's result the rows and columns below eight are a sum over the first of these k, those from eight on over the others,
+// and the rest means nothing.
 #pragma once
 #include "common.h"
 #include "wide.h"
@@ -21,14 +25,15 @@ namespace moe {
 typedef float few_acc __attribute__((ext_vector_type(4)));
 typedef __bf16 few_bf16x8 __attribute__((ext_vector_type(8)));
 
-template <typename T> struct Few {
-    static constexpr int COLS = 256 / sizeof(T);     // of a workgroup
-    static constexpr int ROWS = 16;                  // of a group
-    static constexpr int STEP = 32;                  // k
+template <typename T, bool NARROW = false> struct Few {
+    static constexpr int LANES = NARROW ? 8 : 16;    // to a piece
+    static constexpr int COLS = LANES * 16 / sizeof(T);      // of a workgroup
+    static constexpr int ROWS = LANES;               // of a group
+    static constexpr int STEP = 512 / LANES;         // k
     static constexpr int ACCS = 16 / sizeof(T);      // columns of a lane's load
-    static __device__ __forceinline__ int col(int lane) { return ACCS * (lane & 15); }   // first of a lane's columns
-    static __device__ __forceinline__ int k(int lane) { return 8 * (lane >> 4); }        // first of its k
-    static __device__ __forceinline__ int row(int lane) { return lane & 15; }            // its row in the right operand
+    static __device__ __forceinline__ int col(int lane) { return ACCS * (lane % LANES); }    // first of a lane's columns
+    static __device__ __forceinline__ int k(int lane) { return 8 * (lane / LANES); }         // first of its k
+    static __device__ __forceinline__ int row(int lane) { return lane % LANES; }             // its row in the right operand
 };
 
 // What a step loads: eight k of W's columns, and of GROUPS groups of rows, each in PARTS (bfloat16) that add up to it.
@@ -112,7 +117,7 @@ template <int GROUPS, int PARTS> struct FewStep<float, GROUPS, PARTS> {
 
 // Where the wavefronts' sums of eight rows go: rows a bank's width more apart.
 constexpr int FEW_PASS = 8;
-template <typename T, int WAVES> struct FewSums { float v[WAVES][FEW_PASS][Few<T>::COLS + 4]; };
+template <typename T, int WAVES, bool NARROW = false> struct FewSums { float v[NARROW ? 2 * WAVES : WAVES][FEW_PASS][Few<T, NARROW>::COLS + 4]; };
 
 // Sums over the steps first, first + WAVES, ... below `steps` of K (a multiple of 8), each wavefront its own.  W: the workgroup's
 // first column; cols: columns there are from it on; rows: the rows' parts, row: where the lane's row of each group begins, in bytes (any
@@ -120,14 +125,14 @@ template <typename T, int WAVES> struct FewSums { float v[WAVES][FEW_PASS][Few<T
 // A wavefront waits for a step's loads and has no others under way meanwhile: registers for two steps would leave a CU half the wavefronts
 // (and the compiler waits for both where it copies one's to the other's), and sixteen of them have 128 KiB under way, twice what the memory's
 // latency asks of a CU.
-template <typename T, int GROUPS, int PARTS, int WAVES>
+template <typename T, int GROUPS, int PARTS, int WAVES, bool NARROW = false>
 __device__ __forceinline__ void few_sums(const T* W, unsigned ldw, int cols, const T* const (&rows)[PARTS], const unsigned (&row)[GROUPS], int K, int first,
                                          int steps, few_acc (&acc)[GROUPS][Few<T>::ACCS]) {
     const int lane = threadIdx.x & 63;
     // columns past the last are the first ones again, and not looked at
-    const int c = Few<T>::col(lane);
+    const int c = Few<T, NARROW>::col(lane);
     const unsigned col = c < cols ? c : 0;
-    const int k0 = Few<T>::k(lane);
+    const int k0 = Few<T, NARROW>::k(lane);
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
@@ -135,10 +140,10 @@ __device__ __forceinline__ void few_sums(const T* W, unsigned ldw, int cols, con
 #pragma unroll 1
     for (int s = __builtin_amdgcn_readfirstlane(first); s < steps; s += WAVES) {
         FewStep<T, GROUPS, PARTS> x;
-        const int k = s * Few<T>::STEP + k0;
+        const int k = s * Few<T, NARROW>::STEP + k0;
         x.load(W, ldw, col, k, K);
         x.load_rows(rows, row, k, K);
-        if ((s + 1) * Few<T>::STEP > K) {                  // (nothing meets what was loaded in the place of what is not there)
+        if ((s + 1) * Few<T, NARROW>::STEP > K) {                  // (nothing meets what was loaded in the place of what is not there)
             if (k >= K) x.zero();
         }
         x.multiply(acc);
@@ -146,17 +151,18 @@ __device__ __forceinline__ void few_sums(const T* W, unsigned ldw, int cols, con
 }
 
 // f(row of the groups, column, sum) for the sums of all of them, eight rows at a time; every thread of the workgroup comes here.
-template <typename T, int GROUPS, int WAVES, typename F>
-__device__ __forceinline__ void few_finish(FewSums<T, WAVES>& s, const few_acc (&acc)[GROUPS][Few<T>::ACCS], int rows, int cols, F&& f) {
-    constexpr int COLS = Few<T>::COLS, ACCS = Few<T>::ACCS;
+template <typename T, int GROUPS, int WAVES, bool NARROW = false, typename F>
+__device__ __forceinline__ void few_finish(FewSums<T, WAVES, NARROW>& s, const few_acc (&acc)[GROUPS][Few<T>::ACCS], int rows, int cols, F&& f) {
+    constexpr int COLS = Few<T, NARROW>::COLS, ACCS = Few<T>::ACCS, SUMS = NARROW ? 2 * WAVES : WAVES;
+    static_assert(!NARROW || GROUPS == 1, "eight rows");
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
 #pragma unroll
-    for (int p = 0; p < GROUPS * Few<T>::ROWS / FEW_PASS; ++p) {
+    for (int p = 0; p < GROUPS * Few<T, NARROW>::ROWS / FEW_PASS; ++p) {
         if (p * FEW_PASS >= rows) break;
         // lane l has row l % 16 of the group, and in register j of accumulator i column i of the eight (four) number 4 (l / 16) + j
-        const int g = p * FEW_PASS / Few<T>::ROWS, r0 = p * FEW_PASS % Few<T>::ROWS, r = (lane & 15) - r0;
+        const int g = p * FEW_PASS / Few<T>::ROWS, half = lane >> 5, r0 = NARROW ? 8 * half : p * FEW_PASS % Few<T>::ROWS, r = (lane & 15) - r0;
         if (r >= 0 && r < FEW_PASS) {
-            float* o = &s.v[wid][r][ACCS * 4 * (lane >> 4)];
+            float* o = NARROW ? &s.v[2 * wid + half][r][ACCS * 4 * (lane >> 4 & 1)] : &s.v[wid][r][ACCS * 4 * (lane >> 4)];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -169,7 +175,7 @@ __device__ __forceinline__ void few_finish(FewSums<T, WAVES>& s, const few_acc (
             if (p * FEW_PASS + row >= rows || n >= cols) continue;
             float v = 0.0f;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) v += s.v[w][row][n];
+            for (int w = 0; w < SUMS; ++w) v += s.v[w][row][n];
             f(p * FEW_PASS + row, n, v);
         }
         __syncthreads();

@@ -122,6 +122,14 @@ ROUTERS = {
 
 
 @pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+@pytest.mark.parametrize("T,M,H,E,k", [(1, 64, 16400, 16, 2), (2, 72, 8200, 16, 2), (4, 72, 4104, 16, 4), (7, 136, 4104, 16, 2), (1, 136, 8192, 16, 2), (8, 200, 72, 4, 2),
+                                       (9, 200, 72, 4, 2), (8, 8, 8, 1, 1), (3, 104, 1032, 100, 3), (8, 1096, 136, 8, 8)])
+def test_both_widths_of_the_first_product(T, M, H, E, k, dtype):
+    """Up to eight tokens, with few and with many workgroups for them, and sums that end inside a step."""
+    test_shapes(T, M, H, E, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
 @pytest.mark.parametrize("router", list(ROUTERS))
 @pytest.mark.parametrize("T", [1, 2, 13, 100])
 def test_routers_and_rows_that_lie_apart(T, router, dtype):
