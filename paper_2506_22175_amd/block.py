@@ -22,12 +22,38 @@ from . import binding as B
 _TORCH = {B.MOE_F32: torch.float32, B.MOE_BF16: torch.bfloat16}
 
 
-class Shared:
-    """The shared expert's two products for T rows of M: weights V1 [M,N], V2 [N,M] of `dtype`, biases float or None.  With `training`
-    its gradients dV1, dV2, db1, db2 (float) are overwritten by backward."""
+def _code(name, W):
+    for code, dtype in _TORCH.items():
+        if W.dtype == dtype:
+            return code
+    raise ValueError(f"{name} is {W.dtype}: weights are float32 or bfloat16")
 
-    def __init__(self, T, V1, V2, b1=None, b2=None, training=False, device="cuda:0"):
-        (M, N), dtype = V1.shape, B.MOE_F32 if V1.dtype == torch.float32 else B.MOE_BF16
+
+def _check_weights(device, *weights):
+    """The library is handed addresses: what another type, size or order of the elements would make it read or write is refused here,
+    before anything is allocated.  weights: (name, tensor or None, type, shape); of a vector its elements count."""
+    device = torch.device(device)
+    for name, W, dtype, shape in weights:
+        if W is None:
+            continue
+        fits = W.numel() == shape[0] if len(shape) == 1 else W.shape == shape
+        if W.dtype != dtype or not fits or not W.is_contiguous():
+            raise ValueError(f"{name} has to be contiguous {dtype} {tuple(shape)}; it is {W.dtype} {tuple(W.shape)}, strides {W.stride()}")
+        if W.device.type != device.type or (device.index is not None and W.device.index != device.index):
+            raise ValueError(f"{name} is on {W.device}, the block on {device}")
+
+
+class Shared:
+    """The shared expert's two products for T rows of M: weights V1 [M,N], V2 [N,M], both float32 or both bfloat16 as the rows are, biases
+    float32 or None.  With `training` its gradients dV1, dV2, db1, db2 (float) are overwritten by backward.  rows: width and type of the
+    rows that it is to meet, refused where the weights have others."""
+
+    def __init__(self, T, V1, V2, b1=None, b2=None, training=False, device="cuda:0", rows=None):
+        (M, N), dtype = V1.shape, _code("V1", V1)
+        if rows is not None and rows != (M, dtype):
+            raise ValueError(f"V1 is {V1.dtype} {tuple(V1.shape)}: the block's rows are {_TORCH[rows[1]]} and {rows[0]} wide")
+        _check_weights(device, ("V1", V1, V1.dtype, (M, N)), ("V2", V2, V1.dtype, (N, M)), ("b1", b1, torch.float32, (N,)),
+                       ("b2", b2, torch.float32, (M,)))
         self.V1, self.V2, self.b1, self.b2 = V1, V2, b1, b2
         self.first = B.make_linear_config(T, M, N, dtype, B.MOE_ACT_GELU, 1)
         self.second = B.make_linear_config(T, N, M, dtype, B.MOE_ACT_NONE, 1)
@@ -36,7 +62,7 @@ class Shared:
         if training:
             self.z, self.da = torch.empty_like(self.a), torch.empty_like(self.a)
             self.dV1, self.dV2 = (torch.empty(V.shape, dtype=torch.float32, device=device) for V in (V1, V2))
-            self.db1, self.db2 = (None if b is None else torch.empty_like(b) for b in (b1, b2))
+            self.db1, self.db2 = (None if b is None else torch.empty(b.numel(), dtype=torch.float32, device=device) for b in (b1, b2))
         need = max(B.moe_linear_scratch_bytes(c) for c in (self.first, self.second))
         self.scratch = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
 
@@ -64,6 +90,10 @@ class Block:
 
     def __init__(self, T, M, H, E, k, gain, Wg, W1, W2, bias=None, capacity_factor=1.25, dtype=B.MOE_BF16, eps=1e-6,
                  scores=B.MOE_SOFTMAX, renormalize=0, groups=1, group_k=1, scale=1.0, device="cuda:0", shared=None):
+        f32, i32 = torch.float32, torch.int32
+        _check_weights(device, ("gain", gain, f32, (M,)), ("Wg", Wg, _TORCH[dtype], (M, E)), ("W1", W1, _TORCH[dtype], (E, M, H)),
+                       ("W2", W2, _TORCH[dtype], (E, H, M)), ("bias", bias, f32, (E,)))
+        self.shared = None if shared is None else Shared(T, *shared, training=True, device=device, rows=(M, dtype))
         self.gain, self.Wg, self.W1, self.W2, self.bias = gain, Wg, W1, W2, bias
         self.layer = B.make_config(T, M, H, E, k, capacity_factor, 1, dtype, 0, 1)
         self.norm = B.make_norm_config(T, M, eps, dtype, grad_overwrite=1)
@@ -73,7 +103,6 @@ class Block:
         def new(*shape, dtype=_TORCH[dtype]):
             return torch.empty(shape, dtype=dtype, device=device)
 
-        f32, i32 = torch.float32, torch.int32
         self.h, self.y, self.out, self.dy, self.dx = (new(T, M) for _ in range(5))
         self.rstd, self.logits, self.dlogits = new(T, dtype=f32), new(T, E, dtype=f32), new(T, E, dtype=f32)
         self.topk_idx, self.slot, self.counts = new(T, k, dtype=i32), new(T, k, dtype=i32), new(1, E, dtype=i32)
@@ -86,7 +115,6 @@ class Block:
         self.slot_scratch = new(B.moe_slot_scratch_bytes(self.layer), dtype=torch.uint8)
         self.gate_scratch = new(B.moe_gate_scratch_bytes(self.layer), dtype=torch.uint8)
         self.norm_scratch = new(B.moe_norm_scratch_bytes(self.norm), dtype=torch.uint8)
-        self.shared = None if shared is None else Shared(T, *shared, training=True, device=device)
         # the gradients' list is laid out once: backward writes to the same memory every time
         self.gradients = [self.dgain, self.dWg, self.dW1, self.dW2] + ([] if shared is None else self.shared.gradients())
         self.grad_list = B.make_grad_list(self.gradients, self.gradients)
@@ -130,8 +158,8 @@ class Packed:
     """The experts' weights of a trained block in 4 bits, laid out once."""
 
     def __init__(self, W1, W2):
-        self.E, self.M, self.H = W1.shape
-        dtype = B.MOE_F32 if W1.dtype == torch.float32 else B.MOE_BF16
+        (self.E, self.M, self.H), dtype = W1.shape, _code("W1", W1)
+        _check_weights(W1.device, ("W1", W1, W1.dtype, W1.shape), ("W2", W2, W1.dtype, (self.E, self.H, self.M)))
 
         def pack(W, K, N):
             q = torch.empty((self.E, N, K // 2), dtype=torch.uint8, device=W.device)
@@ -149,6 +177,7 @@ class Served:
     def __init__(self, T, k, gain, Wg, packed, bias=None, dtype=B.MOE_BF16, eps=1e-6, scores=B.MOE_SOFTMAX, renormalize=0,
                  groups=1, group_k=1, scale=1.0, eight_bits=False, device="cuda:0"):
         p, M, H, E = packed, packed.M, packed.H, packed.E
+        _check_weights(device, ("gain", gain, torch.float32, (M,)), ("Wg", Wg, _TORCH[dtype], (M, E)), ("bias", bias, torch.float32, (E,)))
         self.gain, self.Wg, self.bias, self.packed, self.eight_bits = gain, Wg, bias, p, eight_bits
         self.layer = B.make_config(T, M, H, E, k, 1.0, 1, dtype)
         self.norm = B.make_norm_config(T, M, eps, dtype)
@@ -188,12 +217,13 @@ class Few:
 
     def __init__(self, T, k, gain, Wg, W1, W2, bias=None, eps=1e-6, scores=B.MOE_SOFTMAX, renormalize=0, groups=1, group_k=1,
                  scale=1.0, device="cuda:0", shared=None):
-        E, M, H = W1.shape
-        dtype = B.MOE_F32 if W1.dtype == torch.float32 else B.MOE_BF16
+        (E, M, H), dtype = W1.shape, _code("W1", W1)
+        _check_weights(device, ("gain", gain, torch.float32, (M,)), ("Wg", Wg, W1.dtype, (M, E)), ("W1", W1, W1.dtype, (E, M, H)),
+                       ("W2", W2, W1.dtype, (E, H, M)), ("bias", bias, torch.float32, (E,)))
+        self.shared = None if shared is None else Shared(T, *shared, device=device, rows=(M, dtype))
         self.gain, self.Wg, self.W1, self.W2, self.bias = gain, Wg, W1, W2, bias
         self.norm = B.make_norm_config(T, M, eps, dtype)
         self.layer = B.make_few_config(T, M, H, E, k, dtype, scores, groups, group_k, 2, renormalize, scale)
-        self.shared = None if shared is None else Shared(T, *shared, device=device)
         self.h, self.y, self.out = (torch.empty((T, M), dtype=W1.dtype, device=device) for _ in range(3))
         self.logits, self.topk_w = (torch.empty((T, n), dtype=torch.float32, device=device) for n in (E, k))
         self.topk_idx = torch.empty((T, k), dtype=torch.int32, device=device)
