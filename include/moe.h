@@ -505,7 +505,8 @@ typedef struct {
 } moe_linear_config;
 
 /* z = x W + bias;  y = act(z) + residual.  Sums are float; the activation is taken of the float sum (its own error for bfloat16 below
- * 1.2e-4 of it, GeLU's far on the negative side included); z and y are rounded once.
+ * 1.2e-4 of it, GeLU's far on the negative side included; SiLU's
+ * results of less than 1e-36 may be zero there); z and y are rounded once.
  *   x [T,K]; W [K,N]; bias [N] float, may be NULL; residual [T,N], may be NULL, may be y itself (with its stride);
  *   z [T,N] out, may be NULL (kept for backward); y [T,N] out;
  *   scratch: moe_linear_scratch_bytes(cfg) bytes, for this call and the two below, which may share it. */

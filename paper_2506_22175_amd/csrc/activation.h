@@ -4,18 +4,18 @@
 
 namespace moe {
 
-// Phi(z), and exp(-z^2 / 2) on the way: erfc by the five-term rational approximation of Abramowitz & Stegun 7.1.26 (off by
+// Phi(z), and the root of exp(-z^2 / 2) on the way: erfc by the five-term rational approximation of Abramowitz & Stegun 7.1.26 (off by
 // at most 1.5e-7), taken as it is on the negative side, where 1 - erf would lose what is left.  For results that are
 // rounded to bfloat16.
-__device__ __forceinline__ float normal_cdf_fast(float z, float* ex) {
+__device__ __forceinline__ float normal_cdf_fast(float z, float* root) {
     const float x = fabsf(z) * 0.70710678118654752440f;
     const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-    *ex = __builtin_amdgcn_exp2f(-x * x * 1.44269504088896340736f);
+    *root = __builtin_amdgcn_exp2f(x * x * (-0.5f * 1.44269504088896340736f));
     float p = fmaf(t, 1.061405429f, -1.453152027f);
     p = fmaf(t, p, 1.421413741f);
     p = fmaf(t, p, -0.284496736f);
     p = fmaf(t, p, 0.254829592f);
-    const float tail = 0.5f * p * t * *ex;
+    const float tail = 0.5f * p * t * *root * *root;
     return z < 0.0f ? tail : 1.0f - tail;
 }
 __device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-0.70710678118654752440f * z); }
@@ -38,16 +38,27 @@ __device__ __forceinline__ float gelu_tail_f(float z) {
     return fmaf(-a, p * (t * ex), fmaf(0.5f, fabsf(z), 0.5f * z));
 }
 
+// z sigmoid(z).  exp(-z) leaves the range of the reciprocal instruction at -87.3, and that of float soon after, where the result is 1e-36 still.
+// bfloat16: such results are lost, and zero.  (The form that keeps them has one instruction more, and costs the 256 x 256 tile 5 to 20 %, it seems
+// where the epilogue no longer stays in the instruction cache from launch to launch: 8192 x 2048 x 8192 with z kept 235 us and 248,
+// 8192 x 512 x 2048 30 and 36.)
+__device__ __forceinline__ float silu_fast(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z)); }
+// float: the exponential as the square of its root
+__device__ __forceinline__ float silu(float z) {
+    const float root = expf(-0.5f * fabsf(z)), q = 1.0f / fmaf(root, root, 1.0f);
+    return z < 0.0f ? (z * root) * (root * q) : z * q;
+}
+
 // act(z); act is the same for a whole launch
 template <typename T> __device__ __forceinline__ float activate(float z, int act);
 template <> __device__ __forceinline__ float activate<bf16_t>(float z, int act) {
     if (act == MOE_ACT_GELU) return gelu_tail_f(z);
-    if (act == MOE_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z));
+    if (act == MOE_ACT_SILU) return silu_fast(z);
     return z;
 }
 template <> __device__ __forceinline__ float activate<float>(float z, int act) {
     if (act == MOE_ACT_GELU) return z * normal_cdf(z);
-    if (act == MOE_ACT_SILU) return z / (1.0f + expf(-z));
+    if (act == MOE_ACT_SILU) return silu(z);
     return z;
 }
 
@@ -65,20 +76,21 @@ template <typename T, int N> __device__ __forceinline__ void activate_all(const 
     }
 }
 
-// act'(z) = Phi(z) + z phi(z), or s (1 + z (1 - s)) with s the sigmoid of z
+// act'(z) = Phi(z) + z phi(z), or s (1 + z (1 - s)) with s the sigmoid of z.  Exponentials are squares of their roots, which the factors are
+// multiplied with one after the other: a slope is a normal number for some way after its exponential has ceased to be one.
 template <typename T> __device__ __forceinline__ float activation_slope(float z, int act) {
     constexpr bool FAST = sizeof(T) == 2;
     if (act == MOE_ACT_GELU) {
-        float ex, cdf;
-        if (FAST) cdf = normal_cdf_fast(z, &ex);
-        else { cdf = normal_cdf(z); ex = expf(-0.5f * z * z); }
-        return fmaf(z * 0.39894228040143267794f, ex, cdf);
+        float root, cdf;
+        if (FAST) cdf = normal_cdf_fast(z, &root);
+        else { cdf = normal_cdf(z); root = expf(-0.25f * z * z); }
+        return fmaf(z * 0.39894228040143267794f * root, root, cdf);
     }
     if (act == MOE_ACT_SILU) {
-        const float e = FAST ? __builtin_amdgcn_exp2f(-1.44269504088896340736f * fabsf(z)) : expf(-fabsf(z));
+        const float root = FAST ? __builtin_amdgcn_exp2f((-0.5f * 1.44269504088896340736f) * fabsf(z)) : expf(-0.5f * fabsf(z)), e = root * root;
         const float q = FAST ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e);
-        const float s = z < 0.0f ? e * q : q, rest = z < 0.0f ? q : e * q;         // sigmoid(z), 1 - sigmoid(z)
-        return s * fmaf(z, rest, 1.0f);
+        const float f = fmaf(z, z < 0.0f ? q : e * q, 1.0f);                       // 1 + z (1 - sigmoid(z))
+        return z < 0.0f ? (root * f) * (root * q) : q * f;
     }
     return 1.0f;
 }
