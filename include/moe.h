@@ -546,8 +546,8 @@ moe_status moe_grad_table(const moe_grad_tensor* tensors, int32_t count, void* t
 /* norm[0] = the root of the sum of squares of all elements: squares and sum in 64 bits, in an order that depends on the sizes, rounded
  * to float.  NaN or infinity where an element is, 0 without elements.   norm: float out; scratch: 8-byte aligned. */
 moe_status moe_grad_norm(const moe_grad_list* list, float* norm, void* scratch, void* stream);
-/* out = grad * (most / norm[0]) where norm[0] > most, rounded once, else grad.  A norm that is NaN or infinite scales nothing (its step is to
- * be skipped).  norm: float in, of moe_grad_norm or of several processes' together; most: finite, not negative. */
+/* out = grad * (most / norm[0]) where norm[0] > most, computed in 64 bits and rounded once to its type, else grad.
+ * A norm that is NaN or infinite scales nothing (its step is to be skipped).  norm: float in, of moe_grad_norm or of several processes' together; most: finite, not negative. */
 moe_status moe_grad_scale(const moe_grad_list* list, float most, const float* norm, void* stream);
 /* Both: norm out, then the scaling. */
 moe_status moe_grad_clip(const moe_grad_list* list, float most, float* norm, void* scratch, void* stream);

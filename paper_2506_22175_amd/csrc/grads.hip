@@ -57,6 +57,15 @@ __global__ __launch_bounds__(256) void grad_table_kernel(GradTableArgs a, GradCh
 constexpr long long GRAD_KEPT = 128 * 1024 * 1024 / GRAD_CHUNK;
 struct GradArgs { const GradChunk* table; int chunks, kept, partials; double* partial; float* norm; float most; };
 
+// A float that rounds to bfloat16 as d does: 14 bits of its mantissa, the last one set where anything follows it, which float has room for wherever
+// a bfloat16 may come of it.  (d's nearest float may lie in the middle of two bfloat16 where d does not.)
+__device__ __forceinline__ float for_bf16(double d) {
+    const unsigned long long b = __double_as_longlong(d);
+    const unsigned hi = (unsigned)(b >> 32), below = (hi & 63u) | (unsigned)b;
+    const unsigned odd = (hi & ~63u) | (below < 1u ? below : 1u) << 6;
+    return (float)__longlong_as_double((long long)((unsigned long long)odd << 32));
+}
+
 // A chunk and what a thread has of it: units of 16 bytes, and an element behind the last whole one.
 struct Chunk {
     const char* grad; char* out;
@@ -105,21 +114,26 @@ struct Chunk {
     }
     template <bool ONCE> __device__ __forceinline__ void store(double factor) const {
         auto times = [factor](float f) { return (float)((double)f * factor); };
+        auto times_bf16 = [factor](float f) { return for_bf16((double)f * factor); };
 #pragma unroll
         for (int j = 0; j < GRAD_LOADS; ++j) {
             if (unit(j) >= whole) continue;
             Anywhere<16, 2> o;
+            if (bf16) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const unsigned w = v[j].w[q];
-                o.w[q] = bf16 ? pack_bf16x2(times(__uint_as_float(w << 16)), times(__uint_as_float(w & 0xffff0000u)))
-                              : __float_as_uint(times(__uint_as_float(w)));
+                for (int q = 0; q < 4; ++q) {
+                    const unsigned w = v[j].w[q];
+                    o.w[q] = pack_bf16x2(times_bf16(__uint_as_float(w << 16)), times_bf16(__uint_as_float(w & 0xffff0000u)));
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) o.w[q] = __float_as_uint(times(__uint_as_float(v[j].w[q])));
             }
             if (ONCE) store_once_anywhere(out + unit(j) * 16, o); else *reinterpret_cast<Anywhere<16, 2>*>(out + unit(j) * 16) = o;
         }
         if (has_tail()) {
             char* p = out + whole * 16;
-            if (bf16) Elem<bf16_t>::st(reinterpret_cast<bf16_t*>(p) + threadIdx.x, times(tail));
+            if (bf16) Elem<bf16_t>::st(reinterpret_cast<bf16_t*>(p) + threadIdx.x, times_bf16(tail));
             else reinterpret_cast<float*>(p)[threadIdx.x] = times(tail);
         }
     }
