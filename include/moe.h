@@ -525,6 +525,10 @@ moe_status moe_act_bwd(const moe_linear_config* cfg, const void* dy, const void*
 moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* dz, const void* x, const void* W, const void* add, void* dx,
                           float* dW, void* scratch, void* stream);
 moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, size_t* bytes);
+/* Host only.  Rows and columns of the output tiles in which one of the products is computed (of the forward product of up to 32 rows, of a
+ * workgroup), and how many partial sums of an output element another launch adds up (1: none).  All 0 for T = 0. */
+typedef enum { MOE_LINEAR_FWD = 0, MOE_LINEAR_DX = 1, MOE_LINEAR_DW = 2 } moe_linear_gemm;
+moe_status moe_linear_tile(const moe_linear_config* cfg, int32_t gemm, int32_t* rows, int32_t* cols, int32_t* sums);
 
 /* The norm of many tensors together, and clipping by it.  A list of tensors is laid out in device memory once (again when their
  * addresses change) and serves any number of calls, one at a time: two calls that overlap on one table or scratch race. */

@@ -35,6 +35,7 @@ EXPORTS = [
     "moe_norm_fwd", "moe_norm_bwd", "moe_norm_scratch_bytes", "moe_router_fwd", "moe_router_bwd",
     "moe_w4_product", "moe_w4_scratch_bytes", "moe_w4_quantize",
     "moe_few_forward", "moe_few_scratch_bytes", "moe_linear_fwd", "moe_act_bwd", "moe_linear_bwd", "moe_linear_scratch_bytes",
+    "moe_linear_tile",
     "moe_grad_bytes", "moe_grad_table", "moe_grad_norm", "moe_grad_scale", "moe_grad_clip",
 ]
 
@@ -563,6 +564,16 @@ def moe_act_bwd(cfg, dy, z, dz, dbias, scratch, stream=None):
 
 def moe_linear_bwd(cfg, dz, x, W, dx, dW, scratch, add=None, stream=None):
     _check(lib().moe_linear_bwd(_cfg(cfg), _a(dz), _a(x), _a(W), _a(add), _a(dx), _a(dW), _a(scratch), _h(stream)), "moe_linear_bwd")
+
+
+LINEAR_GEMMS = ("fwd", "dx", "dW")
+
+
+def moe_linear_tile(cfg, gemm: str):
+    """(rows, columns, partial sums) of one of LINEAR_GEMMS."""
+    v = [ctypes.c_int32(0) for _ in range(3)]
+    _check(lib().moe_linear_tile(_cfg(cfg), ctypes.c_int32(LINEAR_GEMMS.index(gemm)), *(ctypes.byref(n) for n in v)), "moe_linear_tile")
+    return tuple(n.value for n in v)
 
 
 class MoEGradTensor(ctypes.Structure):

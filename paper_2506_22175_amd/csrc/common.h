@@ -284,7 +284,7 @@ int gemm_bf16_slices(GemmLayout lay, const GemmArgs& a, int least);
 int gemm_f32_slices(const GemmArgs& a, int least);
 int gemm_bf16_dw_parts(int H);   // column blocks the DGELU epilogue reports per row
 int gemm_f32_dw_parts(int H);
-void gemm_bf16_tile(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, int* rows, int* cols);   // of a launch; host only
+void gemm_bf16_tile(GemmLayout lay, int epi, const GemmArgs& a, int* rows, int* cols);   // of a launch; host only
 void gemm_f32_tile(int* rows, int* cols);
 
 // ---- one partition's expert FFN (ffn.hip) ---------------------------------------

@@ -1934,8 +1934,8 @@ int gemm_bf16_slices(GemmLayout lay, const GemmArgs& a, int least) {
     return slices;
 }
 
-void gemm_bf16_tile(GemmLayout lay, GemmEpilogue epi, const GemmArgs& a, int* rows, int* cols) {
-    const TileCost& c = TILE_COSTS[tile_choice(lay, epi, a)];
+void gemm_bf16_tile(GemmLayout lay, int epi, const GemmArgs& a, int* rows, int* cols) {
+    const TileCost& c = TILE_COSTS[!(epi & EPI_SLICES) ? tile_choice(lay, epi_of(epi), a) : lay == GEMM_NN ? slice_choice<GEMM_NN>(a) : slice_choice<GEMM_NT>(a)];
     *rows = c.bm;
     *cols = c.bn;
 }

@@ -92,14 +92,33 @@ moe_status linear_dims(const moe_linear_config* c, LinearDims* d) {
     return MOE_OK;
 }
 
-// Slices of the sum in which a GEMM over the rows goes (few tiles, long sums).
-int gemm_slices(const LinearDims& d, GemmLayout lay, int N, int K) {
+// What the choice of a tile goes by, of the GEMMs over the rows and of the weight gradient's.
+GemmArgs rows_gemm(const LinearDims& d, int N, int K, int act) {
     GemmArgs g = {};
-    g.E = 1; g.Cp = d.block; g.mean_rows = d.block; g.N = N; g.K = K;
+    g.E = d.blocks; g.Cp = d.block; g.mean_rows = up(d.T, d.blocks);
+    g.N = N; g.K = K; g.act = act; g.rows = d.T;
+    return g;
+}
+GemmArgs fwd_gemm(const LinearDims& d) { return rows_gemm(d, d.N, d.K, d.act); }
+GemmArgs dx_gemm(const LinearDims& d) { return rows_gemm(d, d.K, d.N, MOE_ACT_NONE); }
+GemmArgs dw_gemm(const LinearDims& d) {
+    GemmArgs g = {};
+    g.E = d.wblocks; g.Cp = d.wblock; g.mean_rows = up(d.T, d.wblocks); g.rows = d.T;
+    g.Mo = d.K; g.N = d.N;
+    return g;
+}
+// Slices of the sum in which a GEMM over the rows goes (few tiles, long sums), and one of them.
+int gemm_slices(const LinearDims& d, GemmLayout lay, const GemmArgs& g) {
     return d.blocks > 1 ? 1 : d.bf16 ? gemm_bf16_slices(lay, g, 256) : gemm_f32_slices(g, 128);
 }
-int fwd_slices(const LinearDims& d) { return gemm_slices(d, GEMM_NN, d.N, d.K); }
-int dx_slices(const LinearDims& d) { return gemm_slices(d, GEMM_NT, d.K, d.N); }
+int fwd_slices(const LinearDims& d) { return gemm_slices(d, GEMM_NN, fwd_gemm(d)); }
+int dx_slices(const LinearDims& d) { return gemm_slices(d, GEMM_NT, dx_gemm(d)); }
+GemmArgs slice_of(GemmArgs g, int slices) {
+    g.k_total = g.K;
+    g.K = up(up(g.K, slices), 64) * 64;
+    g.E = up(g.k_total, g.K);
+    return g;
+}
 
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
 // A dz of more bytes than this, which would not be found in the memory-side cache by the products behind it anyway, is written past the caches
@@ -187,10 +206,14 @@ template <typename T> moe_status linear_finish_launch(const FewLinearArgs& a, in
     return MOE_OK;
 }
 
+// Slices that have steps to do.
+int few_linear_slices(const LinearDims& d) {
+    const int steps = up(d.K, Few<float>::STEP);
+    return up(steps, up(steps, d.slices));
+}
 template <typename T> moe_status few_linear(const LinearDims& d, FewLinearArgs a, hipStream_t s) {
-    const int steps = up(d.K, Few<T>::STEP);
-    a.steps = up(steps, d.slices);
-    const int slices = up(steps, a.steps);
+    a.steps = up(up(d.K, Few<T>::STEP), d.slices);
+    const int slices = few_linear_slices(d);
     if (slices == 1) a.partial = nullptr;
     const dim3 grid(up(d.N, Few<T>::COLS), slices);
     const int groups = up(d.T, Few<T>::ROWS);
@@ -380,11 +403,7 @@ moe_status gemm(const LinearDims& d, GemmLayout lay, int epi, const GemmArgs& a,
 
 // A product of one block of rows in slices of its sum, whose partial sums the epilogue adds up.  g: A, B, their strides, N, K.
 moe_status sliced(const LinearDims& d, GemmLayout lay, int slices, GemmArgs g, const FewLinearArgs& a, hipStream_t s) {
-    const int total = g.K;
-    g.K = up(up(total, slices), 64) * 64;
-    g.k_total = total;
-    g.E = up(total, g.K);
-    g.Cp = g.mean_rows = d.T;
+    g = slice_of(g, slices);
     g.a_estride = g.K;
     g.b_estride = lay == GEMM_NN ? (long long)g.K * g.ldb : g.K;
     g.C = a.partial;
@@ -421,6 +440,38 @@ extern "C" moe_status moe_linear_scratch_bytes(const moe_linear_config* cfg, siz
     return MOE_OK;
 }
 
+extern "C" moe_status moe_linear_tile(const moe_linear_config* cfg, int32_t gemm, int32_t* rows, int32_t* cols, int32_t* sums) {
+    moe::LinearDims d;
+    MOE_TRY(moe::linear_dims(cfg, &d));
+    if (!rows || !cols || !sums) return MOE_ERR_NULL;
+    if (gemm < MOE_LINEAR_FWD || gemm > MOE_LINEAR_DW) return MOE_ERR_SHAPE;
+    *rows = *cols = *sums = 0;
+    if (d.T == 0) return MOE_OK;
+    if (gemm == MOE_LINEAR_FWD && d.T <= moe::FEW_LINEAR_ROWS) {
+        *rows = (d.T > moe::Few<float>::ROWS ? 2 : 1) * moe::Few<float>::ROWS;
+        *cols = d.bf16 ? moe::Few<moe::bf16_t>::COLS : moe::Few<float>::COLS;
+        *sums = moe::few_linear_slices(d);
+        return MOE_OK;
+    }
+    const moe::GemmLayout lay = gemm == MOE_LINEAR_FWD ? moe::GEMM_NN : gemm == MOE_LINEAR_DX ? moe::GEMM_NT : moe::GEMM_TN;
+    moe::GemmArgs g = gemm == MOE_LINEAR_FWD ? moe::fwd_gemm(d) : gemm == MOE_LINEAR_DX ? moe::dx_gemm(d) : moe::dw_gemm(d);
+    int epi = gemm == MOE_LINEAR_FWD ? moe::EPI_LINEAR : moe::EPI_STORE;
+    if (gemm == MOE_LINEAR_DW) {
+        *sums = d.wblocks;
+        epi = d.wblocks > 1 || d.overwrite ? moe::EPI_STORE_F32 : moe::EPI_ACCUM_F32;
+    } else {
+        const int slices = moe::gemm_slices(d, lay, g);
+        if (slices > 1) {
+            g = moe::slice_of(g, slices);
+            epi = moe::EPI_STORE_F32 | moe::EPI_SLICES;
+        }
+        *sums = slices > 1 ? g.E : 1;
+    }
+    if (d.bf16) moe::gemm_bf16_tile(lay, epi, g, rows, cols);
+    else moe::gemm_f32_tile(rows, cols);
+    return MOE_OK;
+}
+
 extern "C" moe_status moe_linear_fwd(const moe_linear_config* cfg, const void* x, const void* W, const float* bias, const void* residual,
                                      void* z, void* y, void* scratch, void* stream) {
     moe::LinearDims d;
@@ -439,14 +490,12 @@ extern "C" moe_status moe_linear_fwd(const moe_linear_config* cfg, const void* x
         moe::count_launch(moe::LC_GEMM);
         return MOE_OK;
     }
-    moe::GemmArgs g = {};
+    moe::GemmArgs g = moe::fwd_gemm(d);
     g.A = x; g.B = W; g.C = y;
     g.a_estride = d.block * d.ldx; g.b_estride = 0; g.c_estride = d.block * d.ldy;
     g.lda = (int)d.ldx; g.ldb = d.N; g.ldc = (int)d.ldy;
-    g.E = d.blocks; g.Cp = d.block; g.mean_rows = moe::up(d.T, d.blocks);
-    g.N = d.N; g.K = d.K;
     g.Z = z; g.ldz = (int)d.ldz;
-    g.bias = bias; g.R = residual; g.ldr = (int)d.ldr; g.act = d.act; g.rows = d.T;
+    g.bias = bias; g.R = residual; g.ldr = (int)d.ldr;
     const int slices = moe::fwd_slices(d);
     if (slices > 1)
         return moe::sliced(d, moe::GEMM_NN, slices, g,
@@ -496,13 +545,11 @@ extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* d
         !moe::aligned16(scratch))
         return MOE_ERR_UNSUPPORTED;
     if (dx) {
-        moe::GemmArgs g = {};
+        moe::GemmArgs g = moe::dx_gemm(d);
         g.A = dz; g.B = W; g.C = dx;
         g.a_estride = d.block * d.ldz; g.b_estride = 0; g.c_estride = d.block * d.ldx;
         g.lda = (int)d.ldz; g.ldb = d.N; g.ldc = (int)d.ldx;
-        g.E = d.blocks; g.Cp = d.block; g.mean_rows = moe::up(d.T, d.blocks);
-        g.N = d.K; g.K = d.N;
-        g.R = add; g.ldr = (int)d.ldx; g.act = MOE_ACT_NONE; g.rows = d.T;
+        g.R = add; g.ldr = (int)d.ldx;
         const int slices = moe::dx_slices(d);
         if (slices > 1) {
             MOE_TRY(moe::sliced(d, moe::GEMM_NT, slices, g,
@@ -513,14 +560,12 @@ extern "C" moe_status moe_linear_bwd(const moe_linear_config* cfg, const void* d
         }
     }
     if (dW) {
-        moe::GemmArgs g = {};
+        moe::GemmArgs g = moe::dw_gemm(d);
         const bool split = d.wblocks > 1;
         float* parts = (float*)scratch;
         g.A = x; g.B = dz; g.C = split ? parts : dW;
         g.a_estride = d.wblock * d.ldx; g.b_estride = d.wblock * d.ldz; g.c_estride = (long long)d.K * d.N;
         g.lda = (int)d.ldx; g.ldb = (int)d.ldz; g.ldc = d.N;
-        g.E = d.wblocks; g.Cp = d.wblock; g.mean_rows = moe::up(d.T, d.wblocks); g.rows = d.T;
-        g.Mo = d.K; g.N = d.N;
         MOE_TRY(moe::gemm(d, moe::GEMM_TN, (split || d.overwrite ? moe::EPI_STORE_F32 : moe::EPI_ACCUM_F32) | moe::EPI_BLOCKS, g, s));
         if (split) MOE_TRY(moe::join_parts(parts, d.wblocks, (long long)d.K * d.N, dW, d.overwrite, s));
     }
