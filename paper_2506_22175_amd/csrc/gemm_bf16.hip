@@ -1911,9 +1911,11 @@ static moe_status launch_slices(const GemmArgs& a, hipStream_t s) {
     return launch_one<LAY, EPI, CfgT>(a, s);
 }
 // How many slices of K a product of one block of rows goes in, whose partial sums a second launch adds up (1: none).  64 rows, K = 8192,
-// N = 2048: 15.5 us, 41 in one piece.
+// N = 2048: 15.5 us, 41 in one piece.  The launch without slices is the one that there would be: NN is the dense product, whose epilogue the
+// 64 x 64 tile does not have (weighed against that tile's store, 11 % of products of 33 to 8000 rows stayed whole: 1664 rows, K = 5584, N = 432
+// 36.5 us and 28.1 in slices, 84 rows, 2976, 5600 22.7 and 16.1; the other way 4565 rows, 2968, 224 22.1 and 25.5).
 int gemm_bf16_slices(GemmLayout lay, const GemmArgs& a, int least) {
-    const int cus = compute_units();
+    const int cus = compute_units(), whole = lay == GEMM_NN ? EPI_LINEAR : EPI_STORE;
     double fastest = 0.0;
     int slices = 1;
     if ((long long)((a.Cp + 63) / 64) * ((a.N + 127) / 128) >= cus) return 1;
@@ -1923,7 +1925,7 @@ int gemm_bf16_slices(GemmLayout lay, const GemmArgs& a, int least) {
         g.E = (a.K + g.K - 1) / g.K;
         double t;
         if (n == 1) {
-            t = tile_time(TILE_COSTS[tile_choice(lay, EPI_STORE, a)], lay, EPI_STORE, a, cus);
+            t = tile_time(TILE_COSTS[tile_choice(lay, whole, a)], lay, whole, a, cus);
         } else {
             const int c = lay == GEMM_NN ? slice_choice<GEMM_NN>(g) : slice_choice<GEMM_NT>(g);
             // (the partial sums are written and read at some 4 TB/s, their launch takes 3 us)

@@ -17,7 +17,7 @@ FORWARD = [
     ((256, 256, 1), 2965, 200, 4112, (NONE, GELU, SILU)), ((256, 256, 1), 6761, 200, 1200, (NONE,)), ((256, 256, 1), 8192, 512, 2048, (SILU,)),
     ((256, 256, 1), 33064, 472, 136, (GELU,)), ((256, 128, 1), 16669, 840, 136, (NONE,)), ((256, 128, 1), 34058, 7648, 72, (GELU, SILU)),
     ((128, 128, 1), 9959, 360, 144, (NONE, GELU, SILU)), ((64, 128, 1), 299, 376, 88, (NONE, GELU, SILU)),
-    ((64, 64, 10), 67, 3128, 80, (GELU,)), ((64, 128, 2), 72, 2032, 6480, (SILU,)), ((128, 128, 3), 65, 1816, 6896, (NONE, GELU)),
+    ((64, 64, 10), 67, 3128, 80, (GELU,)), ((64, 128, 2), 72, 2032, 6480, (SILU,)), ((128, 128, 3), 65, 1816, 6896, (NONE,)),
 ]
 
 
