@@ -33,9 +33,10 @@ constexpr int ACT_WAVES = 4, ACT_COLS = 512; // of act_bwd_kernel: wavefronts, c
 
 int up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Workgroups that share a column block's K: 256 in all (one row, 8192 x 2048: 11.7 us, with 128 12.7, with 512 12.4; 2048 x 8192 11.0, 12.4, 10.9),
+// Workgroups that share a column block's K: 256 in all, or as many fewer as it takes for a whole number to a block, down to half of them (one row, 8192 x 2048: 11.7 us, with 128 12.7, with 512 12.4; 2048 x 8192 11.0, 12.4, 10.9),
 // or one, which finishes by itself, where K is three steps to a wavefront (one row, 520 x 1000: 4.7 us, 7.3 with a second launch; 1024 x 4096, which is
-// too much, 8.5 and 7.6).
+// too much, 8.5 and 7.6).  Rounded up they would be more than 256, some CUs with two and most with one, and a second launch for wide matrices
+// (K = 4096, N = 16640: 26.5 us in one slice, 33.7 in two; 11008 in two 19.5, in three 23.9; 28 rows, 5152 x 2192 14.1 and 16.2).
 int few_slices(int K, int N, bool bf16) {
     const int columns = up(N, bf16 ? Few<bf16_t>::COLS : Few<float>::COLS), steps = up(K, Few<float>::STEP);
     if (columns >= 256 || steps <= 3 * FEW_WAVES) return 1;
