@@ -363,6 +363,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_first_
 // its own.  (The last workgroup of a column block to finish, adding them up: with fences, which write back and empty the caches of
 // eight dies, 89 us for what takes 14 without; with stores and loads that go past the caches 44.5 us for the whole of one token, 2048/8192,
 // and 37.5 for seven of 520/1000 in float, against 45.1 and 35.5 with the launch.)
+// Two groups of bfloat16 rows in two parts need three registers more than two workgroups to a CU have: they are spilled once for 32 rows, outside
+// the loop over the steps.
 template <typename T, int GROUPS>
 __global__ __launch_bounds__(FEW_WAVES * 64, GROUPS > 2 ? 2 : 4) void few_second_kernel(FewArgs a) {
     __shared__ FewLds<T> lds;

@@ -99,3 +99,20 @@ def test_activation_backward_past_the_caches(dtype, T, N, act):
     """dz of more than 128 MiB, in its own memory and in dy's or z's."""
     assert T * N * (2 if dtype == B.MOE_BF16 else 4) > 128 << 20
     _activation_backward(T, N, act, dtype)
+
+
+@pytest.mark.parametrize("T,K,N", [(5, 136, 264), (20, 4104, 72), (299, 376, 88), (67, 3128, 80), (9959, 360, 144), (2965, 200, 4112)])
+@pytest.mark.parametrize("dtype", [B.MOE_F32, B.MOE_BF16])
+def test_float_vectors_may_begin_anywhere(T, K, N, dtype):
+    """The bias and its gradient, a float behind a multiple of 16 bytes, with guards about the gradient."""
+    g = torch.Generator(device=D).manual_seed(T)
+    x, dy = (torch.randn(s, generator=g, device=D).to(DT[dtype]) for s in ((T, K), (T, N)))
+    W, b = (torch.randn((K, N), generator=g, device=D) * K ** -0.5).to(DT[dtype]), torch.randn(N + 1, generator=g, device=D)
+    cfg = B.make_linear_config(T, K, N, dtype, SILU, 1)
+    scratch, db = _scratch(cfg), torch.full((2, N + 2), 7.0, device=D)
+    out = [[torch.empty((T, N), device=D, dtype=DT[dtype]) for _ in range(3)] for _ in range(2)]
+    for (z, y, dz), bias, d in zip(out, (b[1:], b[1:].clone()), (db[0, 1:-1], db[1, :-2])):
+        B.moe_linear_fwd(cfg, x, W, bias, None, z, y, scratch)
+        B.moe_act_bwd(cfg, dy, z, dz, d, scratch)
+    assert all(torch.equal(p, q) for p, q in zip(*out)) and torch.equal(db[0, 1:-1], db[1, :-2])
+    assert db[0, 0] == 7.0 and (db[:, -1] == 7.0).all() and db[1, -2] == 7.0 and not torch.equal(out[0][0], torch.zeros_like(out[0][0]))
