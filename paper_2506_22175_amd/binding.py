@@ -599,7 +599,8 @@ def moe_grad_table(tensors, table, stream=None) -> MoEGradList:
 
 def make_grad_list(grads, outs=None, stream=None) -> MoEGradList:
     """A list of gradient tensors (contiguous, float32 or bfloat16) with its table, which the returned object keeps alive; the
-    tensors are the caller's to keep.  outs: where the clipped ones go (the gradients themselves for clipping in place), or None."""
+    tensors are the caller's to keep.  It takes some 5 us a tensor on the host, and a launch for every 64: a list is for gradients that stay at
+    their addresses, and made once.  outs: where the clipped ones go (the gradients themselves for clipping in place), or None."""
     import torch
     code = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}
     outs = [None] * len(grads) if outs is None else outs
